@@ -1,9 +1,10 @@
-"""Thin ctypes binding of libstreamindex: same names as include/streamindex.h, argument
+"""Thin ctypes binding of libstreamindex: same names as the headers under include/, argument
 marshalling only.  Tensors are torch tensors living on the GPU; every step of the path runs
 in the library's HIP kernels.  There is no CPU fallback: a missing library is an error."""
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from ctypes import (POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t,
                     c_uint64, c_void_p)
@@ -20,6 +21,7 @@ SI_ERR_WORKSPACE_TOO_SMALL = -3
 SI_ERR_HIP = -4
 SI_MASK_NONE = 0
 SI_MASK_CAUSAL_BLOCK = 1
+SI_MAX_ROW_MOVES = 8
 SI_PROFILE_CLASSES = 7
 PROFILE_CLASS_NAMES = ("score_tile", "filter_scores", "compact", "finalize", "init", "fused", "fused_narrow")
 
@@ -31,6 +33,8 @@ EXPORTS = (
     "si_profile_reset", "si_profile_read", "si_profile_phases", "si_wall_clock_khz", "si_strerror",
     "si_last_hip_error",
     "si_version",
+    "si_quantize_rows", "si_dequantize_rows", "si_quantized_attention", "si_accumulate_workspace_bytes",
+    "si_accumulate_weights", "si_evict_workspace_bytes", "si_evict_rows",
 )
 
 
@@ -40,6 +44,10 @@ class si_dims(Structure):
 
 class si_plan(Structure):
     _fields_ = [("c_S", c_int32), ("c_T", c_int32), ("workspace_bytes", c_size_t)]
+
+
+class si_row_move(Structure):
+    _fields_ = [("src", c_void_p), ("dst", c_void_p), ("row_bytes", c_int32)]
 
 
 class StreamIndexError(RuntimeError):
@@ -114,6 +122,24 @@ def load():
     L.si_last_hip_error.argtypes = []
     L.si_version.restype = c_int32
     L.si_version.argtypes = []
+    L.si_quantize_rows.restype = c_int32
+    L.si_quantize_rows.argtypes = [c_void_p, c_void_p, POINTER(si_dims), c_void_p, c_void_p, c_void_p]
+    L.si_dequantize_rows.restype = c_int32
+    L.si_dequantize_rows.argtypes = [c_void_p, c_void_p, c_void_p, POINTER(si_dims), c_void_p, c_void_p]
+    L.si_quantized_attention.restype = c_int32
+    L.si_quantized_attention.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, POINTER(si_dims), c_int32,
+                                         c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p]
+    L.si_accumulate_workspace_bytes.restype = c_size_t
+    L.si_accumulate_workspace_bytes.argtypes = [POINTER(si_dims)]
+    L.si_accumulate_weights.restype = c_int32
+    L.si_accumulate_weights.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, POINTER(si_dims), c_int32,
+                                        c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_size_t,
+                                        c_void_p]
+    L.si_evict_workspace_bytes.restype = c_size_t
+    L.si_evict_workspace_bytes.argtypes = [c_int32, c_int32]
+    L.si_evict_rows.restype = c_int32
+    L.si_evict_rows.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, POINTER(si_row_move),
+                                c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     _lib = L
     return L
 
@@ -267,6 +293,136 @@ def si_sparse_attention(qa, Kc, idx, m, mask_mode, n_win, scale, out, stream=Non
         _dev_ptr(qa, torch.bfloat16, "qa"), _dev_ptr(Kc, torch.bfloat16, "Kc"),
         _dev_ptr(idx, torch.int32, "idx"), byref(dims), m, ls[2], mask_mode, n_win, float(scale),
         _dev_ptr(out, torch.float32, "out"), _stream_handle(stream)), "si_sparse_attention")
+
+
+# ---- a compressed cache held in 4 bits (include/streamindex_cache.h)
+# The tensors of a call must be on one GPU, the current one: its stream is where the kernels go.
+def _one_device(*tensors):
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"all tensors must be on the current GPU (cuda:{device}), got {t.device}")
+
+
+def _per_batch(t, B, name):
+    """Pointer of an optional int32 [B] tensor."""
+    if t is None:
+        return None
+    if t.shape != (B,):
+        raise ValueError(f"{name} must be [{B}]")
+    return _dev_ptr(t, torch.int32, name)
+
+
+def _cache_rows(rows, start, codes, scales, stream):
+    rs, cs, ss = rows.shape, codes.shape, scales.shape
+    if len(rs) != 3 or len(cs) != 3 or len(ss) != 3:
+        raise ValueError("rows must be [B,S,D], codes [B,T,D/2], scales [B,T,D/32]")
+    B, S, D = rs
+    T = cs[1]
+    if D % 32 or cs != (B, T, D // 2) or ss != (B, T, D // 32):
+        raise ValueError(f"shape mismatch: rows {tuple(rs)}, codes {tuple(cs)}, scales {tuple(ss)}")
+    pointers = (_dev_ptr(rows, torch.bfloat16, "rows"), _per_batch(start, B, "start"),
+                _dev_ptr(codes, torch.uint8, "codes"), _dev_ptr(scales, torch.uint8, "scales"))
+    _one_device(rows, start, codes, scales)
+    return pointers, si_dims(B, S, 1, D, T), _stream_handle(stream)
+
+
+def si_quantize_rows(rows, start, codes, scales, stream=None):
+    """Rows [B,S,D] bf16 into a 4-bit cache: codes [B,T,D/2] and scales [B,T,D/32] uint8; row n of batch b becomes cache row
+    start[b] + n (start: int32 [B] or None = 0), rows that would fall outside the cache are not stored."""
+    (r, at, c, s), dims, st = _cache_rows(rows, start, codes, scales, stream)
+    _check(load().si_quantize_rows(r, at, byref(dims), c, s, st), "si_quantize_rows")
+
+
+def si_dequantize_rows(codes, scales, start, rows, stream=None):
+    """Rows start[b] + n of a 4-bit cache into rows [B,S,D] bf16, as the values the codes stand for (zeros outside the cache)."""
+    (r, at, c, s), dims, st = _cache_rows(rows, start, codes, scales, stream)
+    _check(load().si_dequantize_rows(c, s, at, byref(dims), r, st), "si_dequantize_rows")
+
+
+def _quantized_call(qa, codes, scales, lengths, idx):
+    qs, cs, ss = qa.shape, codes.shape, scales.shape
+    if len(qs) != 4 or len(cs) != 3 or len(ss) != 3:
+        raise ValueError("qa must be [B,S,H,D], codes [B,T,D/2], scales [B,T,D/32]")
+    B, S, H, D = qs
+    T = cs[1]
+    if D % 32 or cs != (B, T, D // 2) or ss != (B, T, D // 32):
+        raise ValueError(f"shape mismatch: qa {tuple(qs)}, codes {tuple(cs)}, scales {tuple(ss)}")
+    k, lists = 0, None
+    if idx is not None:
+        if len(idx.shape) != 3 or idx.shape[:2] != (B, S):
+            raise ValueError(f"idx must be [{B}, {S}, k]")
+        k = idx.shape[2]
+        lists = _dev_ptr(idx, torch.int32, "idx") if k else None
+    return (_dev_ptr(qa, torch.bfloat16, "qa"), _dev_ptr(codes, torch.uint8, "codes"),
+            _dev_ptr(scales, torch.uint8, "scales"), _per_batch(lengths, B, "lengths"), lists), si_dims(B, S, H, D, T), k
+
+
+def si_quantized_attention(qa, codes, scales, lengths, idx, m, mask_mode, n_win, scale, out, lse=None, stream=None):
+    """Attention over TopK(t) U Window(t) on a 4-bit cache: qa [B,S,H,D] bf16, codes [B,T,D/2] and scales [B,T,D/32] uint8,
+    lengths int32 [B] or None (= T), idx [B,S,k] int32 or None (no list), out [B,S,H,D] f32, lse [B,S,H] f32 or None."""
+    pointers, dims, k = _quantized_call(qa, codes, scales, lengths, idx)
+    if out.shape != qa.shape:
+        raise ValueError(f"out must be {tuple(qa.shape)}")
+    to_lse = None
+    if lse is not None:
+        if lse.shape != qa.shape[:3]:
+            raise ValueError(f"lse must be {tuple(qa.shape[:3])}")
+        to_lse = _dev_ptr(lse, torch.float32, "lse")
+    to_out = _dev_ptr(out, torch.float32, "out")
+    _one_device(qa, codes, scales, lengths, idx, out, lse)
+    _check(load().si_quantized_attention(*pointers, byref(dims), m, k, mask_mode, n_win, float(scale), to_out, to_lse,
+                                         _stream_handle(stream)), "si_quantized_attention")
+
+
+def si_accumulate_workspace_bytes(B, S, H, D, T) -> int:
+    return int(load().si_accumulate_workspace_bytes(byref(si_dims(B, S, H, D, T))))
+
+
+def si_accumulate_weights(qa, codes, scales, lengths, idx, m, mask_mode, n_win, scale, lse, weights, workspace=None, stream=None):
+    """Adds what every cache row receives of the softmax of an si_quantized_attention call (same arguments, lse as it wrote
+    it) to weights [B,T] f32; workspace: uint8 GPU tensor of si_accumulate_workspace_bytes, None where that is 0."""
+    pointers, dims, k = _quantized_call(qa, codes, scales, lengths, idx)
+    if lse.shape != qa.shape[:3] or weights.shape != (dims.B, dims.T):
+        raise ValueError(f"lse must be {tuple(qa.shape[:3])}, weights {(dims.B, dims.T)}")
+    ws, ws_bytes = None, 0
+    if workspace is not None and workspace.numel():
+        ws, ws_bytes = _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()
+    from_lse, to = _dev_ptr(lse, torch.float32, "lse"), _dev_ptr(weights, torch.float32, "weights")
+    _one_device(qa, codes, scales, lengths, idx, lse, weights, workspace)
+    _check(load().si_accumulate_weights(*pointers, byref(dims), m, k, mask_mode, n_win, float(scale), from_lse, to, ws,
+                                        ws_bytes, _stream_handle(stream)), "si_accumulate_weights")
+
+
+def si_evict_workspace_bytes(B, T) -> int:
+    return int(load().si_evict_workspace_bytes(B, T))
+
+
+def si_evict_rows(weights, lengths, n_keep, n_sink, n_recent, moves, kept, new_lengths, workspace, stream=None):
+    """Keeps the n_keep rows of each batch with the largest weights [B,T] f32 (the first n_sink and the last n_recent always) and
+    compacts what belongs to them: moves is a list of up to 8 pairs (src [B,T,...], dst [B,n_keep,...]) of one dtype each;
+    kept [B,n_keep] int32 gets the rows that stay, ascending, then -1; new_lengths int32 [B] or None how many."""
+    if len(weights.shape) != 2:
+        raise ValueError("weights must be [B,T]")
+    B, T = weights.shape
+    if kept.shape != (B, n_keep):
+        raise ValueError(f"kept must be {(B, n_keep)}")
+    if len(moves) > SI_MAX_ROW_MOVES:
+        raise ValueError(f"at most {SI_MAX_ROW_MOVES} arrays a call")
+    table = (si_row_move * max(1, len(moves)))()
+    for i, (src, dst) in enumerate(moves):
+        if src.shape[:2] != (B, T) or dst.shape != (B, n_keep, *src.shape[2:]) or src.dtype != dst.dtype:
+            raise ValueError(f"moves[{i}]: src {tuple(src.shape)} {src.dtype}, dst {tuple(dst.shape)} {dst.dtype}")
+        table[i].src = _dev_ptr(src, src.dtype, f"moves[{i}] src")
+        table[i].dst = _dev_ptr(dst, src.dtype, f"moves[{i}] dst")
+        table[i].row_bytes = src.element_size() * math.prod(src.shape[2:])
+        _one_device(src, dst)
+    w, to = _dev_ptr(weights, torch.float32, "weights"), _dev_ptr(kept, torch.int32, "kept")
+    held, new = _per_batch(lengths, B, "lengths"), _per_batch(new_lengths, B, "new_lengths")
+    ws = _dev_ptr(workspace, torch.uint8, "workspace")
+    _one_device(weights, lengths, kept, new_lengths, workspace)
+    _check(load().si_evict_rows(w, held, B, T, n_keep, n_sink, n_recent, table, len(moves), to, new, ws, workspace.numel(),
+                                _stream_handle(stream)), "si_evict_rows")
 
 
 def si_score_tile(q, K, w, m, mask_mode, s0, t0, c_S, c_T, tile, stream=None):

@@ -1,0 +1,494 @@
+// Attention over TopK(t) U Window(t) where the cache is held in 4 bits (si_quantized_attention), and what the cache's rows
+// receive of its softmax (si_accumulate_weights):
+//
+//   out[t,h,:]   = sum_{s in U(t)} p_s V[s,:],   p = softmax_{s in U(t)}( scale * <qa[t,h,:], V[s,:]> )
+//   lse[t,h]     = ln sum_{s in U(t)} exp( scale * <qa[t,h,:], V[s,:]> )
+//   weights[s]  += sum_{t,h} exp( scale * <qa[t,h,:], V[s,:]> - lse[t,h] )
+//
+// V[s, 32 j + i] = code * 2^e(s, j).  Codes times their power are exact in fp16 (exponents -13 .. 13), and so are the queries once a
+// head is scaled by a power of two, which goes into the softmax scale.  So the first product is that of the bf16 operands, and the second one
+// takes the weights in two fp16 parts, 22 mantissa bits, at the cost that two bf16 parts with 16 bits would have.
+
+#include <hip/hip_runtime.h>
+
+#include <atomic>
+#include <type_traits>
+
+#include "attention_set.h"
+#include "si_internal.h"
+#include "streamindex_cache.h"
+
+namespace si {
+
+namespace {
+
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef __fp16 fp16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// The weights are 2^7 times exp2(x - reference): at most 2^15 with the slack of 2^8, so that both fp16 parts of
+// a weight are normal numbers down to 2^-18 of the reference's weight.
+constexpr float kWeightShift = 7.0f;
+
+__device__ __forceinline__ float power_of(unsigned scale_byte) { return __uint_as_float(scale_byte << 23); }
+
+// Rows that batch b holds, and legal rows of query t.
+__device__ __forceinline__ int held_rows(const int32_t* __restrict__ lengths, int b, int T) {
+    return lengths ? min(max(lengths[b], 0), T) : T;
+}
+
+// This lane's part of a query's head (8 values at 16 ks + 8 half) as fp16, times a power of two that brings the head's largest
+// magnitude into [2^14, 2^15), with the sign of the softmax scale; values down to 2^-32 of the largest stay exact.  Returns the factor that
+// takes a product of these operands to the log2 domain: |scale| log2(e) over that power.
+template <int KS>
+__device__ __forceinline__ float load_query(const __bf16* __restrict__ src, float scale_log2e, halfx8 (&qf)[KS]) {
+    uintx4 raw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(src + ks * 16);
+    unsigned top = 0;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = max(top, max(raw[ks][j] & 0x7FFFu, (raw[ks][j] >> 16) & 0x7FFFu));
+    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(both[0], both[1]);
+    const int e = static_cast<int>(top >> 7);        // exponent field of the largest
+    const int up = min(268 - e, 254);                // field of the power: 2^(14 - (e - 127))
+    const float power = __uint_as_float(static_cast<unsigned>(up) << 23) * (scale_log2e < 0.0f ? -1.0f : 1.0f);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float lo = __uint_as_float(raw[ks][j] << 16) * power;
+            const float hi = __uint_as_float(raw[ks][j] & 0xFFFF0000u) * power;
+            const halfx2 pair = __builtin_convertvector(floatx2{lo, hi}, halfx2);
+            qf[ks][2 * j] = pair[0];
+            qf[ks][2 * j + 1] = pair[1];
+        }
+    return __builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up);
+}
+
+// One workgroup = one query; wave w owns heads [32 w, 32 w + 32), all waves share the tiles of 32 rows.  The codes of a tile are read
+// two tiles ahead into registers, turned into fp16 once for all waves and laid in LDS, row-major and swizzled (attention_set.h); from there
+// on a tile's steps are those of sparse_attention_kernel in attention.hip:
+//   S^T[32 rows x 32 heads] = tile . q^T, weights against a running reference, O^T[D x 32 heads] += tile^T . P^T.
+// Dynamic LDS: 2 tiles of 32 x D fp16, the query's list.
+template <int D, int HW>
+__global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(2)))
+void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
+                                const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
+                                const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
+                                float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
+    constexpr int KS = D / 16;
+    constexpr int DB = D / 32;
+    constexpr int kRowBytes = D * 2;
+    constexpr int kTileBytes = kTileKeys * kRowBytes;
+    // a thread turns kUnits runs of kVals values of a tile into fp16
+    constexpr int kVals = D / (2 * HW) < 32 ? D / (2 * HW) : 32;
+    constexpr int kUnits = D / (2 * HW) / kVals;
+    constexpr int kRuns = D / kVals;  // of a row
+    static_assert(kVals == 16 || kVals == 32, "a run lies in one block of 32");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    int* const s_list = reinterpret_cast<int*>(lds + 2 * kTileBytes);
+    __shared__ int s_kept[HW];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int col = lane & 31;
+    const int half = lane >> 5;
+    const int64_t row_q = blockIdx.x;  // b * S + t
+    const int b = static_cast<int>(row_q / S);
+    const int t = static_cast<int>(row_q % S);
+    const int held = held_rows(lengths, b, T);
+    const int legal = legal_count(t, held, m, mask_mode);
+    const int w0 = max(0, legal - n_win);
+    const int n = build_list<HW>(idx + row_q * k, k, held, w0, legal, s_list, s_kept);
+    __syncthreads();
+    const int n_u = __builtin_amdgcn_readfirstlane(n);
+    const int h = 32 * wave + col;
+    if (n_u == 0) {
+        for (int i = threadIdx.x; i < H * D; i += 64 * HW) out[row_q * H * D + i] = 0.0f;
+        if (lse && h < H && half == 0) lse[row_q * H + h] = -__builtin_huge_valf();
+        return;
+    }
+    const int n_tiles = (n_u + kTileKeys - 1) / kTileKeys;
+    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2);
+    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32);
+
+    // ---- this thread's runs of a tile: codes and scale bytes to registers, and from there to LDS
+    typedef std::conditional_t<kVals == 32, uintx4, uintx2> run_t;
+    run_t run[kUnits];
+    unsigned byte[kUnits];
+    auto read = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int unit = u * 64 * HW + static_cast<int>(threadIdx.x);
+            const int64_t row = s_list[tile * kTileKeys + unit / kRuns];
+            const int at = unit % kRuns;
+            run[u] = *reinterpret_cast<const run_t*>(codes_b + row * (D / 2) + at * (kVals / 2));
+            byte[u] = scales_b[row * (D / 32) + at * kVals / 32];
+        }
+    };
+    auto lay = [&](unsigned char* tb) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int unit = u * 64 * HW + static_cast<int>(threadIdx.x);
+            const int r = unit / kRuns, at = unit % kRuns;
+            const float power = power_of(byte[u]);
+#pragma unroll
+            for (int i = 0; i < kVals / 8; ++i) {
+                const unsigned c = run[u][i];
+                const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 0);
+                const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 1);
+                const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 2);
+                const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 3);
+                const halfx8 v = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+                *reinterpret_cast<halfx8*>(tb + tile_slot<D>(r, at * (kVals / 8) + i) * 16) = v;
+            }
+        }
+    };
+    read(0);
+
+    halfx8 qf[KS];
+    const float to_log2 = load_query<KS>(qa + (row_q * H + min(h, H - 1)) * D + half * 8, scale_log2e, qf);
+
+    // LDS byte offsets that do not depend on the tile (attention.hip says how the transposing reads are laid out)
+    int ka[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ka[ks] = tile_slot<D>(col, 2 * ks + half) * 16;
+    int va[DB][2];
+    {
+        const int G = lane >> 4, s = lane & 15;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int r = 8 * w + 4 * (G >> 1) + (s >> 2);
+                const int d = 32 * db + 16 * (G & 1) + 4 * (s & 3);
+                va[db][w] = tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
+            }
+    }
+
+    floatx16 acc[DB];
+    const floatx16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = zero16;
+    float m_ref = -__builtin_huge_valf();  // reference maximum of this lane's head (log2 domain)
+    float l_sum = 0.0f;                    // sum of the weights over this half-wave's rows
+
+    lay(lds);
+    if (n_tiles > 1) read(1);
+    __syncthreads();
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        const unsigned char* tb = lds + (tile & 1) * kTileBytes;
+        // S^T : register j of a lane = row 8 (j / 4) + 4 half + j % 4, head = col
+        floatx16 sacc = zero16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const halfx8 kf = *reinterpret_cast<const halfx8*>(tb + ka[ks]);
+            sacc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[ks], sacc, 0, 0, 0);
+        }
+        // the next tile into the other buffer, which everybody left at the last barrier
+        if (tile + 1 < n_tiles) lay(lds + ((tile + 1) & 1) * kTileBytes);
+        if (tile + 2 < n_tiles) read(tile + 2);
+        const int live = n_u - tile * kTileKeys;
+        const bool ragged = live < kTileKeys;  // rows past the end of U(t), in the last tile
+        if (ragged) {
+            float low = -3.0e38f;
+            asm volatile("" : "+v"(low));  // keeps this block a branch instead of 16 selects per tile
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (8 * (j >> 2) + 4 * half + (j & 3) >= live) sacc[j] = low;  // out of the maximum; weight zeroed below
+        }
+        float smax = sacc[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) smax = fmaxf(smax, sacc[j]);
+        float tmax = smax * to_log2;
+        tmax = fmaxf(tmax, other_half(tmax));  // finite: row 0 of a tile is live
+        const bool raise = tmax > m_ref + kRescaleSlack;
+        if (__ballot(raise) != 0ull) {
+            const float m_new = raise ? tmax : m_ref;
+            const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
+            l_sum *= alpha;
+            m_ref = m_new;
+        }
+        const float shift = kWeightShift - m_ref;
+        float p[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[j], to_log2, shift));
+        if (ragged) {
+            float none = 0.0f;
+            asm volatile("" : "+v"(none));
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (8 * (j >> 2) + 4 * half + (j & 3) >= live) p[j] = none;
+        }
+        halfx8 p_hi[2], p_lo[2];  // p = hi + lo, each rounded to fp16
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) {
+            const float p0 = p[2 * jj], p1 = p[2 * jj + 1];
+            l_sum += p0 + p1;
+            const halfx2 hi = __builtin_convertvector(floatx2{p0, p1}, halfx2);
+            const halfx2 lo = __builtin_convertvector(floatx2{p0 - static_cast<float>(hi[0]), p1 - static_cast<float>(hi[1])}, halfx2);
+            p_hi[jj >> 2][2 * (jj & 3)] = hi[0];
+            p_hi[jj >> 2][2 * (jj & 3) + 1] = hi[1];
+            p_lo[jj >> 2][2 * (jj & 3)] = lo[0];
+            p_lo[jj >> 2][2 * (jj & 3) + 1] = lo[1];
+        }
+        // O^T += tile^T . P^T : contraction index e of step u <-> tile row 16 u + 8 (e / 4) + 4 half + e % 4 on both operands
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
+                const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][0] + u * 16 * kRowBytes)));
+                const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][1] + u * 16 * kRowBytes)));
+                const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_hi[u], acc[db], 0, 0, 0);
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_lo[u], acc[db], 0, 0, 0);
+            }
+        __syncthreads();
+    }
+
+    // ---- out[t, head, d] = O^T[d, head] / l : register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4
+    const float l_all = l_sum + other_half(l_sum);
+    const float inv = 1.0f / l_all;
+    if (h < H) {
+        float* o = out + (row_q * H + h) * D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const floatx4 v = {acc[db][4 * a] * inv, acc[db][4 * a + 1] * inv, acc[db][4 * a + 2] * inv, acc[db][4 * a + 3] * inv};
+                *reinterpret_cast<floatx4*>(o + 32 * db + 8 * a + 4 * half) = v;
+            }
+        if (lse && half == 0) lse[row_q * H + h] = (m_ref - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2;
+    }
+}
+
+// What the rows of U(t) receive of a query: S[32 heads x 32 rows] = q . tile^T with the heads on the M side, so that a lane holds
+// 16 heads of one row and the sum over heads is in-lane (and one exchange).  The codes go from memory to a lane's registers as they are
+// needed there (row = lane % 32, values D/2 * (lane / 32) .. + D/2: the contraction order is permuted alike on the query) and from there to
+// bf16; no LDS but the list.  One workgroup = one query, its waves take every kWeightWaves-th tile, all heads each.
+//   S == 1: every row has one sum a call, added to weights;   S > 1: 64-bit fixed point in the workspace, in any order.
+constexpr int kWeightWaves = 4;
+constexpr double kFixedOne = 4294967296.0;  // 2^32
+
+template <int D, int HB>
+__global__ __launch_bounds__(64 * kWeightWaves)
+void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
+                               const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
+                               const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
+                               float scale_log2e, const float* __restrict__ lse, float* __restrict__ weights,
+                               unsigned long long* __restrict__ sums) {
+    constexpr int KS = D / 16;
+    constexpr int kLoads = D / 64;  // 16-byte pieces of codes a lane holds of a row
+    extern __shared__ __attribute__((aligned(16))) int s_list[];
+    __shared__ int s_kept[kWeightWaves];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int col = lane & 31;
+    const int half = lane >> 5;
+    const int64_t row_q = blockIdx.x;
+    const int b = static_cast<int>(row_q / S);
+    const int t = static_cast<int>(row_q % S);
+    const int held = held_rows(lengths, b, T);
+    const int legal = legal_count(t, held, m, mask_mode);
+    const int w0 = max(0, legal - n_win);
+    const int n = build_list<kWeightWaves>(idx + row_q * k, k, held, w0, legal, s_list, s_kept);
+    __syncthreads();
+    const int n_u = __builtin_amdgcn_readfirstlane(n);
+    const int n_tiles = (n_u + kTileKeys - 1) / kTileKeys;
+    if (wave >= n_tiles) return;
+    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
+    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
+
+    uintx4 run[kLoads];
+    unsigned byte[kLoads];
+    auto read = [&](int tile) {
+        const int64_t row = s_list[tile * kTileKeys + col];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            run[i] = *reinterpret_cast<const uintx4*>(codes_b + row * (D / 2) + i * 16);
+            byte[i] = scales_b[row * (D / 32) + i];
+        }
+    };
+    read(wave);
+
+    bf16x8 qf[HB][KS];     // head 32 hb + col, values D/2 * half + 8 ks .. + 8
+    float minus_lse[HB][16];  // of the heads this lane's results belong to, log2 domain
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) {
+        const __bf16* src = qa + (row_q * H + min(32 * hb + col, H - 1)) * D + half * (D / 2);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[hb][ks] = *reinterpret_cast<const bf16x8*>(src + ks * 8);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int h = 32 * hb + 8 * (j >> 2) + 4 * half + (j & 3);
+            minus_lse[hb][j] = h < H ? -kLog2e * lse[row_q * H + h] : -__builtin_huge_valf();  // no head there: weight 0
+        }
+    }
+    for (int tile = wave; tile < n_tiles; tile += kWeightWaves) {
+        bf16x8 kf[KS];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const float power = power_of(byte[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned c = run[i][j];
+                const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 0);
+                const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 1);
+                const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 2);
+                const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 3);
+                kf[4 * i + j] = bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+            }
+        }
+        if (tile + kWeightWaves < n_tiles) read(tile + kWeightWaves);
+        float sum = 0.0f;
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) {
+            floatx16 acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[hb][ks], kf[ks], acc, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j], scale_log2e, minus_lse[hb][j]));
+        }
+        sum += other_half(sum);
+        const int place = tile * kTileKeys + col;
+        if (half == 0 && place < n_u) {
+            const int64_t at = static_cast<int64_t>(b) * T + s_list[place];
+            if (sums) atomicAdd(sums + at, static_cast<unsigned long long>(static_cast<double>(sum) * kFixedOne + 0.5));
+            else weights[at] += sum;
+        }
+    }
+}
+
+__global__ void clear_sums_kernel(unsigned long long* sums, int64_t n) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
+        sums[i] = 0;
+}
+__global__ void add_sums_kernel(const unsigned long long* __restrict__ sums, int64_t n, float* __restrict__ weights) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
+        if (sums[i]) weights[i] = static_cast<float>(weights[i] + static_cast<double>(sums[i]) * (1.0 / kFixedOne));
+}
+
+struct Call {
+    const __bf16* qa;
+    const unsigned char *codes, *scales;
+    const int32_t *lengths, *idx;
+    si_dims d;
+    int32_t m, mask_mode, k, n_win;
+    float scale_log2e;
+    hipStream_t stream;
+};
+
+template <int D, int HW>
+hipError_t launch_attention(const Call& c, float* out, float* lse) {
+    static std::atomic<size_t> allowed[64];
+    const size_t lds = 2 * static_cast<size_t>(kTileKeys) * D * 2 + list_bytes(c.k, c.n_win);
+    hipError_t e = allow_lds(quantized_attention_kernel<D, HW>, lds, allowed);
+    if (e != hipSuccess) return e;
+    const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
+    hipLaunchKernelGGL((quantized_attention_kernel<D, HW>), dim3(static_cast<unsigned>(rows)), dim3(64 * HW), lds, c.stream, c.qa,
+                       c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e, out,
+                       lse);
+    return hipGetLastError();
+}
+
+template <int D, int HB>
+hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsigned long long* sums) {
+    const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
+    hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>(rows)), dim3(64 * kWeightWaves),
+                       list_bytes(c.k, c.n_win), c.stream, c.qa, c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m,
+                       c.mask_mode, c.k, c.n_win, c.scale_log2e, lse, weights, sums);
+    return hipGetLastError();
+}
+
+si_status check(const void* qa, const void* codes, const void* scales, const int32_t* idx, const si_dims* dims, int32_t m, int32_t k,
+                si_mask_mode mask_mode, int32_t n_win, float scale) {
+    if (!dims || !qa || !codes || !scales || (!idx && k != 0)) return SI_ERR_INVALID_ARG;
+    if (!aligned16(qa) || !aligned16(codes) || !aligned16(scales) || !aligned16(idx)) return SI_ERR_INVALID_ARG;
+    if (dims->B < 1 || dims->S < 1 || dims->H_I < 1 || dims->D < 1 || dims->T < 1 || m < 1 || k < 0 || n_win < 0) return SI_ERR_INVALID_ARG;
+    if (mask_mode != SI_MASK_NONE && mask_mode != SI_MASK_CAUSAL_BLOCK) return SI_ERR_INVALID_ARG;
+    if (!(scale == scale) || scale - scale != 0.0f) return SI_ERR_INVALID_ARG;  // NaN or infinite
+    if (dims->D != 64 && dims->D != 128) return SI_ERR_UNSUPPORTED_SHAPE;
+    if (dims->H_I > kMaxHeads || k > kMaxK || n_win > kMaxK) return SI_ERR_UNSUPPORTED_SHAPE;
+    // a launch has fewer than 2^32 threads in a dimension, up to 256 a query
+    if (static_cast<int64_t>(dims->B) * dims->S >= (int64_t{1} << 24)) return SI_ERR_UNSUPPORTED_SHAPE;
+    return SI_OK;
+}
+
+}  // namespace
+
+}  // namespace si
+
+using namespace si;
+
+extern "C" {
+
+si_status si_quantized_attention(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
+                                 const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,
+                                 int32_t n_win, float scale, float* out, float* lse, void* stream) {
+    const si_status ok = check(qa, codes, scales, idx, dims, m, k, mask_mode, n_win, scale);
+    if (ok != SI_OK) return ok;
+    if (!out || !aligned16(out) || !aligned16(lse)) return SI_ERR_INVALID_ARG;
+    const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
+                    lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
+    const bool two = dims->H_I > 32;
+    return report(dims->D == 128 ? (two ? launch_attention<128, 2>(c, out, lse) : launch_attention<128, 1>(c, out, lse))
+                                 : (two ? launch_attention<64, 2>(c, out, lse) : launch_attention<64, 1>(c, out, lse)));
+}
+
+size_t si_accumulate_workspace_bytes(const si_dims* dims) {
+    if (!dims || dims->B < 1 || dims->S < 1 || dims->T < 1) return 0;
+    return dims->S == 1 ? 0 : static_cast<size_t>(dims->B) * static_cast<size_t>(dims->T) * sizeof(unsigned long long);
+}
+
+si_status si_accumulate_weights(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
+                                const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,
+                                int32_t n_win, float scale, const float* lse, float* weights, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    const si_status ok = check(qa, codes, scales, idx, dims, m, k, mask_mode, n_win, scale);
+    if (ok != SI_OK) return ok;
+    if (!lse || !weights || !aligned16(lse) || !aligned16(weights)) return SI_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(dims->S) * dims->H_I >= (int64_t{1} << 31)) return SI_ERR_UNSUPPORTED_SHAPE;
+    const size_t need = si_accumulate_workspace_bytes(dims);
+    if (need > 0 && (!workspace || !aligned16(workspace))) return SI_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return SI_ERR_WORKSPACE_TOO_SMALL;
+    const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
+                    lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
+    unsigned long long* sums = need > 0 ? static_cast<unsigned long long*>(workspace) : nullptr;
+    const int64_t n = static_cast<int64_t>(dims->B) * dims->T;
+    const unsigned blocks = static_cast<unsigned>(n < (int64_t{1} << 20) ? (n + 255) / 256 : 4096);
+    hipError_t e = hipSuccess;
+    if (sums) {
+        hipLaunchKernelGGL(clear_sums_kernel, dim3(blocks), dim3(256), 0, c.stream, sums, n);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) {
+        const bool two = dims->H_I > 32;
+        e = dims->D == 128 ? (two ? launch_weights<128, 2>(c, lse, weights, sums) : launch_weights<128, 1>(c, lse, weights, sums))
+                           : (two ? launch_weights<64, 2>(c, lse, weights, sums) : launch_weights<64, 1>(c, lse, weights, sums));
+    }
+    if (e == hipSuccess && sums) {
+        hipLaunchKernelGGL(add_sums_kernel, dim3(blocks), dim3(256), 0, c.stream, sums, n, weights);
+        e = hipGetLastError();
+    }
+    return report(e);
+}
+
+}  // extern "C"

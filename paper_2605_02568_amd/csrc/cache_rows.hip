@@ -1,0 +1,152 @@
+// Rows into and out of the 4-bit cache (si_quantize_rows, si_dequantize_rows).
+//
+//   e    = least exponent with max |x| <= 7 * 2^e over a block of 32, in -13 .. 13
+//   code = x / 2^e to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to the even code), beyond 6 to 6
+//   value = code * 2^e
+//
+// All steps are exact but the one rounding: the exponent comes from the bits of the largest magnitude, the conversion
+// instructions divide and multiply by a power of two.  Both kernels are bound by memory: 2 D bytes of bf16 on one side,
+// D / 2 + D / 32 on the other.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "si_internal.h"
+#include "streamindex_cache.h"
+
+namespace si {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLowest = -13, kHighest = 13;  // exponents of a block
+
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Scale byte of a block whose largest magnitude has the bf16 bits `top`: with |x| = 1.f * 2^E, the least e with |x| <= 7 * 2^e is
+// E - 2 where the fraction f (7 bits) is at most 0.75, else E - 1; the sum carries into the exponent field exactly then.
+__device__ __forceinline__ int scale_byte(int top) {
+    const int e = ((top + 0x1F) >> 7) - 2;
+    return min(max(e, 127 + kLowest), 127 + kHighest);
+}
+
+// A thread takes 8 values, four neighbours a block.
+template <int D>
+__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const uintx4* __restrict__ rows, const int32_t* __restrict__ start,
+                                                                 int64_t n_units, int S, int T, unsigned* __restrict__ codes,
+                                                                 unsigned char* __restrict__ scales) {
+    constexpr int kUnits = D / 8;  // of a row
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n_units;
+         i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t n = i / kUnits;  // row of the call
+        const int piece = static_cast<int>(i % kUnits);
+        const int b = static_cast<int>(n / S);
+        const int64_t at = (start ? start[b] : 0) + (n - static_cast<int64_t>(b) * S);
+        const uintx4 x = rows[i];
+        int top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int lo = x[j] & 0x7FFF, hi = (x[j] >> 16) & 0x7FFF;
+            top = max(top, lo > 0x7F80 ? 0 : lo);  // a NaN does not count
+            top = max(top, hi > 0x7F80 ? 0 : hi);
+        }
+        // the block's other three threads are its neighbours: n_units is a multiple of four, so all of them are here
+        top = max(top, __shfl_xor(top, 1));
+        top = max(top, __shfl_xor(top, 2));
+        if (at < 0 || at >= T) continue;  // the same for the block's four threads
+        const int e = scale_byte(top);
+        const float power = __uint_as_float(static_cast<unsigned>(e) << 23);
+        const bf16x8 v = __builtin_bit_cast(bf16x8, x);
+        unsigned packed = 0;
+        packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, bf16x2{v[0], v[1]}, power, 0);
+        packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, bf16x2{v[2], v[3]}, power, 1);
+        packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, bf16x2{v[4], v[5]}, power, 2);
+        packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, bf16x2{v[6], v[7]}, power, 3);
+        const int64_t to = static_cast<int64_t>(b) * T + at;
+        codes[to * kUnits + piece] = packed;
+        if ((piece & 3) == 0) scales[to * (D / 32) + piece / 4] = static_cast<unsigned char>(e);
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const unsigned* __restrict__ codes,
+                                                                   const unsigned char* __restrict__ scales,
+                                                                   const int32_t* __restrict__ start, int64_t n_units, int S, int T,
+                                                                   uintx4* __restrict__ rows) {
+    constexpr int kUnits = D / 8;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n_units;
+         i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t n = i / kUnits;
+        const int piece = static_cast<int>(i % kUnits);
+        const int b = static_cast<int>(n / S);
+        const int64_t at = (start ? start[b] : 0) + (n - static_cast<int64_t>(b) * S);
+        uintx4 x = {0, 0, 0, 0};
+        if (at >= 0 && at < T) {
+            const int64_t from = static_cast<int64_t>(b) * T + at;
+            const unsigned packed = codes[from * kUnits + piece];
+            const float power = __uint_as_float(static_cast<unsigned>(scales[from * (D / 32) + piece / 4]) << 23);
+            x[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(packed, power, 0));
+            x[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(packed, power, 1));
+            x[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(packed, power, 2));
+            x[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(packed, power, 3));
+        }
+        rows[i] = x;
+    }
+}
+
+si_status check(const void* rows, const si_dims* dims, const void* codes, const void* scales) {
+    if (!rows || !dims || !codes || !scales) return SI_ERR_INVALID_ARG;
+    if (dims->B < 1 || dims->S < 1 || dims->D < 1 || dims->T < 1) return SI_ERR_INVALID_ARG;
+    if (!aligned16(rows) || !aligned16(codes) || !aligned16(scales)) return SI_ERR_INVALID_ARG;
+    if (dims->D != 32 && dims->D != 64 && dims->D != 128) return SI_ERR_UNSUPPORTED_SHAPE;
+    return SI_OK;
+}
+
+unsigned blocks_for(int64_t n_units) {
+    return static_cast<unsigned>(std::min<int64_t>((n_units + kThreads - 1) / kThreads, 1 << 20));
+}
+
+}  // namespace
+
+}  // namespace si
+
+using namespace si;
+
+extern "C" {
+
+si_status si_quantize_rows(const void* rows, const int32_t* start, const si_dims* dims, void* codes, void* scales,
+                           void* stream) {
+    const si_status ok = check(rows, dims, codes, scales);
+    if (ok != SI_OK) return ok;
+    const int64_t n_units = static_cast<int64_t>(dims->B) * dims->S * (dims->D / 8);
+#define SI_LAUNCH(DD)                                                                                                        \
+    hipLaunchKernelGGL((quantize_rows_kernel<DD>), dim3(blocks_for(n_units)), dim3(kThreads), 0,                             \
+                       static_cast<hipStream_t>(stream), static_cast<const uintx4*>(rows), start, n_units, dims->S, dims->T, \
+                       static_cast<unsigned*>(codes), static_cast<unsigned char*>(scales))
+    if (dims->D == 128) SI_LAUNCH(128);
+    else if (dims->D == 64) SI_LAUNCH(64);
+    else SI_LAUNCH(32);
+#undef SI_LAUNCH
+    return report(hipGetLastError());
+}
+
+si_status si_dequantize_rows(const void* codes, const void* scales, const int32_t* start, const si_dims* dims, void* rows,
+                             void* stream) {
+    const si_status ok = check(rows, dims, codes, scales);
+    if (ok != SI_OK) return ok;
+    const int64_t n_units = static_cast<int64_t>(dims->B) * dims->S * (dims->D / 8);
+#define SI_LAUNCH(DD)                                                                                               \
+    hipLaunchKernelGGL((dequantize_rows_kernel<DD>), dim3(blocks_for(n_units)), dim3(kThreads), 0,                  \
+                       static_cast<hipStream_t>(stream), static_cast<const unsigned*>(codes),                       \
+                       static_cast<const unsigned char*>(scales), start, n_units, dims->S, dims->T, static_cast<uintx4*>(rows))
+    if (dims->D == 128) SI_LAUNCH(128);
+    else if (dims->D == 64) SI_LAUNCH(64);
+    else SI_LAUNCH(32);
+#undef SI_LAUNCH
+    return report(hipGetLastError());
+}
+
+}  // extern "C"
