@@ -21,16 +21,29 @@ namespace si {
 namespace {
 
 constexpr int kSelectThreads = 1024;
+constexpr int kCountThreads = 512;
 constexpr int kMoveThreads = 256;
-constexpr int kChunk = 256;  // rows a workgroup of the copies takes
+constexpr int kChunk = 256;                      // rows a workgroup of the copies takes
+constexpr int kGroupChunks = 16;
+constexpr int kGroup = kGroupChunks * kChunk;    // rows a workgroup of the histograms and counts takes
 constexpr int kBins = 2048;
+constexpr int kPasses = 3;                       // digits of 11, 11 and 10 bits
+constexpr int kMostRegisterRows = 32 * kSelectThreads;
 
-// Per batch: what the copies have to know.
+// Where a batch stands in the descent, and at its end what the copies have to know.
 struct Border {
-    uint32_t word;  // rows whose word is larger stay ..
-    int32_t equal;  // .. and the first so many of those with this word
+    uint32_t word;  // digits found so far; in the end: rows whose word is larger stay ..
+    int32_t equal;  // rows still to be found among those with these digits; in the end: .. and the first so many of those with this word
     int32_t held;   // rows that the batch holds
     int32_t stay;   // rows that stay
+};
+
+struct Workspace {
+    Border* borders;  // [kPasses + 1][B], the last one is the result
+    int* bins;        // [B][kPasses][kBins], for batches that do not fit one workgroup's registers
+    int2* chunks;     // [B][chunks]: rows above and at the border before a chunk, within its group
+    int2* groups;     // [B][groups]: the same of a whole group
+    size_t bytes;
 };
 
 struct Moves {
@@ -40,132 +53,280 @@ struct Moves {
     int32_t n;
 };
 
-__device__ __forceinline__ uint32_t word_of(float w, int row, int held, int n_sink, int n_recent) {
-    if (row < n_sink || row >= held - n_recent) return 0xFFFFFFFFu;
+struct Rule {
+    int T, n_keep, n_sink, n_recent;
+};
+
+__device__ __forceinline__ uint32_t word_of(float w, int row, int held, const Rule& r) {
+    if (row < r.n_sink || row >= held - r.n_recent) return 0xFFFFFFFFu;
     const uint32_t bits = __float_as_uint(w + 0.0f);  // -0 and +0 are equal
     return w == w ? score_to_ordered(bits) : 0u;
 }
 
-// One workgroup a batch: the border, and for every chunk of rows how many rows stay and how many equal the border's word before it.
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths,
-                                                                     int T, int n_keep, int n_sink, int n_recent, int n_chunks,
-                                                                     Border* __restrict__ borders, int2* __restrict__ chunks,
-                                                                     int32_t* __restrict__ kept, int32_t* __restrict__ new_lengths) {
-    __shared__ int s_bins[kBins];
-    __shared__ int s_waves[kSelectThreads / 64];
-    __shared__ int s_digit, s_above;
-    const int b = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int held = lengths ? min(max(lengths[b], 0), T) : T;
-    const int stay = min(held, n_keep);
-    const float* const w = weights + static_cast<int64_t>(b) * T;
-    uint32_t word = 0;  // the digits found so far
-    int left = stay;    // rows still to be found among those with these digits
-    if (held > n_keep) {
-        int shift = 32;
-        for (int pass = 0; pass < 3; ++pass) {
-            const int bits = pass < 2 ? 11 : 10;
-            const uint32_t seen = pass == 0 ? 0u : 0xFFFFFFFFu << shift;
-            shift -= bits;
-            for (int i = threadIdx.x; i < kBins; i += kSelectThreads) s_bins[i] = 0;
-            __syncthreads();
-            for (int row = threadIdx.x; row < held; row += kSelectThreads) {
-                const uint32_t x = word_of(w[row], row, held, n_sink, n_recent);
-                if ((x & seen) == word) atomicAdd(&s_bins[(x >> shift) & ((1u << bits) - 1)], 1);
-            }
-            __syncthreads();
-            // thread i has bins 2 i and 2 i + 1 from the top: how many rows are in the bins above them
-            const int top = kBins - 1 - 2 * static_cast<int>(threadIdx.x);
-            const int c0 = s_bins[top], c1 = s_bins[top - 1];
-            const int upto = wave_prefix_sum(c0 + c1);
-            if (lane == 63) s_waves[wave] = upto;
-            __syncthreads();
-            int above = upto - (c0 + c1);
-            for (int i = 0; i < wave; ++i) above += s_waves[i];
-            if (above < left && left <= above + c0) {
-                s_digit = top;
-                s_above = above;
-            } else if (above + c0 < left && left <= above + c0 + c1) {
-                s_digit = top - 1;
-                s_above = above + c0;
-            }
-            __syncthreads();
-            word |= static_cast<uint32_t>(s_digit) << shift;
-            left -= s_above;
-            __syncthreads();
-        }
-    } else {
-        left = held;  // every row stays: those above 0, and all that equal it
-    }
-    // chunks in order: a wave counts one chunk, then the counts of the round are added up
-    int stays = 0, equals = 0;  // before this round
-    for (int c0 = 0; c0 < n_chunks; c0 += kSelectThreads / 64) {
-        const int c = c0 + wave;
-        int above = 0, equal = 0;
-        if (c < n_chunks)
-            for (int i = lane; i < kChunk; i += 64) {
-                const int row = c * kChunk + i;
-                if (row < held) {
-                    const uint32_t x = word_of(w[row], row, held, n_sink, n_recent);
-                    above += x > word;
-                    equal += x == word;
-                }
-            }
-        above = lane_value(wave_prefix_sum(above), 63);
-        equal = lane_value(wave_prefix_sum(equal), 63);
-        __syncthreads();  // the last round's counts have been read
-        if (lane == 0) {
-            s_bins[2 * wave] = above;
-            s_bins[2 * wave + 1] = equal;
-        }
-        __syncthreads();
-        int mine_above = stays, mine_equal = equals;
-        for (int i = 0; i < kSelectThreads / 64; ++i) {
-            if (i == wave) { mine_above = stays; mine_equal = equals; }
-            stays += s_bins[2 * i];
-            equals += s_bins[2 * i + 1];
-        }
-        if (lane == 0 && c < n_chunks) chunks[static_cast<int64_t>(b) * n_chunks + c] = make_int2(mine_above + min(mine_equal, left), mine_equal);
-    }
-    for (int j = stay + static_cast<int>(threadIdx.x); j < n_keep; j += kSelectThreads) kept[static_cast<int64_t>(b) * n_keep + j] = -1;
-    if (threadIdx.x == 0) {
-        borders[b] = {word, left, held, stay};
-        if (new_lengths) new_lengths[b] = stay;
-    }
+__device__ __forceinline__ Border first_border(const int32_t* __restrict__ lengths, int b, const Rule& r) {
+    const int held = lengths ? min(max(lengths[b], 0), r.T) : r.T;
+    const int stay = min(held, r.n_keep);
+    return {0u, stay, held, stay};  // where all rows stay: those above 0, and as many as there are that equal it
 }
 
-// Copies rows s_rows[0 .. n) of one array to n rows in a row, in units of type V.
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t digit_mask(int pass) { return pass < 2 ? 0x7FFu : 0x3FFu; }
+__device__ __forceinline__ uint32_t seen_mask(int pass) { return pass == 0 ? 0u : 0xFFFFFFFFu << digit_shift(pass - 1); }
+
+// The digit of the border's word that a histogram of digits gives, into `at`.  The whole workgroup; s_waves: THREADS / 64 + 2 ints.
+template <int THREADS>
+__device__ __forceinline__ void find_digit(const int* bins, int pass, Border& at, int* s_waves) {
+    constexpr int kPer = kBins / THREADS;  // a thread has so many bins, the highest first
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int top = kBins - 1 - kPer * static_cast<int>(threadIdx.x);
+    int c[kPer], mine = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        c[i] = bins[top - i];
+        mine += c[i];
+    }
+    const int upto = wave_prefix_sum(mine);
+    __syncthreads();  // an earlier digit has been read
+    if (lane == 63) s_waves[wave] = upto;
+    __syncthreads();
+    int above = upto - mine;
+    for (int i = 0; i < wave; ++i) above += s_waves[i];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (above < at.equal && at.equal <= above + c[i]) {
+            s_waves[THREADS / 64] = top - i;
+            s_waves[THREADS / 64 + 1] = above;
+        }
+        above += c[i];
+    }
+    __syncthreads();
+    at.word |= static_cast<uint32_t>(s_waves[THREADS / 64]) << digit_shift(pass);
+    at.equal -= s_waves[THREADS / 64 + 1];
+}
+
+// Batches of up to kMostRegisterRows rows: one workgroup a batch keeps the words in registers, KEYS a thread, finds the border and counts the
+// chunks.  Row i * 1024 + thread is a thread's i-th.
+template <int KEYS>
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths,
+                                                                     Rule r, int B, Workspace ws, int n_chunks, int n_groups,
+                                                                     int32_t* __restrict__ kept) {
+    constexpr int kWaves = kSelectThreads / 64;
+    __shared__ int s_bins[kBins];
+    __shared__ int s_waves[kWaves + 2];
+    const int b = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Border at = first_border(lengths, b, r);
+    const float* const w = weights + static_cast<int64_t>(b) * r.T;
+    float raw[KEYS];
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) raw[i] = w[min(i * kSelectThreads + static_cast<int>(threadIdx.x), r.T - 1)];
+    uint32_t x[KEYS];
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) x[i] = word_of(raw[i], i * kSelectThreads + static_cast<int>(threadIdx.x), at.held, r);
+    if (at.held > at.stay) {
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const uint32_t seen = seen_mask(pass), mask = digit_mask(pass);
+            const int shift = digit_shift(pass);
+            for (int i = threadIdx.x; i < kBins; i += kSelectThreads) s_bins[i] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i)
+                if (i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held && (x[i] & seen) == at.word)
+                    atomicAdd(&s_bins[(x[i] >> shift) & mask], 1);
+            __syncthreads();
+            find_digit<kSelectThreads>(s_bins, pass, at, s_waves);
+            __syncthreads();
+        }
+    }
+    // runs of 64 rows in order: run i * 16 + wave; above and equal in one word
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+        const bool here = i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held;
+        const unsigned long long above = __ballot(here && x[i] > at.word), equal = __ballot(here && x[i] == at.word);
+        if (lane == 0) s_bins[i * kWaves + wave] = static_cast<int>(__popcll(above) | (__popcll(equal) << 16));
+    }
+    __syncthreads();
+    if (wave < (KEYS * kWaves + 255) / 256) {  // a lane sums a chunk's four runs, a wave up to 64 chunks; waves behind the first sum those before
+        constexpr int kRunsPerChunk = kChunk / 64;
+        int2 before = {0, 0};
+        for (int v = 0; v < wave; ++v)
+            for (int q = 0; q < kRunsPerChunk; ++q) {
+                const int c = s_bins[(v * 64 + lane) * kRunsPerChunk + q];
+                before.x += c & 0xFFFF;
+                before.y += c >> 16;
+            }
+        before.x = lane_value(wave_prefix_sum(before.x), 63);
+        before.y = lane_value(wave_prefix_sum(before.y), 63);
+        const int chunk = wave * 64 + lane;
+        int2 mine = {0, 0};
+        if (chunk * kRunsPerChunk < KEYS * kWaves)
+            for (int q = 0; q < kRunsPerChunk; ++q) {
+                const int c = s_bins[chunk * kRunsPerChunk + q];
+                mine.x += c & 0xFFFF;
+                mine.y += c >> 16;
+            }
+        before.x += wave_prefix_sum(mine.x) - mine.x;
+        before.y += wave_prefix_sum(mine.y) - mine.y;
+        if (chunk < n_chunks) ws.chunks[static_cast<int64_t>(b) * n_chunks + chunk] = before;
+    }
+    if (static_cast<int>(threadIdx.x) < n_groups) ws.groups[static_cast<int64_t>(b) * n_groups + threadIdx.x] = {0, 0};  // counted from the batch's first row
+    for (int j = at.stay + static_cast<int>(threadIdx.x); j < r.n_keep; j += kSelectThreads) kept[static_cast<int64_t>(b) * r.n_keep + j] = -1;
+    if (threadIdx.x == 0) ws.borders[static_cast<int64_t>(kPasses) * B + b] = at;
+}
+
+// Longer batches: a workgroup a group of rows.  A kernel a digit adds its rows' digits up in the workspace; the next kernel's workgroups
+// each read the digit off the histogram.
+__global__ __launch_bounds__(kCountThreads) void evict_clear_kernel(const int32_t* __restrict__ lengths, Rule r, Workspace ws, int parts,
+                                                                   int32_t* __restrict__ kept) {
+    const int b = blockIdx.x / parts, part = blockIdx.x % parts;
+    int* const bins = ws.bins + static_cast<int64_t>(b) * kPasses * kBins;
+    for (int i = part * kCountThreads + static_cast<int>(threadIdx.x); i < kPasses * kBins; i += parts * kCountThreads) bins[i] = 0;
+    const int stay = first_border(lengths, b, r).stay;
+    for (int64_t j = stay + static_cast<int64_t>(part) * kCountThreads + threadIdx.x; j < r.n_keep; j += parts * kCountThreads)
+        kept[static_cast<int64_t>(b) * r.n_keep + j] = -1;
+}
+
+constexpr int kRowsPerThread = kGroup / kCountThreads;
+
+__device__ __forceinline__ void load_words(const float* __restrict__ w, int first, int held, const Rule& r, uint32_t (&x)[kRowsPerThread]) {
+    float raw[kRowsPerThread];
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i) raw[i] = w[min(first + i * kCountThreads, r.T - 1)];
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i) x[i] = word_of(raw[i], first + i * kCountThreads, held, r);
+}
+
+__global__ __launch_bounds__(kCountThreads) void evict_digits_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths, Rule r,
+                                                                    int B, int pass, Workspace ws, int n_groups) {
+    __shared__ int s_bins[kBins];
+    __shared__ int s_waves[kCountThreads / 64 + 2];
+    const int b = blockIdx.x / n_groups, group = blockIdx.x % n_groups;
+    Border at = first_border(lengths, b, r);
+    if (at.held <= at.stay || group * kGroup >= at.held) return;
+    if (pass == 2) at = ws.borders[static_cast<int64_t>(pass - 1) * B + b];
+    const int first = group * kGroup + static_cast<int>(threadIdx.x);
+    uint32_t x[kRowsPerThread];
+    load_words(weights + static_cast<int64_t>(b) * r.T, first, at.held, r, x);
+    for (int i = threadIdx.x; i < kBins; i += kCountThreads) s_bins[i] = 0;
+    int* const bins = ws.bins + static_cast<int64_t>(b) * kPasses * kBins;
+    if (pass > 0) {
+        find_digit<kCountThreads>(bins + (pass - 1) * kBins, pass - 1, at, s_waves);
+        if (group == 0 && threadIdx.x == 0) ws.borders[static_cast<int64_t>(pass) * B + b] = at;
+    }
+    __syncthreads();
+    const uint32_t seen = seen_mask(pass), mask = digit_mask(pass);
+    const int shift = digit_shift(pass);
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i)
+        if (first + i * kCountThreads < at.held && (x[i] & seen) == at.word) atomicAdd(&s_bins[(x[i] >> shift) & mask], 1);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kCountThreads)
+        if (s_bins[i]) atomicAdd(&bins[pass * kBins + i], s_bins[i]);
+}
+
+__global__ __launch_bounds__(kCountThreads) void evict_count_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths, Rule r,
+                                                                   int B, Workspace ws, int n_chunks, int n_groups) {
+    constexpr int kWaves = kCountThreads / 64;
+    static_assert(kRowsPerThread * kWaves == 64 && kGroupChunks == 16, "a run a lane, four a chunk");
+    __shared__ int s_waves[kWaves + 2];
+    __shared__ int s_runs[64];
+    const int b = blockIdx.x / n_groups, group = blockIdx.x % n_groups;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Border at = first_border(lengths, b, r);
+    if (at.held > at.stay) {
+        at = ws.borders[static_cast<int64_t>(kPasses - 1) * B + b];
+        find_digit<kCountThreads>(ws.bins + (static_cast<int64_t>(b) * kPasses + kPasses - 1) * kBins, kPasses - 1, at, s_waves);
+    }
+    const int first = group * kGroup + static_cast<int>(threadIdx.x);
+    uint32_t x[kRowsPerThread];
+    load_words(weights + static_cast<int64_t>(b) * r.T, first, at.held, r, x);
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i) {
+        const bool here = first + i * kCountThreads < at.held;
+        const unsigned long long above = __ballot(here && x[i] > at.word), equal = __ballot(here && x[i] == at.word);
+        if (lane == 0) s_runs[i * kWaves + wave] = static_cast<int>(__popcll(above) | (__popcll(equal) << 16));
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const int2 mine = {s_runs[lane] & 0xFFFF, s_runs[lane] >> 16};
+        const int2 upto = {wave_prefix_sum(mine.x), wave_prefix_sum(mine.y)};
+        const int chunk = group * kGroupChunks + lane / 4;
+        if (lane % 4 == 0 && chunk < n_chunks)
+            ws.chunks[static_cast<int64_t>(b) * n_chunks + chunk] = {upto.x - mine.x, upto.y - mine.y};
+        if (lane == 63) ws.groups[static_cast<int64_t>(b) * n_groups + group] = upto;
+    }
+    if (group == 0 && threadIdx.x == 0) ws.borders[static_cast<int64_t>(kPasses) * B + b] = at;
+}
+
+// Copies rows s_rows[0 .. n) of one array to n rows in a row, in units of type V, four of a thread on their way at once.
 template <typename V>
 __device__ __forceinline__ void copy_rows(const unsigned char* __restrict__ src, unsigned char* __restrict__ dst, int row_bytes,
                                           const int* s_rows, int n) {
-    const int units = row_bytes / static_cast<int>(sizeof(V));
-    const int64_t total = static_cast<int64_t>(n) * units;
-    for (int64_t i = threadIdx.x; i < total; i += kMoveThreads) {
-        const int j = static_cast<int>(i / units);
-        const int u = static_cast<int>(i - static_cast<int64_t>(j) * units);
-        reinterpret_cast<V*>(dst)[i] = reinterpret_cast<const V*>(src + static_cast<int64_t>(s_rows[j]) * row_bytes)[u];
+    const unsigned units = static_cast<unsigned>(row_bytes) / static_cast<unsigned>(sizeof(V));
+    constexpr int kAhead = 4;
+    if (units <= 4096) {
+        // i / units as a product: exact for i < 2^20 and units <= 2^12 (the excess of the factor adds less than 2^-12)
+        const unsigned inverse = static_cast<unsigned>(((1ull << 32) + units - 1) / units);
+        const unsigned total = static_cast<unsigned>(n) * units;
+        for (unsigned i0 = threadIdx.x; i0 < total; i0 += kAhead * kMoveThreads) {
+            V v[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const unsigned i = min(i0 + a * kMoveThreads, total - 1);
+                const unsigned j = units == 1 ? i : __umulhi(i, inverse);
+                v[a] = reinterpret_cast<const V*>(src + static_cast<int64_t>(s_rows[j]) * row_bytes)[i - j * units];
+            }
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a)
+                if (i0 + a * kMoveThreads < total) reinterpret_cast<V*>(dst)[i0 + a * kMoveThreads] = v[a];
+        }
+        return;
+    }
+    for (int j = 0; j < n; ++j) {  // rows longer than a workgroup's trip
+        const V* const from = reinterpret_cast<const V*>(src + static_cast<int64_t>(s_rows[j]) * row_bytes);
+        V* const to = reinterpret_cast<V*>(dst + static_cast<int64_t>(j) * row_bytes);
+        for (unsigned u = threadIdx.x; u < units; u += kMoveThreads) to[u] = from[u];
     }
 }
 
-__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* __restrict__ weights, int T, int n_keep, int n_sink,
-                                                                 int n_recent, int n_chunks, const Border* __restrict__ borders,
-                                                                 const int2* __restrict__ chunks, Moves moves, int32_t* __restrict__ kept) {
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* __restrict__ weights, Rule r, int B, Workspace ws, int n_chunks,
+                                                                 int n_groups, Moves moves, int32_t* __restrict__ kept,
+                                                                 int32_t* __restrict__ new_lengths) {
+    constexpr int kWaves = kMoveThreads / 64;
     __shared__ int s_rows[kChunk];
-    __shared__ int s_waves[2][kMoveThreads / 64];
+    __shared__ int s_waves[4][kWaves];
     static_assert(kChunk == kMoveThreads, "a thread a row");
     const int64_t b = blockIdx.x / n_chunks;
     const int c = static_cast<int>(blockIdx.x % n_chunks);
-    const Border border = borders[b];
+    const Border border = ws.borders[static_cast<int64_t>(kPasses) * B + b];
+    // lengths may be the same array: no kernel reads it any more
+    if (c == 0 && threadIdx.x == 0 && new_lengths) new_lengths[b] = border.stay;
     if (c * kChunk >= border.held) return;
-    const int2 before = chunks[b * n_chunks + c];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int row = c * kChunk + static_cast<int>(threadIdx.x);
-    uint32_t x = 0;
     const bool here = row < border.held;
-    if (here) x = word_of(weights[b * T + row], row, border.held, n_sink, n_recent);
+    uint32_t x = 0;
+    if (here) x = word_of(weights[b * r.T + row], row, border.held, r);
+    int2 before = {0, 0};  // of the groups before this one
+    for (int g = threadIdx.x; g < c / kGroupChunks; g += kMoveThreads) {
+        const int2 v = ws.groups[b * n_groups + g];
+        before.x += v.x;
+        before.y += v.y;
+    }
     const unsigned long long equal = __ballot(here && x == border.word);
-    if (lane == 0) s_waves[0][wave] = static_cast<int>(__popcll(equal));
+    before.x = wave_prefix_sum(before.x);
+    before.y = wave_prefix_sum(before.y);
+    if (lane == 63) {
+        s_waves[0][wave] = static_cast<int>(__popcll(equal));
+        s_waves[2][wave] = before.x;
+        s_waves[3][wave] = before.y;
+    }
     __syncthreads();
+    before = ws.chunks[b * n_chunks + c];
+    for (int i = 0; i < kWaves; ++i) {
+        before.x += s_waves[2][i];
+        before.y += s_waves[3][i];
+    }
     int rank = before.y + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(equal >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(equal), 0u));
     for (int i = 0; i < wave; ++i) rank += s_waves[0][i];
     const bool stays = here && (x > border.word || (x == border.word && rank < border.equal));
@@ -174,24 +335,45 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* _
     __syncthreads();
     int place = __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(mine >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(mine), 0u));
     int n = 0;
-    for (int i = 0; i < kMoveThreads / 64; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
         if (i < wave) place += s_waves[1][i];
         n += s_waves[1][i];
     }
+    const int64_t to = b * r.n_keep + before.x + min(before.y, border.equal);  // the chunk's first place
     if (stays) {
         s_rows[place] = row;
-        kept[b * n_keep + before.x + place] = row;
+        kept[to + place] = row;
     }
     __syncthreads();
+    if (n == 0) return;
     for (int a = 0; a < moves.n; ++a) {
         const int row_bytes = moves.row_bytes[a];
-        const unsigned char* const src = moves.src[a] + b * T * row_bytes;
-        unsigned char* const dst = moves.dst[a] + (b * n_keep + before.x) * row_bytes;
+        const unsigned char* const src = moves.src[a] + b * r.T * row_bytes;
+        unsigned char* const dst = moves.dst[a] + to * row_bytes;
         if (row_bytes % 16 == 0) copy_rows<uint4>(src, dst, row_bytes, s_rows, n);
         else if (row_bytes % 4 == 0) copy_rows<uint32_t>(src, dst, row_bytes, s_rows, n);
         else if (row_bytes % 2 == 0) copy_rows<uint16_t>(src, dst, row_bytes, s_rows, n);
         else copy_rows<unsigned char>(src, dst, row_bytes, s_rows, n);
     }
+}
+
+int chunks_of(int32_t T) { return static_cast<int>((static_cast<int64_t>(T) + kChunk - 1) / kChunk); }
+int groups_of(int32_t T) { return (chunks_of(T) + kGroupChunks - 1) / kGroupChunks; }
+
+Workspace carve(void* base, int32_t B, int32_t T) {
+    Workspace ws;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        void* p = static_cast<unsigned char*>(base) + at;
+        at += (bytes + 15) / 16 * 16;
+        return p;
+    };
+    ws.borders = static_cast<Border*>(take(static_cast<size_t>(kPasses + 1) * B * sizeof(Border)));
+    ws.bins = static_cast<int*>(take(T > kMostRegisterRows ? static_cast<size_t>(B) * kPasses * kBins * sizeof(int) : 0));
+    ws.chunks = static_cast<int2*>(take(static_cast<size_t>(B) * chunks_of(T) * sizeof(int2)));
+    ws.groups = static_cast<int2*>(take(static_cast<size_t>(B) * groups_of(T) * sizeof(int2)));
+    ws.bytes = at;
+    return ws;
 }
 
 struct Range {
@@ -200,8 +382,6 @@ struct Range {
 };
 bool overlap(const Range& x, const Range& y) { return x.begin < y.begin + y.bytes && y.begin < x.begin + x.bytes; }
 Range range_of(const void* p, size_t bytes) { return {reinterpret_cast<uintptr_t>(p), bytes}; }
-
-int chunks_of(int32_t T) { return static_cast<int>((static_cast<int64_t>(T) + kChunk - 1) / kChunk); }
 
 }  // namespace
 
@@ -213,7 +393,7 @@ extern "C" {
 
 size_t si_evict_workspace_bytes(int32_t B, int32_t T) {
     if (B < 1 || T < 1) return 0;
-    return static_cast<size_t>(B) * (sizeof(Border) + static_cast<size_t>(chunks_of(T)) * sizeof(int2));
+    return carve(nullptr, B, T).bytes;
 }
 
 si_status si_evict_rows(const float* weights, const int32_t* lengths, int32_t B, int32_t T, int32_t n_keep, int32_t n_sink,
@@ -255,15 +435,38 @@ si_status si_evict_rows(const float* weights, const int32_t* lengths, int32_t B,
         for (int j = 0; j < i; ++j)
             if (overlap(written[i], written[j])) return SI_ERR_INVALID_ARG;
     }
-    Border* const borders = static_cast<Border*>(workspace);
-    int2* const chunks = reinterpret_cast<int2*>(borders + B);
+    const Workspace ws = carve(workspace, B, T);
+    const int n_groups = groups_of(T);
+    const Rule r = {T, n_keep, n_sink, n_recent};
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(evict_select_kernel, dim3(B), dim3(kSelectThreads), 0, hs, weights, lengths, T, n_keep, n_sink, n_recent, n_chunks,
-                       borders, chunks, kept, new_lengths);
-    hipError_t e = hipGetLastError();
+    hipError_t e = hipSuccess;
+    if (T <= kMostRegisterRows) {
+#define SI_LAUNCH(KEYS)                                                                                                            \
+    hipLaunchKernelGGL((evict_select_kernel<KEYS>), dim3(B), dim3(kSelectThreads), 0, hs, weights, lengths, r, B, ws, n_chunks, n_groups, \
+                       kept)
+        if (T <= 4 * kSelectThreads) SI_LAUNCH(4);
+        else if (T <= 16 * kSelectThreads) SI_LAUNCH(16);
+        else SI_LAUNCH(32);
+#undef SI_LAUNCH
+        e = hipGetLastError();
+    } else {
+        const unsigned grid = static_cast<unsigned>(B) * static_cast<unsigned>(n_groups);
+        constexpr int kClearParts = 4;
+        hipLaunchKernelGGL(evict_clear_kernel, dim3(static_cast<unsigned>(B) * kClearParts), dim3(kCountThreads), 0, hs, lengths, r, ws,
+                           kClearParts, kept);
+        e = hipGetLastError();
+        for (int pass = 0; pass < kPasses && e == hipSuccess; ++pass) {
+            hipLaunchKernelGGL(evict_digits_kernel, dim3(grid), dim3(kCountThreads), 0, hs, weights, lengths, r, B, pass, ws, n_groups);
+            e = hipGetLastError();
+        }
+        if (e == hipSuccess) {
+            hipLaunchKernelGGL(evict_count_kernel, dim3(grid), dim3(kCountThreads), 0, hs, weights, lengths, r, B, ws, n_chunks, n_groups);
+            e = hipGetLastError();
+        }
+    }
     if (e == hipSuccess) {
         hipLaunchKernelGGL(evict_move_kernel, dim3(static_cast<unsigned>(B) * static_cast<unsigned>(n_chunks)), dim3(kMoveThreads), 0, hs,
-                           weights, T, n_keep, n_sink, n_recent, n_chunks, borders, chunks, mv, kept);
+                           weights, r, B, ws, n_chunks, n_groups, mv, kept, new_lengths);
         e = hipGetLastError();
     }
     return report(e);
