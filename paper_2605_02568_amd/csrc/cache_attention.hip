@@ -11,6 +11,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -280,69 +281,78 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     }
 }
 
-// What the rows of U(t) receive of a query: S[32 heads x 32 rows] = q . tile^T with the heads on the M side, so that a lane holds
-// 16 heads of one row and the sum over heads is in-lane (and one exchange).  The codes go from memory to a lane's registers as they are
-// needed there (row = lane % 32, values D/2 * (lane / 32) .. + D/2: the contraction order is permuted alike on the query) and from there to
-// bf16; no LDS but the list.  One workgroup = one query, its waves take every kWeightWaves-th tile, all heads each.
-//   S == 1: every row has one sum a call, added to weights;   S > 1: 64-bit fixed point in the workspace, in any order.
-constexpr int kWeightWaves = 4;
-constexpr double kFixedOne = 4294967296.0;  // 2^32
+// U(t) in tiles of 32 rows as they stand: the list's, then the window's; a lane knows its own row of a tile (row = lane % 32).
+struct Tiles {
+    const int32_t* list;
+    int k, held, w0, legal, list_tiles;
+    // The row of this lane in tile `tile`, -1 where U(t) has none there: a pad, an entry that the window has, the end of either.
+    __device__ __forceinline__ int row(int tile, int col) const {
+        if (tile < list_tiles) {  // uniform
+            const int j = tile * kTileKeys + col;
+            const int s = list[min(j, k - 1)];
+            return j < k && static_cast<unsigned>(s) < static_cast<unsigned>(held) && !(s >= w0 && s < legal) ? s : -1;
+        }
+        const int s = w0 + (tile - list_tiles) * kTileKeys + col;
+        return s < legal ? s : -1;
+    }
+    __device__ __forceinline__ int count() const { return list_tiles + (legal - w0 + kTileKeys - 1) / kTileKeys; }
+};
+__device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, int64_t row_q, int t, int k, int held, int n_win, int m, int mask_mode) {
+    Tiles u;
+    u.list = idx + row_q * k;
+    u.k = k;
+    u.held = held;
+    u.legal = legal_count(t, held, m, mask_mode);
+    u.w0 = max(0, u.legal - n_win);
+    u.list_tiles = (k + kTileKeys - 1) / kTileKeys;
+    return u;
+}
 
-template <int D, int HB>
-__global__ __launch_bounds__(64 * kWeightWaves)
-void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
-                               const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
-                               const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
-                               float scale_log2e, const float* __restrict__ lse, float* __restrict__ weights,
-                               unsigned long long* __restrict__ sums) {
+// What rows of U(t) receive of a query: S[32 heads x 32 rows] = q . tile^T with the heads on the M side, so that a lane holds 16 heads of
+// one row and the sum over heads is in-lane (and one exchange).  A lane's codes go from memory to its registers as they are needed there
+// (row = lane % 32, values D/2 * (lane / 32) .. + D/2: the contraction order is permuted alike on the query) and on to bf16, in which
+// both operands are exact: neither list nor tile goes through LDS.  The vector units bound it: 64 heads of 128 take 16 matrix instructions a
+// tile, 512 cycles, against 32 conversions, 32 fma, 32 additions and 32 exponentials at a quarter of their rate, 900.
+// One wave: tiles [first, last) of query row_q; add(row, sum) for every row of U(t) there, on the lanes below 32.  s_lse: 64 floats of the wave.
+template <int D, int HB, typename Add>
+__device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
+                                            const unsigned char* __restrict__ scales, const float* __restrict__ lse, int64_t row_q, int H,
+                                            int64_t first_row, const Tiles& u, int first, int last, float scale_log2e, float* s_lse, Add add) {
     constexpr int KS = D / 16;
     constexpr int kLoads = D / 64;  // 16-byte pieces of codes a lane holds of a row
-    extern __shared__ __attribute__((aligned(16))) int s_list[];
-    __shared__ int s_kept[kWeightWaves];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (first >= last) return;
     const int lane = threadIdx.x & 63;
     const int col = lane & 31;
     const int half = lane >> 5;
-    const int64_t row_q = blockIdx.x;
-    const int b = static_cast<int>(row_q / S);
-    const int t = static_cast<int>(row_q % S);
-    const int held = held_rows(lengths, b, T);
-    const int legal = legal_count(t, held, m, mask_mode);
-    const int w0 = max(0, legal - n_win);
-    const int n = build_list<kWeightWaves>(idx + row_q * k, k, held, w0, legal, s_list, s_kept);
-    __syncthreads();
-    const int n_u = __builtin_amdgcn_readfirstlane(n);
-    const int n_tiles = (n_u + kTileKeys - 1) / kTileKeys;
-    if (wave >= n_tiles) return;
-    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
-    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
-
+    const unsigned char* const codes_b = codes + first_row * (D / 2) + half * (D / 4);
+    const unsigned char* const scales_b = scales + first_row * (D / 32) + half * (D / 64);
     uintx4 run[kLoads];
     unsigned byte[kLoads];
-    auto read = [&](int tile) {
-        const int64_t row = s_list[tile * kTileKeys + col];
+    auto read = [&](int s) {
+        const int64_t row = max(s, 0);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             run[i] = *reinterpret_cast<const uintx4*>(codes_b + row * (D / 2) + i * 16);
             byte[i] = scales_b[row * (D / 32) + i];
         }
     };
-    read(wave);
-
-    bf16x8 qf[HB][KS];     // head 32 hb + col, values D/2 * half + 8 ks .. + 8
-    float minus_lse[HB][16];  // of the heads this lane's results belong to, log2 domain
+    int s_now = u.row(first, col);
+    int s_next = first + 1 < last ? u.row(first + 1, col) : -1;
+    s_lse[lane] = lane < H ? -kLog2e * lse[row_q * H + min(lane, H - 1)] : -__builtin_huge_valf();  // no head there: weight 0
+    bf16x8 qf[HB][KS];  // head 32 hb + col, values D/2 * half + 8 ks .. + 8
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
         const __bf16* src = qa + (row_q * H + min(32 * hb + col, H - 1)) * D + half * (D / 2);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[hb][ks] = *reinterpret_cast<const bf16x8*>(src + ks * 8);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int h = 32 * hb + 8 * (j >> 2) + 4 * half + (j & 3);
-            minus_lse[hb][j] = h < H ? -kLog2e * lse[row_q * H + h] : -__builtin_huge_valf();  // no head there: weight 0
-        }
     }
-    for (int tile = wave; tile < n_tiles; tile += kWeightWaves) {
+    read(s_now);
+    floatx4 minus_lse[HB][4];  // of the heads this lane's results belong to, log2 domain
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) minus_lse[hb][a] = *reinterpret_cast<const floatx4*>(s_lse + 32 * hb + 8 * a + 4 * half);
+    for (int tile = first; tile < last; ++tile) {
         bf16x8 kf[KS];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -357,7 +367,11 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
                 kf[4 * i + j] = bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
             }
         }
-        if (tile + kWeightWaves < n_tiles) read(tile + kWeightWaves);
+        const int s = s_now;
+        s_now = s_next;
+        if (tile + 1 < last) read(s_now);
+        if (tile + 2 < last) s_next = u.row(tile + 2, col);
+        if (__ballot(s >= 0) == 0ull) continue;
         float sum = 0.0f;
 #pragma unroll
         for (int hb = 0; hb < HB; ++hb) {
@@ -365,16 +379,74 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[hb][ks], kf[ks], acc, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j], scale_log2e, minus_lse[hb][j]));
+            for (int j = 0; j < 16; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j], scale_log2e, minus_lse[hb][j >> 2][j & 3]));
         }
         sum += other_half(sum);
-        const int place = tile * kTileKeys + col;
-        if (half == 0 && place < n_u) {
-            const int64_t at = static_cast<int64_t>(b) * T + s_list[place];
-            if (sums) atomicAdd(sums + at, static_cast<unsigned long long>(static_cast<double>(sum) * kFixedOne + 0.5));
-            else weights[at] += sum;
-        }
+        if (half == 0 && s >= 0) add(s, sum);
     }
+}
+
+// A sum in units of 2^-32, to the nearest: whole part and fraction apart, both exact in fp32.
+__device__ __forceinline__ unsigned long long to_fixed(float sum) {
+    const float whole = __builtin_truncf(sum);
+    const unsigned lo = static_cast<unsigned>(__builtin_rintf((sum - whole) * 4294967296.0f));
+    return (static_cast<unsigned long long>(static_cast<unsigned>(whole)) << 32) + lo;
+}
+
+constexpr int kWeightWaves = 4;
+// A wave takes `per` tiles of a query (n_parts such parts a query).  S == 1: every row has one sum a call, added to
+// weights;  S > 1: 64-bit sums in the workspace, in any order.
+template <int D, int HB>
+__global__ __launch_bounds__(64 * kWeightWaves)
+void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
+                               const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
+                               const int32_t* __restrict__ idx, int64_t n_items, int n_parts, int per, int S, int H, int T, int m, int mask_mode,
+                               int k, int n_win, float scale_log2e, const float* __restrict__ lse, float* __restrict__ weights,
+                               unsigned long long* __restrict__ sums) {
+    __shared__ __attribute__((aligned(16))) float s_lse[kWeightWaves][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * kWeightWaves + wave;
+    if (item >= n_items) return;
+    const int64_t row_q = item / n_parts;
+    const int part = static_cast<int>(item - row_q * n_parts);
+    const int b = static_cast<int>(row_q / S);
+    const int t = static_cast<int>(row_q - static_cast<int64_t>(b) * S);
+    const Tiles u = tiles_of(idx, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
+    const int64_t first_row = static_cast<int64_t>(b) * T;
+    weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, first_row, u, part * per, min(u.count(), (part + 1) * per), scale_log2e, s_lse[wave],
+                       [&](int s, float sum) {
+                           if (sums) atomicAdd(sums + first_row + s, to_fixed(sum));
+                           else weights[first_row + s] += sum;
+                       });
+}
+
+// Many queries of few rows: a workgroup adds up in LDS what its queries (every n_groups-th wave's worth of a batch) give the batch's rows,
+// and then adds that to the workspace, row after row.
+constexpr int kGatherWaves = 8;
+template <int D, int HB>
+__global__ __launch_bounds__(64 * kGatherWaves)
+void gather_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
+                           const int32_t* __restrict__ lengths, const int32_t* __restrict__ idx, int n_groups, int S, int H, int T, int m,
+                           int mask_mode, int k, int n_win, float scale_log2e, const float* __restrict__ lse,
+                           unsigned long long* __restrict__ sums) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __shared__ __attribute__((aligned(16))) float s_lse[kGatherWaves][64];
+    unsigned long long* const s_sums = reinterpret_cast<unsigned long long*>(lds);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.x / n_groups;
+    const int group = blockIdx.x % n_groups;
+    for (int i = threadIdx.x; i < T; i += 64 * kGatherWaves) s_sums[i] = 0;
+    __syncthreads();
+    const int held = held_rows(lengths, b, T);
+    for (int t = group * kGatherWaves + wave; t < S; t += n_groups * kGatherWaves) {
+        const int64_t row_q = static_cast<int64_t>(b) * S + t;
+        const Tiles u = tiles_of(idx, row_q, t, k, held, n_win, m, mask_mode);
+        weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, static_cast<int64_t>(b) * T, u, 0, u.count(), scale_log2e, s_lse[wave],
+                           [&](int s, float sum) { atomicAdd(s_sums + s, to_fixed(sum)); });
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < T; i += 64 * kGatherWaves)
+        if (s_sums[i]) atomicAdd(sums + static_cast<int64_t>(b) * T + i, s_sums[i]);
 }
 
 __global__ void clear_sums_kernel(unsigned long long* sums, int64_t n) {
@@ -383,7 +455,7 @@ __global__ void clear_sums_kernel(unsigned long long* sums, int64_t n) {
 }
 __global__ void add_sums_kernel(const unsigned long long* __restrict__ sums, int64_t n, float* __restrict__ weights) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
-        if (sums[i]) weights[i] = static_cast<float>(weights[i] + static_cast<double>(sums[i]) * (1.0 / kFixedOne));
+        if (sums[i]) weights[i] = static_cast<float>(weights[i] + static_cast<double>(sums[i]) * (1.0 / 4294967296.0));
 }
 
 struct Call {
@@ -409,12 +481,32 @@ hipError_t launch_attention(const Call& c, float* out, float* lse) {
     return hipGetLastError();
 }
 
+constexpr int kGatherRows = 16384;  // whose sums fit LDS: 128 KiB
+
 template <int D, int HB>
 hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsigned long long* sums) {
     const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
-    hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>(rows)), dim3(64 * kWeightWaves),
-                       list_bytes(c.k, c.n_win), c.stream, c.qa, c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m,
-                       c.mask_mode, c.k, c.n_win, c.scale_log2e, lse, weights, sums);
+    const int tiles = (c.k + kTileKeys - 1) / kTileKeys + (c.n_win + kTileKeys - 1) / kTileKeys;
+    // workgroups a batch, so that there are two a compute unit in all
+    const int n_groups = static_cast<int>(std::min<int64_t>((c.d.S + kGatherWaves - 1) / kGatherWaves, std::max(1, 512 / c.d.B)));
+    if (sums && c.d.T <= kGatherRows && static_cast<int64_t>(c.d.S) * (c.k + c.n_win) >= int64_t{2} * n_groups * c.d.T) {
+        static std::atomic<size_t> allowed[64];
+        const size_t lds = static_cast<size_t>(c.d.T) * sizeof(unsigned long long);
+        hipError_t e = allow_lds(gather_weights_kernel<D, HB>, lds, allowed);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((gather_weights_kernel<D, HB>), dim3(static_cast<unsigned>(c.d.B) * n_groups), dim3(64 * kGatherWaves), lds, c.stream,
+                           c.qa, c.codes, c.scales, c.lengths, c.idx, n_groups, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win,
+                           c.scale_log2e, lse, sums);
+        return hipGetLastError();
+    }
+    // parts of at least two tiles, as many as fill the chip's waves once
+    const int64_t most = std::max<int64_t>(1, 2048 / rows);
+    const int per = static_cast<int>(std::max<int64_t>(2, (tiles + most - 1) / most));
+    const int n_parts = std::max(1, (tiles + per - 1) / per);
+    const int64_t n_items = rows * n_parts;
+    hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>((n_items + kWeightWaves - 1) / kWeightWaves)),
+                       dim3(64 * kWeightWaves), 0, c.stream, c.qa, c.codes, c.scales, c.lengths, c.idx, n_items, n_parts, per, c.d.S, c.d.H_I,
+                       c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e, lse, weights, sums);
     return hipGetLastError();
 }
 
