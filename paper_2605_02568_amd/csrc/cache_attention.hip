@@ -48,14 +48,14 @@ __device__ __forceinline__ int held_rows(const int32_t* __restrict__ lengths, in
     return lengths ? min(max(lengths[b], 0), T) : T;
 }
 
-// This lane's part of a query's head (8 values at 16 ks + 8 half) as fp16, times a power of two that brings the head's largest
+// This lane's part of a query's head (8 values at STEP ks + HALF half) as fp16, times a power of two that brings the head's largest
 // magnitude into [2^14, 2^15), with the sign of the softmax scale; values down to 2^-32 of the largest stay exact.  Returns the factor that
 // takes a product of these operands to the log2 domain: |scale| log2(e) over that power.
-template <int KS>
-__device__ __forceinline__ float load_query(const __bf16* __restrict__ src, float scale_log2e, halfx8 (&qf)[KS]) {
+template <int KS, int STEP, int HALF>
+__device__ __forceinline__ float load_query(const __bf16* __restrict__ src, float scale_log2e, int half, halfx8 (&qf)[KS]) {
     uintx4 raw[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(src + ks * 16);
+    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(src + ks * STEP + half * HALF);
     unsigned top = 0;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -77,6 +77,67 @@ __device__ __forceinline__ float load_query(const __bf16* __restrict__ src, floa
             qf[ks][2 * j + 1] = pair[1];
         }
     return __builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up);
+}
+
+// Weights as two fp16 parts, p = hi + lo, each rounded to nearest; returns their sum.
+__device__ __forceinline__ float split_weights(const float (&p)[16], halfx8 (&hi)[2], halfx8 (&lo)[2]) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int jj = 0; jj < 8; ++jj) {
+        const float p0 = p[2 * jj], p1 = p[2 * jj + 1];
+        sum += p0 + p1;
+        const halfx2 a = __builtin_convertvector(floatx2{p0, p1}, halfx2);
+        const halfx2 r = __builtin_convertvector(floatx2{p0 - static_cast<float>(a[0]), p1 - static_cast<float>(a[1])}, halfx2);
+        hi[jj >> 2][2 * (jj & 3)] = a[0];
+        hi[jj >> 2][2 * (jj & 3) + 1] = a[1];
+        lo[jj >> 2][2 * (jj & 3)] = r[0];
+        lo[jj >> 2][2 * (jj & 3) + 1] = r[1];
+    }
+    return sum;
+}
+
+// O^T += tile^T . P^T : contraction index e of step u <-> tile row 16 u + 8 (e / 4) + 4 half + e % 4 on both operands.
+template <int D>
+__device__ __forceinline__ void add_values(const unsigned char* tb, const int (&va)[D / 32][2], const halfx8 (&p_hi)[2], const halfx8 (&p_lo)[2],
+                                           floatx16 (&acc)[D / 32]) {
+    typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+            const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][0] + u * 32 * D)));
+            const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][1] + u * 32 * D)));
+            const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_hi[u], acc[db], 0, 0, 0);
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_lo[u], acc[db], 0, 0, 0);
+        }
+}
+
+// U(t) in tiles of 32 rows as they stand: the list's, then the window's; a lane knows its own row of a tile (row = lane % 32).
+struct Tiles {
+    const int32_t* list;
+    int k, held, w0, legal, list_tiles;
+    // The row of this lane in tile `tile`, -1 where U(t) has none there: a pad, an entry that the window has, the end of either.
+    __device__ __forceinline__ int row(int tile, int col) const {
+        if (tile < list_tiles) {  // uniform
+            const int j = tile * kTileKeys + col;
+            const int s = list[min(j, k - 1)];
+            return j < k && static_cast<unsigned>(s) < static_cast<unsigned>(held) && !(s >= w0 && s < legal) ? s : -1;
+        }
+        const int s = w0 + (tile - list_tiles) * kTileKeys + col;
+        return s < legal ? s : -1;
+    }
+    __device__ __forceinline__ int count() const { return list_tiles + (legal - w0 + kTileKeys - 1) / kTileKeys; }
+};
+__device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, int64_t row_q, int t, int k, int held, int n_win, int m, int mask_mode) {
+    Tiles u;
+    u.list = idx + row_q * k;
+    u.k = k;
+    u.held = held;
+    u.legal = legal_count(t, held, m, mask_mode);
+    u.w0 = max(0, u.legal - n_win);
+    u.list_tiles = (k + kTileKeys - 1) / kTileKeys;
+    return u;
 }
 
 // One workgroup = one query; wave w owns heads [32 w, 32 w + 32), all waves share the tiles of 32 rows.  The codes of a tile are read
@@ -161,7 +222,7 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     read(0);
 
     halfx8 qf[KS];
-    const float to_log2 = load_query<KS>(qa + (row_q * H + min(h, H - 1)) * D + half * 8, scale_log2e, qf);
+    const float to_log2 = load_query<KS, 16, 8>(qa + (row_q * H + min(h, H - 1)) * D, scale_log2e, half, qf);
 
     // LDS byte offsets that do not depend on the tile (attention.hip says how the transposing reads are laid out)
     int ka[KS];
@@ -238,30 +299,9 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
             for (int j = 0; j < 16; ++j)
                 if (8 * (j >> 2) + 4 * half + (j & 3) >= live) p[j] = none;
         }
-        halfx8 p_hi[2], p_lo[2];  // p = hi + lo, each rounded to fp16
-#pragma unroll
-        for (int jj = 0; jj < 8; ++jj) {
-            const float p0 = p[2 * jj], p1 = p[2 * jj + 1];
-            l_sum += p0 + p1;
-            const halfx2 hi = __builtin_convertvector(floatx2{p0, p1}, halfx2);
-            const halfx2 lo = __builtin_convertvector(floatx2{p0 - static_cast<float>(hi[0]), p1 - static_cast<float>(hi[1])}, halfx2);
-            p_hi[jj >> 2][2 * (jj & 3)] = hi[0];
-            p_hi[jj >> 2][2 * (jj & 3) + 1] = hi[1];
-            p_lo[jj >> 2][2 * (jj & 3)] = lo[0];
-            p_lo[jj >> 2][2 * (jj & 3) + 1] = lo[1];
-        }
-        // O^T += tile^T . P^T : contraction index e of step u <-> tile row 16 u + 8 (e / 4) + 4 half + e % 4 on both operands
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
-                const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][0] + u * 16 * kRowBytes)));
-                const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][1] + u * 16 * kRowBytes)));
-                const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_hi[u], acc[db], 0, 0, 0);
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_lo[u], acc[db], 0, 0, 0);
-            }
+        halfx8 p_hi[2], p_lo[2];
+        l_sum += split_weights(p, p_hi, p_lo);
+        add_values<D>(tb, va, p_hi, p_lo, acc);
         __syncthreads();
     }
 
@@ -281,31 +321,186 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     }
 }
 
-// U(t) in tiles of 32 rows as they stand: the list's, then the window's; a lane knows its own row of a tile (row = lane % 32).
-struct Tiles {
-    const int32_t* list;
-    int k, held, w0, legal, list_tiles;
-    // The row of this lane in tile `tile`, -1 where U(t) has none there: a pad, an entry that the window has, the end of either.
-    __device__ __forceinline__ int row(int tile, int col) const {
-        if (tile < list_tiles) {  // uniform
-            const int j = tile * kTileKeys + col;
-            const int s = list[min(j, k - 1)];
-            return j < k && static_cast<unsigned>(s) < static_cast<unsigned>(held) && !(s >= w0 && s < legal) ? s : -1;
+// Few queries, which would leave most of the chip idle and walk their tiles one after the other: a workgroup takes one query and one block of 32
+// heads, and each of its waves every eighth tile, with a reference, sums and accumulators of its own; the waves' results are joined at the end.  A
+// wave's rows are read straight into its registers (a lane's row is lane % 32 of the tile, its values D/2 * (lane / 32) .. + D/2), where they are
+// the first product's operand as they are (the contraction order is permuted alike on the query); only for the second product they go
+// through LDS, into a tile of the wave's own: no wave waits for another until the end.
+// Dynamic LDS: a tile of 32 x D fp16 a wave, and the joined heads: 32 x (D + 1) floats a wave.
+constexpr int kFewWaves = 8;
+template <int D>
+constexpr int few_lds_bytes() { return kFewWaves * kTileKeys * D * 4; }
+template <int D>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
+                                    const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
+                                    const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
+                                    int head_blocks, float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
+    constexpr int W = kFewWaves;
+    constexpr int KS = D / 16;
+    constexpr int DB = D / 32;
+    constexpr int kLoads = D / 64;  // 16-byte pieces of codes a lane holds of a row
+    constexpr int kRowBytes = D * 2;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    __shared__ float s_ref[W][32], s_sum[W][32];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int col = lane & 31;
+    const int half = lane >> 5;
+    const int64_t row_q = blockIdx.x / head_blocks;
+    const int h0 = 32 * static_cast<int>(blockIdx.x % head_blocks);
+    const int b = static_cast<int>(row_q / S);
+    const int t = static_cast<int>(row_q - static_cast<int64_t>(b) * S);
+    const Tiles u = tiles_of(idx, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
+    const int n_tiles = u.count();
+    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
+    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
+    uintx4 run[kLoads];
+    unsigned byte[kLoads];
+    auto read = [&](int s) {
+        const int64_t row = max(s, 0);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            run[i] = *reinterpret_cast<const uintx4*>(codes_b + row * (D / 2) + i * 16);
+            byte[i] = scales_b[row * (D / 32) + i];
         }
-        const int s = w0 + (tile - list_tiles) * kTileKeys + col;
-        return s < legal ? s : -1;
+    };
+    int s_now = wave < n_tiles ? u.row(wave, col) : -1;
+    int s_next = wave + W < n_tiles ? u.row(wave + W, col) : -1;
+    halfx8 qf[KS];
+    const float to_log2 = load_query<KS, 8, D / 2>(qa + (row_q * H + min(h0 + col, H - 1)) * D, scale_log2e, half, qf);
+    read(s_now);
+
+    unsigned char* const tb = lds + wave * kTileKeys * kRowBytes;
+    int put[D / 16];  // where the lane's pieces of its row go
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) put[i] = tile_slot<D>(col, half * (D / 16) + i) * 16;
+    int va[DB][2];
+    {
+        const int G = lane >> 4, s = lane & 15;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int r = 8 * w + 4 * (G >> 1) + (s >> 2);
+                const int d = 32 * db + 16 * (G & 1) + 4 * (s & 3);
+                va[db][w] = tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
+            }
     }
-    __device__ __forceinline__ int count() const { return list_tiles + (legal - w0 + kTileKeys - 1) / kTileKeys; }
-};
-__device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, int64_t row_q, int t, int k, int held, int n_win, int m, int mask_mode) {
-    Tiles u;
-    u.list = idx + row_q * k;
-    u.k = k;
-    u.held = held;
-    u.legal = legal_count(t, held, m, mask_mode);
-    u.w0 = max(0, u.legal - n_win);
-    u.list_tiles = (k + kTileKeys - 1) / kTileKeys;
-    return u;
+    floatx16 acc[DB];
+    const floatx16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = zero16;
+    float m_ref = -__builtin_huge_valf();
+    float l_sum = 0.0f;
+
+    for (int tile = wave; tile < n_tiles; tile += W) {
+        halfx8 kf[KS];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const float power = power_of(byte[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned c = run[i][j];
+                const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 0);
+                const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 1);
+                const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 2);
+                const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 3);
+                kf[4 * i + j] = halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+            }
+        }
+        const unsigned live = static_cast<unsigned>(__ballot(s_now >= 0));  // bit r: row r of the tile is in U(t)
+        s_now = s_next;
+        if (tile + W < n_tiles) read(s_now);
+        if (tile + 2 * W < n_tiles) s_next = u.row(tile + 2 * W, col);
+        if (live == 0) continue;
+        // the wave's LDS accesses are done in order: the transposing reads of the tile before come first, those of this one after
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<halfx8*>(tb + put[i]) = kf[i];
+        floatx16 sacc = zero16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sacc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], sacc, 0, 0, 0);
+        if (live != 0xFFFFFFFFu) {
+            float low = -3.0e38f;
+            asm volatile("" : "+v"(low));
+            const unsigned mine = live >> (4 * half);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) sacc[j] = low;
+        }
+        float smax = sacc[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) smax = fmaxf(smax, sacc[j]);
+        // finite: some row of the tile is live (with a scale of 0 rows that are not would weigh as much: they are taken out below)
+        float tmax = smax * to_log2;
+        tmax = fmaxf(tmax, other_half(tmax));
+        const bool raise = tmax > m_ref + kRescaleSlack;
+        if (__ballot(raise) != 0ull) {
+            const float m_new = raise ? tmax : m_ref;
+            const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
+            l_sum *= alpha;
+            m_ref = m_new;
+        }
+        const float shift = kWeightShift - m_ref;
+        float p[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[j], to_log2, shift));
+        if (live != 0xFFFFFFFFu) {
+            float none = 0.0f;
+            asm volatile("" : "+v"(none));
+            const unsigned mine = live >> (4 * half);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) p[j] = none;
+        }
+        halfx8 p_hi[2], p_lo[2];
+        l_sum += split_weights(p, p_hi, p_lo);
+        add_values<D>(tb, va, p_hi, p_lo, acc);
+    }
+
+    // ---- join: the largest reference of the waves, sums and accumulators brought to it
+    if (half == 0) s_ref[wave][col] = m_ref;
+    l_sum += other_half(l_sum);
+    if (half == 0) s_sum[wave][col] = l_sum;
+    __syncthreads();  // also: every wave is done with its tile
+    float m_all = s_ref[0][col];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m_all = fmaxf(m_all, s_ref[w][col]);
+    const float alpha = m_ref == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m_ref - m_all);
+    // [wave][piece of four d][head], so that both the stores and the loads of a wave go through all banks
+    floatx4* const s_acc = reinterpret_cast<floatx4*>(lds);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const floatx4 v = {acc[db][4 * a] * alpha, acc[db][4 * a + 1] * alpha, acc[db][4 * a + 2] * alpha, acc[db][4 * a + 3] * alpha};
+            s_acc[(wave * (D / 4) + 8 * db + 2 * a + half) * 32 + col] = v;
+        }
+    __syncthreads();
+    float l_all = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const float r = s_ref[w][col];
+        l_all += r == -__builtin_huge_valf() ? 0.0f : s_sum[w][col] * __builtin_amdgcn_exp2f(r - m_all);
+    }
+    const float inv = l_all > 0.0f ? 1.0f / l_all : 0.0f;
+    const int h = h0 + col;
+    if (h < H) {
+#pragma unroll
+        for (int i = 0; i < D / 4 / (2 * W); ++i) {
+            const int piece = i * 2 * W + 2 * wave + half;
+            floatx4 v = s_acc[piece * 32 + col];
+#pragma unroll
+            for (int w = 1; w < W; ++w) v += s_acc[(w * (D / 4) + piece) * 32 + col];
+            *reinterpret_cast<floatx4*>(out + (row_q * H + h) * D + 4 * piece) = v * inv;
+        }
+        if (lse && wave == 0 && half == 0)
+            lse[row_q * H + h] = l_all > 0.0f ? (m_all - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2 : -__builtin_huge_valf();
+    }
 }
 
 // What rows of U(t) receive of a query: S[32 heads x 32 rows] = q . tile^T with the heads on the M side, so that a lane holds 16 heads of
@@ -481,6 +676,22 @@ hipError_t launch_attention(const Call& c, float* out, float* lse) {
     return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_few(const Call& c, float* out, float* lse) {
+    static std::atomic<size_t> allowed[64];
+    hipError_t e = allow_lds(quantized_attention_few_kernel<D>, few_lds_bytes<D>(), allowed);
+    if (e != hipSuccess) return e;
+    const int head_blocks = (c.d.H_I + 31) / 32;
+    const int64_t grid = static_cast<int64_t>(c.d.B) * c.d.S * head_blocks;
+    hipLaunchKernelGGL((quantized_attention_few_kernel<D>), dim3(static_cast<unsigned>(grid)), dim3(64 * kFewWaves), few_lds_bytes<D>(), c.stream,
+                       c.qa, c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, head_blocks,
+                       c.scale_log2e, out, lse);
+    return hipGetLastError();
+}
+
+// One round of the chip's compute units.
+bool few_queries(const si_dims& d) { return static_cast<int64_t>(d.B) * d.S * ((d.H_I + 31) / 32) <= 256; }
+
 constexpr int kGatherRows = 16384;  // whose sums fit LDS: 128 KiB
 
 template <int D, int HB>
@@ -541,6 +752,7 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
     const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
                     lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
     const bool two = dims->H_I > 32;
+    if (few_queries(*dims)) return report(dims->D == 128 ? launch_few<128>(c, out, lse) : launch_few<64>(c, out, lse));
     return report(dims->D == 128 ? (two ? launch_attention<128, 2>(c, out, lse) : launch_attention<128, 1>(c, out, lse))
                                  : (two ? launch_attention<64, 2>(c, out, lse) : launch_attention<64, 1>(c, out, lse)));
 }
