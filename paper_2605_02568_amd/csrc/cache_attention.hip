@@ -79,19 +79,68 @@ __device__ __forceinline__ float load_query(const __bf16* __restrict__ src, floa
     return __builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up);
 }
 
-// Weights as two fp16 parts, p = hi + lo, each rounded to nearest; returns their sum.
-__device__ __forceinline__ float split_weights(const float (&p)[16], halfx8 (&hi)[2], halfx8 (&lo)[2]) {
-    float sum = 0.0f;
+// Weights as two fp16 parts, p = hi + lo, each rounded to nearest.  The remainder is an fma that takes hi as it is and rounds to fp16 at once:
+// three instructions a pair of weights (the factor 1 comes from a register, as the compiler would otherwise convert hi, subtract and convert).
+__device__ __forceinline__ void split_weights(const float (&p)[16], halfx8 (&hi)[2], halfx8 (&lo)[2]) {
+    float one = 1.0f;
+    asm("" : "+s"(one));
 #pragma unroll
     for (int jj = 0; jj < 8; ++jj) {
         const float p0 = p[2 * jj], p1 = p[2 * jj + 1];
-        sum += p0 + p1;
         const halfx2 a = __builtin_convertvector(floatx2{p0, p1}, halfx2);
-        const halfx2 r = __builtin_convertvector(floatx2{p0 - static_cast<float>(a[0]), p1 - static_cast<float>(a[1])}, halfx2);
         hi[jj >> 2][2 * (jj & 3)] = a[0];
         hi[jj >> 2][2 * (jj & 3) + 1] = a[1];
-        lo[jj >> 2][2 * (jj & 3)] = r[0];
-        lo[jj >> 2][2 * (jj & 3) + 1] = r[1];
+        lo[jj >> 2][2 * (jj & 3)] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[0]), one, p0));
+        lo[jj >> 2][2 * (jj & 3) + 1] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[1]), one, p1));
+    }
+}
+
+// Weights of a tile's rows for one head, 2^7 exp2(x - m_ref) with x = to_log2 * s, and their sum over this half-wave's rows; `live`: bit r says whether
+// row r of the tile counts.  m_ref is some earlier tile's maximum.  Whether it still does is read off the sum, which is needed anyway: only where a
+// head's weights exceed 2^15 in sum (m_ref too low, or still -inf) the tile's maximum is taken, m_ref raised to it, and what was
+// accumulated brought down: raise(alpha).  Every tile's maximum and its exchange between the half-waves would cost 13 instructions and
+// the wait for them before the first exponential.
+template <typename Raise>
+__device__ __forceinline__ float weigh(floatx16& s, float to_log2, unsigned live, int half, float& m_ref, float (&p)[16], Raise raise) {
+    if (live != 0xFFFFFFFFu) {  // the last tile, or one with pads
+        float low = -3.0e38f;
+        asm volatile("" : "+v"(low));  // keeps this block a branch instead of 16 selects per tile
+        const unsigned mine = live >> (4 * half);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) s[j] = low;
+    }
+    float sum;
+    auto exponentials = [&]() {
+        const float shift = kWeightShift - m_ref;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], to_log2, shift));
+        if (live != 0xFFFFFFFFu) {  // a scale of 0 takes no row out
+            float none = 0.0f;
+            asm volatile("" : "+v"(none));
+            const unsigned mine = live >> (4 * half);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) p[j] = none;
+        }
+        sum = p[0] + p[1];
+#pragma unroll
+        for (int j = 2; j < 16; ++j) sum += p[j];
+    };
+    exponentials();
+    const bool over = !(sum <= 32768.0f);
+    if (__ballot(over) != 0ull) {
+        float top = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+        top *= to_log2;
+        top = fmaxf(top, other_half(top));  // of the head: both half-waves decide alike
+        const float theirs = other_half(over ? 1.0f : 0.0f);  // outside of the condition below: every lane takes part in the exchange
+        const bool up = over || theirs != 0.0f;
+        const float m_new = up ? fmaxf(top, m_ref) : m_ref;
+        raise(__builtin_amdgcn_exp2f(m_ref - m_new));  // 1 where nothing changes, 0 on the first tile
+        m_ref = m_new;
+        exponentials();
     }
     return sum;
 }
@@ -201,7 +250,8 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
             byte[u] = scales_b[row * (D / 32) + at * kVals / 32];
         }
     };
-    auto lay = [&](unsigned char* tb) {
+    auto lay = [&](auto buf_tag) {
+        unsigned char* const tb = lds + decltype(buf_tag)::value * kTileBytes;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int unit = u * 64 * HW + static_cast<int>(threadIdx.x);
@@ -248,11 +298,13 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     float m_ref = -__builtin_huge_valf();  // reference maximum of this lane's head (log2 domain)
     float l_sum = 0.0f;                    // sum of the weights over this half-wave's rows
 
-    lay(lds);
+    lay(std::integral_constant<int, 0>{});
     if (n_tiles > 1) read(1);
     __syncthreads();
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        const unsigned char* tb = lds + (tile & 1) * kTileBytes;
+    // One tile; the buffer is a compile-time constant so that every LDS address is a loop-invariant register plus an immediate offset.
+    auto step = [&](int tile, auto buf_tag) {
+        constexpr int buf = decltype(buf_tag)::value;
+        const unsigned char* tb = lds + buf * kTileBytes;
         // S^T : register j of a lane = row 8 (j / 4) + 4 half + j % 4, head = col
         floatx16 sacc = zero16;
 #pragma unroll
@@ -261,48 +313,26 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
             sacc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[ks], sacc, 0, 0, 0);
         }
         // the next tile into the other buffer, which everybody left at the last barrier
-        if (tile + 1 < n_tiles) lay(lds + ((tile + 1) & 1) * kTileBytes);
+        if (tile + 1 < n_tiles) lay(std::integral_constant<int, buf ^ 1>{});
         if (tile + 2 < n_tiles) read(tile + 2);
-        const int live = n_u - tile * kTileKeys;
-        const bool ragged = live < kTileKeys;  // rows past the end of U(t), in the last tile
-        if (ragged) {
-            float low = -3.0e38f;
-            asm volatile("" : "+v"(low));  // keeps this block a branch instead of 16 selects per tile
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (8 * (j >> 2) + 4 * half + (j & 3) >= live) sacc[j] = low;  // out of the maximum; weight zeroed below
-        }
-        float smax = sacc[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) smax = fmaxf(smax, sacc[j]);
-        float tmax = smax * to_log2;
-        tmax = fmaxf(tmax, other_half(tmax));  // finite: row 0 of a tile is live
-        const bool raise = tmax > m_ref + kRescaleSlack;
-        if (__ballot(raise) != 0ull) {
-            const float m_new = raise ? tmax : m_ref;
-            const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+        const int left = n_u - tile * kTileKeys;  // rows of U(t) from this tile on
+        const unsigned live = left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
+        float p[16];
+        l_sum += weigh(sacc, to_log2, live, half, m_ref, p, [&](float alpha) {
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
             l_sum *= alpha;
-            m_ref = m_new;
-        }
-        const float shift = kWeightShift - m_ref;
-        float p[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[j], to_log2, shift));
-        if (ragged) {
-            float none = 0.0f;
-            asm volatile("" : "+v"(none));
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (8 * (j >> 2) + 4 * half + (j & 3) >= live) p[j] = none;
-        }
+        });
         halfx8 p_hi[2], p_lo[2];
-        l_sum += split_weights(p, p_hi, p_lo);
+        split_weights(p, p_hi, p_lo);
         add_values<D>(tb, va, p_hi, p_lo, acc);
         __syncthreads();
+    };
+    for (int tile = 0; tile < n_tiles; tile += 2) {
+        step(tile, std::integral_constant<int, 0>{});
+        if (tile + 1 < n_tiles) step(tile + 1, std::integral_constant<int, 1>{});
     }
 
     // ---- out[t, head, d] = O^T[d, head] / l : register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4
@@ -420,45 +450,16 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
         floatx16 sacc = zero16;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) sacc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], sacc, 0, 0, 0);
-        if (live != 0xFFFFFFFFu) {
-            float low = -3.0e38f;
-            asm volatile("" : "+v"(low));
-            const unsigned mine = live >> (4 * half);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) sacc[j] = low;
-        }
-        float smax = sacc[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) smax = fmaxf(smax, sacc[j]);
-        // finite: some row of the tile is live (with a scale of 0 rows that are not would weigh as much: they are taken out below)
-        float tmax = smax * to_log2;
-        tmax = fmaxf(tmax, other_half(tmax));
-        const bool raise = tmax > m_ref + kRescaleSlack;
-        if (__ballot(raise) != 0ull) {
-            const float m_new = raise ? tmax : m_ref;
-            const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+        float p[16];
+        l_sum += weigh(sacc, to_log2, live, half, m_ref, p, [&](float alpha) {
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
             l_sum *= alpha;
-            m_ref = m_new;
-        }
-        const float shift = kWeightShift - m_ref;
-        float p[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[j], to_log2, shift));
-        if (live != 0xFFFFFFFFu) {
-            float none = 0.0f;
-            asm volatile("" : "+v"(none));
-            const unsigned mine = live >> (4 * half);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) p[j] = none;
-        }
+        });
         halfx8 p_hi[2], p_lo[2];
-        l_sum += split_weights(p, p_hi, p_lo);
+        split_weights(p, p_hi, p_lo);
         add_values<D>(tb, va, p_hi, p_lo, acc);
     }
 
