@@ -76,7 +76,8 @@ __device__ __forceinline__ float load_query(const __bf16* __restrict__ src, floa
             qf[ks][2 * j] = pair[0];
             qf[ks][2 * j + 1] = pair[1];
         }
-    return __builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up);
+    // not 0, so that -inf times it is -inf: a logit that such a factor makes is 0 either way
+    return fmaxf(__builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up), 1.1754944e-38f);
 }
 
 // Weights as two fp16 parts, p = hi + lo, each rounded to nearest.  The remainder is an fma that takes hi as it is and rounds to fp16 at once:
@@ -102,8 +103,8 @@ __device__ __forceinline__ void split_weights(const float (&p)[16], halfx8 (&hi)
 // the wait for them before the first exponential.
 template <typename Raise>
 __device__ __forceinline__ float weigh(floatx16& s, float to_log2, unsigned live, int half, float& m_ref, float (&p)[16], Raise raise) {
-    if (live != 0xFFFFFFFFu) {  // the last tile, or one with pads
-        float low = -3.0e38f;
+    if (live != 0xFFFFFFFFu) {  // the last tile, or one with pads: their weights become 0 (to_log2 is never 0)
+        float low = -__builtin_huge_valf();
         asm volatile("" : "+v"(low));  // keeps this block a branch instead of 16 selects per tile
         const unsigned mine = live >> (4 * half);
 #pragma unroll
@@ -115,20 +116,12 @@ __device__ __forceinline__ float weigh(floatx16& s, float to_log2, unsigned live
         const float shift = kWeightShift - m_ref;
 #pragma unroll
         for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], to_log2, shift));
-        if (live != 0xFFFFFFFFu) {  // a scale of 0 takes no row out
-            float none = 0.0f;
-            asm volatile("" : "+v"(none));
-            const unsigned mine = live >> (4 * half);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) p[j] = none;
-        }
         sum = p[0] + p[1];
 #pragma unroll
         for (int j = 2; j < 16; ++j) sum += p[j];
     };
     exponentials();
-    const bool over = !(sum <= 32768.0f);
+    const bool over = !(sum <= 32768.0f);  // also where the first tile's rows that do not count gave inf - inf
     if (__ballot(over) != 0ull) {
         float top = s[0];
 #pragma unroll
@@ -143,23 +136,6 @@ __device__ __forceinline__ float weigh(floatx16& s, float to_log2, unsigned live
         exponentials();
     }
     return sum;
-}
-
-// O^T += tile^T . P^T : contraction index e of step u <-> tile row 16 u + 8 (e / 4) + 4 half + e % 4 on both operands.
-template <int D>
-__device__ __forceinline__ void add_values(const unsigned char* tb, const int (&va)[D / 32][2], const halfx8 (&p_hi)[2], const halfx8 (&p_lo)[2],
-                                           floatx16 (&acc)[D / 32]) {
-    typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-            const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][0] + u * 32 * D)));
-            const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + va[db][1] + u * 32 * D)));
-            const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_hi[u], acc[db], 0, 0, 0);
-            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_lo[u], acc[db], 0, 0, 0);
-        }
 }
 
 // U(t) in tiles of 32 rows as they stand: the list's, then the window's; a lane knows its own row of a tile (row = lane % 32).
@@ -189,28 +165,135 @@ __device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, int64
     return u;
 }
 
-// One workgroup = one query; wave w owns heads [32 w, 32 w + 32), all waves share the tiles of 32 rows.  The codes of a tile are read
-// two tiles ahead into registers, turned into fp16 once for all waves and laid in LDS, row-major and swizzled (attention_set.h); from there
-// on a tile's steps are those of sparse_attention_kernel in attention.hip:
-//   S^T[32 rows x 32 heads] = tile . q^T, weights against a running reference, O^T[D x 32 heads] += tile^T . P^T.
-// Dynamic LDS: 2 tiles of 32 x D fp16, the query's list.
+// A lane's part of the tiles of 32 rows that its wave takes: row lane % 32, values D/2 * (lane / 32) .. + D/2, read from memory as codes and
+// scale bytes.  As fp16 they are the first product's operand as they are (the contraction order is permuted alike on the query); for the
+// second one they go through LDS, into a tile of the wave's own, row-major and swizzled (attention_set.h).  A wave's LDS accesses are done in
+// order, so no wave waits for another.
+// The scale bytes stay as they were read until they are used: taken apart at once they would be waited for at once.
+template <int D>
+struct Rows {
+    static constexpr int kLoads = D / 64;  // 16-byte pieces of codes, a scale byte each
+    uintx4 run[kLoads];
+    std::conditional_t<D == 128, uint16_t, uint8_t> bytes;
+    __device__ __forceinline__ void read(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, int64_t row) {
+        bytes = *reinterpret_cast<const decltype(bytes)*>(scales + row * (D / 32));
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) run[i] = *reinterpret_cast<const uintx4*>(codes + row * (D / 2) + i * 16);
+    }
+    __device__ __forceinline__ float power(int i) const { return power_of((static_cast<unsigned>(bytes) >> (8 * i)) & 0xFFu); }
+    // values 8 ks .. 8 ks + 8 of the lane's part
+    __device__ __forceinline__ halfx8 values(int ks) const {
+        const float p = power(ks / 4);
+        const unsigned c = run[ks / 4][ks % 4];
+        const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 0);
+        const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 1);
+        const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 2);
+        const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
+        return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    }
+    // the same in bf16
+    __device__ __forceinline__ bf16x8 values_bf16(int ks) const {
+        const float p = power(ks / 4);
+        const unsigned c = run[ks / 4][ks % 4];
+        const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 0);
+        const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 1);
+        const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 2);
+        const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 3);
+        return bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    }
+};
+
+// LDS offsets of a wave's tile at `base` (a multiple of 2 D): where the lane's pieces of its row go, and the transposing reads (attention.hip
+// says how these are laid out).  The swizzle takes numbers of pieces apart by exclusive or, so all offsets of a kind are one register's with bits
+// turned over: a piece's is put ^ 16 i.
+template <int D>
+struct Places {
+    static constexpr int kReads = 4;
+    int put, va[kReads];
+    __device__ __forceinline__ Places(int lane, int base) {
+        const int col = lane & 31, half = lane >> 5;
+        put = base + tile_slot<D>(col, half * (D / 16)) * 16;
+        const int G = lane >> 4, s = lane & 15;
+        const int r = 4 * (G >> 1) + (s >> 2), d = 16 * (G & 1) + 4 * (s & 3);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            if (D == 128) va[i] = base + tile_slot<D>(r, (32 * i + d) / 8) * 16 + ((d % 8) / 4) * 8;
+            else va[i] = base + tile_slot<D>(r + 8 * (i & 1), (32 * (i >> 1) + d) / 8) * 16 + ((d % 8) / 4) * 8;
+        }
+    }
+    __device__ __forceinline__ int put_at(int i) const { return put ^ (16 * i); }
+    // d block db, rows 8 w + ..: for D = 128 row + 8 turns over the piece's bit 3, which is the block's bit 1
+    __device__ __forceinline__ int read_at(int db, int w) const { return D == 128 ? va[db ^ (2 * w)] + w * 8 * 2 * D : va[2 * db + w]; }
+};
+
+// O^T += tile^T . P^T : contraction index e of step u <-> tile row 16 u + 8 (e / 4) + 4 half + e % 4 on both operands.
+template <int D>
+__device__ __forceinline__ void add_values(const unsigned char* tb, const Places<D>& at, const halfx8 (&p_hi)[2], const halfx8 (&p_lo)[2],
+                                           floatx16 (&acc)[D / 32]) {
+    typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+            const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + at.read_at(db, 0) + u * 32 * D)));
+            const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(tb + at.read_at(db, 1) + u * 32 * D)));
+            const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_hi[u], acc[db], 0, 0, 0);
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p_lo[u], acc[db], 0, 0, 0);
+        }
+}
+
+// What a wave has of a query's block of 32 heads: O^T (register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4, head = lane % 32),
+// reference maximum of the lane's head (log2 domain) and the sum of the weights over the half-wave's rows.
+template <int D>
+struct Heads {
+    floatx16 acc[D / 32];
+    float m_ref, l_sum;
+    __device__ __forceinline__ Heads() : m_ref(-__builtin_huge_valf()), l_sum(0.0f) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[db][j] = 0.0f;
+    }
+    // The scores of a tile, whose rows go to LDS on the way: after this `rows` may be read anew, while the rest of the tile's steps run.
+    __device__ __forceinline__ floatx16 scores(const Rows<D>& rows, const halfx8 (&qf)[D / 16], unsigned char* lds, const Places<D>& at) const {
+        floatx16 s = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            const halfx8 v = rows.values(ks);
+            *reinterpret_cast<halfx8*>(lds + at.put_at(ks)) = v;
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, qf[ks], s, 0, 0, 0);
+        }
+        return s;
+    }
+    // Weights and second product; `live`: bit r says whether row r of the tile counts (not 0).
+    __device__ __forceinline__ void take(floatx16& s, unsigned live, float to_log2, int half, const unsigned char* lds, const Places<D>& at) {
+        float p[16];
+        l_sum += weigh(s, to_log2, live, half, m_ref, p, [&](float alpha) {
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
+            l_sum *= alpha;
+        });
+        halfx8 p_hi[2], p_lo[2];
+        split_weights(p, p_hi, p_lo);
+        add_values<D>(lds, at, p_hi, p_lo, acc);
+    }
+};
+
+// One workgroup = one query; wave w owns heads [32 w, 32 w + 32) and goes through the query's list (attention_set.h) by itself.
+// Dynamic LDS: a tile of 32 x D fp16 a wave, the list.
 template <int D, int HW>
-__global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(3)))
 void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                 const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
                                 const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
                                 float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
-    constexpr int KS = D / 16;
     constexpr int DB = D / 32;
-    constexpr int kRowBytes = D * 2;
-    constexpr int kTileBytes = kTileKeys * kRowBytes;
-    // a thread turns kUnits runs of kVals values of a tile into fp16
-    constexpr int kVals = D / (2 * HW) < 32 ? D / (2 * HW) : 32;
-    constexpr int kUnits = D / (2 * HW) / kVals;
-    constexpr int kRuns = D / kVals;  // of a row
-    static_assert(kVals == 16 || kVals == 32, "a run lies in one block of 32");
+    constexpr int kTileBytes = kTileKeys * D * 2;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    int* const s_list = reinterpret_cast<int*>(lds + 2 * kTileBytes);
+    int* const s_list = reinterpret_cast<int*>(lds + HW * kTileBytes);
     __shared__ int s_kept[HW];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -233,130 +316,44 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
         return;
     }
     const int n_tiles = (n_u + kTileKeys - 1) / kTileKeys;
-    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2);
-    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32);
-
-    // ---- this thread's runs of a tile: codes and scale bytes to registers, and from there to LDS
-    typedef std::conditional_t<kVals == 32, uintx4, uintx2> run_t;
-    run_t run[kUnits];
-    unsigned byte[kUnits];
-    auto read = [&](int tile) {
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int unit = u * 64 * HW + static_cast<int>(threadIdx.x);
-            const int64_t row = s_list[tile * kTileKeys + unit / kRuns];
-            const int at = unit % kRuns;
-            run[u] = *reinterpret_cast<const run_t*>(codes_b + row * (D / 2) + at * (kVals / 2));
-            byte[u] = scales_b[row * (D / 32) + at * kVals / 32];
-        }
+    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
+    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
+    Rows<D> rows;
+    rows.read(codes_b, scales_b, s_list[col]);
+    halfx8 qf[D / 16];
+    const float to_log2 = load_query<D / 16, 8, D / 2>(qa + (row_q * H + min(h, H - 1)) * D, scale_log2e, half, qf);
+    const Places<D> at(lane, wave * kTileBytes);
+    Heads<D> o;
+    // rows of U(t) from tile on: a tile's worth, or the last ones
+    auto live = [&](int tile) {
+        const int left = n_u - tile * kTileKeys;
+        return left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
     };
-    auto lay = [&](auto buf_tag) {
-        unsigned char* const tb = lds + decltype(buf_tag)::value * kTileBytes;
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int unit = u * 64 * HW + static_cast<int>(threadIdx.x);
-            const int r = unit / kRuns, at = unit % kRuns;
-            const float power = power_of(byte[u]);
-#pragma unroll
-            for (int i = 0; i < kVals / 8; ++i) {
-                const unsigned c = run[u][i];
-                const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 0);
-                const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 1);
-                const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 2);
-                const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 3);
-                const halfx8 v = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-                *reinterpret_cast<halfx8*>(tb + tile_slot<D>(r, at * (kVals / 8) + i) * 16) = v;
-            }
-        }
-    };
-    read(0);
-
-    halfx8 qf[KS];
-    const float to_log2 = load_query<KS, 16, 8>(qa + (row_q * H + min(h, H - 1)) * D, scale_log2e, half, qf);
-
-    // LDS byte offsets that do not depend on the tile (attention.hip says how the transposing reads are laid out)
-    int ka[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) ka[ks] = tile_slot<D>(col, 2 * ks + half) * 16;
-    int va[DB][2];
-    {
-        const int G = lane >> 4, s = lane & 15;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int r = 8 * w + 4 * (G >> 1) + (s >> 2);
-                const int d = 32 * db + 16 * (G & 1) + 4 * (s & 3);
-                va[db][w] = tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
-            }
+    int s_next = n_tiles > 1 ? s_list[kTileKeys + col] : 0;
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        floatx16 x = o.scores(rows, qf, lds, at);
+        if (tile + 1 < n_tiles) rows.read(codes_b, scales_b, s_next);
+        if (tile + 2 < n_tiles) s_next = s_list[(tile + 2) * kTileKeys + col];
+        o.take(x, live(tile), to_log2, half, lds, at);
     }
-
-    floatx16 acc[DB];
-    const floatx16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-    for (int db = 0; db < DB; ++db) acc[db] = zero16;
-    float m_ref = -__builtin_huge_valf();  // reference maximum of this lane's head (log2 domain)
-    float l_sum = 0.0f;                    // sum of the weights over this half-wave's rows
-
-    lay(std::integral_constant<int, 0>{});
-    if (n_tiles > 1) read(1);
-    __syncthreads();
-    // One tile; the buffer is a compile-time constant so that every LDS address is a loop-invariant register plus an immediate offset.
-    auto step = [&](int tile, auto buf_tag) {
-        constexpr int buf = decltype(buf_tag)::value;
-        const unsigned char* tb = lds + buf * kTileBytes;
-        // S^T : register j of a lane = row 8 (j / 4) + 4 half + j % 4, head = col
-        floatx16 sacc = zero16;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const halfx8 kf = *reinterpret_cast<const halfx8*>(tb + ka[ks]);
-            sacc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[ks], sacc, 0, 0, 0);
-        }
-        // the next tile into the other buffer, which everybody left at the last barrier
-        if (tile + 1 < n_tiles) lay(std::integral_constant<int, buf ^ 1>{});
-        if (tile + 2 < n_tiles) read(tile + 2);
-        const int left = n_u - tile * kTileKeys;  // rows of U(t) from this tile on
-        const unsigned live = left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
-        float p[16];
-        l_sum += weigh(sacc, to_log2, live, half, m_ref, p, [&](float alpha) {
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
-            l_sum *= alpha;
-        });
-        halfx8 p_hi[2], p_lo[2];
-        split_weights(p, p_hi, p_lo);
-        add_values<D>(tb, va, p_hi, p_lo, acc);
-        __syncthreads();
-    };
-    for (int tile = 0; tile < n_tiles; tile += 2) {
-        step(tile, std::integral_constant<int, 0>{});
-        if (tile + 1 < n_tiles) step(tile + 1, std::integral_constant<int, 1>{});
-    }
-
-    // ---- out[t, head, d] = O^T[d, head] / l : register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4
-    const float l_all = l_sum + other_half(l_sum);
+    const float l_all = o.l_sum + other_half(o.l_sum);
     const float inv = 1.0f / l_all;
     if (h < H) {
-        float* o = out + (row_q * H + h) * D;
+        float* to = out + (row_q * H + h) * D;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                const floatx4 v = {acc[db][4 * a] * inv, acc[db][4 * a + 1] * inv, acc[db][4 * a + 2] * inv, acc[db][4 * a + 3] * inv};
-                *reinterpret_cast<floatx4*>(o + 32 * db + 8 * a + 4 * half) = v;
+                const floatx4 v = {o.acc[db][4 * a] * inv, o.acc[db][4 * a + 1] * inv, o.acc[db][4 * a + 2] * inv, o.acc[db][4 * a + 3] * inv};
+                *reinterpret_cast<floatx4*>(to + 32 * db + 8 * a + 4 * half) = v;
             }
-        if (lse && half == 0) lse[row_q * H + h] = (m_ref - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2;
+        if (lse && half == 0) lse[row_q * H + h] = (o.m_ref - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2;
     }
 }
 
 // Few queries, which would leave most of the chip idle and walk their tiles one after the other: a workgroup takes one query and one block of 32
-// heads, and each of its waves every eighth tile, with a reference, sums and accumulators of its own; the waves' results are joined at the end.  A
-// wave's rows are read straight into its registers (a lane's row is lane % 32 of the tile, its values D/2 * (lane / 32) .. + D/2), where they are
-// the first product's operand as they are (the contraction order is permuted alike on the query); only for the second product they go
-// through LDS, into a tile of the wave's own: no wave waits for another until the end.
-// Dynamic LDS: a tile of 32 x D fp16 a wave, and the joined heads: 32 x (D + 1) floats a wave.
+// heads, and each of its waves every eighth tile, with a reference, sums and accumulators of its own; the waves' results are joined at the end.
+// Dynamic LDS: a tile of 32 x D fp16 a wave; for the join 32 x D floats a wave.
 constexpr int kFewWaves = 8;
 template <int D>
 constexpr int few_lds_bytes() { return kFewWaves * kTileKeys * D * 4; }
@@ -367,10 +364,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
                                     const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
                                     int head_blocks, float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
     constexpr int W = kFewWaves;
-    constexpr int KS = D / 16;
     constexpr int DB = D / 32;
-    constexpr int kLoads = D / 64;  // 16-byte pieces of codes a lane holds of a row
-    constexpr int kRowBytes = D * 2;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     __shared__ float s_ref[W][32], s_sum[W][32];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -385,100 +379,39 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
     const int n_tiles = u.count();
     const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
     const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
-    uintx4 run[kLoads];
-    unsigned byte[kLoads];
-    auto read = [&](int s) {
-        const int64_t row = max(s, 0);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            run[i] = *reinterpret_cast<const uintx4*>(codes_b + row * (D / 2) + i * 16);
-            byte[i] = scales_b[row * (D / 32) + i];
-        }
-    };
     int s_now = wave < n_tiles ? u.row(wave, col) : -1;
     int s_next = wave + W < n_tiles ? u.row(wave + W, col) : -1;
-    halfx8 qf[KS];
-    const float to_log2 = load_query<KS, 8, D / 2>(qa + (row_q * H + min(h0 + col, H - 1)) * D, scale_log2e, half, qf);
-    read(s_now);
-
-    unsigned char* const tb = lds + wave * kTileKeys * kRowBytes;
-    int put[D / 16];  // where the lane's pieces of its row go
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) put[i] = tile_slot<D>(col, half * (D / 16) + i) * 16;
-    int va[DB][2];
-    {
-        const int G = lane >> 4, s = lane & 15;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int r = 8 * w + 4 * (G >> 1) + (s >> 2);
-                const int d = 32 * db + 16 * (G & 1) + 4 * (s & 3);
-                va[db][w] = tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
-            }
-    }
-    floatx16 acc[DB];
-    const floatx16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-    for (int db = 0; db < DB; ++db) acc[db] = zero16;
-    float m_ref = -__builtin_huge_valf();
-    float l_sum = 0.0f;
-
+    halfx8 qf[D / 16];
+    const float to_log2 = load_query<D / 16, 8, D / 2>(qa + (row_q * H + min(h0 + col, H - 1)) * D, scale_log2e, half, qf);
+    Rows<D> rows;
+    rows.read(codes_b, scales_b, max(s_now, 0));
+    const Places<D> at(lane, wave * kTileKeys * D * 2);
+    Heads<D> o;
     for (int tile = wave; tile < n_tiles; tile += W) {
-        halfx8 kf[KS];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const float power = power_of(byte[i]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned c = run[i][j];
-                const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 0);
-                const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 1);
-                const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 2);
-                const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, power, 3);
-                kf[4 * i + j] = halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-            }
-        }
-        const unsigned live = static_cast<unsigned>(__ballot(s_now >= 0));  // bit r: row r of the tile is in U(t)
+        const unsigned live = static_cast<unsigned>(__ballot(s_now >= 0));
+        floatx16 x = o.scores(rows, qf, lds, at);
         s_now = s_next;
-        if (tile + W < n_tiles) read(s_now);
+        if (tile + W < n_tiles) rows.read(codes_b, scales_b, max(s_now, 0));
         if (tile + 2 * W < n_tiles) s_next = u.row(tile + 2 * W, col);
-        if (live == 0) continue;
-        // the wave's LDS accesses are done in order: the transposing reads of the tile before come first, those of this one after
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<halfx8*>(tb + put[i]) = kf[i];
-        floatx16 sacc = zero16;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sacc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], sacc, 0, 0, 0);
-        float p[16];
-        l_sum += weigh(sacc, to_log2, live, half, m_ref, p, [&](float alpha) {
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[db][j] *= alpha;
-            l_sum *= alpha;
-        });
-        halfx8 p_hi[2], p_lo[2];
-        split_weights(p, p_hi, p_lo);
-        add_values<D>(tb, va, p_hi, p_lo, acc);
+        if (live != 0) o.take(x, live, to_log2, half, lds, at);
     }
 
     // ---- join: the largest reference of the waves, sums and accumulators brought to it
-    if (half == 0) s_ref[wave][col] = m_ref;
-    l_sum += other_half(l_sum);
+    if (half == 0) s_ref[wave][col] = o.m_ref;
+    const float l_sum = o.l_sum + other_half(o.l_sum);
     if (half == 0) s_sum[wave][col] = l_sum;
     __syncthreads();  // also: every wave is done with its tile
     float m_all = s_ref[0][col];
 #pragma unroll
     for (int w = 1; w < W; ++w) m_all = fmaxf(m_all, s_ref[w][col]);
-    const float alpha = m_ref == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m_ref - m_all);
+    const float alpha = o.m_ref == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(o.m_ref - m_all);
     // [wave][piece of four d][head], so that both the stores and the loads of a wave go through all banks
     floatx4* const s_acc = reinterpret_cast<floatx4*>(lds);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const floatx4 v = {acc[db][4 * a] * alpha, acc[db][4 * a + 1] * alpha, acc[db][4 * a + 2] * alpha, acc[db][4 * a + 3] * alpha};
+            const floatx4 v = {o.acc[db][4 * a] * alpha, o.acc[db][4 * a + 1] * alpha, o.acc[db][4 * a + 2] * alpha, o.acc[db][4 * a + 3] * alpha};
             s_acc[(wave * (D / 4) + 8 * db + 2 * a + half) * 32 + col] = v;
         }
     __syncthreads();
@@ -515,23 +448,13 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
                                             const unsigned char* __restrict__ scales, const float* __restrict__ lse, int64_t row_q, int H,
                                             int64_t first_row, const Tiles& u, int first, int last, float scale_log2e, float* s_lse, Add add) {
     constexpr int KS = D / 16;
-    constexpr int kLoads = D / 64;  // 16-byte pieces of codes a lane holds of a row
     if (first >= last) return;
     const int lane = threadIdx.x & 63;
     const int col = lane & 31;
     const int half = lane >> 5;
     const unsigned char* const codes_b = codes + first_row * (D / 2) + half * (D / 4);
     const unsigned char* const scales_b = scales + first_row * (D / 32) + half * (D / 64);
-    uintx4 run[kLoads];
-    unsigned byte[kLoads];
-    auto read = [&](int s) {
-        const int64_t row = max(s, 0);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            run[i] = *reinterpret_cast<const uintx4*>(codes_b + row * (D / 2) + i * 16);
-            byte[i] = scales_b[row * (D / 32) + i];
-        }
-    };
+    Rows<D> next;
     int s_now = u.row(first, col);
     int s_next = first + 1 < last ? u.row(first + 1, col) : -1;
     s_lse[lane] = lane < H ? -kLog2e * lse[row_q * H + min(lane, H - 1)] : -__builtin_huge_valf();  // no head there: weight 0
@@ -542,7 +465,7 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[hb][ks] = *reinterpret_cast<const bf16x8*>(src + ks * 8);
     }
-    read(s_now);
+    next.read(codes_b, scales_b, max(s_now, 0));
     floatx4 minus_lse[HB][4];  // of the heads this lane's results belong to, log2 domain
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb)
@@ -551,21 +474,10 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
     for (int tile = first; tile < last; ++tile) {
         bf16x8 kf[KS];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const float power = power_of(byte[i]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned c = run[i][j];
-                const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 0);
-                const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 1);
-                const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 2);
-                const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 3);
-                kf[4 * i + j] = bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-            }
-        }
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = next.values_bf16(ks);
         const int s = s_now;
         s_now = s_next;
-        if (tile + 1 < last) read(s_now);
+        if (tile + 1 < last) next.read(codes_b, scales_b, max(s_now, 0));
         if (tile + 2 < last) s_next = u.row(tile + 2, col);
         if (__ballot(s >= 0) == 0ull) continue;
         float sum = 0.0f;
@@ -667,7 +579,7 @@ struct Call {
 template <int D, int HW>
 hipError_t launch_attention(const Call& c, float* out, float* lse) {
     static std::atomic<size_t> allowed[64];
-    const size_t lds = 2 * static_cast<size_t>(kTileKeys) * D * 2 + list_bytes(c.k, c.n_win);
+    const size_t lds = HW * static_cast<size_t>(kTileKeys) * D * 2 + list_bytes(c.k, c.n_win);
     hipError_t e = allow_lds(quantized_attention_kernel<D, HW>, lds, allowed);
     if (e != hipSuccess) return e;
     const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
