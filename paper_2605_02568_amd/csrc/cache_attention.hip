@@ -18,6 +18,7 @@
 #include "attention_set.h"
 #include "si_internal.h"
 #include "streamindex_cache.h"
+#include "wave_ops.h"
 
 namespace si {
 
@@ -48,36 +49,38 @@ __device__ __forceinline__ int held_rows(const int32_t* __restrict__ lengths, in
     return lengths ? min(max(lengths[b], 0), T) : T;
 }
 
-// This lane's part of a query's head (8 values at STEP ks + HALF half) as fp16, times a power of two that brings the head's largest
-// magnitude into [2^14, 2^15), with the sign of the softmax scale; values down to 2^-32 of the largest stay exact.  Returns the factor that
-// takes a product of these operands to the log2 domain: |scale| log2(e) over that power.
-template <int KS, int STEP, int HALF>
-__device__ __forceinline__ float load_query(const __bf16* __restrict__ src, float scale_log2e, int half, halfx8 (&qf)[KS]) {
-    uintx4 raw[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(src + ks * STEP + half * HALF);
+// A lane's part of a query's head, 8 bf16 values an element, as the products take it: fp16, times a power of two that brings the head's
+// largest magnitude (bits `top` of largest(), over all lanes that have a part) into [2^14, 2^15), with the sign of the softmax scale; values
+// down to 2^-32 of the largest stay exact.  The factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.
+template <int N>
+__device__ __forceinline__ unsigned largest(const uintx4 (&raw)[N]) {
     unsigned top = 0;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, max(raw[ks][j] & 0x7FFFu, (raw[ks][j] >> 16) & 0x7FFFu));
-    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    top = max(both[0], both[1]);
-    const int e = static_cast<int>(top >> 7);        // exponent field of the largest
-    const int up = min(268 - e, 254);                // field of the power: 2^(14 - (e - 127))
-    const float power = __uint_as_float(static_cast<unsigned>(up) << 23) * (scale_log2e < 0.0f ? -1.0f : 1.0f);
+        for (int j = 0; j < 4; ++j) top = max(top, max(raw[i][j] & 0x7FFFu, (raw[i][j] >> 16) & 0x7FFFu));
+    return top;
+}
+// The power, and in to_log2 that factor.
+__device__ __forceinline__ float query_power(unsigned top, float scale_log2e, float& to_log2) {
+    const int e = static_cast<int>(top >> 7);  // exponent field of the largest
+    const int up = min(268 - e, 254);          // field of the power: 2^(14 - (e - 127))
+    // not 0, so that -inf times it is -inf: a logit that such a factor makes is 0 either way
+    to_log2 = fmaxf(__builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up), 1.1754944e-38f);
+    return __uint_as_float(static_cast<unsigned>(up) << 23) * (scale_log2e < 0.0f ? -1.0f : 1.0f);
+}
+template <int N>
+__device__ __forceinline__ void scale_query(const uintx4 (&raw)[N], float power, halfx8 (&qf)[N]) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float lo = __uint_as_float(raw[ks][j] << 16) * power;
-            const float hi = __uint_as_float(raw[ks][j] & 0xFFFF0000u) * power;
+            const float lo = __uint_as_float(raw[i][j] << 16) * power;
+            const float hi = __uint_as_float(raw[i][j] & 0xFFFF0000u) * power;
             const halfx2 pair = __builtin_convertvector(floatx2{lo, hi}, halfx2);
-            qf[ks][2 * j] = pair[0];
-            qf[ks][2 * j + 1] = pair[1];
+            qf[i][2 * j] = pair[0];
+            qf[i][2 * j + 1] = pair[1];
         }
-    // not 0, so that -inf times it is -inf: a logit that such a factor makes is 0 either way
-    return fmaxf(__builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up), 1.1754944e-38f);
 }
 
 // Weights as two fp16 parts, p = hi + lo, each rounded to nearest.  The remainder is an fma that takes hi as it is and rounds to fp16 at once:
@@ -321,7 +324,14 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     Rows<D> rows;
     rows.read(codes_b, scales_b, s_list[col]);
     halfx8 qf[D / 16];
-    const float to_log2 = load_query<D / 16, 8, D / 2>(qa + (row_q * H + min(h, H - 1)) * D, scale_log2e, half, qf);
+    uintx4 raw[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(qa + (row_q * H + min(h, H - 1)) * D + half * (D / 2) + ks * 8);
+    unsigned top = largest(raw);
+    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(both[0], both[1]);
+    float to_log2;
+    scale_query(raw, query_power(top, scale_log2e, to_log2), qf);
     const Places<D> at(lane, wave * kTileBytes);
     Heads<D> o;
     // rows of U(t) from tile on: a tile's worth, or the last ones
@@ -351,88 +361,241 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     }
 }
 
-// Few queries, which would leave most of the chip idle and walk their tiles one after the other: a workgroup takes one query and one block of 32
-// heads, and each of its waves every eighth tile, with a reference, sums and accumulators of its own; the waves' results are joined at the end.
-// Dynamic LDS: a tile of 32 x D fp16 a wave; for the join 32 x D floats a wave.
-constexpr int kFewWaves = 8;
+// Few queries, which would leave most of the chip idle and walk their tiles one after the other: a workgroup takes one query and one block of
+// 16 heads, and each of its 8 or 16 waves every 8th or 16th tile, with a reference, sums and accumulators of its own; the waves' results are joined at
+// the end.  The steps are those of the kernel above with the matrix instructions of half the size (16 x 16 x 32): half the work of a tile and
+// half the registers a wave, so that twice the waves share out the tiles on twice the compute units.  With DS = 2 two workgroups share a block of
+// heads: both score all rows, each has half of d in the second product, the rows in LDS and the join.  A lane's part of a tile: rows lane % 16 and
+// lane % 16 + 16, values D/4 * (lane / 16) .. + D/4; of the scores: rows 4 (lane / 16) + 0 .. 3 and those + 16, head lane % 16.
+// All workgroups of a query are on one XCD (32 queries, 1152 rows: 12.9 -> 9.8 us; each XCD's L2 read the rows again).  Bound by a wave's chain
+// of dependent steps: of 9.5 us at 32 queries and 1152 rows 4.3 are launch, first tile and join, 1 a tile of a wave.
+// Dynamic LDS: a tile of 32 x D fp16 a wave; for the join 16 x D / DS floats a wave.
+constexpr int kFewHeads = 16;
+constexpr int kXcds = 8;
+template <int D, int WAVES>
+constexpr int few_lds_bytes() { return WAVES * kTileKeys * D * 2; }
+
 template <int D>
-constexpr int few_lds_bytes() { return kFewWaves * kTileKeys * D * 4; }
-template <int D>
-__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2)))
+struct HalfRows {
+    typedef std::conditional_t<D == 128, uintx4, uintx2> run_t;
+    run_t run[2];
+    uint8_t bytes[2];
+    __device__ __forceinline__ void read(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, int64_t row, int which) {
+        bytes[which] = scales[row * (D / 32)];
+        run[which] = *reinterpret_cast<const run_t*>(codes + row * (D / 2));
+    }
+    __device__ __forceinline__ halfx8 values(int which, int ks) const {
+        const float p = power_of(bytes[which]);
+        const unsigned c = run[which][ks];
+        const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 0);
+        const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 1);
+        const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 2);
+        const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
+        return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    }
+};
+
+template <int D, int DS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4)))
 void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                     const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
                                     const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
-                                    int head_blocks, float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
-    constexpr int W = kFewWaves;
-    constexpr int DB = D / 32;
+                                    int64_t n_queries, int head_blocks, float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
+    constexpr int W = WAVES;
+    constexpr int KS = D / 32;   // matrix instructions along d in the first product
+    constexpr int DB = D / 16 / DS;  // blocks of 16 d in the second
+    constexpr int kPieces = D / 4 / DS;  // of four d
+    constexpr int kTileBytes = kTileKeys * D * 2;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    __shared__ float s_ref[W][32], s_sum[W][32];
+    __shared__ float s_ref[W][kFewHeads], s_sum[W][kFewHeads];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    const int col = lane & 31;
-    const int half = lane >> 5;
-    const int64_t row_q = blockIdx.x / head_blocks;
-    const int h0 = 32 * static_cast<int>(blockIdx.x % head_blocks);
+    const int col = lane & 15;   // row of a half tile, head
+    const int quarter = lane >> 4;
+    // workgroups go round the chip's eight XCDs: all of a query are on one, whose L2 then has the rows for all of them
+    const unsigned turn = blockIdx.x / kXcds;
+    const int part = static_cast<int>(turn % DS);  // of d
+    const int h0 = kFewHeads * static_cast<int>(turn / DS % head_blocks);
+    const int64_t row_q = static_cast<int64_t>(turn / DS / head_blocks) * kXcds + blockIdx.x % kXcds;
+    if (row_q >= n_queries) return;
     const int b = static_cast<int>(row_q / S);
     const int t = static_cast<int>(row_q - static_cast<int64_t>(b) * S);
     const Tiles u = tiles_of(idx, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
     const int n_tiles = u.count();
-    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
-    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
-    int s_now = wave < n_tiles ? u.row(wave, col) : -1;
-    int s_next = wave + W < n_tiles ? u.row(wave + W, col) : -1;
-    halfx8 qf[D / 16];
-    const float to_log2 = load_query<D / 16, 8, D / 2>(qa + (row_q * H + min(h0 + col, H - 1)) * D, scale_log2e, half, qf);
-    Rows<D> rows;
-    rows.read(codes_b, scales_b, max(s_now, 0));
-    const Places<D> at(lane, wave * kTileKeys * D * 2);
-    Heads<D> o;
-    for (int tile = wave; tile < n_tiles; tile += W) {
-        const unsigned live = static_cast<unsigned>(__ballot(s_now >= 0));
-        floatx16 x = o.scores(rows, qf, lds, at);
-        s_now = s_next;
-        if (tile + W < n_tiles) rows.read(codes_b, scales_b, max(s_now, 0));
-        if (tile + 2 * W < n_tiles) s_next = u.row(tile + 2 * W, col);
-        if (live != 0) o.take(x, live, to_log2, half, lds, at);
-    }
+    const int waves = min(W, n_tiles);  // that have a tile
+    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + quarter * (D / 8);
+    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + quarter * D / 128;
 
-    // ---- join: the largest reference of the waves, sums and accumulators brought to it
-    if (half == 0) s_ref[wave][col] = o.m_ref;
-    const float l_sum = o.l_sum + other_half(o.l_sum);
-    if (half == 0) s_sum[wave][col] = l_sum;
-    __syncthreads();  // also: every wave is done with its tile
-    float m_all = s_ref[0][col];
+    float m_ref = -__builtin_huge_valf();
+    float l_sum = 0.0f;
+    floatx4 acc[DB];  // register j of block db = d row 16 (DB part + db) + 4 quarter + j, head = col
 #pragma unroll
-    for (int w = 1; w < W; ++w) m_all = fmaxf(m_all, s_ref[w][col]);
-    const float alpha = o.m_ref == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(o.m_ref - m_all);
-    // [wave][piece of four d][head], so that both the stores and the loads of a wave go through all banks
-    floatx4* const s_acc = reinterpret_cast<floatx4*>(lds);
+    for (int db = 0; db < DB; ++db) acc[db] = floatx4{0, 0, 0, 0};
+    // the query, one or two heads a wave, to fp16 and to LDS: pieces of 8 values turned over by the head's number as those of a tile's rows
+    __shared__ __attribute__((aligned(16))) _Float16 s_query[kFewHeads * D];
+    __shared__ float s_scale[kFewHeads];
+    constexpr int kHeadsPerWave = kFewHeads / W;
+    constexpr int kPair = D / 64;  // values of a lane
+    typedef std::conditional_t<D == 128, unsigned, uint16_t> pair_t;
+    unsigned pair[kHeadsPerWave];
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int i = 0; i < kHeadsPerWave; ++i)
+        pair[i] = reinterpret_cast<const pair_t*>(qa + (row_q * H + min(h0 + wave + i * W, H - 1)) * D)[lane];
+    int s_now[2] = {-1, -1}, s_next[2] = {-1, -1};
+    HalfRows<D> rows;
+    if (wave < waves) {
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const floatx4 v = {o.acc[db][4 * a] * alpha, o.acc[db][4 * a + 1] * alpha, o.acc[db][4 * a + 2] * alpha, o.acc[db][4 * a + 3] * alpha};
-            s_acc[(wave * (D / 4) + 8 * db + 2 * a + half) * 32 + col] = v;
-        }
-    __syncthreads();
-    float l_all = 0.0f;
+        for (int i = 0; i < 2; ++i) s_now[i] = u.row(wave, col + 16 * i);
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        const float r = s_ref[w][col];
-        l_all += r == -__builtin_huge_valf() ? 0.0f : s_sum[w][col] * __builtin_amdgcn_exp2f(r - m_all);
+        for (int i = 0; i < 2; ++i) s_next[i] = wave + W < n_tiles ? u.row(wave + W, col + 16 * i) : -1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) rows.read(codes_b, scales_b, max(s_now[i], 0), i);
     }
-    const float inv = l_all > 0.0f ? 1.0f / l_all : 0.0f;
-    const int h = h0 + col;
-    if (h < H) {
 #pragma unroll
-        for (int i = 0; i < D / 4 / (2 * W); ++i) {
-            const int piece = i * 2 * W + 2 * wave + half;
-            floatx4 v = s_acc[piece * 32 + col];
+    for (int i = 0; i < kHeadsPerWave; ++i) {
+        const int head = wave + i * W;
+        const unsigned top = wave_max(max(pair[i] & 0x7FFFu, (pair[i] >> 16) & 0x7FFFu));
+        float to_log2;
+        const float power = query_power(top, scale_log2e, to_log2);
+        const int at = head * D + (((lane * kPair / 8) ^ (head % (D / 8))) * 8 + lane * kPair % 8);
+        s_query[at] = static_cast<_Float16>(__uint_as_float(pair[i] << 16) * power);
+        if (kPair == 2) s_query[at + 1] = static_cast<_Float16>(__uint_as_float(pair[i] & 0xFFFF0000u) * power);
+        if (lane == 0) s_scale[head] = to_log2;
+    }
+    __syncthreads();
+    if (wave < waves) {
+        halfx8 qf[KS];
 #pragma unroll
-            for (int w = 1; w < W; ++w) v += s_acc[(w * (D / 4) + piece) * 32 + col];
-            *reinterpret_cast<floatx4*>(out + (row_q * H + h) * D + 4 * piece) = v * inv;
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const halfx8*>(s_query + (col * (D / 8) + ((quarter * KS + ks) ^ (col % (D / 8)))) * 8);
+        const float to_log2 = s_scale[col];
+        const int base = wave * kTileBytes;
+        int put[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) put[i] = base + tile_slot<D>(col + 16 * i, quarter * (D / 32)) * 16;
+        // transposing reads: source lane s of a 16-lane group points at 4 consecutive d of row 4 quarter + s / 4 (+ 16)
+        const int s4 = lane & 15;
+        const int va = base + tile_slot<D>(4 * quarter + (s4 >> 2), (s4 & 3) >> 1) * 16 + (s4 & 1) * 8;
+
+        for (int tile = wave; tile < n_tiles; tile += W) {
+            unsigned live = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) live |= (static_cast<unsigned>(__ballot(s_now[i] >= 0)) & 0xFFFFu) << (16 * i);
+            floatx4 x[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const halfx8 v = rows.values(i, ks);
+                    if (DS == 1 || quarter / (4 / DS) == part) *reinterpret_cast<halfx8*>(lds + (put[i] ^ (16 * ks))) = v;
+                    x[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, qf[ks], x[i], 0, 0, 0);
+                }
+                s_now[i] = s_next[i];
+                if (tile + W < n_tiles) rows.read(codes_b, scales_b, max(s_now[i], 0), i);
+                if (tile + 2 * W < n_tiles) s_next[i] = u.row(tile + 2 * W, col + 16 * i);
+            }
+            if (live == 0) continue;
+            if (live != 0xFFFFFFFFu) {
+                float low = -__builtin_huge_valf();
+                asm volatile("" : "+v"(low));
+                const unsigned mine = live >> (4 * quarter);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (!((mine >> (16 * (j >> 2) + (j & 3))) & 1)) x[j >> 2][j & 3] = low;
+            }
+            float p[8], sum;
+            auto exponentials = [&]() {  // weigh() above says why without a maximum first
+                const float shift = kWeightShift - m_ref;
+                sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], to_log2, shift));
+                    sum += p[j];
+                }
+            };
+            const bool first = m_ref == -__builtin_huge_valf();  // the same for all lanes
+            unsigned long long over = ~0ull;
+            if (__builtin_expect(__ballot(first) == 0ull, 1)) {
+                exponentials();
+                over = __ballot(!(sum <= 32768.0f));
+            }
+            if (over != 0ull) {
+                over |= over >> 32;
+                over |= over >> 16;  // bit h: head h, in any quarter
+                float highest = x[0][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) highest = fmaxf(highest, x[j >> 2][j & 3]);
+                highest *= to_log2;
+                highest = fmaxf(highest, __shfl_xor(highest, 16));
+                highest = fmaxf(highest, __shfl_xor(highest, 32));
+                const float m_new = (over >> col) & 1 ? fmaxf(highest, m_ref) : m_ref;
+                const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+                l_sum *= alpha;
+                m_ref = m_new;
+                exponentials();
+            }
+            l_sum += sum;
+            float one = 1.0f;
+            asm("" : "+s"(one));
+            halfx8 p_hi, p_lo;
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj) {
+                const halfx2 a = __builtin_convertvector(floatx2{p[2 * jj], p[2 * jj + 1]}, halfx2);
+                p_hi[2 * jj] = a[0];
+                p_hi[2 * jj + 1] = a[1];
+                p_lo[2 * jj] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[0]), one, p[2 * jj]));
+                p_lo[2 * jj + 1] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[1]), one, p[2 * jj + 1]));
+            }
+            // contraction index e <-> tile row 16 (e / 4) + 4 quarter + e % 4 on both operands
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
+                const unsigned char* from = lds + (va ^ (32 * (DB * part + db)));
+                const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)from));
+                const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(from + 16 * D * 2)));
+                const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+                acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi, acc[db], 0, 0, 0);
+                acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo, acc[db], 0, 0, 0);
+            }
         }
-        if (lse && wave == 0 && half == 0)
+        l_sum += __shfl_xor(l_sum, 16);
+        l_sum += __shfl_xor(l_sum, 32);
+        if (quarter == 0) s_ref[wave][col] = m_ref;
+    }
+    // ---- join: the largest reference of the waves, sums and accumulators brought to it
+    __syncthreads();  // also: every wave is done with its tile
+    float m_all = -__builtin_huge_valf();
+#pragma unroll
+    for (int w = 0; w < W; ++w) m_all = fmaxf(m_all, w < waves ? s_ref[w][col] : -__builtin_huge_valf());
+    floatx4* const s_acc = reinterpret_cast<floatx4*>(lds);  // [wave][piece of four d][head]
+    if (wave < waves) {
+        const float alpha = m_ref == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m_ref - m_all);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) s_acc[(wave * kPieces + 4 * db + quarter) * kFewHeads + col] = acc[db] * alpha;
+        if (quarter == 0) s_sum[wave][col] = l_sum * alpha;
+    }
+    __syncthreads();
+    const int h = h0 + col;
+    if (h >= H) return;
+    for (int piece = 4 * wave + quarter; piece < kPieces; piece += 4 * W) {
+        float l_all = 0.0f;
+        floatx4 v = {0, 0, 0, 0};
+        if (waves == W) {  // unrolled, the reads wait for LDS once: 1 us of 12.7 at 16 waves
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                l_all += s_sum[w][col];
+                v += s_acc[(w * kPieces + piece) * kFewHeads + col];
+            }
+        } else {
+            for (int w = 0; w < waves; ++w) {
+                l_all += s_sum[w][col];
+                v += s_acc[(w * kPieces + piece) * kFewHeads + col];
+            }
+        }
+        *reinterpret_cast<floatx4*>(out + (row_q * H + h) * D + part * (D / DS) + 4 * piece) = v * (l_all > 0.0f ? 1.0f / l_all : 0.0f);
+        if (lse && piece == 0 && part == 0)
             lse[row_q * H + h] = l_all > 0.0f ? (m_all - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2 : -__builtin_huge_valf();
     }
 }
@@ -589,21 +752,38 @@ hipError_t launch_attention(const Call& c, float* out, float* lse) {
     return hipGetLastError();
 }
 
-template <int D>
+template <int D, int DS, int WAVES>
 hipError_t launch_few(const Call& c, float* out, float* lse) {
     static std::atomic<size_t> allowed[64];
-    hipError_t e = allow_lds(quantized_attention_few_kernel<D>, few_lds_bytes<D>(), allowed);
+    constexpr int kBytes = few_lds_bytes<D, WAVES>();
+    hipError_t e = allow_lds(quantized_attention_few_kernel<D, DS, WAVES>, kBytes, allowed);
     if (e != hipSuccess) return e;
-    const int head_blocks = (c.d.H_I + 31) / 32;
-    const int64_t grid = static_cast<int64_t>(c.d.B) * c.d.S * head_blocks;
-    hipLaunchKernelGGL((quantized_attention_few_kernel<D>), dim3(static_cast<unsigned>(grid)), dim3(64 * kFewWaves), few_lds_bytes<D>(), c.stream,
-                       c.qa, c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, head_blocks,
+    const int head_blocks = (c.d.H_I + kFewHeads - 1) / kFewHeads;
+    const int64_t n_queries = static_cast<int64_t>(c.d.B) * c.d.S;
+    const int64_t grid = (n_queries + kXcds - 1) / kXcds * kXcds * head_blocks * DS;
+    hipLaunchKernelGGL((quantized_attention_few_kernel<D, DS, WAVES>), dim3(static_cast<unsigned>(grid)), dim3(64 * WAVES), kBytes, c.stream, c.qa,
+                       c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, n_queries, head_blocks,
                        c.scale_log2e, out, lse);
     return hipGetLastError();
 }
 
-// One round of the chip's compute units.
-bool few_queries(const si_dims& d) { return static_cast<int64_t>(d.B) * d.S * ((d.H_I + 31) / 32) <= 256; }
+// Blocks of 16 heads of all queries, and the rows a query may attend to, decide.  Measured (us; B queries of 64 heads of 128, 4 B blocks):
+// the kernel for many queries against this one's, rows 1152: B = 32 33 -> 9.5, 128 34 -> 16, 192 34 -> 23, 256 35 -> 29, 384 47 -> 40, 512 47 -> 52;
+// 384 rows: 128 15 -> 9, 192 15.2 -> 13.1, 256 15.8 -> 16.0; 64 rows: 32 5.5 -> 4.6, 160 6.9 -> 8.7.
+bool few_queries(const si_dims& d, int k, int n_win) {
+    const int64_t blocks = static_cast<int64_t>(d.B) * d.S * ((d.H_I + kFewHeads - 1) / kFewHeads);
+    return blocks <= 512 || (blocks < 1024 && k + n_win >= 384) || (blocks <= 1536 && k + n_win >= 1024);
+}
+// Halves of d where these fit the chip's compute units once (B = 32: 10.4 -> 9.5, B = 48: 10.6 -> 13.4); 16 waves where a workgroup has a unit to
+// itself and more than five tiles a wave (B = 32, rows 1152 / 1536 / 2048 / 4096: 8 waves 9.5 / 11.7 / 14.3 / 23.8, 16 waves 9.8 / 11.2 / 13.2 / 20.1;
+// B = 64: 11.0 / 13.5 / 17.0 / - and 11.6 / 13.5 / 16.0 / -).
+template <int D>
+hipError_t launch_few(const Call& c, float* out, float* lse) {
+    const int64_t blocks = static_cast<int64_t>(c.d.B) * c.d.S * ((c.d.H_I + kFewHeads - 1) / kFewHeads);
+    const bool wide = c.k + c.n_win > 1536;
+    if (blocks <= 128) return wide ? launch_few<D, 2, 16>(c, out, lse) : launch_few<D, 2, 8>(c, out, lse);
+    return wide && blocks <= 256 ? launch_few<D, 1, 16>(c, out, lse) : launch_few<D, 1, 8>(c, out, lse);
+}
 
 constexpr int kGatherRows = 16384;  // whose sums fit LDS: 128 KiB
 
@@ -665,7 +845,7 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
     const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
                     lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
     const bool two = dims->H_I > 32;
-    if (few_queries(*dims)) return report(dims->D == 128 ? launch_few<128>(c, out, lse) : launch_few<64>(c, out, lse));
+    if (few_queries(*dims, k, n_win)) return report(dims->D == 128 ? launch_few<128>(c, out, lse) : launch_few<64>(c, out, lse));
     return report(dims->D == 128 ? (two ? launch_attention<128, 2>(c, out, lse) : launch_attention<128, 1>(c, out, lse))
                                  : (two ? launch_attention<64, 2>(c, out, lse) : launch_attention<64, 1>(c, out, lse)));
 }

@@ -206,6 +206,11 @@ NONE, CAUSAL = P.SI_MASK_NONE, P.SI_MASK_CAUSAL_BLOCK
     (1, 530, 40, 64, 300, 2, 33, CAUSAL, 33, [200]),
     (600, 1, 33, 128, 40, 1, 20, NONE, 4, None),      # many batches of one query
     (37, 16, 32, 128, 64, 1, 40, NONE, 8, None),
+    (40, 1, 64, 128, 1700, 1, 1600, NONE, 0, None),   # long lists of a middling number of queries
+    (66, 1, 33, 64, 1650, 1, 1600, NONE, 30, None),
+    (1, 200, 64, 128, 500, 1, 400, CAUSAL, 20, None),  # more workgroups than compute units, rows for each
+    (130, 2, 64, 64, 450, 1, 390, NONE, 0, None),
+    (9, 3, 16, 128, 800, 1, 700, NONE, 128, None),     # a number of queries that no eight divide
 ])
 def test_attention_and_weights(B, S, H, D, T, m, k, mask, n_win, lengths):
     print(f"attention B={B} S={S} H={H} D={D} T={T} m={m} k={k} mask={mask} n_win={n_win} lengths={lengths}", flush=True)
