@@ -144,23 +144,24 @@ __device__ __forceinline__ float weigh(floatx16& s, float to_log2, unsigned live
 // U(t) in tiles of 32 rows as they stand: the list's, then the window's; a lane knows its own row of a tile (row = lane % 32).
 struct Tiles {
     const int32_t* list;
-    int k, held, w0, legal, list_tiles;
-    // The row of this lane in tile `tile`, -1 where U(t) has none there: a pad, an entry that the window has, the end of either.
-    __device__ __forceinline__ int row(int tile, int col) const {
-        if (tile < list_tiles) {  // uniform
-            const int j = tile * kTileKeys + col;
-            const int s = list[min(j, k - 1)];
-            return j < k && static_cast<unsigned>(s) < static_cast<unsigned>(held) && !(s >= w0 && s < legal) ? s : -1;
-        }
-        const int s = w0 + (tile - list_tiles) * kTileKeys + col;
-        return s < legal ? s : -1;
+    int k, last, held, w0, legal, list_tiles;
+    // What the list has at this lane's place of tile `tile` (of the window's tiles: of its last one).  On its own, and without a branch, so that a
+    // loop can ask for a tile's entries well before it needs them: judged at once they would be waited for at once.
+    __device__ __forceinline__ int entry(int tile, int col) const { return list[min(tile * kTileKeys + col, last)]; }
+    // The row that this lane has of tile `tile`, with what entry() gave; -1 where U(t) has none there: a pad, an entry that the window has, the
+    // end of either.
+    __device__ __forceinline__ int row(int entry, int tile, int col) const {
+        const bool listed = (tile * kTileKeys + col < k) & (static_cast<unsigned>(entry) < static_cast<unsigned>(held)) & !((entry >= w0) & (entry < legal));
+        const int in_window = w0 + (tile - list_tiles) * kTileKeys + col;
+        return tile < list_tiles ? (listed ? entry : -1) : (in_window < legal ? in_window : -1);
     }
     __device__ __forceinline__ int count() const { return list_tiles + (legal - w0 + kTileKeys - 1) / kTileKeys; }
 };
-__device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, int64_t row_q, int t, int k, int held, int n_win, int m, int mask_mode) {
+__device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, const void* readable, int64_t row_q, int t, int k, int held, int n_win, int m, int mask_mode) {
     Tiles u;
-    u.list = idx + row_q * k;
+    u.list = k > 0 ? idx + row_q * k : static_cast<const int32_t*>(readable);  // without lists: anything that may be read
     u.k = k;
+    u.last = max(k - 1, 0);
     u.held = held;
     u.legal = legal_count(t, held, m, mask_mode);
     u.w0 = max(0, u.legal - n_win);
@@ -339,11 +340,11 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
         const int left = n_u - tile * kTileKeys;
         return left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
     };
-    int s_next = n_tiles > 1 ? s_list[kTileKeys + col] : 0;
+    int s_next = s_list[min(1, n_tiles - 1) * kTileKeys + col];
     for (int tile = 0; tile < n_tiles; ++tile) {
         floatx16 x = o.scores(rows, qf, lds, at);
-        if (tile + 1 < n_tiles) rows.read(codes_b, scales_b, s_next);
-        if (tile + 2 < n_tiles) s_next = s_list[(tile + 2) * kTileKeys + col];
+        rows.read(codes_b, scales_b, s_next);
+        s_next = s_list[min(tile + 2, n_tiles - 1) * kTileKeys + col];
         o.take(x, live(tile), to_log2, half, lds, at);
     }
     const float l_all = o.l_sum + other_half(o.l_sum);
@@ -420,7 +421,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
     if (row_q >= n_queries) return;
     const int b = static_cast<int>(row_q / S);
     const int t = static_cast<int>(row_q - static_cast<int64_t>(b) * S);
-    const Tiles u = tiles_of(idx, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
+    const Tiles u = tiles_of(idx, qa, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
     const int n_tiles = u.count();
     const int waves = min(W, n_tiles);  // that have a tile
     const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + quarter * (D / 8);
@@ -441,15 +442,18 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
 #pragma unroll
     for (int i = 0; i < kHeadsPerWave; ++i)
         pair[i] = reinterpret_cast<const pair_t*>(qa + (row_q * H + min(h0 + wave + i * W, H - 1)) * D)[lane];
-    int s_now[2] = {-1, -1}, s_next[2] = {-1, -1};
+    int s_now[2] = {-1, -1}, next[2] = {-1, -1};
     HalfRows<D> rows;
     if (wave < waves) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) s_now[i] = u.row(wave, col + 16 * i);
+        for (int i = 0; i < 2; ++i) s_now[i] = u.entry(wave, col + 16 * i);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) s_next[i] = wave + W < n_tiles ? u.row(wave + W, col + 16 * i) : -1;
+        for (int i = 0; i < 2; ++i) next[i] = u.entry(wave + W, col + 16 * i);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) rows.read(codes_b, scales_b, max(s_now[i], 0), i);
+        for (int i = 0; i < 2; ++i) {
+            s_now[i] = u.row(s_now[i], wave, col + 16 * i);
+            rows.read(codes_b, scales_b, max(s_now[i], 0), i);
+        }
     }
 #pragma unroll
     for (int i = 0; i < kHeadsPerWave; ++i) {
@@ -490,10 +494,11 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
                     if (DS == 1 || quarter / (4 / DS) == part) *reinterpret_cast<halfx8*>(lds + (put[i] ^ (16 * ks))) = v;
                     x[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, qf[ks], x[i], 0, 0, 0);
                 }
-                s_now[i] = s_next[i];
-                if (tile + W < n_tiles) rows.read(codes_b, scales_b, max(s_now[i], 0), i);
-                if (tile + 2 * W < n_tiles) s_next[i] = u.row(tile + 2 * W, col + 16 * i);
+                s_now[i] = u.row(next[i], tile + W, col + 16 * i);
+                rows.read(codes_b, scales_b, max(s_now[i], 0), i);
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) next[i] = u.entry(tile + 2 * W, col + 16 * i);
             if (live == 0) continue;
             if (live != 0xFFFFFFFFu) {
                 float low = -__builtin_huge_valf();
@@ -600,16 +605,49 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
     }
 }
 
+// A query's heads as the first product's operand, one wave: head 32 hb + lane % 32, values D/2 * (lane / 32) + 8 ks .. + 8; of H heads the last
+// stands in for those there are not.  Whole lines are read and parted out through 4 KiB of LDS: read head by head into the registers a line
+// would be asked for eight times.
+template <int D, int HB>
+__device__ __forceinline__ void load_heads(const __bf16* __restrict__ query, int H, unsigned char* buffer, bf16x8 (&qf)[HB][D / 16]) {
+    constexpr int KS = D / 16;
+    constexpr int kRounds = D / 64;  // four pieces of 8 values of each half of a head a round
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    uintx4 piece[HB][kRounds][4];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int head = i * 8 + lane / 8, p = lane % 8;
+                piece[hb][r][i] = *reinterpret_cast<const uintx4*>(query + static_cast<int64_t>(min(32 * hb + head, H - 1)) * D + ((p / 4) * KS + 4 * r + p % 4) * 8);
+            }
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {  // the wave's LDS accesses are done in order
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int head = i * 8 + lane / 8, p = lane % 8;
+                *reinterpret_cast<uintx4*>(buffer + (head * 8 + (p ^ (head % 8))) * 16) = piece[hb][r][i];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) qf[hb][4 * r + k] = *reinterpret_cast<const bf16x8*>(buffer + (col * 8 + ((half * 4 + k) ^ (col % 8))) * 16);
+        }
+}
+
 // What rows of U(t) receive of a query: S[32 heads x 32 rows] = q . tile^T with the heads on the M side, so that a lane holds 16 heads of
 // one row and the sum over heads is in-lane (and one exchange).  A lane's codes go from memory to its registers as they are needed there
 // (row = lane % 32, values D/2 * (lane / 32) .. + D/2: the contraction order is permuted alike on the query) and on to bf16, in which
 // both operands are exact: neither list nor tile goes through LDS.  The vector units bound it: 64 heads of 128 take 16 matrix instructions a
-// tile, 512 cycles, against 32 conversions, 32 fma, 32 additions and 32 exponentials at a quarter of their rate, 900.
-// One wave: tiles [first, last) of query row_q; add(row, sum) for every row of U(t) there, on the lanes below 32.  s_lse: 64 floats of the wave.
+// tile, 512 cycles, against 32 conversions, 32 fma, 32 additions and 32 exponentials, which take longer.
+// One wave: tiles [first, last) of query row_q; add(row, sum) for every row of U(t) there, on the lanes below 32.  lds: kWeighBytes of the wave.
+constexpr int kWeighBytes = 4096 + 256;
 template <int D, int HB, typename Add>
 __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                             const unsigned char* __restrict__ scales, const float* __restrict__ lse, int64_t row_q, int H,
-                                            int64_t first_row, const Tiles& u, int first, int last, float scale_log2e, float* s_lse, Add add) {
+                                            int64_t first_row, const Tiles& u, int first, int last, float scale_log2e, unsigned char* lds, Add add) {
     constexpr int KS = D / 16;
     if (first >= last) return;
     const int lane = threadIdx.x & 63;
@@ -617,41 +655,39 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
     const int half = lane >> 5;
     const unsigned char* const codes_b = codes + first_row * (D / 2) + half * (D / 4);
     const unsigned char* const scales_b = scales + first_row * (D / 32) + half * (D / 64);
-    Rows<D> next;
-    int s_now = u.row(first, col);
-    int s_next = first + 1 < last ? u.row(first + 1, col) : -1;
+    float* const s_lse = reinterpret_cast<float*>(lds + 4096);
+    int s_now = u.row(u.entry(first, col), first, col);
+    int next = u.entry(first + 1, col);
     s_lse[lane] = lane < H ? -kLog2e * lse[row_q * H + min(lane, H - 1)] : -__builtin_huge_valf();  // no head there: weight 0
-    bf16x8 qf[HB][KS];  // head 32 hb + col, values D/2 * half + 8 ks .. + 8
-#pragma unroll
-    for (int hb = 0; hb < HB; ++hb) {
-        const __bf16* src = qa + (row_q * H + min(32 * hb + col, H - 1)) * D + half * (D / 2);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[hb][ks] = *reinterpret_cast<const bf16x8*>(src + ks * 8);
-    }
-    next.read(codes_b, scales_b, max(s_now, 0));
-    floatx4 minus_lse[HB][4];  // of the heads this lane's results belong to, log2 domain
-#pragma unroll
-    for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) minus_lse[hb][a] = *reinterpret_cast<const floatx4*>(s_lse + 32 * hb + 8 * a + 4 * half);
+    bf16x8 qf[HB][KS];
+    load_heads<D, HB>(qa + row_q * H * D, H, lds, qf);
+    Rows<D> rows;
+    rows.read(codes_b, scales_b, max(s_now, 0));
     for (int tile = first; tile < last; ++tile) {
-        bf16x8 kf[KS];
+        floatx16 x[HB];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[ks] = next.values_bf16(ks);
+        for (int hb = 0; hb < HB; ++hb) x[hb] = floatx16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const bf16x8 v = rows.values_bf16(ks);
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb) x[hb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[hb][ks], v, x[hb], 0, 0, 0);
+        }
         const int s = s_now;
-        s_now = s_next;
-        if (tile + 1 < last) next.read(codes_b, scales_b, max(s_now, 0));
-        if (tile + 2 < last) s_next = u.row(tile + 2, col);
+        // also behind the last tile, where nothing comes of them: without branches the loads on their way can be told apart when one is waited for
+        s_now = u.row(next, tile + 1, col);
+        rows.read(codes_b, scales_b, max(s_now, 0));
+        next = u.entry(tile + 2, col);
         if (__ballot(s >= 0) == 0ull) continue;
         float sum = 0.0f;
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) {
-            floatx16 acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[hb][ks], kf[ks], acc, 0, 0, 0);
+            for (int a = 0; a < 4; ++a) {
+                const floatx4 minus_lse = *reinterpret_cast<const floatx4*>(s_lse + 32 * hb + 8 * a + 4 * half);  // of these heads
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j], scale_log2e, minus_lse[hb][j >> 2][j & 3]));
-        }
+                for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[hb][4 * a + j], scale_log2e, minus_lse[j]));
+            }
         sum += other_half(sum);
         if (half == 0 && s >= 0) add(s, sum);
     }
@@ -668,23 +704,25 @@ constexpr int kWeightWaves = 4;
 // A wave takes `per` tiles of a query (n_parts such parts a query).  S == 1: every row has one sum a call, added to
 // weights;  S > 1: 64-bit sums in the workspace, in any order.
 template <int D, int HB>
-__global__ __launch_bounds__(64 * kWeightWaves)
+__global__ __launch_bounds__(64 * kWeightWaves) __attribute__((amdgpu_waves_per_eu(3)))
 void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
-                               const int32_t* __restrict__ idx, int64_t n_items, int n_parts, int per, int S, int H, int T, int m, int mask_mode,
+                               const int32_t* __restrict__ idx, int64_t n_queries, int n_parts, int per, int S, int H, int T, int m, int mask_mode,
                                int k, int n_win, float scale_log2e, const float* __restrict__ lse, float* __restrict__ weights,
                                unsigned long long* __restrict__ sums) {
-    __shared__ __attribute__((aligned(16))) float s_lse[kWeightWaves][64];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kWeightWaves][kWeighBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * kWeightWaves + wave;
-    if (item >= n_items) return;
-    const int64_t row_q = item / n_parts;
-    const int part = static_cast<int>(item - row_q * n_parts);
+    // all workgroups of a query are on one XCD, as in the kernel for few queries
+    const int groups = (n_parts + kWeightWaves - 1) / kWeightWaves;
+    const unsigned turn = blockIdx.x / kXcds;
+    const int64_t row_q = static_cast<int64_t>(turn / groups) * kXcds + blockIdx.x % kXcds;
+    const int part = static_cast<int>(turn % groups) * kWeightWaves + wave;
+    if (row_q >= n_queries || part >= n_parts) return;
     const int b = static_cast<int>(row_q / S);
     const int t = static_cast<int>(row_q - static_cast<int64_t>(b) * S);
-    const Tiles u = tiles_of(idx, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
+    const Tiles u = tiles_of(idx, qa, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
     const int64_t first_row = static_cast<int64_t>(b) * T;
-    weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, first_row, u, part * per, min(u.count(), (part + 1) * per), scale_log2e, s_lse[wave],
+    weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, first_row, u, part * per, min(u.count(), (part + 1) * per), scale_log2e, lds[wave],
                        [&](int s, float sum) {
                            if (sums) atomicAdd(sums + first_row + s, to_fixed(sum));
                            else weights[first_row + s] += sum;
@@ -692,31 +730,30 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
 }
 
 // Many queries of few rows: a workgroup adds up in LDS what its queries (every n_groups-th wave's worth of a batch) give the batch's rows,
-// and then adds that to the workspace, row after row.
-constexpr int kGatherWaves = 8;
-template <int D, int HB>
-__global__ __launch_bounds__(64 * kGatherWaves)
+// and then adds that to the workspace, row after row.  Added up there at once, the sums wait for one another: 8192 queries of 640 of 2048 rows took
+// 657 us, 12 adds a nanosecond.
+template <int D, int HB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(3)))
 void gather_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                            const int32_t* __restrict__ lengths, const int32_t* __restrict__ idx, int n_groups, int S, int H, int T, int m,
                            int mask_mode, int k, int n_win, float scale_log2e, const float* __restrict__ lse,
                            unsigned long long* __restrict__ sums) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    __shared__ __attribute__((aligned(16))) float s_lse[kGatherWaves][64];
-    unsigned long long* const s_sums = reinterpret_cast<unsigned long long*>(lds);
+    unsigned long long* const s_sums = reinterpret_cast<unsigned long long*>(lds + WAVES * kWeighBytes);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / n_groups;
     const int group = blockIdx.x % n_groups;
-    for (int i = threadIdx.x; i < T; i += 64 * kGatherWaves) s_sums[i] = 0;
+    for (int i = threadIdx.x; i < T; i += 64 * WAVES) s_sums[i] = 0;
     __syncthreads();
     const int held = held_rows(lengths, b, T);
-    for (int t = group * kGatherWaves + wave; t < S; t += n_groups * kGatherWaves) {
+    for (int t = group * WAVES + wave; t < S; t += n_groups * WAVES) {
         const int64_t row_q = static_cast<int64_t>(b) * S + t;
-        const Tiles u = tiles_of(idx, row_q, t, k, held, n_win, m, mask_mode);
-        weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, static_cast<int64_t>(b) * T, u, 0, u.count(), scale_log2e, s_lse[wave],
+        const Tiles u = tiles_of(idx, qa, row_q, t, k, held, n_win, m, mask_mode);
+        weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, static_cast<int64_t>(b) * T, u, 0, u.count(), scale_log2e, lds + wave * kWeighBytes,
                            [&](int s, float sum) { atomicAdd(s_sums + s, to_fixed(sum)); });
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < T; i += 64 * kGatherWaves)
+    for (int i = threadIdx.x; i < T; i += 64 * WAVES)
         if (s_sums[i]) atomicAdd(sums + static_cast<int64_t>(b) * T + i, s_sums[i]);
 }
 
@@ -785,31 +822,42 @@ hipError_t launch_few(const Call& c, float* out, float* lse) {
     return wide && blocks <= 256 ? launch_few<D, 1, 16>(c, out, lse) : launch_few<D, 1, 8>(c, out, lse);
 }
 
-constexpr int kGatherRows = 16384;  // whose sums fit LDS: 128 KiB
+template <int D, int HB, int WAVES>
+hipError_t launch_gather(const Call& c, int most_groups, const float* lse, unsigned long long* sums) {
+    static std::atomic<size_t> allowed[64];
+    const int n_groups = std::min((c.d.S + WAVES - 1) / WAVES, std::max(1, most_groups / c.d.B));  // of a batch
+    const size_t lds = WAVES * kWeighBytes + static_cast<size_t>(c.d.T) * sizeof(unsigned long long);
+    hipError_t e = allow_lds(gather_weights_kernel<D, HB, WAVES>, lds, allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((gather_weights_kernel<D, HB, WAVES>), dim3(static_cast<unsigned>(c.d.B) * n_groups), dim3(64 * WAVES), lds, c.stream, c.qa,
+                       c.codes, c.scales, c.lengths, c.idx, n_groups, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e,
+                       lse, sums);
+    return hipGetLastError();
+}
+
+constexpr int kGatherRows = 15360;  // whose sums fit LDS beside the waves' parts: 120 KiB
+static_assert(8 * kWeighBytes + kGatherRows * 8 <= 159 * 1024, "the longest cache fits");
+
+// Many queries in one go over rows whose sums fit LDS; three workgroups of four waves a compute unit while LDS holds three, then one of eight.
+// Measured (us): sums in the workspace at once / 8 waves, 256 workgroups / 4 waves, 768 workgroups, 64 heads of 128: 8192 queries of 640 of 2048 rows
+// 657 / 116 / 106, 4000 of 1128 of 4000 381 / 104 / 95, 2 x 6000 of 428 of 6000 358 / 124 / 137, 10000 of 164 of 10000 114 / 63 / 90, 300 of 100 of 300
+// 22 / 16 / 17; few queries, whose tiles are then not shared out: 64 of 640 of 4000 8.7 / 28 / 22, 64 x 4 of 640 of 8192 16 / 25 / 26.
+bool gathers(const si_dims& d) {
+    return d.T <= kGatherRows && (d.S >= 128 || (d.S >= 16 && static_cast<int64_t>(d.B) * d.S >= 1024));
+}
 
 template <int D, int HB>
 hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsigned long long* sums) {
+    if (gathers(c.d)) return c.d.T <= 4096 ? launch_gather<D, HB, 4>(c, 768, lse, sums) : launch_gather<D, HB, 8>(c, 256, lse, sums);
     const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
     const int tiles = (c.k + kTileKeys - 1) / kTileKeys + (c.n_win + kTileKeys - 1) / kTileKeys;
-    // workgroups a batch, so that there are two a compute unit in all
-    const int n_groups = static_cast<int>(std::min<int64_t>((c.d.S + kGatherWaves - 1) / kGatherWaves, std::max(1, 512 / c.d.B)));
-    if (sums && c.d.T <= kGatherRows && static_cast<int64_t>(c.d.S) * (c.k + c.n_win) >= int64_t{2} * n_groups * c.d.T) {
-        static std::atomic<size_t> allowed[64];
-        const size_t lds = static_cast<size_t>(c.d.T) * sizeof(unsigned long long);
-        hipError_t e = allow_lds(gather_weights_kernel<D, HB>, lds, allowed);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((gather_weights_kernel<D, HB>), dim3(static_cast<unsigned>(c.d.B) * n_groups), dim3(64 * kGatherWaves), lds, c.stream,
-                           c.qa, c.codes, c.scales, c.lengths, c.idx, n_groups, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win,
-                           c.scale_log2e, lse, sums);
-        return hipGetLastError();
-    }
     // parts of at least two tiles, as many as fill the chip's waves once
     const int64_t most = std::max<int64_t>(1, 2048 / rows);
     const int per = static_cast<int>(std::max<int64_t>(2, (tiles + most - 1) / most));
     const int n_parts = std::max(1, (tiles + per - 1) / per);
-    const int64_t n_items = rows * n_parts;
-    hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>((n_items + kWeightWaves - 1) / kWeightWaves)),
-                       dim3(64 * kWeightWaves), 0, c.stream, c.qa, c.codes, c.scales, c.lengths, c.idx, n_items, n_parts, per, c.d.S, c.d.H_I,
+    const int64_t grid = (rows + kXcds - 1) / kXcds * kXcds * ((n_parts + kWeightWaves - 1) / kWeightWaves);
+    hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWeightWaves), 0, c.stream, c.qa, c.codes,
+                       c.scales, c.lengths, c.idx, rows, n_parts, per, c.d.S, c.d.H_I,
                        c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e, lse, weights, sums);
     return hipGetLastError();
 }
