@@ -73,9 +73,10 @@ __device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : p
 __device__ __forceinline__ uint32_t digit_mask(int pass) { return pass < 2 ? 0x7FFu : 0x3FFu; }
 __device__ __forceinline__ uint32_t seen_mask(int pass) { return pass == 0 ? 0u : 0xFFFFFFFFu << digit_shift(pass - 1); }
 
-// The digit of the border's word that a histogram of digits gives, into `at`.  The whole workgroup; s_waves: THREADS / 64 + 2 ints.
+// The highest digit down to which a histogram counts the rows still to be found; at.equal becomes how many of them have this digit.  The whole
+// workgroup; s_waves: THREADS / 64 + 2 ints.
 template <int THREADS>
-__device__ __forceinline__ void find_digit(const int* bins, int pass, Border& at, int* s_waves) {
+__device__ __forceinline__ int find_digit(const int* bins, Border& at, int* s_waves) {
     constexpr int kPer = kBins / THREADS;  // a thread has so many bins, the highest first
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int top = kBins - 1 - kPer * static_cast<int>(threadIdx.x);
@@ -89,8 +90,8 @@ __device__ __forceinline__ void find_digit(const int* bins, int pass, Border& at
     __syncthreads();  // an earlier digit has been read
     if (lane == 63) s_waves[wave] = upto;
     __syncthreads();
-    int above = upto - mine;
-    for (int i = 0; i < wave; ++i) above += s_waves[i];
+    const int earlier = lane < wave ? s_waves[lane] : 0;  // all at once: a loop would wait for LDS wave after wave
+    int above = upto - mine + lane_value(wave_prefix_sum(earlier), 63);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         if (above < at.equal && at.equal <= above + c[i]) {
@@ -100,12 +101,14 @@ __device__ __forceinline__ void find_digit(const int* bins, int pass, Border& at
         above += c[i];
     }
     __syncthreads();
-    at.word |= static_cast<uint32_t>(s_waves[THREADS / 64]) << digit_shift(pass);
     at.equal -= s_waves[THREADS / 64 + 1];
+    return s_waves[THREADS / 64];
 }
 
 // Batches of up to kMostRegisterRows rows: one workgroup a batch keeps the words in registers, KEYS a thread, finds the border and counts the
-// chunks.  Row i * 1024 + thread is a thread's i-th.
+// chunks.  Row i * 1024 + thread is a thread's i-th.  The digits are those of a word's distance from the smallest one, from its highest bit on: weights
+// spread over that range, where their upper 11 bits (sign, exponent) are a few dozen numbers whose counts in LDS wait for one another; the
+// smallest word itself, which rows that received nothing share, is counted by ballots (32 batches of 16411 rows, a third of them 0: 24 -> NEW us).
 template <int KEYS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths,
                                                                      Rule r, int B, Workspace ws, int n_chunks, int n_groups,
@@ -113,35 +116,75 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const floa
     constexpr int kWaves = kSelectThreads / 64;
     __shared__ int s_bins[kBins];
     __shared__ int s_waves[kWaves + 2];
+    __shared__ uint32_t s_range[2][kWaves];
     const int b = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Border at = first_border(lengths, b, r);
     const float* const w = weights + static_cast<int64_t>(b) * r.T;
     float raw[KEYS];
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) raw[i] = w[min(i * kSelectThreads + static_cast<int>(threadIdx.x), r.T - 1)];
+    for (int i = 0; i < KEYS; ++i)
+        if (i * kSelectThreads < r.T) raw[i] = w[min(i * kSelectThreads + static_cast<int>(threadIdx.x), r.T - 1)];
     uint32_t x[KEYS];
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) x[i] = word_of(raw[i], i * kSelectThreads + static_cast<int>(threadIdx.x), at.held, r);
+    for (int i = 0; i < KEYS; ++i)
+        if (i * kSelectThreads < r.T) x[i] = word_of(raw[i], i * kSelectThreads + static_cast<int>(threadIdx.x), at.held, r);
     if (at.held > at.stay) {
-        for (int pass = 0; pass < kPasses; ++pass) {
-            const uint32_t seen = seen_mask(pass), mask = digit_mask(pass);
-            const int shift = digit_shift(pass);
-            for (int i = threadIdx.x; i < kBins; i += kSelectThreads) s_bins[i] = 0;
-            __syncthreads();
+        // more rows are held than stay, so first and last ones do not overlap; they stay, and these are left to be found:
+        at.equal -= r.n_sink + r.n_recent;
+        if (at.equal == 0) {
+            at.word = 0xFFFFFFFFu;  // nothing else
+            at.equal = at.stay;
+        } else {
+            uint32_t low = 0xFFFFFFFFu, high = 0;
 #pragma unroll
             for (int i = 0; i < KEYS; ++i)
-                if (i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held && (x[i] & seen) == at.word)
-                    atomicAdd(&s_bins[(x[i] >> shift) & mask], 1);
+                if (i * kSelectThreads < at.held && i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held && x[i] != 0xFFFFFFFFu) {
+                    low = min(low, x[i]);
+                    high = max(high, x[i]);
+                }
+            low = wave_min(low);
+            high = wave_max(high);
+            if (lane == 0) {
+                s_range[0][wave] = low;
+                s_range[1][wave] = high;
+            }
             __syncthreads();
-            find_digit<kSelectThreads>(s_bins, pass, at, s_waves);
-            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                low = min(low, s_range[0][i]);
+                high = max(high, s_range[1][i]);
+            }
+            // words of low .. low + 2^(shift + digits) - 1 are in question
+            int shift = max(0, 32 - __clz(static_cast<int>(high - low)) - 11);
+            uint32_t span = high - low;  // largest distance in question
+            while (true) {
+                for (int i = threadIdx.x; i < kBins; i += kSelectThreads) s_bins[i] = 0;
+                __syncthreads();
+                int lowest = 0;
+#pragma unroll
+                for (int i = 0; i < KEYS; ++i) {
+                    if (i * kSelectThreads >= at.held) break;  // uniform
+                    const bool here = i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held && x[i] != 0xFFFFFFFFu && x[i] >= low && x[i] - low <= span;
+                    lowest += static_cast<int>(__popcll(__ballot(here && x[i] == low)));
+                    if (here && x[i] != low) atomicAdd(&s_bins[(x[i] - low) >> shift], 1);
+                }
+                if (lane == 0) atomicAdd(&s_bins[0], lowest);
+                __syncthreads();
+                const int digit = find_digit<kSelectThreads>(s_bins, at, s_waves);
+                __syncthreads();
+                low += static_cast<uint32_t>(digit) << shift;
+                if (shift == 0) break;
+                span = (1u << shift) - 1;
+                shift = max(0, shift - 11);
+            }
+            at.word = low;
         }
     }
     // runs of 64 rows in order: run i * 16 + wave; above and equal in one word
 #pragma unroll
     for (int i = 0; i < KEYS; ++i) {
-        const bool here = i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held;
+        const bool here = i * kSelectThreads < at.held && i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held;
         const unsigned long long above = __ballot(here && x[i] > at.word), equal = __ballot(here && x[i] == at.word);
         if (lane == 0) s_bins[i * kWaves + wave] = static_cast<int>(__popcll(above) | (__popcll(equal) << 16));
     }
@@ -210,7 +253,7 @@ __global__ __launch_bounds__(kCountThreads) void evict_digits_kernel(const float
     for (int i = threadIdx.x; i < kBins; i += kCountThreads) s_bins[i] = 0;
     int* const bins = ws.bins + static_cast<int64_t>(b) * kPasses * kBins;
     if (pass > 0) {
-        find_digit<kCountThreads>(bins + (pass - 1) * kBins, pass - 1, at, s_waves);
+        at.word |= static_cast<uint32_t>(find_digit<kCountThreads>(bins + (pass - 1) * kBins, at, s_waves)) << digit_shift(pass - 1);
         if (group == 0 && threadIdx.x == 0) ws.borders[static_cast<int64_t>(pass) * B + b] = at;
     }
     __syncthreads();
@@ -235,7 +278,7 @@ __global__ __launch_bounds__(kCountThreads) void evict_count_kernel(const float*
     Border at = first_border(lengths, b, r);
     if (at.held > at.stay) {
         at = ws.borders[static_cast<int64_t>(kPasses - 1) * B + b];
-        find_digit<kCountThreads>(ws.bins + (static_cast<int64_t>(b) * kPasses + kPasses - 1) * kBins, kPasses - 1, at, s_waves);
+        at.word |= static_cast<uint32_t>(find_digit<kCountThreads>(ws.bins + (static_cast<int64_t>(b) * kPasses + kPasses - 1) * kBins, at, s_waves));
     }
     const int first = group * kGroup + static_cast<int>(threadIdx.x);
     uint32_t x[kRowsPerThread];
@@ -298,15 +341,16 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* _
     static_assert(kChunk == kMoveThreads, "a thread a row");
     const int64_t b = blockIdx.x / n_chunks;
     const int c = static_cast<int>(blockIdx.x % n_chunks);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = c * kChunk + static_cast<int>(threadIdx.x);
+    const float w = weights[b * r.T + min(row, r.T - 1)];  // these three at once
+    const int2 before_chunk = ws.chunks[b * n_chunks + c];
     const Border border = ws.borders[static_cast<int64_t>(kPasses) * B + b];
     // lengths may be the same array: no kernel reads it any more
     if (c == 0 && threadIdx.x == 0 && new_lengths) new_lengths[b] = border.stay;
     if (c * kChunk >= border.held) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = c * kChunk + static_cast<int>(threadIdx.x);
     const bool here = row < border.held;
-    uint32_t x = 0;
-    if (here) x = word_of(weights[b * r.T + row], row, border.held, r);
+    const uint32_t x = here ? word_of(w, row, border.held, r) : 0u;
     int2 before = {0, 0};  // of the groups before this one
     for (int g = threadIdx.x; g < c / kGroupChunks; g += kMoveThreads) {
         const int2 v = ws.groups[b * n_groups + g];
@@ -322,7 +366,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* _
         s_waves[3][wave] = before.y;
     }
     __syncthreads();
-    before = ws.chunks[b * n_chunks + c];
+    before = before_chunk;
     for (int i = 0; i < kWaves; ++i) {
         before.x += s_waves[2][i];
         before.y += s_waves[3][i];

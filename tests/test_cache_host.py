@@ -163,16 +163,33 @@ def test_binding_checks_shapes_and_types_first(monkeypatch):
         P.si_evict_rows(w[0], None, n, 0, 0, [], kept, None, ws)
 
 
-def test_tensors_of_another_gpu_are_refused(monkeypatch):
-    class Elsewhere:
-        device = torch.device("cuda", 1)
+def test_tensors_and_streams_of_another_gpu_are_refused(monkeypatch):
+    class OnGpu(torch.Tensor):
+        """A host tensor that says it is on a GPU: the checks come before any use of it."""
+        gpu = 0
 
         def get_device(self):
-            return 1
+            return self.gpu
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    def at(gpu):
+        t = torch.zeros(4).as_subclass(OnGpu)
+        t.gpu = gpu
+        return t
+
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 5
+
+    monkeypatch.setattr(binding, "_current_gpu", lambda: 0)
+    assert binding._gpu_of(at(0), "x") == 0
+    with pytest.raises(ValueError):  # not the current GPU
+        binding._gpu_of(at(1), "x")
+    with pytest.raises(TypeError):
+        binding._gpu_of(torch.zeros(4), "x")
+    with pytest.raises((TypeError, ValueError)):  # another GPU than the call's first tensor
+        binding._ptr(at(1), torch.float32, 0, "x")
     with pytest.raises(ValueError):
-        binding._one_device(None, Elsewhere())
+        binding._stream_on(Stream(), 0)
+    assert binding._stream_on(Stream(), 1) == 5
 
 
 def test_reference_by_hand():
