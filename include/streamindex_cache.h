@@ -11,7 +11,7 @@
  *          value i is in byte i / 2 of the row, in the low half where i is even;
  *   scale  byte e + 127 of the power 2^e that values 32 j .. 32 j + 31 are multiples of, -13 <= e <= 13.
  * The cache is codes [B,T,D/2] and scales [B,T,D/32] bytes: 68 bytes a row of 128 in place of 256 in bf16.
- * What a row's codes stand for is exact in bf16 and in fp16.
+ * What a row's codes stand for is exact in bf16 and in fp16.  Scale bytes outside 114 .. 140 make no sense; no call writes them.
  */
 #ifndef STREAMINDEX_CACHE_H
 #define STREAMINDEX_CACHE_H
@@ -21,6 +21,9 @@
 #ifdef __cplusplus
 extern "C" {
 #endif
+
+/* Limits, SI_ERR_UNSUPPORTED_SHAPE beyond them: D as stated at each call; for the attention and its weights H <= 64, k <= 4096,
+ * n_win <= 4096, B S <= 2^24 - 8, T <= 2^30; for the eviction T <= 2^30, and B times T / 256 below 2^24. */
 
 /* Rows into the cache: row n of batch b becomes cache row start[b] + n.
  *   rows   device [B,S,D] bf16     S new rows a batch (dims->S; dims->H_I is not used); D = 32, 64 or 128
@@ -66,7 +69,7 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
  *   weights    device [B,T] f32      rows that are in no U(t) stay as they are
  *   workspace  device, si_accumulate_workspace_bytes(dims) bytes: none with S = 1 (may be NULL then), else 8 B T
  * A query's heads are summed in fp32, queries in 64-bit fixed point (units of 2^-32), so that the same call gives the
- * same bits.  S * H < 2^31 (SI_ERR_UNSUPPORTED_SHAPE beyond). */
+ * same bits. */
 size_t si_accumulate_workspace_bytes(const si_dims* dims);
 si_status si_accumulate_weights(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
                                 const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,

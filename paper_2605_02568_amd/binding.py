@@ -396,7 +396,7 @@ def si_quantized_attention(qa, codes, scales, lengths, idx, m, mask_mode, n_win,
     if lse is not None and lse.shape != qa.shape[:3]:
         raise ValueError(f"lse must be {tuple(qa.shape[:3])}")
     _check(load().si_quantized_attention(
-        q, c, s, held, lists, dims, m, k, mask_mode, n_win, scale, _ptr(out, torch.float32, gpu, "out"),
+        q, c, s, held, lists, dims, m, k, mask_mode, n_win, float(scale), _ptr(out, torch.float32, gpu, "out"),
         None if lse is None else _ptr(lse, torch.float32, gpu, "lse"), _stream_on(stream, gpu)), "si_quantized_attention")
 
 
@@ -414,7 +414,7 @@ def si_accumulate_weights(qa, codes, scales, lengths, idx, m, mask_mode, n_win, 
     if ws_bytes:
         ws = _ptr(workspace, torch.uint8, gpu, "workspace")
     _check(load().si_accumulate_weights(
-        q, c, s, held, lists, dims, m, k, mask_mode, n_win, scale, _ptr(lse, torch.float32, gpu, "lse"),
+        q, c, s, held, lists, dims, m, k, mask_mode, n_win, float(scale), _ptr(lse, torch.float32, gpu, "lse"),
         _ptr(weights, torch.float32, gpu, "weights"), ws, ws_bytes, _stream_on(stream, gpu)), "si_accumulate_weights")
 
 

@@ -766,6 +766,9 @@ __global__ void add_sums_kernel(const unsigned long long* __restrict__ sums, int
         if (sums[i]) weights[i] = static_cast<float>(weights[i] + static_cast<double>(sums[i]) * (1.0 / 4294967296.0));
 }
 
+constexpr int64_t kMostQueries = (int64_t{1} << 24) - 8;
+constexpr int32_t kMostRows = 1 << 30;
+
 struct Call {
     const __bf16* qa;
     const unsigned char *codes, *scales;
@@ -871,8 +874,8 @@ si_status check(const void* qa, const void* codes, const void* scales, const int
     if (!(scale == scale) || scale - scale != 0.0f) return SI_ERR_INVALID_ARG;  // NaN or infinite
     if (dims->D != 64 && dims->D != 128) return SI_ERR_UNSUPPORTED_SHAPE;
     if (dims->H_I > kMaxHeads || k > kMaxK || n_win > kMaxK) return SI_ERR_UNSUPPORTED_SHAPE;
-    // a launch has fewer than 2^32 threads in a dimension, up to 256 a query
-    if (static_cast<int64_t>(dims->B) * dims->S >= (int64_t{1} << 24)) return SI_ERR_UNSUPPORTED_SHAPE;
+    // a launch has fewer than 2^32 threads in a dimension, up to 256 a query, queries in eights; row numbers beyond a window's end fit 32 bits
+    if (static_cast<int64_t>(dims->B) * dims->S > kMostQueries || dims->T > kMostRows) return SI_ERR_UNSUPPORTED_SHAPE;
     return SI_OK;
 }
 
@@ -910,7 +913,6 @@ si_status si_accumulate_weights(const void* qa, const void* codes, const void* s
     const si_status ok = check(qa, codes, scales, idx, dims, m, k, mask_mode, n_win, scale);
     if (ok != SI_OK) return ok;
     if (!lse || !weights || !aligned16(lse) || !aligned16(weights)) return SI_ERR_INVALID_ARG;
-    if (static_cast<int64_t>(dims->S) * dims->H_I >= (int64_t{1} << 31)) return SI_ERR_UNSUPPORTED_SHAPE;
     const size_t need = si_accumulate_workspace_bytes(dims);
     if (need > 0 && (!workspace || !aligned16(workspace))) return SI_ERR_INVALID_ARG;
     if (workspace_bytes < need) return SI_ERR_WORKSPACE_TOO_SMALL;

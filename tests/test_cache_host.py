@@ -54,6 +54,8 @@ def _attention_calls(**bad):
     (dict(dims=(2, 3, 4, 32, 50)), P.SI_ERR_UNSUPPORTED_SHAPE), (dict(dims=(2, 3, 65, 64, 50)), P.SI_ERR_UNSUPPORTED_SHAPE),
     (dict(k=4097), P.SI_ERR_UNSUPPORTED_SHAPE), (dict(n_win=4097), P.SI_ERR_UNSUPPORTED_SHAPE),
     (dict(dims=(16, 1 << 20, 4, 64, 50)), P.SI_ERR_UNSUPPORTED_SHAPE),
+    (dict(dims=(1, (1 << 24) - 7, 4, 64, 50)), P.SI_ERR_UNSUPPORTED_SHAPE),
+    (dict(dims=(1, 1, 4, 64, (1 << 30) + 1)), P.SI_ERR_UNSUPPORTED_SHAPE),
 ])
 def test_attention_and_weights_refusals(bad, status):
     assert _attention_calls(**bad) == (status, status)
