@@ -1,7 +1,7 @@
 /*
  * libstreamindex -- a compressed cache that is held in 4 bits and bounded in length, for serving.
  * Same library, same conventions as streamindex.h: caller-owned device pointers, contiguous row-major,
- * 16-byte aligned (other alignments are refused); work is enqueued on `stream` and the call returns
+ * 16-byte aligned (start, lengths and new_lengths 4-byte; other alignments are refused); work is enqueued on `stream` and the call returns
  * without synchronising; nothing is allocated; only kernel launches are enqueued, so a call can be
  * captured into a HIP graph; argument errors are reported before anything is launched.  Two calls
  * that share a workspace, or of which one writes what the other reads or writes, must not overlap in time.
@@ -23,7 +23,8 @@ extern "C" {
 #endif
 
 /* Limits, SI_ERR_UNSUPPORTED_SHAPE beyond them: D as stated at each call; for the attention and its weights H <= 64, k <= 4096,
- * n_win <= 4096, B S <= 2^24 - 8, T <= 2^30; for the eviction T <= 2^30, and B times T / 256 below 2^24. */
+ * n_win <= 4096, B S <= 2^24 - 8, T <= 2^30; for the eviction T <= 2^30, B < 2^22, and
+ * B times T / 256 (rounded up) below 2^24. */
 
 /* Rows into the cache: row n of batch b becomes cache row start[b] + n.
  *   rows   device [B,S,D] bf16     S new rows a batch (dims->S; dims->H_I is not used); D = 32, 64 or 128

@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "attention_set.h"
+#include "cache_call.h"
 #include "si_internal.h"
 #include "streamindex_cache.h"
 #include "wave_ops.h"
@@ -865,10 +866,10 @@ hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsig
     return hipGetLastError();
 }
 
-si_status check(const void* qa, const void* codes, const void* scales, const int32_t* idx, const si_dims* dims, int32_t m, int32_t k,
-                si_mask_mode mask_mode, int32_t n_win, float scale) {
+si_status check(const void* qa, const void* codes, const void* scales, const int32_t* lengths, const int32_t* idx, const si_dims* dims,
+                int32_t m, int32_t k, si_mask_mode mask_mode, int32_t n_win, float scale) {
     if (!dims || !qa || !codes || !scales || (!idx && k != 0)) return SI_ERR_INVALID_ARG;
-    if (!aligned16(qa) || !aligned16(codes) || !aligned16(scales) || !aligned16(idx)) return SI_ERR_INVALID_ARG;
+    if (!aligned16(qa) || !aligned16(codes) || !aligned16(scales) || !aligned16(idx) || !aligned4(lengths)) return SI_ERR_INVALID_ARG;
     if (dims->B < 1 || dims->S < 1 || dims->H_I < 1 || dims->D < 1 || dims->T < 1 || m < 1 || k < 0 || n_win < 0) return SI_ERR_INVALID_ARG;
     if (mask_mode != SI_MASK_NONE && mask_mode != SI_MASK_CAUSAL_BLOCK) return SI_ERR_INVALID_ARG;
     if (!(scale == scale) || scale - scale != 0.0f) return SI_ERR_INVALID_ARG;  // NaN or infinite
@@ -890,7 +891,7 @@ extern "C" {
 si_status si_quantized_attention(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
                                  const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,
                                  int32_t n_win, float scale, float* out, float* lse, void* stream) {
-    const si_status ok = check(qa, codes, scales, idx, dims, m, k, mask_mode, n_win, scale);
+    const si_status ok = check(qa, codes, scales, lengths, idx, dims, m, k, mask_mode, n_win, scale);
     if (ok != SI_OK) return ok;
     if (!out || !aligned16(out) || !aligned16(lse)) return SI_ERR_INVALID_ARG;
     const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
@@ -910,7 +911,7 @@ si_status si_accumulate_weights(const void* qa, const void* codes, const void* s
                                 const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,
                                 int32_t n_win, float scale, const float* lse, float* weights, void* workspace,
                                 size_t workspace_bytes, void* stream) {
-    const si_status ok = check(qa, codes, scales, idx, dims, m, k, mask_mode, n_win, scale);
+    const si_status ok = check(qa, codes, scales, lengths, idx, dims, m, k, mask_mode, n_win, scale);
     if (ok != SI_OK) return ok;
     if (!lse || !weights || !aligned16(lse) || !aligned16(weights)) return SI_ERR_INVALID_ARG;
     const size_t need = si_accumulate_workspace_bytes(dims);

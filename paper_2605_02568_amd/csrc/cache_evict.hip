@@ -12,6 +12,7 @@
 
 #include <algorithm>
 
+#include "cache_call.h"
 #include "si_internal.h"
 #include "streamindex_cache.h"
 #include "wave_ops.h"
@@ -447,7 +448,7 @@ si_status si_evict_rows(const float* weights, const int32_t* lengths, int32_t B,
     if (B < 1 || T < 1 || n_keep < 1 || n_keep > T || n_sink < 0 || n_recent < 0 || n_sink > n_keep || n_recent > n_keep - n_sink)
         return SI_ERR_INVALID_ARG;
     if (n_moves < 0 || n_moves > SI_MAX_ROW_MOVES) return SI_ERR_INVALID_ARG;
-    if (!aligned16(weights) || !aligned16(kept) || !aligned16(workspace)) return SI_ERR_INVALID_ARG;
+    if (!aligned16(weights) || !aligned16(kept) || !aligned16(workspace) || !aligned4(lengths) || !aligned4(new_lengths)) return SI_ERR_INVALID_ARG;
     const int n_chunks = chunks_of(T);
     if (static_cast<int64_t>(B) * n_chunks >= (int64_t{1} << 32) / kMoveThreads || B >= (1 << 22) || T > (1 << 30)) return SI_ERR_UNSUPPORTED_SHAPE;
     if (workspace_bytes < si_evict_workspace_bytes(B, T)) return SI_ERR_WORKSPACE_TOO_SMALL;

@@ -12,6 +12,7 @@
 
 #include <algorithm>
 
+#include "cache_call.h"
 #include "si_internal.h"
 #include "streamindex_cache.h"
 
@@ -97,10 +98,10 @@ __global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const unsigne
     }
 }
 
-si_status check(const void* rows, const si_dims* dims, const void* codes, const void* scales) {
+si_status check(const void* rows, const int32_t* start, const si_dims* dims, const void* codes, const void* scales) {
     if (!rows || !dims || !codes || !scales) return SI_ERR_INVALID_ARG;
     if (dims->B < 1 || dims->S < 1 || dims->D < 1 || dims->T < 1) return SI_ERR_INVALID_ARG;
-    if (!aligned16(rows) || !aligned16(codes) || !aligned16(scales)) return SI_ERR_INVALID_ARG;
+    if (!aligned16(rows) || !aligned16(codes) || !aligned16(scales) || !aligned4(start)) return SI_ERR_INVALID_ARG;
     if (dims->D != 32 && dims->D != 64 && dims->D != 128) return SI_ERR_UNSUPPORTED_SHAPE;
     return SI_OK;
 }
@@ -119,7 +120,7 @@ extern "C" {
 
 si_status si_quantize_rows(const void* rows, const int32_t* start, const si_dims* dims, void* codes, void* scales,
                            void* stream) {
-    const si_status ok = check(rows, dims, codes, scales);
+    const si_status ok = check(rows, start, dims, codes, scales);
     if (ok != SI_OK) return ok;
     const int64_t n_units = static_cast<int64_t>(dims->B) * dims->S * (dims->D / 8);
 #define SI_LAUNCH(DD)                                                                                                        \
@@ -135,7 +136,7 @@ si_status si_quantize_rows(const void* rows, const int32_t* start, const si_dims
 
 si_status si_dequantize_rows(const void* codes, const void* scales, const int32_t* start, const si_dims* dims, void* rows,
                              void* stream) {
-    const si_status ok = check(rows, dims, codes, scales);
+    const si_status ok = check(rows, start, dims, codes, scales);
     if (ok != SI_OK) return ok;
     const int64_t n_units = static_cast<int64_t>(dims->B) * dims->S * (dims->D / 8);
 #define SI_LAUNCH(DD)                                                                                               \

@@ -571,8 +571,6 @@ si_status run_short_rows(const void* q, const void* K, const float* w, const si_
 }
 }  // namespace
 
-si_status report(hipError_t e) { return e == hipSuccess ? SI_OK : hip_fail(e); }
-
 // Per query row of a tile: a key buffer of 2k + c_T slots (a row is cut back to k as soon as
 // it holds 2k, and one key tile adds at most c_T), a count and a threshold.
 RowBuffers carve_workspace(void* base, int64_t rows_, int64_t k, int64_t c_T) {

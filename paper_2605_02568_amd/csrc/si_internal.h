@@ -74,11 +74,6 @@ constexpr int kFusedRowSlack = 384;
 // to a third.
 constexpr int kFusedDefaultRows = 131072;
 
-// The status of a call whose last HIP call returned e; keeps the code for si_last_hip_error.
-si_status report(hipError_t e);
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
 // Per-row state of the current query tile, carved from the caller's workspace.
 struct RowBuffers {
     key64_t* keys;   // [rows, cap] unsorted

@@ -22,6 +22,7 @@ def _rows_call(rows=0x1000, codes=0x2000, scales=0x3000, dims=(2, 3, 1, 64, 5), 
 @pytest.mark.parametrize("bad,status", [
     (dict(rows=None), P.SI_ERR_INVALID_ARG), (dict(codes=None), P.SI_ERR_INVALID_ARG), (dict(scales=None), P.SI_ERR_INVALID_ARG),
     (dict(rows=0x1008), P.SI_ERR_INVALID_ARG), (dict(codes=0x2004), P.SI_ERR_INVALID_ARG), (dict(scales=0x3001), P.SI_ERR_INVALID_ARG),
+    (dict(start=0x4002), P.SI_ERR_INVALID_ARG),
     (dict(dims=(0, 3, 1, 64, 5)), P.SI_ERR_INVALID_ARG), (dict(dims=(2, 0, 1, 64, 5)), P.SI_ERR_INVALID_ARG),
     (dict(dims=(2, 3, 1, 64, 0)), P.SI_ERR_INVALID_ARG), (dict(dims=(2, 3, 1, 0, 5)), P.SI_ERR_INVALID_ARG),
     (dict(dims=(2, 3, 1, 96, 5)), P.SI_ERR_UNSUPPORTED_SHAPE), (dict(dims=(2, 3, 1, 256, 5)), P.SI_ERR_UNSUPPORTED_SHAPE),
@@ -48,6 +49,7 @@ def _attention_calls(**bad):
     (dict(idx=None), P.SI_ERR_INVALID_ARG), (dict(dims=None), P.SI_ERR_INVALID_ARG),
     (dict(qa=0x1008), P.SI_ERR_INVALID_ARG), (dict(codes=0x2008), P.SI_ERR_INVALID_ARG), (dict(scales=0x3004), P.SI_ERR_INVALID_ARG),
     (dict(idx=0x5004), P.SI_ERR_INVALID_ARG), (dict(lse=0x7004), P.SI_ERR_INVALID_ARG),
+    (dict(lengths=0x4001), P.SI_ERR_INVALID_ARG),
     (dict(m=0), P.SI_ERR_INVALID_ARG), (dict(k=-1), P.SI_ERR_INVALID_ARG), (dict(n_win=-1), P.SI_ERR_INVALID_ARG),
     (dict(mask=2), P.SI_ERR_INVALID_ARG), (dict(scale=float("nan")), P.SI_ERR_INVALID_ARG), (dict(scale=float("-inf")), P.SI_ERR_INVALID_ARG),
     (dict(dims=(2, 3, 0, 64, 50)), P.SI_ERR_INVALID_ARG), (dict(dims=(2, 3, 4, 64, 0)), P.SI_ERR_INVALID_ARG),
@@ -103,6 +105,8 @@ def _evict_call(**bad):
     (dict(moves=((0x100008, 0x200000, 4),)), P.SI_ERR_INVALID_ARG), (dict(moves=((0x100000, 0x200004, 4),)), P.SI_ERR_INVALID_ARG),
     (dict(moves=tuple((0x100000 * i, 0x1000000 * i, 4) for i in range(1, 10))), P.SI_ERR_INVALID_ARG),
     (dict(weights=0x10004), P.SI_ERR_INVALID_ARG), (dict(kept=0x30008), P.SI_ERR_INVALID_ARG), (dict(ws=0x40004), P.SI_ERR_INVALID_ARG),
+    (dict(lengths=0x20002), P.SI_ERR_INVALID_ARG), (dict(new_lengths=0x20401), P.SI_ERR_INVALID_ARG),
+    (dict(B=1 << 22, T=200, n_keep=100, n_sink=0, n_recent=0), P.SI_ERR_UNSUPPORTED_SHAPE),
     (dict(B=0), P.SI_ERR_INVALID_ARG), (dict(T=0), P.SI_ERR_INVALID_ARG), (dict(n_keep=0), P.SI_ERR_INVALID_ARG),
     (dict(n_keep=1001), P.SI_ERR_INVALID_ARG), (dict(n_sink=-1), P.SI_ERR_INVALID_ARG), (dict(n_recent=-1), P.SI_ERR_INVALID_ARG),
     (dict(n_sink=300, n_recent=301), P.SI_ERR_INVALID_ARG), (dict(n_sink=1, n_recent=2 ** 31 - 1), P.SI_ERR_INVALID_ARG),
