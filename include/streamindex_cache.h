@@ -58,6 +58,8 @@ si_status si_dequantize_rows(const void* codes, const void* scales, const int32_
  *   out      device [B,S,H,D] f32,  lse device [B,S,H] f32 or NULL
  * fp32 products, statistics and sums; the weights enter the second product with 22 mantissa bits, or to 2^-32 of their sum where that
  * is more.
+ * A head whose query is not finite, or whose logits are not, gets NaN in out and lse, and no other head does.  scale has to be finite,
+ * scale * log2(e) too (SI_ERR_INVALID_ARG).
  * No workspace.  The same call gives the same bits. */
 si_status si_quantized_attention(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
                                  const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,
@@ -69,6 +71,7 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
  *   lse        device [B,S,H] f32    as that call wrote it
  *   weights    device [B,T] f32      rows that are in no U(t) stay as they are
  *   workspace  device, si_accumulate_workspace_bytes(dims) bytes: none with S = 1 (may be NULL then), else 8 B T
+ * A query with a head whose lse is NaN adds nothing.
  * A query's heads are summed in fp32, queries in 64-bit fixed point (units of 2^-32), so that the same call gives the
  * same bits. */
 size_t si_accumulate_workspace_bytes(const si_dims* dims);

@@ -600,9 +600,9 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
                 v += s_acc[(w * kPieces + piece) * kFewHeads + col];
             }
         }
-        *reinterpret_cast<floatx4*>(out + (row_q * H + h) * D + part * (D / DS) + 4 * piece) = v * (l_all > 0.0f ? 1.0f / l_all : 0.0f);
+        *reinterpret_cast<floatx4*>(out + (row_q * H + h) * D + part * (D / DS) + 4 * piece) = v * (l_all == 0.0f ? 0.0f : 1.0f / l_all);
         if (lse && piece == 0 && part == 0)
-            lse[row_q * H + h] = l_all > 0.0f ? (m_all - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2 : -__builtin_huge_valf();
+            lse[row_q * H + h] = l_all == 0.0f ? -__builtin_huge_valf() : (m_all - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2;
     }
 }
 
@@ -690,7 +690,8 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
                 for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[hb][4 * a + j], scale_log2e, minus_lse[j]));
             }
         sum += other_half(sum);
-        if (half == 0 && s >= 0) add(s, sum);
+        // a sum that is no number (some head's lse is none) is not added: it would stay in the weights for good, and has no fixed-point form
+        if (half == 0 && s >= 0 && sum < 4294967296.0f) add(s, sum);
     }
 }
 
@@ -872,7 +873,8 @@ si_status check(const void* qa, const void* codes, const void* scales, const int
     if (!aligned16(qa) || !aligned16(codes) || !aligned16(scales) || !aligned16(idx) || !aligned4(lengths)) return SI_ERR_INVALID_ARG;
     if (dims->B < 1 || dims->S < 1 || dims->H_I < 1 || dims->D < 1 || dims->T < 1 || m < 1 || k < 0 || n_win < 0) return SI_ERR_INVALID_ARG;
     if (mask_mode != SI_MASK_NONE && mask_mode != SI_MASK_CAUSAL_BLOCK) return SI_ERR_INVALID_ARG;
-    if (!(scale == scale) || scale - scale != 0.0f) return SI_ERR_INVALID_ARG;  // NaN or infinite
+    const float scale_log2e = scale * kLog2e;
+    if (scale_log2e - scale_log2e != 0.0f) return SI_ERR_INVALID_ARG;  // NaN, infinite, or not to be had in log2 units
     if (dims->D != 64 && dims->D != 128) return SI_ERR_UNSUPPORTED_SHAPE;
     if (dims->H_I > kMaxHeads || k > kMaxK || n_win > kMaxK) return SI_ERR_UNSUPPORTED_SHAPE;
     // a launch has fewer than 2^32 threads in a dimension, up to 256 a query, queries in eights; row numbers beyond a window's end fit 32 bits

@@ -52,6 +52,7 @@ def _attention_calls(**bad):
     (dict(lengths=0x4001), P.SI_ERR_INVALID_ARG),
     (dict(m=0), P.SI_ERR_INVALID_ARG), (dict(k=-1), P.SI_ERR_INVALID_ARG), (dict(n_win=-1), P.SI_ERR_INVALID_ARG),
     (dict(mask=2), P.SI_ERR_INVALID_ARG), (dict(scale=float("nan")), P.SI_ERR_INVALID_ARG), (dict(scale=float("-inf")), P.SI_ERR_INVALID_ARG),
+    (dict(scale=2.5e38), P.SI_ERR_INVALID_ARG), (dict(scale=-3e38), P.SI_ERR_INVALID_ARG),
     (dict(dims=(2, 3, 0, 64, 50)), P.SI_ERR_INVALID_ARG), (dict(dims=(2, 3, 4, 64, 0)), P.SI_ERR_INVALID_ARG),
     (dict(dims=(2, 3, 4, 32, 50)), P.SI_ERR_UNSUPPORTED_SHAPE), (dict(dims=(2, 3, 65, 64, 50)), P.SI_ERR_UNSUPPORTED_SHAPE),
     (dict(k=4097), P.SI_ERR_UNSUPPORTED_SHAPE), (dict(n_win=4097), P.SI_ERR_UNSUPPORTED_SHAPE),

@@ -266,6 +266,29 @@ def test_entries_outside_the_rows_held_are_skipped(S):
     _check(q, codes, scales, [60, 100], idx, 1, NONE, 5, 0.1)
 
 
+@pytest.mark.parametrize("S,H,D,k,n_win", [(1, 33, 128, 90, 9), (3, 20, 64, 40, 0), (260, 40, 128, 60, 5)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_queries_that_are_not_finite(S, H, D, k, n_win, bad):
+    """The head has NaN, no other head or query anything else than without it; its query gives no row a weight."""
+    B, T = 2, 150
+    q, codes, scales, idx = _problem(17, B, S, H, D, T, k, None, NONE, 1)
+    idx[1, S - 1, :] = np.arange(k)  # that query has rows
+    clean, clean_lse, _ = _run(q, codes, scales, None, idx, 1, NONE, n_win, 0.1)
+    spoilt = q.clone()
+    spoilt[1, S - 1, H - 2, 5] = bad
+    out, lse, weights = _run(spoilt, codes, scales, None, idx, 1, NONE, n_win, 0.1)
+    assert np.isnan(lse[1, S - 1, H - 2]) and np.all(np.isnan(out[1, S - 1, H - 2]))
+    out[1, S - 1, H - 2], lse[1, S - 1, H - 2] = clean[1, S - 1, H - 2], clean_lse[1, S - 1, H - 2]
+    assert np.array_equal(out, clean) and np.array_equal(lse, clean_lse)
+    if n_win == 0:  # the same as if that query's list were empty
+        lists = idx.copy()
+        lists[1, S - 1] = -1
+        assert np.array_equal(weights, _run(q, codes, scales, None, lists, 1, NONE, n_win, 0.1)[2])
+    assert np.all(np.isfinite(weights))
+    if S == 1:
+        assert np.all(weights[1] == 0.5)
+
+
 def test_weights_of_many_queries_in_one_row():
     """One row that every query and head gives everything: sums that fp32 alone would lose count in."""
     B, S, H, D, T = 1, 5000, 64, 64, 3
