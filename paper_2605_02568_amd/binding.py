@@ -313,7 +313,7 @@ def _gpu_of(t, name: str) -> int:
 
 
 def _ptr(t, dtype, gpu: int, name: str) -> int:
-    if t.dtype is dtype and t.get_device() == gpu and t.is_contiguous():
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == gpu and t.is_contiguous():
         return t.data_ptr()
     _dev_ptr(t, dtype, name)  # says what is wrong with the tensor
     raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's first tensor on cuda:{gpu}")
@@ -336,8 +336,14 @@ def _stream_on(stream, gpu: int) -> int:
     return int(stream.cuda_stream)
 
 
+def _int32(*sizes) -> None:
+    if max(sizes) >= 2 ** 31:
+        raise ValueError(f"sizes {sizes}: the library takes sizes below 2^31")
+
+
 @functools.lru_cache(maxsize=1024)
 def _sizes(B, S, H, D, T):
+    _int32(B, S, H, D, T)
     return byref(si_dims(B, S, H, D, T))
 
 
@@ -419,6 +425,7 @@ def si_accumulate_weights(qa, codes, scales, lengths, idx, m, mask_mode, n_win, 
 
 
 def si_evict_workspace_bytes(B, T) -> int:
+    _int32(B, T)
     return int(load().si_evict_workspace_bytes(B, T))
 
 
@@ -429,6 +436,7 @@ def si_evict_rows(weights, lengths, n_keep, n_sink, n_recent, moves, kept, new_l
     if len(weights.shape) != 2:
         raise ValueError("weights must be [B,T]")
     B, T = weights.shape
+    _int32(B, T, n_sink, n_recent)
     if kept.shape != (B, n_keep):
         raise ValueError(f"kept must be {(B, n_keep)}")
     if len(moves) > SI_MAX_ROW_MOVES:
@@ -442,7 +450,9 @@ def si_evict_rows(weights, lengths, n_keep, n_sink, n_recent, moves, kept, new_l
     for entry, (src, dst) in zip(table, moves):
         dtype = src.dtype
         entry.src, entry.dst = _ptr(src, dtype, gpu, "src of a move"), _ptr(dst, dtype, gpu, "dst of a move")
-        entry.row_bytes = dtype.itemsize * math.prod(src.shape[2:])
+        row_bytes = dtype.itemsize * math.prod(src.shape[2:])
+        _int32(row_bytes)
+        entry.row_bytes = row_bytes
     _check(load().si_evict_rows(
         _ptr(weights, torch.float32, gpu, "weights"), _per_batch(lengths, B, gpu, "lengths"), B, T, n_keep, n_sink, n_recent, table,
         len(moves), _ptr(kept, torch.int32, gpu, "kept"), _per_batch(new_lengths, B, gpu, "new_lengths"),

@@ -108,8 +108,9 @@ __device__ __forceinline__ int find_digit(const int* bins, Border& at, int* s_wa
 
 // Batches of up to kMostRegisterRows rows: one workgroup a batch keeps the words in registers, KEYS a thread, finds the border and counts the
 // chunks.  Row i * 1024 + thread is a thread's i-th.  The digits are those of a word's distance from the smallest one, from its highest bit on: weights
-// spread over that range, where their upper 11 bits (sign, exponent) are a few dozen numbers whose counts in LDS wait for one another; the
-// smallest word itself, which rows that received nothing share, is counted by ballots (32 batches of 16411 rows, a third of them 0: 24 -> NEW us).
+// spread over that range, where their upper 11 bits (sign, exponent) are a few dozen numbers; the smallest word itself, which rows that received
+// nothing share, is counted by ballots.  A chain of dependent steps bounds it, not the counts' conflicts: 32 batches of 16411 rows, a third of
+// them 0, take 20 us, as much as with digits of the words themselves (24 with a branch a row and prefix sums that waited for LDS once a wave).
 template <int KEYS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths,
                                                                      Rule r, int B, Workspace ws, int n_chunks, int n_groups,

@@ -170,6 +170,19 @@ def test_binding_checks_shapes_and_types_first(monkeypatch):
         P.si_evict_rows(w[0], None, n, 0, 0, [], kept, None, ws)
 
 
+def test_binding_refuses_sizes_beyond_int32():
+    for sizes in ((2 ** 31, 1, 1, 64, 1), (1, 1, 1, 64, 2 ** 32 + 5)):
+        with pytest.raises(ValueError):
+            P.si_accumulate_workspace_bytes(*sizes)
+    with pytest.raises(ValueError):
+        P.si_evict_workspace_bytes(1, 2 ** 32 + 5)
+    meta = lambda *s: torch.empty(s, device="meta", dtype=torch.uint8)  # noqa: E731
+    with pytest.raises((ValueError, TypeError)):
+        P.si_evict_rows(torch.empty((1, 2 ** 32 + 5), device="meta"), None, 4, 0, 0, [], meta(1, 4), None, meta(64))
+    with pytest.raises(TypeError):  # not a tensor
+        binding._ptr(None, torch.uint8, 0, "workspace")
+
+
 def test_tensors_and_streams_of_another_gpu_are_refused(monkeypatch):
     class OnGpu(torch.Tensor):
         """A host tensor that says it is on a GPU: the checks come before any use of it."""

@@ -374,6 +374,23 @@ def test_evict(B, T, n_keep, n_sink, n_recent, lengths, kind):
     _evict(w, lengths, n_keep, n_sink, n_recent, _arrays(rng, B, T, (4, 64)), alias=lengths is not None and kind == "ties")
 
 
+@pytest.mark.parametrize("B,T,n_keep,n_sink,n_recent,lengths", [
+    (2, 4097, 4096, 0, 1, None), (1, 16385, 9000, 4, 128, None), (3, 32768, 20000, 0, 0, [32768, 20001, 16385]), (2, 32769, 3, 0, 0, [32769, 2]),
+    (3, 50000, 30000, 1, 1, [0, 30001, 50000]), (3, 20000, 64, 60, 4, [20000, 65, 64]), (2, 40000, 64, 60, 4, [40000, 65]),
+])
+@pytest.mark.parametrize("kind", ["one", "spread", "near"])
+def test_evict_sizes_of_each_kind(B, T, n_keep, n_sink, n_recent, lengths, kind):
+    """Around the sizes where another kernel or another number of rows a thread begins; all weights alike, far apart, and of one exponent."""
+    print(f"evict B={B} T={T} n_keep={n_keep} n_sink={n_sink} n_recent={n_recent} lengths={lengths} {kind}", flush=True)
+    rng = np.random.default_rng(T)
+    w = np.full((B, T), 2.5, dtype=np.float32)
+    if kind == "spread":
+        w = (rng.choice([-1.0, 1.0], (B, T)) * np.exp(15 * rng.standard_normal((B, T)))).astype(np.float32)
+    if kind == "near":
+        w = (1 + rng.integers(0, 5000, (B, T)) * 2.0 ** -23).astype(np.float32)
+    _evict(w, lengths, n_keep, n_sink, n_recent, _arrays(rng, B, T, (4,)))
+
+
 @pytest.mark.parametrize("widths", [(), (1,), (2, 3), (16, 32, 48), (256, 64, 4, 4), (5, 6, 10, 12, 20, 100, 7, 260)])
 def test_evict_row_sizes(widths):
     rng = np.random.default_rng(len(widths))
