@@ -43,6 +43,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 // a weight are normal numbers down to 2^-18 of the reference's weight.
 constexpr float kWeightShift = 7.0f;
 
+// Between what some lanes of a wave write to LDS and others of it read there: the hardware does a wave's LDS accesses in order, and this keeps
+// the compiler to that order.  No instruction comes of it.
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
+
 __device__ __forceinline__ float power_of(unsigned scale_byte) { return __uint_as_float(scale_byte << 23); }
 
 // Rows that batch b holds, and legal rows of query t.
@@ -173,7 +177,7 @@ __device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, const
 // A lane's part of the tiles of 32 rows that its wave takes: row lane % 32, values D/2 * (lane / 32) .. + D/2, read from memory as codes and
 // scale bytes.  As fp16 they are the first product's operand as they are (the contraction order is permuted alike on the query); for the
 // second one they go through LDS, into a tile of the wave's own, row-major and swizzled (attention_set.h).  A wave's LDS accesses are done in
-// order, so no wave waits for another.
+// order (wave_order()), so no wave waits for another.
 // The scale bytes stay as they were read until they are used: taken apart at once they would be waited for at once.
 template <int D>
 struct Rows {
@@ -283,7 +287,9 @@ struct Heads {
         });
         halfx8 p_hi[2], p_lo[2];
         split_weights(p, p_hi, p_lo);
+        wave_order();
         add_values<D>(lds, at, p_hi, p_lo, acc);
+        wave_order();
     }
 };
 
@@ -554,6 +560,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
                 p_lo[2 * jj] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[0]), one, p[2 * jj]));
                 p_lo[2 * jj + 1] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[1]), one, p[2 * jj + 1]));
             }
+            wave_order();
             // contraction index e <-> tile row 16 (e / 4) + 4 quarter + e % 4 on both operands
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
@@ -565,6 +572,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
                 acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi, acc[db], 0, 0, 0);
                 acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo, acc[db], 0, 0, 0);
             }
+            wave_order();
         }
         l_sum += __shfl_xor(l_sum, 16);
         l_sum += __shfl_xor(l_sum, 32);
@@ -627,14 +635,16 @@ __device__ __forceinline__ void load_heads(const __bf16* __restrict__ query, int
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {  // the wave's LDS accesses are done in order
+        for (int r = 0; r < kRounds; ++r) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int head = i * 8 + lane / 8, p = lane % 8;
                 *reinterpret_cast<uintx4*>(buffer + (head * 8 + (p ^ (head % 8))) * 16) = piece[hb][r][i];
             }
+            wave_order();
 #pragma unroll
             for (int k = 0; k < 4; ++k) qf[hb][4 * r + k] = *reinterpret_cast<const bf16x8*>(buffer + (col * 8 + ((half * 4 + k) ^ (col % 8))) * 16);
+            wave_order();
         }
 }
 
