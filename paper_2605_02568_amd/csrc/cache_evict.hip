@@ -4,14 +4,16 @@
 // A weight is compared as a 32-bit word whose unsigned order is that of the weights: NaN 0, then -inf .. +inf, and rows that
 // always stay above all.  The n_keep-th largest word of a batch is found by radix descent over 11, 11 and 10 bits; rows above it
 // stay, and of those that equal it as many of the first as there is room for.  Then each workgroup takes a chunk of rows, lists those that stay
-// (where its list begins is known from the counts of the chunks before it) and copies what belongs to them.
+// (where its list begins is known from the counts of the chunks before it) and copies what belongs to them.  Small calls do all of it in one launch.
 //
 // The copies bound it: 2 * n_keep * (bytes of a row in all arrays).
 
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
+#include "attention_set.h"
 #include "cache_call.h"
 #include "si_internal.h"
 #include "streamindex_cache.h"
@@ -21,7 +23,7 @@ namespace si {
 
 namespace {
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 1024;             // 512: 32 batches of 16411 rows 1.3 times as long, 2048 rows alike
 constexpr int kCountThreads = 512;
 constexpr int kMoveThreads = 256;
 constexpr int kChunk = 256;                      // rows a workgroup of the copies takes
@@ -29,12 +31,12 @@ constexpr int kGroupChunks = 16;
 constexpr int kGroup = kGroupChunks * kChunk;    // rows a workgroup of the histograms and counts takes
 constexpr int kBins = 2048;
 constexpr int kPasses = 3;                       // digits of 11, 11 and 10 bits
-constexpr int kMostRegisterRows = 32 * kSelectThreads;
+constexpr int kMostSelectRows = 32768;
 
 // Where a batch stands in the descent, and at its end what the copies have to know.
 struct Border {
     uint32_t word;  // digits found so far; in the end: rows whose word is larger stay ..
-    int32_t equal;  // rows still to be found among those with these digits; in the end: .. and the first so many of those with this word
+    int32_t equal;  // rows still to be found among those with these digits; in the end: .. and the first so many of those with this word (maybe 0)
     int32_t held;   // rows that the batch holds
     int32_t stay;   // rows that stay
 };
@@ -75,7 +77,7 @@ __device__ __forceinline__ uint32_t digit_mask(int pass) { return pass < 2 ? 0x7
 __device__ __forceinline__ uint32_t seen_mask(int pass) { return pass == 0 ? 0u : 0xFFFFFFFFu << digit_shift(pass - 1); }
 
 // The highest digit down to which a histogram counts the rows still to be found; at.equal becomes how many of them have this digit.  The whole
-// workgroup; s_waves: THREADS / 64 + 2 ints.
+// workgroup, once a kernel; s_waves: THREADS / 64 + 2 ints.
 template <int THREADS>
 __device__ __forceinline__ int find_digit(const int* bins, Border& at, int* s_waves) {
     constexpr int kPer = kBins / THREADS;  // a thread has so many bins, the highest first
@@ -88,7 +90,6 @@ __device__ __forceinline__ int find_digit(const int* bins, Border& at, int* s_wa
         mine += c[i];
     }
     const int upto = wave_prefix_sum(mine);
-    __syncthreads();  // an earlier digit has been read
     if (lane == 63) s_waves[wave] = upto;
     __syncthreads();
     const int earlier = lane < wave ? s_waves[lane] : 0;  // all at once: a loop would wait for LDS wave after wave
@@ -106,112 +107,183 @@ __device__ __forceinline__ int find_digit(const int* bins, Border& at, int* s_wa
     return s_waves[THREADS / 64];
 }
 
-// Batches of up to kMostRegisterRows rows: one workgroup a batch keeps the words in registers, KEYS a thread, finds the border and counts the
-// chunks.  Row i * 1024 + thread is a thread's i-th.  The digits are those of a word's distance from the smallest one, from its highest bit on: weights
-// spread over that range, where their upper 11 bits (sign, exponent) are a few dozen numbers; the smallest word itself, which rows that received
-// nothing share, is counted by ballots.  A chain of dependent steps bounds it, not the counts' conflicts: 32 batches of 16411 rows, a third of
-// them 0, take 20 us, as much as with digits of the words themselves (24 with a branch a row and prefix sums that waited for LDS once a wave).
-template <int KEYS>
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths,
-                                                                     Rule r, int B, Workspace ws, int n_chunks, int n_groups,
-                                                                     int32_t* __restrict__ kept) {
+// Batches of up to kMostSelectRows rows: one workgroup has the words of a batch in LDS, finds the border and counts runs of 64 rows.  The digits, of 9
+// bits, are those of a word's distance from the smallest one, from its highest bit on: weights spread over that range, where their upper bits (sign,
+// exponent) are a few dozen numbers; the smallest word itself, which rows that received nothing share, is counted by ballots.  Every wave finds the
+// digit by itself.  Once a digit is down to 64 rows, these are listed, and each counts those above it.
+// What bounds it is a chain of dependent steps, and the way of its instructions from L2, where each launch begins anew: with the words in registers
+// and every loop over them unrolled, 32 batches of 16411 rows took 19.9 us with 18 KiB of code, and 23 where the list of 64 rows made it 30; as it
+// stands 11.5, and 2048 rows 4.4 in place of 6.1.
+constexpr int kSelectDigit = 9;
+constexpr int kSelectBins = 1 << kSelectDigit;
+constexpr int kSelectRounds = 4;  // that 32 bits have
+constexpr int kFewRows = 64;
+struct SelectShared {
+    int bins[kSelectRounds][kSelectBins];
+    int lowest[kSelectRounds];
+    int runs[kMostSelectRows / 64];  // rows of a run above the border and, in the upper half, those at it
+    uint32_t range[2][kSelectThreads / 64];
+    uint32_t few[kFewRows];
+    int n_few;
+};
+
+// The whole workgroup; `words`: LDS for a batch's, whole runs.  It may read the runs' counts when this returns.
+__device__ __forceinline__ Border select_rows(const float* __restrict__ w, const int32_t* __restrict__ lengths, int b, const Rule& r, SelectShared& sh,
+                                              uint32_t* words) {
     constexpr int kWaves = kSelectThreads / 64;
-    __shared__ int s_bins[kBins];
-    __shared__ int s_waves[kWaves + 2];
-    __shared__ uint32_t s_range[2][kWaves];
-    const int b = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    typedef const __attribute__((address_space(1))) void gbl_void;
+    typedef __attribute__((address_space(3))) void lds_void;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Border at = first_border(lengths, b, r);
-    const float* const w = weights + static_cast<int64_t>(b) * r.T;
-    float raw[KEYS];
-#pragma unroll
-    for (int i = 0; i < KEYS; ++i)
-        if (i * kSelectThreads < r.T) raw[i] = w[min(i * kSelectThreads + static_cast<int>(threadIdx.x), r.T - 1)];
-    uint32_t x[KEYS];
-#pragma unroll
-    for (int i = 0; i < KEYS; ++i)
-        if (i * kSelectThreads < r.T) x[i] = word_of(raw[i], i * kSelectThreads + static_cast<int>(threadIdx.x), at.held, r);
+    const int n_runs = (at.held + 63) / 64;
+    // a wave's own runs, here and below
+    for (int run = wave; run < n_runs; run += kWaves)
+        __builtin_amdgcn_global_load_lds((gbl_void*)(w + min(run * 64 + lane, r.T - 1)), (lds_void*)(words + run * 64), 4, 0, 0);
+    for (int i = threadIdx.x; i < kSelectRounds * kSelectBins; i += kSelectThreads) sh.bins[0][i] = 0;
+    if (threadIdx.x < kSelectRounds) sh.lowest[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.n_few = 0;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    uint32_t low = 0xFFFFFFFFu, high = 0;
+    for (int row = threadIdx.x; row < n_runs * 64; row += kSelectThreads) {
+        const uint32_t x = row < at.held ? word_of(__uint_as_float(words[row]), row, at.held, r) : 0xFFFFFFFFu;
+        words[row] = x;
+        low = min(low, x);
+        high = max(high, x == 0xFFFFFFFFu ? 0u : x);  // rows that always stay, or are not there, do not count
+    }
     if (at.held > at.stay) {
         // more rows are held than stay, so first and last ones do not overlap; they stay, and these are left to be found:
         at.equal -= r.n_sink + r.n_recent;
         if (at.equal == 0) {
-            at.word = 0xFFFFFFFFu;  // nothing else
-            at.equal = at.stay;
+            at.word = 0xFFFFFFFEu;  // nothing else
         } else {
-            uint32_t low = 0xFFFFFFFFu, high = 0;
-#pragma unroll
-            for (int i = 0; i < KEYS; ++i)
-                if (i * kSelectThreads < at.held && i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held && x[i] != 0xFFFFFFFFu) {
-                    low = min(low, x[i]);
-                    high = max(high, x[i]);
-                }
             low = wave_min(low);
             high = wave_max(high);
             if (lane == 0) {
-                s_range[0][wave] = low;
-                s_range[1][wave] = high;
+                sh.range[0][wave] = low;
+                sh.range[1][wave] = high;
             }
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) {
-                low = min(low, s_range[0][i]);
-                high = max(high, s_range[1][i]);
-            }
-            // words of low .. low + 2^(shift + digits) - 1 are in question
-            int shift = max(0, 32 - __clz(static_cast<int>(high - low)) - 11);
-            uint32_t span = high - low;  // largest distance in question
-            while (true) {
-                for (int i = threadIdx.x; i < kBins; i += kSelectThreads) s_bins[i] = 0;
-                __syncthreads();
+            low = wave_min(sh.range[0][lane % kWaves]);
+            high = wave_max(sh.range[1][lane % kWaves]);
+            int there;  // rows with the word in the end
+            for (int round = 0;; ++round) {
+                // the words low .. high are in question: low itself, and the distances from low + 1, whose digit counts
+                const uint32_t span = high - low;
+                const int shift = max(0, 32 - __clz(static_cast<int>(span)) - kSelectDigit);
                 int lowest = 0;
-#pragma unroll
-                for (int i = 0; i < KEYS; ++i) {
-                    if (i * kSelectThreads >= at.held) break;  // uniform
-                    const bool here = i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held && x[i] != 0xFFFFFFFFu && x[i] >= low && x[i] - low <= span;
-                    lowest += static_cast<int>(__popcll(__ballot(here && x[i] == low)));
-                    if (here && x[i] != low) atomicAdd(&s_bins[(x[i] - low) >> shift], 1);
+                for (int row = threadIdx.x; row < n_runs * 64; row += kSelectThreads) {
+                    const uint32_t far = words[row] - low;
+                    lowest += static_cast<int>(__popcll(__ballot(far == 0)));
+                    if (far - 1 < span) atomicAdd(&sh.bins[round][(far - 1) >> shift], 1);
                 }
-                if (lane == 0) atomicAdd(&s_bins[0], lowest);
+                if (lane == 0 && lowest > 0) atomicAdd(&sh.lowest[round], lowest);
                 __syncthreads();
-                const int digit = find_digit<kSelectThreads>(s_bins, at, s_waves);
-                __syncthreads();
-                low += static_cast<uint32_t>(digit) << shift;
+                // a lane has 8 bins, the highest first
+                constexpr int kPer = kSelectBins / 64;
+                const int top = kSelectBins - 1 - kPer * lane;
+                int c[kPer], mine = 0;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    c[i] = sh.bins[round][top - i];
+                    mine += c[i];
+                }
+                const int upto = wave_prefix_sum(mine);
+                const unsigned long long in = __ballot(at.equal <= upto);
+                if (in == 0ull) {  // as a rule rows that received nothing
+                    at.equal -= lane_value(upto, 63);
+                    there = sh.lowest[round];
+                    break;
+                }
+                const int at_lane = __ffsll(in) - 1;
+                int left = at.equal - lane_value(upto - mine, at_lane), digit = kSelectBins - 1 - kPer * at_lane;
+                there = lane_value(c[0], at_lane);
+#pragma unroll
+                for (int i = 1; i < kPer; ++i)
+                    if (left > there) {
+                        left -= there;
+                        there = lane_value(c[i], at_lane);
+                        --digit;
+                    }
+                at.equal = left;
+                low += 1 + (static_cast<uint32_t>(digit) << shift);
                 if (shift == 0) break;
-                span = (1u << shift) - 1;
-                shift = max(0, shift - 11);
+                high = min(low + ((1u << shift) - 1), high);
+                if (there <= kFewRows) {
+                    for (int row = threadIdx.x; row < n_runs * 64; row += kSelectThreads) {
+                        const uint32_t x = words[row];
+                        if (x - low <= high - low) sh.few[atomicAdd(&sh.n_few, 1)] = x - low;  // `there` of them
+                    }
+                    __syncthreads();
+                    const uint32_t far = sh.few[min(lane, there - 1)];
+                    unsigned long long alive = there == 64 ? ~0ull : (1ull << there) - 1;
+                    for (int bit = shift - 1; bit >= 0; --bit) {
+                        const unsigned long long ones = __ballot((far >> bit) & 1) & alive;
+                        const int n = static_cast<int>(__popcll(ones));
+                        if (at.equal <= n) {
+                            alive = ones;
+                            low += 1u << bit;
+                        } else {
+                            alive &= ~ones;
+                            at.equal -= n;
+                        }
+                    }
+                    there = static_cast<int>(__popcll(alive));
+                    break;
+                }
             }
             at.word = low;
+            if (at.equal == there) {  // all of them: the rows above the word before it (there is one, as not all rows stay)
+                at.word -= 1;
+                at.equal = 0;
+            }
         }
     }
-    // runs of 64 rows in order: run i * 16 + wave; above and equal in one word
-#pragma unroll
-    for (int i = 0; i < KEYS; ++i) {
-        const bool here = i * kSelectThreads < at.held && i * kSelectThreads + static_cast<int>(threadIdx.x) < at.held;
-        const unsigned long long above = __ballot(here && x[i] > at.word), equal = __ballot(here && x[i] == at.word);
-        if (lane == 0) s_bins[i * kWaves + wave] = static_cast<int>(__popcll(above) | (__popcll(equal) << 16));
+    for (int run = wave; run * 64 < r.T; run += kWaves) {
+        int n = 0;
+        if (run < n_runs) {
+            const uint32_t x = words[run * 64 + lane];
+            const bool here = run * 64 + lane < at.held;
+            n = static_cast<int>(__popcll(__ballot(here && x > at.word)) | (__popcll(__ballot(here && x == at.word)) << 16));
+        }
+        if (lane == 0) sh.runs[run] = n;
     }
     __syncthreads();
-    if (wave < (KEYS * kWaves + 255) / 256) {  // a lane sums a chunk's four runs, a wave up to 64 chunks; waves behind the first sum those before
-        constexpr int kRunsPerChunk = kChunk / 64;
+    return at;
+}
+
+constexpr int kRunsPerChunk = kChunk / 64;
+
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths,
+                                                                     Rule r, int B, Workspace ws, int n_chunks, int n_groups,
+                                                                     int32_t* __restrict__ kept) {
+    extern __shared__ uint32_t words[];
+    __shared__ SelectShared sh;
+    const int b = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Border at = select_rows(weights + static_cast<int64_t>(b) * r.T, lengths, b, r, sh, words);
+    if (wave * 64 < n_chunks) {  // a lane sums a chunk's runs, a wave 64 chunks; waves behind the first sum those before
+        const int n_runs = (r.T + 63) / 64;
+        auto counts = [&](int chunk) {
+            int2 n = {0, 0};
+#pragma unroll
+            for (int q = 0; q < kRunsPerChunk; ++q) {
+                const int run = chunk * kRunsPerChunk + q;
+                const int c = run < n_runs ? sh.runs[run] : 0;
+                n.x += c & 0xFFFF;
+                n.y += c >> 16;
+            }
+            return n;
+        };
         int2 before = {0, 0};
-        for (int v = 0; v < wave; ++v)
-            for (int q = 0; q < kRunsPerChunk; ++q) {
-                const int c = s_bins[(v * 64 + lane) * kRunsPerChunk + q];
-                before.x += c & 0xFFFF;
-                before.y += c >> 16;
-            }
-        before.x = lane_value(wave_prefix_sum(before.x), 63);
-        before.y = lane_value(wave_prefix_sum(before.y), 63);
+        for (int v = 0; v < wave; ++v) {
+            const int2 n = counts(v * 64 + lane);
+            before.x += n.x;
+            before.y += n.y;
+        }
+        const int2 mine = counts(wave * 64 + lane);
+        before.x = lane_value(wave_prefix_sum(before.x), 63) + wave_prefix_sum(mine.x) - mine.x;
+        before.y = lane_value(wave_prefix_sum(before.y), 63) + wave_prefix_sum(mine.y) - mine.y;
         const int chunk = wave * 64 + lane;
-        int2 mine = {0, 0};
-        if (chunk * kRunsPerChunk < KEYS * kWaves)
-            for (int q = 0; q < kRunsPerChunk; ++q) {
-                const int c = s_bins[chunk * kRunsPerChunk + q];
-                mine.x += c & 0xFFFF;
-                mine.y += c >> 16;
-            }
-        before.x += wave_prefix_sum(mine.x) - mine.x;
-        before.y += wave_prefix_sum(mine.y) - mine.y;
         if (chunk < n_chunks) ws.chunks[static_cast<int64_t>(b) * n_chunks + chunk] = before;
     }
     if (static_cast<int>(threadIdx.x) < n_groups) ws.groups[static_cast<int64_t>(b) * n_groups + threadIdx.x] = {0, 0};  // counted from the batch's first row
@@ -303,8 +375,13 @@ __global__ __launch_bounds__(kCountThreads) void evict_count_kernel(const float*
     if (group == 0 && threadIdx.x == 0) ws.borders[static_cast<int64_t>(kPasses) * B + b] = at;
 }
 
+// Lanes of a ballot before this one.
+__device__ __forceinline__ int lanes_below(unsigned long long lanes) {
+    return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(lanes), 0u)));
+}
+
 // Copies rows s_rows[0 .. n) of one array to n rows in a row, in units of type V, four of a thread on their way at once.
-template <typename V>
+template <typename V, int THREADS>
 __device__ __forceinline__ void copy_rows(const unsigned char* __restrict__ src, unsigned char* __restrict__ dst, int row_bytes,
                                           const int* s_rows, int n) {
     const unsigned units = static_cast<unsigned>(row_bytes) / static_cast<unsigned>(sizeof(V));
@@ -313,43 +390,59 @@ __device__ __forceinline__ void copy_rows(const unsigned char* __restrict__ src,
         // i / units as a product: exact for i < 2^20 and units <= 2^12 (the excess of the factor adds less than 2^-12)
         const unsigned inverse = static_cast<unsigned>(((1ull << 32) + units - 1) / units);
         const unsigned total = static_cast<unsigned>(n) * units;
-        for (unsigned i0 = threadIdx.x; i0 < total; i0 += kAhead * kMoveThreads) {
+        for (unsigned i0 = threadIdx.x; i0 < total; i0 += kAhead * THREADS) {
             V v[kAhead];
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
-                const unsigned i = min(i0 + a * kMoveThreads, total - 1);
+                const unsigned i = min(i0 + a * THREADS, total - 1);
                 const unsigned j = units == 1 ? i : __umulhi(i, inverse);
                 v[a] = reinterpret_cast<const V*>(src + static_cast<int64_t>(s_rows[j]) * row_bytes)[i - j * units];
             }
 #pragma unroll
             for (int a = 0; a < kAhead; ++a)
-                if (i0 + a * kMoveThreads < total) reinterpret_cast<V*>(dst)[i0 + a * kMoveThreads] = v[a];
+                if (i0 + a * THREADS < total) reinterpret_cast<V*>(dst)[i0 + a * THREADS] = v[a];
         }
         return;
     }
     for (int j = 0; j < n; ++j) {  // rows longer than a workgroup's trip
         const V* const from = reinterpret_cast<const V*>(src + static_cast<int64_t>(s_rows[j]) * row_bytes);
         V* const to = reinterpret_cast<V*>(dst + static_cast<int64_t>(j) * row_bytes);
-        for (unsigned u = threadIdx.x; u < units; u += kMoveThreads) to[u] = from[u];
+        for (unsigned u = threadIdx.x; u < units; u += THREADS) to[u] = from[u];
+    }
+}
+
+// Rows s_rows[0 .. n) of batch b in every parts-th array, to places from `to` on.
+template <int THREADS>
+__device__ __forceinline__ void copy_chunk(const Moves& moves, int part, int parts, int64_t b, const Rule& r, int64_t to, const int* s_rows, int n) {
+    for (int a = part; a < moves.n; a += parts) {
+        const int row_bytes = moves.row_bytes[a];
+        const unsigned char* const src = moves.src[a] + b * r.T * row_bytes;
+        unsigned char* const dst = moves.dst[a] + to * row_bytes;
+        if (row_bytes % 16 == 0) copy_rows<uint4, THREADS>(src, dst, row_bytes, s_rows, n);
+        else if (row_bytes % 4 == 0) copy_rows<uint32_t, THREADS>(src, dst, row_bytes, s_rows, n);
+        else if (row_bytes % 2 == 0) copy_rows<uint16_t, THREADS>(src, dst, row_bytes, s_rows, n);
+        else copy_rows<unsigned char, THREADS>(src, dst, row_bytes, s_rows, n);
     }
 }
 
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* __restrict__ weights, Rule r, int B, Workspace ws, int n_chunks,
-                                                                 int n_groups, Moves moves, int32_t* __restrict__ kept,
+                                                                 int n_groups, Moves moves, int parts, int32_t* __restrict__ kept,
                                                                  int32_t* __restrict__ new_lengths) {
     constexpr int kWaves = kMoveThreads / 64;
     __shared__ int s_rows[kChunk];
     __shared__ int s_waves[4][kWaves];
     static_assert(kChunk == kMoveThreads, "a thread a row");
-    const int64_t b = blockIdx.x / n_chunks;
-    const int c = static_cast<int>(blockIdx.x % n_chunks);
+    // a workgroup copies every parts-th array of a chunk's rows
+    const int part = static_cast<int>(blockIdx.x % parts);
+    const int64_t b = blockIdx.x / parts / n_chunks;
+    const int c = static_cast<int>(blockIdx.x / parts % n_chunks);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int row = c * kChunk + static_cast<int>(threadIdx.x);
     const float w = weights[b * r.T + min(row, r.T - 1)];  // these three at once
     const int2 before_chunk = ws.chunks[b * n_chunks + c];
     const Border border = ws.borders[static_cast<int64_t>(kPasses) * B + b];
     // lengths may be the same array: no kernel reads it any more
-    if (c == 0 && threadIdx.x == 0 && new_lengths) new_lengths[b] = border.stay;
+    if (c == 0 && part == 0 && threadIdx.x == 0 && new_lengths) new_lengths[b] = border.stay;
     if (c * kChunk >= border.held) return;
     const bool here = row < border.held;
     const uint32_t x = here ? word_of(w, row, border.held, r) : 0u;
@@ -373,13 +466,13 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* _
         before.x += s_waves[2][i];
         before.y += s_waves[3][i];
     }
-    int rank = before.y + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(equal >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(equal), 0u));
+    int rank = before.y + lanes_below(equal);
     for (int i = 0; i < wave; ++i) rank += s_waves[0][i];
     const bool stays = here && (x > border.word || (x == border.word && rank < border.equal));
     const unsigned long long mine = __ballot(stays);
     if (lane == 0) s_waves[1][wave] = static_cast<int>(__popcll(mine));
     __syncthreads();
-    int place = __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(mine >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(mine), 0u));
+    int place = lanes_below(mine);
     int n = 0;
     for (int i = 0; i < kWaves; ++i) {
         if (i < wave) place += s_waves[1][i];
@@ -388,20 +481,70 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const float* _
     const int64_t to = b * r.n_keep + before.x + min(before.y, border.equal);  // the chunk's first place
     if (stays) {
         s_rows[place] = row;
-        kept[to + place] = row;
+        if (part == 0) kept[to + place] = row;
     }
     __syncthreads();
     if (n == 0) return;
-    for (int a = 0; a < moves.n; ++a) {
-        const int row_bytes = moves.row_bytes[a];
-        const unsigned char* const src = moves.src[a] + b * r.T * row_bytes;
-        unsigned char* const dst = moves.dst[a] + to * row_bytes;
-        if (row_bytes % 16 == 0) copy_rows<uint4>(src, dst, row_bytes, s_rows, n);
-        else if (row_bytes % 4 == 0) copy_rows<uint32_t>(src, dst, row_bytes, s_rows, n);
-        else if (row_bytes % 2 == 0) copy_rows<uint16_t>(src, dst, row_bytes, s_rows, n);
-        else copy_rows<unsigned char>(src, dst, row_bytes, s_rows, n);
-    }
+    copy_chunk<kMoveThreads>(moves, part, parts, b, r, to, s_rows, n);
 }
+
+// Few rows in all: a workgroup a chunk and array, each of which finds its batch's border by itself.  One launch and no way through the workspace.
+// `lengths` is read by all of them, so new_lengths must be elsewhere.
+__global__ __launch_bounds__(kSelectThreads) void evict_few_kernel(const float* __restrict__ weights, const int32_t* __restrict__ lengths, Rule r,
+                                                                  int n_chunks, Moves moves, int parts, int32_t* __restrict__ kept,
+                                                                  int32_t* __restrict__ new_lengths) {
+    extern __shared__ uint32_t words[];
+    __shared__ SelectShared sh;
+    __shared__ int s_rows[kChunk];
+    const int part = static_cast<int>(blockIdx.x % parts);
+    const int b = static_cast<int>(blockIdx.x / parts / n_chunks);
+    const int c = static_cast<int>(blockIdx.x / parts % n_chunks);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Border at = select_rows(weights + static_cast<int64_t>(b) * r.T, lengths, b, r, sh, words);
+    const int64_t first_place = static_cast<int64_t>(b) * r.n_keep;
+    if (c == 0 && part == 0) {
+        if (threadIdx.x == 0 && new_lengths) new_lengths[b] = at.stay;
+        for (int j = at.stay + static_cast<int>(threadIdx.x); j < r.n_keep; j += kSelectThreads) kept[first_place + j] = -1;
+    }
+    if (c * kChunk >= at.held) return;
+    // rows above the border and at it before the chunk, and before its runs (both counts in one word)
+    unsigned counted = 0;
+    for (int run = lane; run < c * kRunsPerChunk; run += 64) counted += static_cast<unsigned>(sh.runs[run]);
+    unsigned before[kRunsPerChunk + 1];
+    before[0] = static_cast<unsigned>(lane_value(wave_prefix_sum(static_cast<int>(counted)), 63));
+#pragma unroll
+    for (int q = 0; q < kRunsPerChunk; ++q) {
+        const int run = c * kRunsPerChunk + q;
+        before[q + 1] = before[q] + (run * 64 < r.T ? static_cast<unsigned>(sh.runs[run]) : 0u);
+    }
+    auto stay_before = [&](unsigned n) { return static_cast<int>(n & 0xFFFFu) + min(static_cast<int>(n >> 16), at.equal); };
+    const int first = stay_before(before[0]), n = stay_before(before[kRunsPerChunk]) - first;
+#pragma unroll
+    for (int q = 0; q < kRunsPerChunk; ++q)
+        if (wave == q) {
+            const int row = c * kChunk + static_cast<int>(threadIdx.x);
+            const bool here = row < at.held;
+            const uint32_t x = here ? words[row] : 0u;
+            const unsigned long long equal = __ballot(here && x == at.word);
+            const int rank = static_cast<int>(before[q] >> 16) + lanes_below(equal);
+            const bool stays = here && (x > at.word || (x == at.word && rank < at.equal));
+            const unsigned long long mine = __ballot(stays);
+            const int place = stay_before(before[q]) + lanes_below(mine);
+            if (stays) {
+                s_rows[place - first] = row;
+                if (part == 0) kept[first_place + place] = row;
+            }
+        }
+    __syncthreads();
+    if (n > 0) copy_chunk<kSelectThreads>(moves, part, parts, b, r, first_place + first, s_rows, n);
+}
+
+// Up to so many chunks in all one launch does (a compute unit has two of its workgroups at once), up to so many of them with a workgroup an array, so that
+// no array waits for another one.  Measured (us, two launches / one / one with a workgroup an array; rows of 64 + 4 + 4 + 256 bytes, three quarters stay):
+// 1 x 512 rows 11 / 8.1 / 6.3, 1 x 2048 12.8 / 9.6 / 7.5, 8 x 2048 13.6 / 10.2 / 8.8, 1 x 16384 20.6 / 17.2 / 15.9, 1 x 32768 29.9 / 25.9 / 26.0,
+// 32 x 2048 17.5 / 12.5 / -, 64 x 2048 21.8 / 18.1 / -, 8 x 16384 28.6 / 28.7 / -, 32 x 16384 68 / 101 / -.
+constexpr int64_t kFewChunks = 512;
+constexpr int64_t kFewestChunks = 100;
 
 int chunks_of(int32_t T) { return static_cast<int>((static_cast<int64_t>(T) + kChunk - 1) / kChunk); }
 int groups_of(int32_t T) { return (chunks_of(T) + kGroupChunks - 1) / kGroupChunks; }
@@ -415,7 +558,7 @@ Workspace carve(void* base, int32_t B, int32_t T) {
         return p;
     };
     ws.borders = static_cast<Border*>(take(static_cast<size_t>(kPasses + 1) * B * sizeof(Border)));
-    ws.bins = static_cast<int*>(take(T > kMostRegisterRows ? static_cast<size_t>(B) * kPasses * kBins * sizeof(int) : 0));
+    ws.bins = static_cast<int*>(take(T > kMostSelectRows ? static_cast<size_t>(B) * kPasses * kBins * sizeof(int) : 0));
     ws.chunks = static_cast<int2*>(take(static_cast<size_t>(B) * chunks_of(T) * sizeof(int2)));
     ws.groups = static_cast<int2*>(take(static_cast<size_t>(B) * groups_of(T) * sizeof(int2)));
     ws.bytes = at;
@@ -486,33 +629,42 @@ si_status si_evict_rows(const float* weights, const int32_t* lengths, int32_t B,
     const Rule r = {T, n_keep, n_sink, n_recent};
     hipStream_t hs = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
-    if (T <= kMostRegisterRows) {
-#define SI_LAUNCH(KEYS)                                                                                                            \
-    hipLaunchKernelGGL((evict_select_kernel<KEYS>), dim3(B), dim3(kSelectThreads), 0, hs, weights, lengths, r, B, ws, n_chunks, n_groups, \
-                       kept)
-        if (T <= 4 * kSelectThreads) SI_LAUNCH(4);
-        else if (T <= 16 * kSelectThreads) SI_LAUNCH(16);
-        else SI_LAUNCH(32);
-#undef SI_LAUNCH
+    const int64_t grid = static_cast<int64_t>(B) * n_chunks;
+    const int parts = grid <= kFewestChunks ? std::max(1, std::min(n_moves, static_cast<int32_t>(kFewChunks / grid))) : 1;  // of a chunk
+    if (grid <= kFewChunks && T <= kMostSelectRows && (!lengths || lengths != new_lengths)) {
+        static std::atomic<size_t> allowed[64];
+        const size_t lds = static_cast<size_t>((T + 63) / 64 * 64) * sizeof(uint32_t);
+        e = allow_lds(evict_few_kernel, lds, allowed);
+        if (e != hipSuccess) return report(e);
+        hipLaunchKernelGGL(evict_few_kernel, dim3(static_cast<unsigned>(grid * parts)), dim3(kSelectThreads), lds, hs, weights, lengths, r, n_chunks, mv,
+                           parts, kept, new_lengths);
+        return report(hipGetLastError());
+    }
+    if (T <= kMostSelectRows) {
+static std::atomic<size_t> allowed[64];
+        const size_t lds = static_cast<size_t>((T + 63) / 64 * 64) * sizeof(uint32_t);
+        e = allow_lds(evict_select_kernel, lds, allowed);
+        if (e != hipSuccess) return report(e);
+        hipLaunchKernelGGL(evict_select_kernel, dim3(B), dim3(kSelectThreads), lds, hs, weights, lengths, r, B, ws, n_chunks, n_groups, kept);
         e = hipGetLastError();
     } else {
-        const unsigned grid = static_cast<unsigned>(B) * static_cast<unsigned>(n_groups);
+        const unsigned groups = static_cast<unsigned>(B) * static_cast<unsigned>(n_groups);
         constexpr int kClearParts = 4;
         hipLaunchKernelGGL(evict_clear_kernel, dim3(static_cast<unsigned>(B) * kClearParts), dim3(kCountThreads), 0, hs, lengths, r, ws,
                            kClearParts, kept);
         e = hipGetLastError();
         for (int pass = 0; pass < kPasses && e == hipSuccess; ++pass) {
-            hipLaunchKernelGGL(evict_digits_kernel, dim3(grid), dim3(kCountThreads), 0, hs, weights, lengths, r, B, pass, ws, n_groups);
+            hipLaunchKernelGGL(evict_digits_kernel, dim3(groups), dim3(kCountThreads), 0, hs, weights, lengths, r, B, pass, ws, n_groups);
             e = hipGetLastError();
         }
         if (e == hipSuccess) {
-            hipLaunchKernelGGL(evict_count_kernel, dim3(grid), dim3(kCountThreads), 0, hs, weights, lengths, r, B, ws, n_chunks, n_groups);
+            hipLaunchKernelGGL(evict_count_kernel, dim3(groups), dim3(kCountThreads), 0, hs, weights, lengths, r, B, ws, n_chunks, n_groups);
             e = hipGetLastError();
         }
     }
     if (e == hipSuccess) {
-        hipLaunchKernelGGL(evict_move_kernel, dim3(static_cast<unsigned>(B) * static_cast<unsigned>(n_chunks)), dim3(kMoveThreads), 0, hs,
-                           weights, r, B, ws, n_chunks, n_groups, mv, kept, new_lengths);
+        hipLaunchKernelGGL(evict_move_kernel, dim3(static_cast<unsigned>(grid * parts)), dim3(kMoveThreads), 0, hs, weights, r, B, ws, n_chunks,
+                           n_groups, mv, parts, kept, new_lengths);
         e = hipGetLastError();
     }
     return report(e);

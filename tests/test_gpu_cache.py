@@ -391,11 +391,35 @@ def test_evict_sizes_of_each_kind(B, T, n_keep, n_sink, n_recent, lengths, kind)
     _evict(w, lengths, n_keep, n_sink, n_recent, _arrays(rng, B, T, (4,)))
 
 
+@pytest.mark.parametrize("T", [300, 3000, 20000, 40000])
+@pytest.mark.parametrize("n_keep", [40, 200])
+def test_evict_among_infinities(T, n_keep):
+    """The border among the largest weights there can be, with NaN the smallest, beside rows that stay whatever theirs are."""
+    rng = np.random.default_rng(T)
+    w = rng.choice(np.array([np.inf, np.nan], dtype=np.float32), (2, T))
+    _evict(w, None, n_keep, 4, 9, _arrays(rng, 2, T, (4,)))
+    w[:, ::3] = np.finfo(np.float32).max
+    w[:, 60:] = np.where(np.isinf(w[:, 60:]), np.float32(1), w[:, 60:])
+    _evict(w, [T - 1, 299], n_keep, 4, 9, _arrays(rng, 2, T, (4,)))
+
+
 @pytest.mark.parametrize("widths", [(), (1,), (2, 3), (16, 32, 48), (256, 64, 4, 4), (5, 6, 10, 12, 20, 100, 7, 260)])
 def test_evict_row_sizes(widths):
     rng = np.random.default_rng(len(widths))
     w = rng.standard_normal((3, 700)).astype(np.float32)
     _evict(w, [700, 300, 650], 400, 2, 33, _arrays(rng, 3, 700, widths))
+
+
+@pytest.mark.parametrize("B,T", [(1, 130), (1, 25000), (1, 25700), (7, 3500), (32, 4000), (33, 4096), (2, 32768), (512, 200), (513, 200)])
+@pytest.mark.parametrize("alias", [False, True])
+def test_evict_by_one_launch_and_by_two(B, T, alias):
+    """Around the numbers of rows from which on another launch or another share of the arrays is taken; lengths rewritten or not."""
+    print(f"evict B={B} T={T} alias={alias}", flush=True)
+    rng = np.random.default_rng(B + T)
+    w = np.where(rng.random((B, T)) < 0.3, 0, np.exp(2 * rng.standard_normal((B, T)))).astype(np.float32)
+    lengths = rng.integers(0, T + 1, B).tolist()
+    lengths[-1] = T
+    _evict(w, lengths, max(1, T * 2 // 3), 4, 11, _arrays(rng, B, T, (16, 4, 1)), alias=alias)
 
 
 def test_evict_moves_arrays_of_any_type():
