@@ -54,6 +54,13 @@ __device__ __forceinline__ int held_rows(const int32_t* __restrict__ lengths, in
     return lengths ? min(max(lengths[b], 0), T) : T;
 }
 
+// ln(l * 2^(m_ref - 7)).  The logarithm instruction gets the mantissa alone: of l itself, whose logarithm is up to 20, its last place is 2e-6, and it
+// was off by -0.2 of that on the average, which all weights that are then made of lse share.
+__device__ __forceinline__ float log_sum(float m_ref, float l) {
+    const float e = static_cast<float>(__builtin_amdgcn_frexp_expf(l)) - kWeightShift;
+    return __builtin_fmaf(m_ref + e, kLn2, __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l)) * kLn2);
+}
+
 // A lane's part of a query's head, 8 bf16 values an element, as the products take it: fp16, times a power of two that brings the head's
 // largest magnitude (bits `top` of largest(), over all lanes that have a part) into [2^14, 2^15), with the sign of the softmax scale; values
 // down to 2^-32 of the largest stay exact.  The factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.
@@ -365,7 +372,7 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
                 const floatx4 v = {o.acc[db][4 * a] * inv, o.acc[db][4 * a + 1] * inv, o.acc[db][4 * a + 2] * inv, o.acc[db][4 * a + 3] * inv};
                 *reinterpret_cast<floatx4*>(to + 32 * db + 8 * a + 4 * half) = v;
             }
-        if (lse && half == 0) lse[row_q * H + h] = (o.m_ref - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2;
+        if (lse && half == 0) lse[row_q * H + h] = log_sum(o.m_ref, l_all);
     }
 }
 
@@ -610,7 +617,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
         }
         *reinterpret_cast<floatx4*>(out + (row_q * H + h) * D + part * (D / DS) + 4 * piece) = v * (l_all == 0.0f ? 0.0f : 1.0f / l_all);
         if (lse && piece == 0 && part == 0)
-            lse[row_q * H + h] = l_all == 0.0f ? -__builtin_huge_valf() : (m_all - kWeightShift + __builtin_amdgcn_logf(l_all)) * kLn2;
+            lse[row_q * H + h] = l_all == 0.0f ? -__builtin_huge_valf() : log_sum(m_all, l_all);
     }
 }
 
