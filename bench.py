@@ -146,9 +146,10 @@ def _consumer(P, W, wl, K, out_idx, args, dev):
         inside = (e >= w0[None, s0:s1, None]) & (e < legal[None, s0:s1, None])
         n_u += int(((e >= 0) & ~inside).sum()) + wl.B * int((legal[s0:s1] - w0[s0:s1]).sum())
     flop = 4.0 * n_u * H_A * D  # two products of 2 * |U| * H_A * D each
-    # measured traffic from the committed rocprofv3 summary, only if it was taken on this attention.hip
+    # measured traffic from the committed rocprofv3 summary, only if it was taken on these sources
     import hashlib
-    sha = hashlib.sha256(open(os.path.join(ROOT, "paper_2605_02568_amd", "csrc", "attention.hip"), "rb").read()).hexdigest()[:16]
+    sources = [os.path.join(ROOT, "paper_2605_02568_amd", "csrc", name) for name in ("attention.hip", "attention_set.h")]
+    sha = hashlib.sha256(b"".join(open(f, "rb").read() for f in sources)).hexdigest()[:16]
     traffic, traffic_sha = None, None
     summary = os.path.join(ROOT, "profiles", f"sparse_attention_{wl.name}.txt")
     if n_win == 128 and os.path.exists(summary):
