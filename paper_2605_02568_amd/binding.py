@@ -5,8 +5,8 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import math
 import os
+import struct
 from ctypes import (POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t,
                     c_uint64, c_void_p)
 
@@ -139,7 +139,7 @@ def load():
     L.si_evict_workspace_bytes.restype = c_size_t
     L.si_evict_workspace_bytes.argtypes = [c_int32, c_int32]
     L.si_evict_rows.restype = c_int32
-    L.si_evict_rows.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, POINTER(si_row_move),
+    L.si_evict_rows.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p,
                                 c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     _lib = L
     return L
@@ -313,8 +313,11 @@ def _gpu_of(t, name: str) -> int:
 
 
 def _ptr(t, dtype, gpu: int, name: str) -> int:
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == gpu and t.is_contiguous():
-        return t.data_ptr()
+    try:
+        if t.dtype is dtype and t.get_device() == gpu and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:  # not a tensor
+        pass
     _dev_ptr(t, dtype, name)  # says what is wrong with the tensor
     raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's first tensor on cuda:{gpu}")
 
@@ -424,6 +427,12 @@ def si_accumulate_weights(qa, codes, scales, lengths, idx, m, mask_mode, n_win, 
         _ptr(weights, torch.float32, gpu, "weights"), ws, ws_bytes, _stream_on(stream, gpu)), "si_accumulate_weights")
 
 
+@functools.lru_cache(maxsize=None)
+def _row_moves(n):
+    """Layout of n si_row_move."""
+    return struct.Struct("=" + "QQi4x" * n)
+
+
 def si_evict_workspace_bytes(B, T) -> int:
     _int32(B, T)
     return int(load().si_evict_workspace_bytes(B, T))
@@ -443,16 +452,17 @@ def si_evict_rows(weights, lengths, n_keep, n_sink, n_recent, moves, kept, new_l
         raise ValueError(f"at most {SI_MAX_ROW_MOVES} arrays a call")
     for i, (src, dst) in enumerate(moves):
         ss, ds = src.shape, dst.shape
-        if len(ss) < 2 or ss[0] != B or ss[1] != T or len(ds) < 2 or ds[0] != B or ds[1] != n_keep or ss[2:] != ds[2:] or src.dtype != dst.dtype:
+        if ds[:2] != (B, n_keep) or ss != (B, T) + ds[2:] or src.dtype is not dst.dtype:
             raise ValueError(f"moves[{i}]: src {tuple(ss)} {src.dtype}, dst {tuple(ds)} {dst.dtype}")
     gpu = _gpu_of(weights, "weights")
-    table = (si_row_move * SI_MAX_ROW_MOVES)()
-    for entry, (src, dst) in zip(table, moves):
-        dtype = src.dtype
-        entry.src, entry.dst = _ptr(src, dtype, gpu, "src of a move"), _ptr(dst, dtype, gpu, "dst of a move")
-        row_bytes = dtype.itemsize * math.prod(src.shape[2:])
-        _int32(row_bytes)
-        entry.row_bytes = row_bytes
+    rows = max(1, B * T)
+    entries = []
+    for src, dst in moves:
+        dtype, row_bytes = src.dtype, src.nbytes // rows
+        if row_bytes >= 2 ** 31:
+            raise ValueError(f"rows of {row_bytes} bytes: the library takes sizes below 2^31")
+        entries += (_ptr(src, dtype, gpu, "src of a move"), _ptr(dst, dtype, gpu, "dst of a move"), row_bytes)
+    table = _row_moves(len(moves)).pack(*entries)  # of si_row_move, whose fields one by one would cost the host more than the launch
     _check(load().si_evict_rows(
         _ptr(weights, torch.float32, gpu, "weights"), _per_batch(lengths, B, gpu, "lengths"), B, T, n_keep, n_sink, n_recent, table,
         len(moves), _ptr(kept, torch.int32, gpu, "kept"), _per_batch(new_lengths, B, gpu, "new_lengths"),
