@@ -568,7 +568,8 @@ def _replays(call, outputs):
         assert same(eager, again)
 
 
-@pytest.mark.parametrize("B,S,H,D,T,k,n_win", [(5, 1, 64, 128, 700, 300, 17), (1, 400, 40, 64, 500, 60, 8), (2, 3, 20, 128, 300, 100, 0)])
+@pytest.mark.parametrize("B,S,H,D,T,k,n_win", [(5, 1, 64, 128, 700, 300, 17), (1, 400, 40, 64, 500, 60, 8), (2, 3, 20, 128, 300, 100, 0),
+                                                  (2, 2, 8, 64, 40000, 50, 4), (40, 1, 16, 64, 3600, 40, 4), (1, 1, 64, 128, 3000, 1700, 64)])
 def test_side_streams_and_replays(B, S, H, D, T, k, n_win):
     q, codes, scales, idx = _problem(21, B, S, H, D, T, k, None, NONE, 1)
     q, codes, scales, idx = q.to(DEV), _gpu(codes), _gpu(scales), _gpu(idx)
@@ -590,6 +591,83 @@ def test_side_streams_and_replays(B, S, H, D, T, k, n_win):
     _replays(lambda o, s: P.si_evict_rows(w, lengths, n, 4, 32, [(codes, o[0]), (w, o[1])], o[2], o[3], ws, stream=s),
              (torch.empty((B, n, D // 2), dtype=torch.uint8, device=DEV), torch.empty((B, n), device=DEV),
               torch.empty((B, n), dtype=torch.int32, device=DEV), torch.empty((B,), dtype=torch.int32, device=DEV)))
+
+
+@pytest.mark.parametrize("B,S", [(1, (1 << 24) - 8), (2, (1 << 23) - 4), ((1 << 24) - 8, 1)])
+def test_the_most_queries_a_call_takes(B, S):
+    """Every query sees its batch's one row: that comes out, and receives a weight of 1 a query."""
+    H, D, T = 1, 64, 1
+    print(f"B={B} S={S}", flush=True)
+    q = torch.ones((B, S, H, D), dtype=torch.bfloat16, device=DEV)
+    codes = (torch.arange(B, device=DEV) % 251).to(torch.uint8).view(B, 1, 1).expand(B, T, D // 2).contiguous()
+    scales = torch.full((B, T, D // 32), 127, dtype=torch.uint8, device=DEV)
+    V = torch.empty((B, T, D), dtype=torch.bfloat16, device=DEV)
+    P.si_dequantize_rows(codes, scales, None, V)
+    out, lse = torch.full((B, S, H, D), float("nan"), device=DEV), torch.full((B, S, H), float("nan"), device=DEV)
+    P.si_quantized_attention(q, codes, scales, None, None, 1, NONE, 1, 0.125, out, lse)
+    # The one weight p is also its sum.  (hi + lo) V / p: the two parts are p to 2^-22 of it, their products with V exact; a rounding each
+    # of their sum, of the quotient 1 / p and of the product with it.
+    want = V.float().view(B, 1, 1, D)
+    off = ((out - want).abs() / want.abs().clamp(min=0.5)).max().item()
+    assert off <= 2.0 ** -22 + 4 * R.U, off
+    # one row: its logit itself, whose products are exact; the factor to log2 and back round five times
+    x = V.float().sum(dim=2).view(B, 1, 1) * 0.125
+    assert bool(((lse - x).abs() <= 5 * R.U * x.abs() + 2.0 ** -20).all())
+    weights = torch.zeros((B, T), device=DEV)
+    nbytes = P.si_accumulate_workspace_bytes(B, S, H, D, T)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV) if nbytes else None
+    P.si_accumulate_weights(q, codes, scales, None, None, 1, NONE, 1, 0.125, lse, weights, ws)
+    # exp(logit - lse): both logits and what lse is off by, in units of a logit of up to 48
+    assert bool(((weights - S).abs() <= S * 2.0 ** -16).all())
+
+
+def test_the_most_batches_eviction_takes():
+    B, T = (1 << 22) - 1, 2
+    w = torch.zeros((B, T), device=DEV)
+    w[::3, 1] = 1.0
+    kept, new = torch.empty((B, 1), dtype=torch.int32, device=DEV), torch.empty((B,), dtype=torch.int32, device=DEV)
+    src = torch.arange(2 * B, dtype=torch.int32, device=DEV).view(B, T)
+    dst = torch.empty((B, 1), dtype=torch.int32, device=DEV)
+    ws = torch.empty(P.si_evict_workspace_bytes(B, T), dtype=torch.uint8, device=DEV)
+    P.si_evict_rows(w, None, 1, 0, 0, [(src, dst)], kept, new, ws)
+    assert torch.equal(kept[:, 0], (w[:, 1] > 0).int()) and bool((new == 1).all())
+    assert torch.equal(dst, src.gather(1, kept.long()))
+
+
+@pytest.mark.parametrize("T", [700, 40000])
+def test_two_calls_at_once(T):
+    """Two streams, each with its own outputs and workspace, on the same inputs."""
+    B, S, H, D, k, n = 3, 40, 40, 128, 200, 400
+    q, codes, scales, idx = _problem(31, B, S, H, D, 700, k, None, NONE, 1)
+    q, idx = q.to(DEV), _gpu(idx)
+    codes = torch.cat([_gpu(codes), torch.zeros((B, T - 700, D // 2), dtype=torch.uint8, device=DEV)], dim=1)
+    scales = torch.cat([_gpu(scales), torch.full((B, T - 700, D // 32), 127, dtype=torch.uint8, device=DEV)], dim=1)
+    given = torch.rand((B, T), device=DEV)
+
+    def outputs():
+        return (torch.zeros((B, S, H, D), device=DEV), torch.zeros((B, S, H), device=DEV), torch.zeros((B, T), device=DEV),
+                torch.zeros((B, n, D // 2), dtype=torch.uint8, device=DEV), torch.zeros((B, n), dtype=torch.int32, device=DEV),
+                torch.randint(0, 256, (8 * B * T,), dtype=torch.uint8, device=DEV),
+                torch.randint(0, 256, (P.si_evict_workspace_bytes(B, T),), dtype=torch.uint8, device=DEV))
+
+    def run(o, stream):
+        P.si_quantized_attention(q, codes, scales, None, idx, 1, NONE, 9, 0.1, o[0], o[1], stream=stream)
+        P.si_accumulate_weights(q, codes, scales, None, idx, 1, NONE, 9, 0.1, o[1], o[2], o[5], stream=stream)
+        P.si_evict_rows(given, None, n, 4, 32, [(codes, o[3])], o[4], None, o[6], stream=stream)
+
+    alone = outputs()
+    run(alone, None)
+    sides, results = [torch.cuda.Stream() for _ in range(2)], [outputs() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o, side in zip(results, sides):
+            o[2].zero_()
+        torch.cuda.synchronize()
+        for o, side in zip(results, sides):
+            run(o, side)
+        torch.cuda.synchronize()
+        for o in results:
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(alone[:5], o[:5]))
 
 
 def test_refusals_of_the_binding():
