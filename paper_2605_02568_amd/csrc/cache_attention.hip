@@ -300,13 +300,191 @@ struct Heads {
     }
 };
 
+// The same for a block of 16 heads (narrow_..), with the matrix instructions of half the size (16 x 16 x 32): half the work of a tile and half the
+// registers.  A lane's part of a tile: rows lane % 16 and lane % 16 + 16, values D/4 * (lane / 16) .. + D/4; of the scores: rows 4 (lane / 16) + 0 .. 3
+// and those + 16, head lane % 16.  Of the second product the `part`-th of DS parts of d: register j of block db = d row 16 (DB part + db) + 4 (lane / 16) + j.
+template <int D>
+struct HalfRows {
+    typedef std::conditional_t<D == 128, uintx4, uintx2> run_t;
+    run_t run[2];
+    uint8_t bytes[2];
+    __device__ __forceinline__ void read(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, int64_t row, int which) {
+        bytes[which] = scales[row * (D / 32)];
+        run[which] = *reinterpret_cast<const run_t*>(codes + row * (D / 2));
+    }
+    __device__ __forceinline__ halfx8 values(int which, int ks) const {
+        const float p = power_of(bytes[which]);
+        const unsigned c = run[which][ks];
+        const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 0);
+        const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 1);
+        const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 2);
+        const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
+        return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    }
+};
+
+// LDS offsets for such a block, of a wave's tile at `base`: where the lane's pieces of its two rows go, where its transposing reads begin (source lane s
+// of 16 points at 4 consecutive d of row 4 (lane / 16) + s / 4, and 16 rows on).
+template <int D>
+struct NarrowPlaces {
+    int put[2], va;
+    __device__ __forceinline__ NarrowPlaces(int lane, int base) {
+        const int col = lane & 15, quarter = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) put[i] = base + tile_slot<D>(col + 16 * i, quarter * (D / 32)) * 16;
+        va = base + tile_slot<D>(4 * quarter + (col >> 2), (col & 3) >> 1) * 16 + (col & 1) * 8;
+    }
+};
+
+// The scores of half i of a tile, whose rows go to LDS on the way.
+template <int D, int DS>
+__device__ __forceinline__ floatx4 narrow_scores(const HalfRows<D>& rows, int i, const halfx8 (&qf)[D / 32], unsigned char* lds, int put, int quarter,
+                                                 int part) {
+    floatx4 x = {0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+        const halfx8 v = rows.values(i, ks);
+        if (DS == 1 || quarter / (4 / DS) == part) *reinterpret_cast<halfx8*>(lds + (put ^ (16 * ks))) = v;
+        x = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, qf[ks], x, 0, 0, 0);
+    }
+    return x;
+}
+
+// Weights and second product of a tile; `live`: bit r says whether row r of it counts (not 0).
+template <int D, int DS>
+__device__ __forceinline__ void narrow_take(floatx4 (&acc)[D / 16 / DS], float& m_ref, float& l_sum, floatx4 (&x)[2], unsigned live, float to_log2, int col,
+                                            int quarter, const unsigned char* lds, const NarrowPlaces<D>& at, int part) {
+    constexpr int DB = D / 16 / DS;
+    if (live != 0xFFFFFFFFu) {
+        float low = -__builtin_huge_valf();
+        asm volatile("" : "+v"(low));
+        const unsigned mine = live >> (4 * quarter);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!((mine >> (16 * (j >> 2) + (j & 3))) & 1)) x[j >> 2][j & 3] = low;
+    }
+    float p[8], sum;
+    auto exponentials = [&]() {  // weigh() above says why without a maximum first
+        const float shift = kWeightShift - m_ref;
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], to_log2, shift));
+            sum += p[j];
+        }
+    };
+    unsigned long long over = __ballot(m_ref == -__builtin_huge_valf());  // all heads on the first tile, later none but those of NaN
+    if (__builtin_expect(over != ~0ull, 1)) {
+        exponentials();
+        over |= __ballot(!(sum <= 32768.0f));
+    }
+    if (over != 0ull) {
+        over |= over >> 32;
+        over |= over >> 16;  // bit h: head h, in any quarter
+        float highest = x[0][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) highest = fmaxf(highest, x[j >> 2][j & 3]);
+        highest *= to_log2;
+        highest = fmaxf(highest, __shfl_xor(highest, 16));
+        highest = fmaxf(highest, __shfl_xor(highest, 32));
+        const float m_new = (over >> col) & 1 ? fmaxf(highest, m_ref) : m_ref;
+        const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+        l_sum *= alpha;
+        m_ref = m_new;
+        exponentials();
+    }
+    l_sum += sum;
+    float one = 1.0f;
+    asm("" : "+s"(one));
+    halfx8 p_hi, p_lo;
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+        const halfx2 a = __builtin_convertvector(floatx2{p[2 * jj], p[2 * jj + 1]}, halfx2);
+        p_hi[2 * jj] = a[0];
+        p_hi[2 * jj + 1] = a[1];
+        p_lo[2 * jj] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[0]), one, p[2 * jj]));
+        p_lo[2 * jj + 1] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[1]), one, p[2 * jj + 1]));
+    }
+    wave_order();
+    // contraction index e <-> tile row 16 (e / 4) + 4 quarter + e % 4 on both operands
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
+        const unsigned char* from = lds + (at.va ^ (32 * (DB * part + db)));
+        const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)from));
+        const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(from + 16 * D * 2)));
+        const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi, acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo, acc[db], 0, 0, 0);
+    }
+    wave_order();
+}
+
+// A wave's way through a query's list with a block of up to 16 heads from h0 on; base: of its tile in `lds`.
+template <int D, typename Live>
+__device__ __forceinline__ void narrow_query(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes_b, const unsigned char* __restrict__ scales_b,
+                                             const int* s_list, int n_tiles, Live live, int64_t row_q, int h0, int H, float scale_log2e, unsigned char* lds,
+                                             int base, float* __restrict__ out, float* __restrict__ lse) {
+    constexpr int KS = D / 32;
+    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+    const int h = h0 + col;
+    codes_b += quarter * (D / 8);
+    scales_b += quarter * D / 128;
+    HalfRows<D> rows;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rows.read(codes_b, scales_b, s_list[col + 16 * i], i);
+    uintx4 raw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(qa + (row_q * H + min(h, H - 1)) * D + quarter * (D / 4) + ks * 8);
+    unsigned top = largest(raw);
+    top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 16)));
+    top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 32)));
+    float to_log2;
+    halfx8 qf[KS];
+    scale_query(raw, query_power(top, scale_log2e, to_log2), qf);
+    const NarrowPlaces<D> at(lane, base);
+    floatx4 acc[D / 16];
+    float m_ref = -__builtin_huge_valf(), l_sum = 0.0f;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) acc[db] = floatx4{0, 0, 0, 0};
+    int next[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) next[i] = s_list[min(1, n_tiles - 1) * kTileKeys + col + 16 * i];
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        floatx4 x[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x[i] = narrow_scores<D, 1>(rows, i, qf, lds, at.put[i], quarter, 0);
+            rows.read(codes_b, scales_b, next[i], i);
+            next[i] = s_list[min(tile + 2, n_tiles - 1) * kTileKeys + col + 16 * i];
+        }
+        narrow_take<D, 1>(acc, m_ref, l_sum, x, live(tile), to_log2, col, quarter, lds, at, 0);
+    }
+    l_sum += __shfl_xor(l_sum, 16);
+    l_sum += __shfl_xor(l_sum, 32);
+    const float inv = 1.0f / l_sum;
+    constexpr int kSlots = D / 4;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) *reinterpret_cast<floatx4*>(lds + base + (col * kSlots + ((4 * db + quarter) ^ col)) * 16) = acc[db] * inv;
+    wave_order();
+#pragma unroll
+    for (int i = 0; i < kSlots / 4; ++i) {
+        const int head = i * (64 / kSlots) + lane / kSlots, slot = lane % kSlots;
+        const floatx4 v = *reinterpret_cast<const floatx4*>(lds + base + (head * kSlots + (slot ^ head)) * 16);
+        if (h0 + head < H) __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(out + (row_q * H + h0 + head) * D + 4 * slot));
+    }
+    if (lse && quarter == 0 && h < H) lse[row_q * H + h] = log_sum(m_ref, l_sum);
+}
+
 // One workgroup = one query; wave w owns heads [32 w, 32 w + 32) and goes through the query's list (attention_set.h) by itself: each wave turns the
 // codes it needs into a tile of its own, which costs the conversions twice and no barrier (a tile shared by two waves: 560 us, a wave by itself 520).
 // Bound by power and issue together: 16384 queries of 640 rows, 64 heads of 128, take 445 to 515 us (300 GFLOP, 450 with the second part of the
 // weights; the first kernel after a pause is the fastest); the clock is then 1.84 GHz, the matrix pipe 53 % busy, the vector units 60 %, the units that
 // return gathered codes 81 %.  The form si_sparse_attention has of this, on rows of 256 bytes in place of 68, takes 475 to 500.
 // Dynamic LDS: a tile of 32 x D fp16 a wave, the list.
-template <int D, int HW>
+template <int D, int HW, bool NARROW>
 __global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(3)))
 void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                 const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
@@ -337,8 +515,19 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
         return;
     }
     const int n_tiles = (n_u + kTileKeys - 1) / kTileKeys;
-    const unsigned char* const codes_b = codes + static_cast<int64_t>(b) * T * (D / 2) + half * (D / 4);
-    const unsigned char* const scales_b = scales + static_cast<int64_t>(b) * T * (D / 32) + half * (D / 64);
+    const unsigned char* codes_b = codes + static_cast<int64_t>(b) * T * (D / 2);
+    const unsigned char* scales_b = scales + static_cast<int64_t>(b) * T * (D / 32);
+    // rows of U(t) from tile on: a tile's worth, or the last ones
+    auto live = [&](int tile) {
+        const int left = n_u - tile * kTileKeys;
+        return left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
+    };
+    if (NARROW && (HW == 1 || wave == HW - 1)) {
+        narrow_query<D>(qa, codes_b, scales_b, s_list, n_tiles, live, row_q, 32 * wave, H, scale_log2e, lds, wave * kTileBytes, out, lse);
+        return;
+    }
+    codes_b += half * (D / 4);
+    scales_b += half * (D / 64);
     Rows<D> rows;
     rows.read(codes_b, scales_b, s_list[col]);
     halfx8 qf[D / 16];
@@ -352,11 +541,6 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     scale_query(raw, query_power(top, scale_log2e, to_log2), qf);
     const Places<D> at(lane, wave * kTileBytes);
     Heads<D> o;
-    // rows of U(t) from tile on: a tile's worth, or the last ones
-    auto live = [&](int tile) {
-        const int left = n_u - tile * kTileKeys;
-        return left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
-    };
     int s_next = s_list[min(1, n_tiles - 1) * kTileKeys + col];
     for (int tile = 0; tile < n_tiles; ++tile) {
         floatx16 x = o.scores(rows, qf, lds, at);
@@ -395,10 +579,8 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
 
 // Few queries, which would leave most of the chip idle and walk their tiles one after the other: a workgroup takes one query and one block of
 // 16 heads, and each of its 8 or 16 waves every 8th or 16th tile, with a reference, sums and accumulators of its own; the waves' results are joined at
-// the end.  The steps are those of the kernel above with the matrix instructions of half the size (16 x 16 x 32): half the work of a tile and
-// half the registers a wave, so that twice the waves share out the tiles on twice the compute units.  With DS = 2 two workgroups share a block of
-// heads: both score all rows, each has half of d in the second product, the rows in LDS and the join.  A lane's part of a tile: rows lane % 16 and
-// lane % 16 + 16, values D/4 * (lane / 16) .. + D/4; of the scores: rows 4 (lane / 16) + 0 .. 3 and those + 16, head lane % 16.
+// the end.  With blocks of 16 heads twice the waves share out the tiles on twice the compute units.  With DS = 2 two workgroups share a block of
+// heads: both score all rows, each has half of d in the second product, the rows in LDS and the join.
 // All workgroups of a query are on one XCD (32 queries, 1152 rows: 12.9 -> 9.8 us; each XCD's L2 read the rows again).  Bound by a wave's chain
 // of dependent steps: of 9.5 us at 32 queries and 1152 rows 4.3 are launch, first tile and join, 1 a tile of a wave.
 // Dynamic LDS: a tile of 32 x D fp16 a wave; for the join 16 x D / DS floats a wave.
@@ -407,26 +589,6 @@ constexpr int kXcds = 8;
 template <int D, int WAVES>
 constexpr int few_lds_bytes() { return WAVES * kTileKeys * D * 2; }
 
-template <int D>
-struct HalfRows {
-    typedef std::conditional_t<D == 128, uintx4, uintx2> run_t;
-    run_t run[2];
-    uint8_t bytes[2];
-    __device__ __forceinline__ void read(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, int64_t row, int which) {
-        bytes[which] = scales[row * (D / 32)];
-        run[which] = *reinterpret_cast<const run_t*>(codes + row * (D / 2));
-    }
-    __device__ __forceinline__ halfx8 values(int which, int ks) const {
-        const float p = power_of(bytes[which]);
-        const unsigned c = run[which][ks];
-        const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 0);
-        const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 1);
-        const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 2);
-        const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
-        return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-    }
-};
-
 template <int D, int DS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4)))
 void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
@@ -434,7 +596,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
                                     const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
                                     int64_t n_queries, int head_blocks, float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
     constexpr int W = WAVES;
-    constexpr int KS = D / 32;   // matrix instructions along d in the first product
+    constexpr int KS = D / 32;       // matrix instructions along d in the first product
     constexpr int DB = D / 16 / DS;  // blocks of 16 d in the second
     constexpr int kPieces = D / 4 / DS;  // of four d
     constexpr int kTileBytes = kTileKeys * D * 2;
@@ -503,14 +665,7 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const halfx8*>(s_query + (col * (D / 8) + ((quarter * KS + ks) ^ (col % (D / 8)))) * 8);
         const float to_log2 = s_scale[col];
-        const int base = wave * kTileBytes;
-        int put[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) put[i] = base + tile_slot<D>(col + 16 * i, quarter * (D / 32)) * 16;
-        // transposing reads: source lane s of a 16-lane group points at 4 consecutive d of row 4 quarter + s / 4 (+ 16)
-        const int s4 = lane & 15;
-        const int va = base + tile_slot<D>(4 * quarter + (s4 >> 2), (s4 & 3) >> 1) * 16 + (s4 & 1) * 8;
-
+        const NarrowPlaces<D> at(lane, wave * kTileBytes);
         for (int tile = wave; tile < n_tiles; tile += W) {
             unsigned live = 0;
 #pragma unroll
@@ -518,85 +673,14 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
             floatx4 x[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                x[i] = floatx4{0, 0, 0, 0};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const halfx8 v = rows.values(i, ks);
-                    if (DS == 1 || quarter / (4 / DS) == part) *reinterpret_cast<halfx8*>(lds + (put[i] ^ (16 * ks))) = v;
-                    x[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, qf[ks], x[i], 0, 0, 0);
-                }
+                x[i] = narrow_scores<D, DS>(rows, i, qf, lds, at.put[i], quarter, part);
                 s_now[i] = u.row(next[i], tile + W, col + 16 * i);
                 rows.read(codes_b, scales_b, max(s_now[i], 0), i);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) next[i] = u.entry(tile + 2 * W, col + 16 * i);
             if (live == 0) continue;
-            if (live != 0xFFFFFFFFu) {
-                float low = -__builtin_huge_valf();
-                asm volatile("" : "+v"(low));
-                const unsigned mine = live >> (4 * quarter);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (!((mine >> (16 * (j >> 2) + (j & 3))) & 1)) x[j >> 2][j & 3] = low;
-            }
-            float p[8], sum;
-            auto exponentials = [&]() {  // weigh() above says why without a maximum first
-                const float shift = kWeightShift - m_ref;
-                sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], to_log2, shift));
-                    sum += p[j];
-                }
-            };
-            const bool first = m_ref == -__builtin_huge_valf();  // the same for all lanes
-            unsigned long long over = ~0ull;
-            if (__builtin_expect(__ballot(first) == 0ull, 1)) {
-                exponentials();
-                over = __ballot(!(sum <= 32768.0f));
-            }
-            if (over != 0ull) {
-                over |= over >> 32;
-                over |= over >> 16;  // bit h: head h, in any quarter
-                float highest = x[0][0];
-#pragma unroll
-                for (int j = 1; j < 8; ++j) highest = fmaxf(highest, x[j >> 2][j & 3]);
-                highest *= to_log2;
-                highest = fmaxf(highest, __shfl_xor(highest, 16));
-                highest = fmaxf(highest, __shfl_xor(highest, 32));
-                const float m_new = (over >> col) & 1 ? fmaxf(highest, m_ref) : m_ref;
-                const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) acc[db] *= alpha;
-                l_sum *= alpha;
-                m_ref = m_new;
-                exponentials();
-            }
-            l_sum += sum;
-            float one = 1.0f;
-            asm("" : "+s"(one));
-            halfx8 p_hi, p_lo;
-#pragma unroll
-            for (int jj = 0; jj < 4; ++jj) {
-                const halfx2 a = __builtin_convertvector(floatx2{p[2 * jj], p[2 * jj + 1]}, halfx2);
-                p_hi[2 * jj] = a[0];
-                p_hi[2 * jj + 1] = a[1];
-                p_lo[2 * jj] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[0]), one, p[2 * jj]));
-                p_lo[2 * jj + 1] = static_cast<_Float16>(__builtin_fmaf(-static_cast<float>(a[1]), one, p[2 * jj + 1]));
-            }
-            wave_order();
-            // contraction index e <-> tile row 16 (e / 4) + 4 quarter + e % 4 on both operands
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
-                const unsigned char* from = lds + (va ^ (32 * (DB * part + db)));
-                const halfx4 v0 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)from));
-                const halfx4 v1 = __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4*)(from + 16 * D * 2)));
-                const halfx8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_hi, acc[db], 0, 0, 0);
-                acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_lo, acc[db], 0, 0, 0);
-            }
-            wave_order();
+            narrow_take<D, DS>(acc, m_ref, l_sum, x, live, to_log2, col, quarter, lds, at, part);
         }
         l_sum += __shfl_xor(l_sum, 16);
         l_sum += __shfl_xor(l_sum, 32);
@@ -816,14 +900,14 @@ struct Call {
     hipStream_t stream;
 };
 
-template <int D, int HW>
+template <int D, int HW, bool NARROW>
 hipError_t launch_attention(const Call& c, float* out, float* lse) {
     static std::atomic<size_t> allowed[64];
     const size_t lds = HW * static_cast<size_t>(kTileKeys) * D * 2 + list_bytes(c.k, c.n_win);
-    hipError_t e = allow_lds(quantized_attention_kernel<D, HW>, lds, allowed);
+    hipError_t e = allow_lds(quantized_attention_kernel<D, HW, NARROW>, lds, allowed);
     if (e != hipSuccess) return e;
     const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
-    hipLaunchKernelGGL((quantized_attention_kernel<D, HW>), dim3(static_cast<unsigned>(rows)), dim3(64 * HW), lds, c.stream, c.qa,
+    hipLaunchKernelGGL((quantized_attention_kernel<D, HW, NARROW>), dim3(static_cast<unsigned>(rows)), dim3(64 * HW), lds, c.stream, c.qa,
                        c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e, out,
                        lse);
     return hipGetLastError();
@@ -842,6 +926,16 @@ hipError_t launch_few(const Call& c, float* out, float* lse) {
                        c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, n_queries, head_blocks,
                        c.scale_log2e, out, lse);
     return hipGetLastError();
+}
+
+// A wave a block of 32 heads; a last block of up to 16 takes the matrix instructions of half the size.  With those of the full size and without
+// (us): 8192 queries of 640 rows, 16 heads of 128 110 -> 75, 40 heads 210 -> 182, 48 heads of 64 127 -> 110, 3000 of 264 rows, 9 heads of 128 24 -> 17.
+template <int D>
+hipError_t launch_attention(const Call& c, float* out, float* lse) {
+    const int H = c.d.H_I;
+    if (H <= 16) return launch_attention<D, 1, true>(c, out, lse);
+    if (H <= 32) return launch_attention<D, 1, false>(c, out, lse);
+    return H <= 48 ? launch_attention<D, 2, true>(c, out, lse) : launch_attention<D, 2, false>(c, out, lse);
 }
 
 // Blocks of 16 heads of all queries, and the rows a query may attend to, decide.  Measured (us; B queries of 64 heads of 128, 4 B blocks):
@@ -933,10 +1027,8 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
     if (!out || !aligned16(out) || !aligned16(lse)) return SI_ERR_INVALID_ARG;
     const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
                     lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
-    const bool two = dims->H_I > 32;
     if (few_queries(*dims, k, n_win)) return report(dims->D == 128 ? launch_few<128>(c, out, lse) : launch_few<64>(c, out, lse));
-    return report(dims->D == 128 ? (two ? launch_attention<128, 2>(c, out, lse) : launch_attention<128, 1>(c, out, lse))
-                                 : (two ? launch_attention<64, 2>(c, out, lse) : launch_attention<64, 1>(c, out, lse)));
+    return report(dims->D == 128 ? launch_attention<128>(c, out, lse) : launch_attention<64>(c, out, lse));
 }
 
 size_t si_accumulate_workspace_bytes(const si_dims* dims) {

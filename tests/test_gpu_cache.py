@@ -266,7 +266,8 @@ def test_entries_outside_the_rows_held_are_skipped(S):
     _check(q, codes, scales, [60, 100], idx, 1, NONE, 5, 0.1)
 
 
-@pytest.mark.parametrize("S,H,D,k,n_win", [(1, 33, 128, 90, 9), (3, 20, 64, 40, 0), (260, 40, 128, 60, 5)])
+@pytest.mark.parametrize("S,H,D,k,n_win", [(1, 33, 128, 90, 9), (3, 20, 64, 40, 0), (260, 40, 128, 60, 5), (1, 64, 128, 140, 9), (260, 16, 64, 120, 0),
+                                           (600, 64, 64, 120, 0), (600, 20, 128, 140, 9)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_queries_that_are_not_finite(S, H, D, k, n_win, bad):
     """The head has NaN, no other head or query anything else than without it; its query gives no row a weight."""
