@@ -38,6 +38,7 @@ typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eRest = 1.925962989e-8f;  // log2(e) - kLog2e: left out of an lse of 7, 9e-8 too much for every row alike
 constexpr float kLn2 = 0.6931471805599453f;
 // The weights are 2^7 times exp2(x - reference): at most 2^15 with the slack of 2^8, so that both fp16 parts of
 // a weight are normal numbers down to 2^-18 of the reference's weight.
@@ -777,7 +778,8 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
     float* const s_lse = reinterpret_cast<float*>(lds + 4096);
     int s_now = u.row(u.entry(first, col), first, col);
     int next = u.entry(first + 1, col);
-    s_lse[lane] = lane < H ? -kLog2e * lse[row_q * H + min(lane, H - 1)] : -__builtin_huge_valf();  // no head there: weight 0
+    const float given = lse[row_q * H + min(lane, H - 1)];
+    s_lse[lane] = lane < H ? __builtin_fmaf(-kLog2e, given, -kLog2eRest * given) : -__builtin_huge_valf();  // no head there: weight 0
     bf16x8 qf[HB][KS];
     load_heads<D, HB>(qa + row_q * H * D, H, lds, qf);
     Rows<D> rows;
@@ -996,13 +998,15 @@ hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsig
     return hipGetLastError();
 }
 
+float in_log2(float scale) { return static_cast<float>(scale * 1.4426950408889634); }
+
 si_status check(const void* qa, const void* codes, const void* scales, const int32_t* lengths, const int32_t* idx, const si_dims* dims,
                 int32_t m, int32_t k, si_mask_mode mask_mode, int32_t n_win, float scale) {
     if (!dims || !qa || !codes || !scales || (!idx && k != 0)) return SI_ERR_INVALID_ARG;
     if (!aligned16(qa) || !aligned16(codes) || !aligned16(scales) || !aligned16(idx) || !aligned4(lengths)) return SI_ERR_INVALID_ARG;
     if (dims->B < 1 || dims->S < 1 || dims->H_I < 1 || dims->D < 1 || dims->T < 1 || m < 1 || k < 0 || n_win < 0) return SI_ERR_INVALID_ARG;
     if (mask_mode != SI_MASK_NONE && mask_mode != SI_MASK_CAUSAL_BLOCK) return SI_ERR_INVALID_ARG;
-    const float scale_log2e = scale * kLog2e;
+    const float scale_log2e = in_log2(scale);
     if (scale_log2e - scale_log2e != 0.0f) return SI_ERR_INVALID_ARG;  // NaN, infinite, or not to be had in log2 units
     if (dims->D != 64 && dims->D != 128) return SI_ERR_UNSUPPORTED_SHAPE;
     if (dims->H_I > kMaxHeads || k > kMaxK || n_win > kMaxK) return SI_ERR_UNSUPPORTED_SHAPE;
@@ -1026,7 +1030,7 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
     if (ok != SI_OK) return ok;
     if (!out || !aligned16(out) || !aligned16(lse)) return SI_ERR_INVALID_ARG;
     const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
-                    lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
+                    lengths, idx, *dims, m, mask_mode, k, n_win, in_log2(scale), static_cast<hipStream_t>(stream)};
     if (few_queries(*dims, k, n_win)) return report(dims->D == 128 ? launch_few<128>(c, out, lse) : launch_few<64>(c, out, lse));
     return report(dims->D == 128 ? launch_attention<128>(c, out, lse) : launch_attention<64>(c, out, lse));
 }
@@ -1047,7 +1051,7 @@ si_status si_accumulate_weights(const void* qa, const void* codes, const void* s
     if (need > 0 && (!workspace || !aligned16(workspace))) return SI_ERR_INVALID_ARG;
     if (workspace_bytes < need) return SI_ERR_WORKSPACE_TOO_SMALL;
     const Call c = {static_cast<const __bf16*>(qa), static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
-                    lengths, idx, *dims, m, mask_mode, k, n_win, scale * kLog2e, static_cast<hipStream_t>(stream)};
+                    lengths, idx, *dims, m, mask_mode, k, n_win, in_log2(scale), static_cast<hipStream_t>(stream)};
     unsigned long long* sums = need > 0 ? static_cast<unsigned long long*>(workspace) : nullptr;
     const int64_t n = static_cast<int64_t>(dims->B) * dims->T;
     const unsigned blocks = static_cast<unsigned>(n < (int64_t{1} << 20) ? (n + 255) / 256 : 4096);
