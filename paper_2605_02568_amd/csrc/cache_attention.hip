@@ -554,6 +554,8 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     // out through the wave's tile, 64 (D = 64: 32) d of 32 heads at a time, so that it is written by whole lines, and past the caches' other contents:
     // a lane's own pieces, 16 bytes of each of 32 heads a store, took 241 us in place of 204 where a query has 128 rows, 432 / 418 where 512.
     constexpr int kSlots = kTileBytes / (32 * 16);  // pieces of four d
+    float* const to = out + (row_q * H + 32 * wave) * D;
+    const unsigned mine = static_cast<unsigned>(lane / kSlots * D + 4 * (lane % kSlots));
 #pragma unroll
     for (int part = 0; part < D / (4 * kSlots); ++part) {
         unsigned char* const stage = lds + wave * kTileBytes;
@@ -570,8 +572,8 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
         for (int i = 0; i < kSlots / 2; ++i) {
             const int head = i * (64 / kSlots) + lane / kSlots, slot = lane % kSlots;
             const floatx4 v = *reinterpret_cast<const floatx4*>(stage + (head * kSlots + (slot ^ (head % kSlots))) * 16);
-            if (32 * wave + head < H)
-                __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(out + (row_q * H + 32 * wave + head) * D + 4 * (part * kSlots + slot)));
+            // one address a lane; the rest is the same for all
+            if (head < H - 32 * wave) __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(to + (i * (64 / kSlots) * D + part * 4 * kSlots) + mine));
         }
         wave_order();
     }
