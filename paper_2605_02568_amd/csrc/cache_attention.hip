@@ -482,8 +482,8 @@ __device__ __forceinline__ void narrow_query(const __bf16* __restrict__ qa, cons
 // One workgroup = one query; wave w owns heads [32 w, 32 w + 32) and goes through the query's list (attention_set.h) by itself: each wave turns the
 // codes it needs into a tile of its own, which costs the conversions twice and no barrier (a tile shared by two waves: 560 us, a wave by itself 520).
 // Bound by power and issue together: 16384 queries of 640 rows, 64 heads of 128, take 445 to 515 us (300 GFLOP, 450 with the second part of the
-// weights; the first kernel after a pause is the fastest); the clock is then 1.84 GHz, the matrix pipe 53 % busy, the vector units 60 %, the units that
-// return gathered codes 81 %.  The form si_sparse_attention has of this, on rows of 256 bytes in place of 68, takes 475 to 500.
+// weights; the first kernel after a pause is the fastest); the clock is then 1.82 GHz, the matrix pipe 53 % busy, the vector units 64 %, the units that
+// return gathered codes 79 %.  The form si_sparse_attention has of this, on rows of 256 bytes in place of 68, takes 475 to 500.
 // Dynamic LDS: a tile of 32 x D fp16 a wave, the list.
 template <int D, int HW, bool NARROW>
 __global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(3)))
@@ -853,7 +853,7 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
                        });
 }
 
-// Many queries of few rows: 8192 of 640 of 2048 rows, 64 heads of 128, take 95 us of 106 in this kernel: vector units 55 %, matrix pipe 36 %, issue of
+// Many queries of few rows: 8192 of 640 of 2048 rows, 64 heads of 128, take 95 us of 106 in this kernel: vector units 57 %, matrix pipe 36 %, issue of
 // three waves a SIMD the rest (without exponentials 12 us less, without products 27, without reads of rows 15).  A workgroup adds up in LDS what its queries (every n_groups-th wave's worth of a batch) give the batch's rows,
 // and then adds that to the workspace, row after row.  Added up there at once, the sums wait for one another: 8192 queries of 640 of 2048 rows took
 // 657 us, 12 adds a nanosecond.
