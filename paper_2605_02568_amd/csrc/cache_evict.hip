@@ -113,9 +113,9 @@ __device__ __forceinline__ int find_digit(const int* bins, Border& at, int* s_wa
 // bits, are those of a word's distance from the smallest one, from its highest bit on: weights spread over that range, where their upper bits (sign,
 // exponent) are a few dozen numbers; the smallest word itself, which rows that received nothing share, is counted by ballots.  Every wave finds the
 // digit by itself.  Once a digit is down to 64 rows, these are listed, and each counts those above it.
-// What bounds it is a chain of dependent steps, and the way of its instructions from L2, where each launch begins anew: with the words in registers
-// and every loop over them unrolled, 32 batches of 16411 rows took 19.9 us with 18 KiB of code, and 23 where the list of 64 rows made it 30; as it
-// stands 11.5, and 2048 rows 4.4 in place of 6.1.
+// What bounds it is a chain of short steps between barriers, which 16 waves on one compute unit do in turn: 2048 rows take 8,500 cycles, a digit
+// about 2,700 of them.  With the words in registers (4, 16 or 32 a thread, every loop over them unrolled), digits of 11 bits, and no list of the last
+// rows, 32 batches of 16411 rows took 19.9 us and 2048 rows 6.1; as it stands 11.5 and 4.4.
 constexpr int kSelectDigit = 9;
 constexpr int kSelectBins = 1 << kSelectDigit;
 constexpr int kSelectRounds = 4;  // that 32 bits have
