@@ -166,7 +166,8 @@ struct Tiles {
     __device__ __forceinline__ int row(int entry, int tile, int col) const {
         const bool listed = (tile * kTileKeys + col < k) & (static_cast<unsigned>(entry) < static_cast<unsigned>(held)) & !((entry >= w0) & (entry < legal));
         const int in_window = w0 + (tile - list_tiles) * kTileKeys + col;
-        return tile < list_tiles ? (listed ? entry : -1) : (in_window < legal ? in_window : -1);
+        const int from_list = (tile - list_tiles) >> 31;  // all bits or none: a choice by a branch would cut the loop's body in pieces
+        return ((listed ? entry : -1) & from_list) | ((in_window < legal ? in_window : -1) & ~from_list);
     }
     __device__ __forceinline__ int count() const { return list_tiles + (legal - w0 + kTileKeys - 1) / kTileKeys; }
 };
