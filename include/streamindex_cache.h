@@ -96,7 +96,7 @@ typedef struct {
  *                rows of dst behind them stay as they are.  dst must overlap neither another array of the call nor src.
  *                row_bytes >= 1; src and dst aligned to 16 bytes.
  *   kept         device [B,n_keep] int32: the rows that stay, ascending, then -1
- *   new_lengths  device [B] int32 or NULL: how many stay (may be `lengths` itself)
+ *   new_lengths  device [B] int32 or NULL: how many stay (may be `lengths` itself; small calls then take two launches in place of one)
  *   workspace    device, si_evict_workspace_bytes(B, T) bytes
  * 1 <= n_keep <= T; n_sink, n_recent >= 0, n_sink + n_recent <= n_keep. */
 size_t si_evict_workspace_bytes(int32_t B, int32_t T);

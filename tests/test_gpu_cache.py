@@ -211,6 +211,11 @@ NONE, CAUSAL = P.SI_MASK_NONE, P.SI_MASK_CAUSAL_BLOCK
     (1, 200, 64, 128, 500, 1, 400, CAUSAL, 20, None),  # more workgroups than compute units, rows for each
     (130, 2, 64, 64, 450, 1, 390, NONE, 0, None),
     (9, 3, 16, 128, 800, 1, 700, NONE, 128, None),     # a number of queries that no eight divide
+    (1, 700, 9, 128, 350, 2, 100, CAUSAL, 7, None),    # many queries whose last block of heads has up to 16
+    (2, 400, 16, 64, 300, 1, 70, NONE, 0, [300, 31]),
+    (1, 1100, 1, 64, 90, 12, 20, CAUSAL, 5, None),
+    (1, 300, 48, 64, 300, 1, 64, CAUSAL, 32, None),
+    (1, 520, 17, 128, 200, 3, 33, CAUSAL, 0, [150]),
 ])
 def test_attention_and_weights(B, S, H, D, T, m, k, mask, n_win, lengths):
     print(f"attention B={B} S={S} H={H} D={D} T={T} m={m} k={k} mask={mask} n_win={n_win} lengths={lengths}", flush=True)
@@ -220,7 +225,7 @@ def test_attention_and_weights(B, S, H, D, T, m, k, mask, n_win, lengths):
     assert rel <= 2e-6  # rounding of logits of size 16 (log2 units) at random: 3e-7; of the weights' two parts: 1e-7
 
 
-@pytest.mark.parametrize("S,H,D", [(3, 20, 128), (40, 64, 128), (5, 33, 64)])
+@pytest.mark.parametrize("S,H,D", [(3, 20, 128), (40, 64, 128), (5, 33, 64), (300, 10, 128)])
 @pytest.mark.parametrize("scale", [-0.2, 0.0, -0.0, 1e-30, 3.0, 1e-3])
 def test_scales_of_the_softmax(S, H, D, scale):
     q, codes, scales, idx = _problem(11, 2, S, H, D, 200, 90, None, NONE, 1)
@@ -237,7 +242,7 @@ def test_sizes_of_values(S, q_size, spread, scale):
     _check(q, codes, scales, None, idx, 1, NONE, 33, scale)
 
 
-@pytest.mark.parametrize("S", [1, 30])
+@pytest.mark.parametrize("S", [1, 30, 550])
 def test_rising_logits(S):
     """The reference maximum is raised late and often; the largest and the smallest exponents of a cache."""
     B, H, D, T = 1, 8, 64, 300
