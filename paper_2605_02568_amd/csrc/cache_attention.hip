@@ -64,7 +64,7 @@ __device__ __forceinline__ float log_sum(float m_ref, float l) {
 
 // A lane's part of a query's head, 8 bf16 values an element, as the products take it: fp16, times a power of two that brings the head's
 // largest magnitude (bits `top` of largest(), over all lanes that have a part) into [2^14, 2^15), with the sign of the softmax scale; values
-// down to 2^-32 of the largest stay exact.  The factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.
+// down to 2^-31 of the largest stay exact.  The factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.
 template <int N>
 __device__ __forceinline__ unsigned largest(const uintx4 (&raw)[N]) {
     unsigned top = 0;
