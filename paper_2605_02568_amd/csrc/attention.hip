@@ -597,7 +597,7 @@ si_status si_sparse_attention(const void* qa, const void* Kc, const int32_t* idx
     if (d.D == 128) SI_LAUNCH(128);
     else SI_LAUNCH(64);
 #undef SI_LAUNCH
-    return e == hipSuccess ? SI_OK : SI_ERR_HIP;
+    return e == hipSuccess ? SI_OK : hip_fail(e);
 }
 
 }  // extern "C"

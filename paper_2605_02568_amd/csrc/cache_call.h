@@ -4,12 +4,12 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "streamindex.h"
+#include "si_internal.h"
 
 namespace si {
 
 // The status of a call whose last HIP call returned e.
-inline si_status report(hipError_t e) { return e == hipSuccess ? SI_OK : SI_ERR_HIP; }
+inline si_status report(hipError_t e) { return e == hipSuccess ? SI_OK : hip_fail(e); }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 // One number a batch (lengths, start): read one at a time.

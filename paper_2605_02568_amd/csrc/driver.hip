@@ -36,10 +36,14 @@ thread_local int32_t g_last_hip_error = 0;
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+}  // namespace
+
 si_status hip_fail(hipError_t e) {
     g_last_hip_error = static_cast<int32_t>(e);
     return SI_ERR_HIP;
 }
+
+namespace {
 
 // ---- per-kernel timing (benchmark aid) --------------------------------------------------
 struct Profiler {

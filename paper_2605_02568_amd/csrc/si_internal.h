@@ -9,6 +9,9 @@
 
 namespace si {
 
+// The status of a call whose HIP call returned e, not hipSuccess: si_last_hip_error() gives e from now on.
+si_status hip_fail(hipError_t e);
+
 // A (score, index) pair packed so that unsigned 64-bit comparison is the total order of
 // Section 4.1: larger key = better entry.  High word: order-preserving image of the fp32
 // score (-0 folded onto +0 so that they tie); low word: ~index, so that the smaller index
