@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "attention_set.h"
@@ -209,9 +210,9 @@ struct Rows {
         const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
         return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
     }
-    // the same in bf16
-    __device__ __forceinline__ bf16x8 values_bf16(int ks) const {
-        const float p = power(ks / 4);
+    // the same in bf16, times 2^(exponent)
+    __device__ __forceinline__ bf16x8 values_bf16(int ks, int exponent) const {
+        const float p = power_of(((static_cast<unsigned>(bytes) >> (8 * (ks / 4))) & 0xFFu) + static_cast<unsigned>(exponent));
         const unsigned c = run[ks / 4][ks % 4];
         const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 0);
         const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 1);
@@ -726,6 +727,15 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
     }
 }
 
+// The product of a query and a row where the query's bf16 values enter as they are, which may be anything bf16 holds: to_log2 * <q, 2^exponent V> is
+// the logit in log2 units.  V is below 2^16 and D 2^7 at most, so exponent -27 keeps every sum below 2^124, and where |scale| is below 1 what fp32
+// then loses at its lower end is nothing to the logit.  With larger scales a sum that fp32 cannot hold is of a logit it cannot hold either, and from 2^32
+// on, where the lower end matters, the rows are 2^27 times as large.  It costs nothing: the exponent is added to a row's scale byte as that is shifted.
+struct BareProduct {
+    float to_log2;
+    int exponent;
+};
+
 // A query's heads as the first product's operand, one wave: head 32 hb + lane % 32, values D/2 * (lane / 32) + 8 ks .. + 8; of H heads the last
 // stands in for those there are not.  Whole lines are read and parted out through 4 KiB of LDS: read head by head into the registers a line
 // would be asked for eight times.
@@ -763,14 +773,14 @@ __device__ __forceinline__ void load_heads(const __bf16* __restrict__ query, int
 // What rows of U(t) receive of a query: S[32 heads x 32 rows] = q . tile^T with the heads on the M side, so that a lane holds 16 heads of
 // one row and the sum over heads is in-lane (and one exchange).  A lane's codes go from memory to its registers as they are needed there
 // (row = lane % 32, values D/2 * (lane / 32) .. + D/2: the contraction order is permuted alike on the query) and on to bf16, in which
-// both operands are exact: neither list nor tile goes through LDS.  The vector units bound it: 64 heads of 128 take 16 matrix instructions a
+// both operands are exact, the row's with the factor of BareProduct: neither list nor tile goes through LDS.  The vector units bound it: 64 heads of 128 take 16 matrix instructions a
 // tile, 512 cycles, against 32 conversions, 32 fma, 32 additions and 32 exponentials, which take longer.
 // One wave: tiles [first, last) of query row_q; add(row, sum) for every row of U(t) there, on the lanes below 32.  lds: kWeighBytes of the wave.
 constexpr int kWeighBytes = 4096 + 256;
 template <int D, int HB, typename Add>
 __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                             const unsigned char* __restrict__ scales, const float* __restrict__ lse, int64_t row_q, int H,
-                                            int64_t first_row, const Tiles& u, int first, int last, float scale_log2e, unsigned char* lds, Add add) {
+                                            int64_t first_row, const Tiles& u, int first, int last, BareProduct product, unsigned char* lds, Add add) {
     constexpr int KS = D / 16;
     if (first >= last) return;
     const int lane = threadIdx.x & 63;
@@ -793,7 +803,7 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
         for (int hb = 0; hb < HB; ++hb) x[hb] = floatx16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const bf16x8 v = rows.values_bf16(ks);
+            const bf16x8 v = rows.values_bf16(ks, product.exponent);
 #pragma unroll
             for (int hb = 0; hb < HB; ++hb) x[hb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[hb][ks], v, x[hb], 0, 0, 0);
         }
@@ -810,7 +820,7 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
             for (int a = 0; a < 4; ++a) {
                 const floatx4 minus_lse = *reinterpret_cast<const floatx4*>(s_lse + 32 * hb + 8 * a + 4 * half);  // of these heads
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[hb][4 * a + j], scale_log2e, minus_lse[j]));
+                for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[hb][4 * a + j], product.to_log2, minus_lse[j]));
             }
         sum += other_half(sum);
         // a sum that is no number (some head's lse is none) is not added: it would stay in the weights for good, and has no fixed-point form
@@ -833,7 +843,7 @@ __global__ __launch_bounds__(64 * kWeightWaves) __attribute__((amdgpu_waves_per_
 void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
                                const int32_t* __restrict__ idx, int64_t n_queries, int n_parts, int per, int S, int H, int T, int m, int mask_mode,
-                               int k, int n_win, float scale_log2e, const float* __restrict__ lse, float* __restrict__ weights,
+                               int k, int n_win, BareProduct product, const float* __restrict__ lse, float* __restrict__ weights,
                                unsigned long long* __restrict__ sums) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[kWeightWaves][kWeighBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -847,7 +857,7 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
     const int t = static_cast<int>(row_q - static_cast<int64_t>(b) * S);
     const Tiles u = tiles_of(idx, qa, row_q, t, k, held_rows(lengths, b, T), n_win, m, mask_mode);
     const int64_t first_row = static_cast<int64_t>(b) * T;
-    weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, first_row, u, part * per, min(u.count(), (part + 1) * per), scale_log2e, lds[wave],
+    weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, first_row, u, part * per, min(u.count(), (part + 1) * per), product, lds[wave],
                        [&](int s, float sum) {
                            if (sums) atomicAdd(sums + first_row + s, to_fixed(sum));
                            else weights[first_row + s] += sum;
@@ -862,7 +872,7 @@ template <int D, int HB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(3)))
 void gather_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                            const int32_t* __restrict__ lengths, const int32_t* __restrict__ idx, int n_groups, int S, int H, int T, int m,
-                           int mask_mode, int k, int n_win, float scale_log2e, const float* __restrict__ lse,
+                           int mask_mode, int k, int n_win, BareProduct product, const float* __restrict__ lse,
                            unsigned long long* __restrict__ sums) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     unsigned long long* const s_sums = reinterpret_cast<unsigned long long*>(lds + WAVES * kWeighBytes);
@@ -875,7 +885,7 @@ void gather_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* _
     for (int t = group * WAVES + wave; t < S; t += n_groups * WAVES) {
         const int64_t row_q = static_cast<int64_t>(b) * S + t;
         const Tiles u = tiles_of(idx, qa, row_q, t, k, held, n_win, m, mask_mode);
-        weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, static_cast<int64_t>(b) * T, u, 0, u.count(), scale_log2e, lds + wave * kWeighBytes,
+        weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, static_cast<int64_t>(b) * T, u, 0, u.count(), product, lds + wave * kWeighBytes,
                            [&](int s, float sum) { atomicAdd(s_sums + s, to_fixed(sum)); });
     }
     __syncthreads();
@@ -961,6 +971,12 @@ hipError_t launch_few(const Call& c, float* out, float* lse) {
     return wide && blocks <= 256 ? launch_few<D, 1, 16>(c, out, lse) : launch_few<D, 1, 8>(c, out, lse);
 }
 
+BareProduct bare_product(float scale_log2e) {
+    const float size = std::fabs(scale_log2e);
+    const int exponent = size < 1.0f ? -27 : size < 4294967296.0f ? 0 : 27;
+    return {std::ldexp(scale_log2e, -exponent), exponent};
+}
+
 template <int D, int HB, int WAVES>
 hipError_t launch_gather(const Call& c, int most_groups, const float* lse, unsigned long long* sums) {
     static std::atomic<size_t> allowed[64];
@@ -969,7 +985,7 @@ hipError_t launch_gather(const Call& c, int most_groups, const float* lse, unsig
     hipError_t e = allow_lds(gather_weights_kernel<D, HB, WAVES>, lds, allowed);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((gather_weights_kernel<D, HB, WAVES>), dim3(static_cast<unsigned>(c.d.B) * n_groups), dim3(64 * WAVES), lds, c.stream, c.qa,
-                       c.codes, c.scales, c.lengths, c.idx, n_groups, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e,
+                       c.codes, c.scales, c.lengths, c.idx, n_groups, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, bare_product(c.scale_log2e),
                        lse, sums);
     return hipGetLastError();
 }
@@ -997,7 +1013,7 @@ hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsig
     const int64_t grid = (rows + kXcds - 1) / kXcds * kXcds * ((n_parts + kWeightWaves - 1) / kWeightWaves);
     hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWeightWaves), 0, c.stream, c.qa, c.codes,
                        c.scales, c.lengths, c.idx, rows, n_parts, per, c.d.S, c.d.H_I,
-                       c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e, lse, weights, sums);
+                       c.d.T, c.m, c.mask_mode, c.k, c.n_win, bare_product(c.scale_log2e), lse, weights, sums);
     return hipGetLastError();
 }
 
