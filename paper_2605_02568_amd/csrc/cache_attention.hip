@@ -37,6 +37,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+typedef unsigned short shortx2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLog2eRest = 1.925962989e-8f;  // log2(e) - kLog2e: left out of an lse of 7, 9e-8 too much for every row alike
@@ -63,26 +64,53 @@ __device__ __forceinline__ float log_sum(float m_ref, float l) {
     return __builtin_fmaf(m_ref + e, kLn2, __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l)) * kLn2);
 }
 
+// The product of a query and a row where the query's bf16 values enter as they are, which may be anything bf16 holds: to_log2 * <q, 2^exponent V> is
+// the logit in log2 units.  V is below 2^16 and D 2^7 at most, so exponent -27 keeps every sum below 2^124, and where |scale| is below 1 what fp32
+// then loses at its lower end is nothing to the logit.  With larger scales a sum that fp32 cannot hold is of a logit it cannot hold either, and from 2^32
+// on, where the lower end matters, the rows are 2^27 times as large.  A scale of 0 is one of 2^-126 on rows 2^-64 times as large, whose logits are
+// below 2^-38: not 0, so that -inf times it is -inf.  It costs nothing: the exponent is added to a row's scale byte as that is shifted.
+struct BareProduct {
+    float to_log2;
+    int exponent;
+};
+
 // A lane's part of a query's head, 8 bf16 values an element, as the products take it: fp16, times a power of two that brings the head's
-// largest magnitude (bits `top` of largest(), over all lanes that have a part) into [2^14, 2^15), with the sign of the softmax scale; values
-// down to 2^-31 of the largest stay exact.  The factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.
+// largest magnitude into [2^14, 2^15), with the sign of the softmax scale; values of exponents down to 31 below the largest one's stay exact.  The
+// factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.  A block of heads one of which holds smaller values
+// too, or needs a factor that fp32 does not hold, takes the bare product instead, at twice the conversions: rows of zeros where the query's large
+// values are would leave logits that consist of what fp16 lost.
+
+// Magnitudes of a head's values, as bf16's bits: in the low half the largest, in the high half 2^16 less the smallest that is not 0 (or 0).  Of two
+// parts: the larger of each half.
+__device__ __forceinline__ unsigned joint(unsigned a, unsigned b) {
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(shortx2, a), __builtin_bit_cast(shortx2, b)));
+}
 template <int N>
-__device__ __forceinline__ unsigned largest(const uintx4 (&raw)[N]) {
-    unsigned top = 0;
+__device__ __forceinline__ unsigned extent(const uintx4 (&raw)[N]) {
+    shortx2 top = {0, 0}, low = {0, 0};
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, max(raw[i][j] & 0x7FFFu, (raw[i][j] >> 16) & 0x7FFFu));
-    return top;
+        for (int j = 0; j < 4; ++j) {
+            const shortx2 size = __builtin_bit_cast(shortx2, raw[i][j] & 0x7FFF7FFFu);
+            top = __builtin_elementwise_max(top, size);
+            low = __builtin_elementwise_max(low, static_cast<shortx2>(shortx2{0, 0} - size));
+        }
+    return static_cast<unsigned>(max(top[0], top[1])) | (static_cast<unsigned>(max(low[0], low[1])) << 16);
 }
-// The power, and in to_log2 that factor.
-__device__ __forceinline__ float query_power(unsigned top, float scale_log2e, float& to_log2) {
-    const int e = static_cast<int>(top >> 7);  // exponent field of the largest
-    const int up = min(268 - e, 254);          // field of the power: 2^(14 - (e - 127))
+// The power, in to_log2 that factor, and in border the bits below which a value (but 0) is too small for fp16; denormal numbers have the least exponent's
+// steps.  A head that is not finite has NaN whatever the power, and makes no demands: other heads' bits do not depend on it.
+__device__ __forceinline__ float query_power(unsigned top, float scale_log2e, float& to_log2, unsigned& border) {
+    const int e = top < 0x7F80u ? static_cast<int>(top >> 7) : 0;  // exponent field of the largest
+    const int up = min(268 - e, 254);                              // field of the power: 2^(14 - (e - 127))
     // not 0, so that -inf times it is -inf: a logit that such a factor makes is 0 either way
     to_log2 = fmaxf(__builtin_ldexpf(__builtin_fabsf(scale_log2e), 127 - up), 1.1754944e-38f);
+    border = static_cast<unsigned>(max(e - 31, 0)) << 7;
+    border = max(border, 1u);
     return __uint_as_float(static_cast<unsigned>(up) << 23) * (scale_log2e < 0.0f ? -1.0f : 1.0f);
 }
+// Whether a block has a head that needs the bare product: `lost` where a lane has values below a head's border.
+__device__ __forceinline__ bool needs_bare(bool lost, float to_log2) { return __ballot(lost | (to_log2 == __builtin_huge_valf())) != 0ull; }
 template <int N>
 __device__ __forceinline__ void scale_query(const uintx4 (&raw)[N], float power, halfx8 (&qf)[N]) {
 #pragma unroll
@@ -184,6 +212,22 @@ __device__ __forceinline__ Tiles tiles_of(const int32_t* __restrict__ idx, const
     return u;
 }
 
+// Eight codes as the values they stand for, `power` the row's power of two.
+__device__ __forceinline__ halfx8 f16_values(unsigned codes, float power) {
+    const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, power, 0);
+    const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, power, 1);
+    const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, power, 2);
+    const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, power, 3);
+    return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+}
+__device__ __forceinline__ bf16x8 bf16_values(unsigned codes, float power) {
+    const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, power, 0);
+    const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, power, 1);
+    const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, power, 2);
+    const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, power, 3);
+    return bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+}
+
 // A lane's part of the tiles of 32 rows that its wave takes: row lane % 32, values D/2 * (lane / 32) .. + D/2, read from memory as codes and
 // scale bytes.  As fp16 they are the first product's operand as they are (the contraction order is permuted alike on the query); for the
 // second one they go through LDS, into a tile of the wave's own, row-major and swizzled (attention_set.h).  A wave's LDS accesses are done in
@@ -199,26 +243,14 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) run[i] = *reinterpret_cast<const uintx4*>(codes + row * (D / 2) + i * 16);
     }
-    __device__ __forceinline__ float power(int i) const { return power_of((static_cast<unsigned>(bytes) >> (8 * i)) & 0xFFu); }
+    __device__ __forceinline__ unsigned byte(int i) const { return (static_cast<unsigned>(bytes) >> (8 * i)) & 0xFFu; }
     // values 8 ks .. 8 ks + 8 of the lane's part
     __device__ __forceinline__ halfx8 values(int ks) const {
-        const float p = power(ks / 4);
-        const unsigned c = run[ks / 4][ks % 4];
-        const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 0);
-        const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 1);
-        const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 2);
-        const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
-        return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+        return f16_values(run[ks / 4][ks % 4], power_of(byte(ks / 4)));
     }
     // the same in bf16, times 2^(exponent)
     __device__ __forceinline__ bf16x8 values_bf16(int ks, int exponent) const {
-        const float p = power_of(((static_cast<unsigned>(bytes) >> (8 * (ks / 4))) & 0xFFu) + static_cast<unsigned>(exponent));
-        const unsigned c = run[ks / 4][ks % 4];
-        const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 0);
-        const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 1);
-        const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 2);
-        const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, p, 3);
-        return bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+        return bf16_values(run[ks / 4][ks % 4], power_of(byte(ks / 4) + static_cast<unsigned>(exponent)));
     }
 };
 
@@ -316,13 +348,10 @@ struct HalfRows {
         run[which] = *reinterpret_cast<const run_t*>(codes + row * (D / 2));
     }
     __device__ __forceinline__ halfx8 values(int which, int ks) const {
-        const float p = power_of(bytes[which]);
-        const unsigned c = run[which][ks];
-        const halfx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 0);
-        const halfx2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 1);
-        const halfx2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 2);
-        const halfx2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, p, 3);
-        return halfx8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+        return f16_values(run[which][ks], power_of(bytes[which]));
+    }
+    __device__ __forceinline__ bf16x8 values_bf16(int which, int ks, int exponent) const {
+        return bf16_values(run[which][ks], power_of(bytes[which] + static_cast<unsigned>(exponent)));
     }
 };
 
@@ -351,6 +380,46 @@ __device__ __forceinline__ floatx4 narrow_scores(const HalfRows<D>& rows, int i,
         x = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, qf[ks], x, 0, 0, 0);
     }
     return x;
+}
+
+// The number as one that the compiler does not know: what is made of it in a loop is not kept in registers from before the loop.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// A condition that the compiler does not join with the one before it, of which it is the other case: it would lay out the rare way first, and hold
+// there what the other one needs.
+__device__ __forceinline__ int known_late(int condition) {
+    condition = __builtin_amdgcn_readfirstlane(condition);
+    asm volatile("" : "+s"(condition));
+    return condition;
+}
+
+// The same of both halves by the bare product, whose query is as it stands in qa: lane lane % 16 has head lane % 16.  A step after the other, nothing read
+// ahead: what the second conversion takes comes from the registers of the form above, which nearly all calls run.
+template <int D>
+__device__ __forceinline__ void bare_query(const __bf16* __restrict__ head, int quarter, BareProduct product, bf16x8 (&qf)[D / 32]) {
+    const unsigned sign = product.to_log2 < 0.0f ? 0x80008000u : 0u;  // the factor that follows is above 0
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uintx4*>(head + quarter * (D / 4) + ks * 8) ^ sign);
+}
+template <int D, int DS>
+__device__ __forceinline__ void bare_scores(const unsigned char* __restrict__ codes_b, const unsigned char* __restrict__ scales_b, const int (&row)[2],
+                                            const bf16x8 (&qf)[D / 32], int exponent, unsigned char* lds, const NarrowPlaces<D>& at, int quarter, int part,
+                                            floatx4 (&x)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        HalfRows<D> rows;
+        rows.read(codes_b, scales_b, row[i], i);
+        x[i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) {
+            if (DS == 1 || quarter / (4 / DS) == part) *reinterpret_cast<halfx8*>(lds + (at.put[i] ^ (16 * ks))) = rows.values(i, ks);
+            x[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rows.values_bf16(i, ks, exponent), qf[ks], x[i], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
 }
 
 // Weights and second product of a tile; `live`: bit r says whether row r of it counts (not 0).
@@ -425,46 +494,12 @@ __device__ __forceinline__ void narrow_take(floatx4 (&acc)[D / 16 / DS], float& 
     wave_order();
 }
 
-// A wave's way through a query's list with a block of up to 16 heads from h0 on; base: of its tile in `lds`.
-template <int D, typename Live>
-__device__ __forceinline__ void narrow_query(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes_b, const unsigned char* __restrict__ scales_b,
-                                             const int* s_list, int n_tiles, Live live, int64_t row_q, int h0, int H, float scale_log2e, unsigned char* lds,
-                                             int base, float* __restrict__ out, float* __restrict__ lse) {
-    constexpr int KS = D / 32;
-    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+// The end of such a block's way: sums over the quarters, out through the wave's tile.
+template <int D>
+__device__ __forceinline__ void narrow_out(int lane, floatx4 (&acc)[D / 16], float m_ref, float l_sum, int64_t row_q, int h0, int H, unsigned char* lds,
+                                           int base, float* __restrict__ out, float* __restrict__ lse) {
+    const int col = lane & 15, quarter = lane >> 4;
     const int h = h0 + col;
-    codes_b += quarter * (D / 8);
-    scales_b += quarter * D / 128;
-    HalfRows<D> rows;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) rows.read(codes_b, scales_b, s_list[col + 16 * i], i);
-    uintx4 raw[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(qa + (row_q * H + min(h, H - 1)) * D + quarter * (D / 4) + ks * 8);
-    unsigned top = largest(raw);
-    top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 16)));
-    top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 32)));
-    float to_log2;
-    halfx8 qf[KS];
-    scale_query(raw, query_power(top, scale_log2e, to_log2), qf);
-    const NarrowPlaces<D> at(lane, base);
-    floatx4 acc[D / 16];
-    float m_ref = -__builtin_huge_valf(), l_sum = 0.0f;
-#pragma unroll
-    for (int db = 0; db < D / 16; ++db) acc[db] = floatx4{0, 0, 0, 0};
-    int next[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) next[i] = s_list[min(1, n_tiles - 1) * kTileKeys + col + 16 * i];
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        floatx4 x[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            x[i] = narrow_scores<D, 1>(rows, i, qf, lds, at.put[i], quarter, 0);
-            rows.read(codes_b, scales_b, next[i], i);
-            next[i] = s_list[min(tile + 2, n_tiles - 1) * kTileKeys + col + 16 * i];
-        }
-        narrow_take<D, 1>(acc, m_ref, l_sum, x, live(tile), to_log2, col, quarter, lds, at, 0);
-    }
     l_sum += __shfl_xor(l_sum, 16);
     l_sum += __shfl_xor(l_sum, 32);
     const float inv = 1.0f / l_sum;
@@ -479,6 +514,80 @@ __device__ __forceinline__ void narrow_query(const __bf16* __restrict__ qa, cons
         if (h0 + head < H) __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(out + (row_q * H + h0 + head) * D + 4 * slot));
     }
     if (lse && quarter == 0 && h < H) lse[row_q * H + h] = log_sum(m_ref, l_sum);
+    wave_order();
+}
+
+// A wave's way through a query's list with a block of up to 16 heads from h0 on, by the bare product; base: of its tile in `lds`.
+template <int D, typename Live>
+__device__ __forceinline__ void bare_heads(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes_b, const unsigned char* __restrict__ scales_b,
+                                           const int* s_list, int n_tiles, Live live, int64_t row_q, int h0, int H, BareProduct product, unsigned char* lds,
+                                           int base, float* __restrict__ out, float* __restrict__ lse) {
+    const int lane = fresh(threadIdx.x & 63), col = lane & 15, quarter = lane >> 4;
+    bf16x8 qf[D / 32];
+    bare_query<D>(qa + (row_q * H + min(h0 + col, H - 1)) * D, quarter, product, qf);
+    const float to_log2 = __builtin_fabsf(product.to_log2);
+    floatx4 acc[D / 16];
+    float m_ref = -__builtin_huge_valf(), l_sum = 0.0f;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) acc[db] = floatx4{0, 0, 0, 0};
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        const NarrowPlaces<D> at(fresh(lane), base);
+        const int row[2] = {s_list[tile * kTileKeys + col], s_list[tile * kTileKeys + col + 16]};
+        floatx4 x[2];
+        bare_scores<D, 1>(codes_b + quarter * (D / 8), scales_b + quarter * D / 128, row, qf, product.exponent, lds, at, quarter, 0, x);
+        narrow_take<D, 1>(acc, m_ref, l_sum, x, live(tile), to_log2, col, quarter, lds, at, 0);
+    }
+    narrow_out<D>(fresh(lane), acc, m_ref, l_sum, row_q, h0, H, lds, base, out, lse);
+}
+
+// The same in fp16.
+template <int D, typename Live>
+__device__ __forceinline__ void narrow_query(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes_b, const unsigned char* __restrict__ scales_b,
+                                             const int* s_list, int n_tiles, Live live, int64_t row_q, int h0, int H, float scale_log2e, BareProduct product,
+                                             unsigned char* lds, int base, float* __restrict__ out, float* __restrict__ lse) {
+    constexpr int KS = D / 32;
+    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+    const int h = h0 + col;
+    codes_b += quarter * (D / 8);
+    scales_b += quarter * D / 128;
+    HalfRows<D> rows;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rows.read(codes_b, scales_b, s_list[col + 16 * i], i);
+    uintx4 raw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(qa + (row_q * H + min(h, H - 1)) * D + quarter * (D / 4) + ks * 8);
+    unsigned sizes = extent(raw);
+    sizes = joint(sizes, static_cast<unsigned>(__shfl_xor(static_cast<int>(sizes), 16)));
+    sizes = joint(sizes, static_cast<unsigned>(__shfl_xor(static_cast<int>(sizes), 32)));
+    float to_log2;
+    unsigned border;
+    const float power = query_power(sizes & 0xFFFFu, scale_log2e, to_log2, border);
+    const int bare_block = needs_bare(0x10000u - (sizes >> 16) < border, to_log2);
+    if (!bare_block) {
+        halfx8 qf[KS];
+        scale_query(raw, power, qf);
+        const NarrowPlaces<D> at(lane, base);
+        floatx4 acc[D / 16];
+        float m_ref = -__builtin_huge_valf(), l_sum = 0.0f;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) acc[db] = floatx4{0, 0, 0, 0};
+        int next[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) next[i] = s_list[min(1, n_tiles - 1) * kTileKeys + col + 16 * i];
+        for (int tile = 0; tile < n_tiles; ++tile) {
+            floatx4 x[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[i] = narrow_scores<D, 1>(rows, i, qf, lds, at.put[i], quarter, 0);
+                rows.read(codes_b, scales_b, next[i], i);
+                next[i] = s_list[min(tile + 2, n_tiles - 1) * kTileKeys + col + 16 * i];
+            }
+            narrow_take<D, 1>(acc, m_ref, l_sum, x, live(tile), to_log2, col, quarter, lds, at, 0);
+        }
+        narrow_out<D>(lane, acc, m_ref, l_sum, row_q, h0, H, lds, base, out, lse);
+    }
+    if (__builtin_expect(known_late(bare_block), 0))
+        bare_heads<D>(qa, codes_b - quarter * (D / 8), scales_b - quarter * D / 128, s_list, n_tiles, live, row_q, h0, H, product, lds, base, out, lse);
 }
 
 // One workgroup = one query; wave w owns heads [32 w, 32 w + 32) and goes through the query's list (attention_set.h) by itself: each wave turns the
@@ -492,7 +601,7 @@ __global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(3)))
 void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                 const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
                                 const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
-                                float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
+                                float scale_log2e, BareProduct product, float* __restrict__ out, float* __restrict__ lse) {
     constexpr int kTileBytes = kTileKeys * D * 2;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int* const s_list = reinterpret_cast<int*>(lds + HW * kTileBytes);
@@ -526,7 +635,7 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
         return left >= kTileKeys ? 0xFFFFFFFFu : (1u << left) - 1;
     };
     if (NARROW && (HW == 1 || wave == HW - 1)) {
-        narrow_query<D>(qa, codes_b, scales_b, s_list, n_tiles, live, row_q, 32 * wave, H, scale_log2e, lds, wave * kTileBytes, out, lse);
+        narrow_query<D>(qa, codes_b, scales_b, s_list, n_tiles, live, row_q, 32 * wave, H, scale_log2e, product, lds, wave * kTileBytes, out, lse);
         return;
     }
     codes_b += half * (D / 4);
@@ -537,49 +646,59 @@ void quantized_attention_kernel(const __bf16* __restrict__ qa, const unsigned ch
     uintx4 raw[D / 16];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) raw[ks] = *reinterpret_cast<const uintx4*>(qa + (row_q * H + min(h, H - 1)) * D + half * (D / 2) + ks * 8);
-    unsigned top = largest(raw);
-    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    top = max(both[0], both[1]);
+    const unsigned mine_extent = extent(raw);
+    const auto both = __builtin_amdgcn_permlane32_swap(mine_extent, mine_extent, false, false);
     float to_log2;
-    scale_query(raw, query_power(top, scale_log2e, to_log2), qf);
+    unsigned border;
+    const unsigned sizes = joint(both[0], both[1]);
+    const float power = query_power(sizes & 0xFFFFu, scale_log2e, to_log2, border);
     const Places<D> at(lane, wave * kTileBytes);
     Heads<D> o;
-    int s_next = s_list[min(1, n_tiles - 1) * kTileKeys + col];
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        floatx16 x = o.scores(rows, qf, lds, at);
-        rows.read(codes_b, scales_b, s_next);
-        s_next = s_list[min(tile + 2, n_tiles - 1) * kTileKeys + col];
-        o.take(x, live(tile), to_log2, half, lds, at);
-    }
-    const float l_all = o.l_sum + other_half(o.l_sum);
-    const float inv = 1.0f / l_all;
-    // out through the wave's tile, 64 (D = 64: 32) d of 32 heads at a time, so that it is written by whole lines, and past the caches' other contents:
-    // a lane's own pieces, 16 bytes of each of 32 heads a store, took 241 us in place of 204 where a query has 128 rows, 432 / 418 where 512.
-    constexpr int kSlots = kTileBytes / (32 * 16);  // pieces of four d
-    float* const to = out + (row_q * H + 32 * wave) * D;
-    const unsigned mine = static_cast<unsigned>(lane / kSlots * D + 4 * (lane % kSlots));
-#pragma unroll
-    for (int part = 0; part < D / (4 * kSlots); ++part) {
-        unsigned char* const stage = lds + wave * kTileBytes;
-#pragma unroll
-        for (int db = 0; db < kSlots / 8; ++db)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const floatx16& acc = o.acc[part * (kSlots / 8) + db];
-                const floatx4 v = {acc[4 * a] * inv, acc[4 * a + 1] * inv, acc[4 * a + 2] * inv, acc[4 * a + 3] * inv};
-                *reinterpret_cast<floatx4*>(stage + (col * kSlots + ((8 * db + 2 * a + half) ^ (col % kSlots))) * 16) = v;
-            }
-        wave_order();
-#pragma unroll
-        for (int i = 0; i < kSlots / 2; ++i) {
-            const int head = i * (64 / kSlots) + lane / kSlots, slot = lane % kSlots;
-            const floatx4 v = *reinterpret_cast<const floatx4*>(stage + (head * kSlots + (slot ^ (head % kSlots))) * 16);
-            // one address a lane; the rest is the same for all
-            if (head < H - 32 * wave) __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(to + (i * (64 / kSlots) * D + part * 4 * kSlots) + mine));
+    const int bare_block = needs_bare(0x10000u - (sizes >> 16) < border, to_log2);
+    if (!bare_block) {
+        scale_query(raw, power, qf);
+        int s_next = s_list[min(1, n_tiles - 1) * kTileKeys + col];
+        for (int tile = 0; tile < n_tiles; ++tile) {
+            floatx16 x = o.scores(rows, qf, lds, at);
+            rows.read(codes_b, scales_b, s_next);
+            s_next = s_list[min(tile + 2, n_tiles - 1) * kTileKeys + col];
+            o.take(x, live(tile), to_log2, half, lds, at);
         }
-        wave_order();
+        const float l_all = o.l_sum + other_half(o.l_sum);
+        const float inv = 1.0f / l_all;
+        // out through the wave's tile, 64 (D = 64: 32) d of 32 heads at a time, so that it is written by whole lines, and past the caches' other contents:
+        // a lane's own pieces, 16 bytes of each of 32 heads a store, took 241 us in place of 204 where a query has 128 rows, 432 / 418 where 512.
+        constexpr int kSlots = kTileBytes / (32 * 16);  // pieces of four d
+        float* const to = out + (row_q * H + 32 * wave) * D;
+        const unsigned mine = static_cast<unsigned>(lane / kSlots * D + 4 * (lane % kSlots));
+#pragma unroll
+        for (int part = 0; part < D / (4 * kSlots); ++part) {
+            unsigned char* const stage = lds + wave * kTileBytes;
+#pragma unroll
+            for (int db = 0; db < kSlots / 8; ++db)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const floatx16& acc = o.acc[part * (kSlots / 8) + db];
+                    const floatx4 v = {acc[4 * a] * inv, acc[4 * a + 1] * inv, acc[4 * a + 2] * inv, acc[4 * a + 3] * inv};
+                    *reinterpret_cast<floatx4*>(stage + (col * kSlots + ((8 * db + 2 * a + half) ^ (col % kSlots))) * 16) = v;
+                }
+            wave_order();
+#pragma unroll
+            for (int i = 0; i < kSlots / 2; ++i) {
+                const int head = i * (64 / kSlots) + lane / kSlots, slot = lane % kSlots;
+                const floatx4 v = *reinterpret_cast<const floatx4*>(stage + (head * kSlots + (slot ^ (head % kSlots))) * 16);
+                // one address a lane; the rest is the same for all
+                if (head < H - 32 * wave) __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(to + (i * (64 / kSlots) * D + part * 4 * kSlots) + mine));
+            }
+            wave_order();
+        }
+        if (lse && half == 0 && h < H) lse[row_q * H + h] = log_sum(o.m_ref, l_all);
     }
-    if (lse && half == 0 && h < H) lse[row_q * H + h] = log_sum(o.m_ref, l_all);
+    if (__builtin_expect(known_late(bare_block), 0)) {
+#pragma unroll 1
+        for (int h0 = 32 * wave; h0 < min(32 * wave + 32, H); h0 += 16)
+            bare_heads<D>(qa, codes_b - half * (D / 4), scales_b - half * (D / 64), s_list, n_tiles, live, row_q, h0, H, product, lds, wave * kTileBytes, out, lse);
+    }
 }
 
 // Few queries, which would leave most of the chip idle and walk their tiles one after the other: a workgroup takes one query and one block of
@@ -599,7 +718,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4)))
 void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes,
                                     const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
                                     const int32_t* __restrict__ idx, int S, int H, int T, int m, int mask_mode, int k, int n_win,
-                                    int64_t n_queries, int head_blocks, float scale_log2e, float* __restrict__ out, float* __restrict__ lse) {
+                                    int64_t n_queries, int head_blocks, float scale_log2e, BareProduct product, float* __restrict__ out, float* __restrict__ lse) {
     constexpr int W = WAVES;
     constexpr int KS = D / 32;       // matrix instructions along d in the first product
     constexpr int DB = D / 16 / DS;  // blocks of 16 d in the second
@@ -633,6 +752,8 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
     // the query, one or two heads a wave, to fp16 and to LDS: pieces of 8 values turned over by the head's number as those of a tile's rows
     __shared__ __attribute__((aligned(16))) _Float16 s_query[kFewHeads * D];
     __shared__ float s_scale[kFewHeads];
+    __shared__ int s_lost[W];  // whether one of a wave's heads needs the bare product
+    bool lost = false;
     constexpr int kHeadsPerWave = kFewHeads / W;
     constexpr int kPair = D / 64;  // values of a lane
     typedef std::conditional_t<D == 128, unsigned, uint16_t> pair_t;
@@ -656,25 +777,34 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
 #pragma unroll
     for (int i = 0; i < kHeadsPerWave; ++i) {
         const int head = wave + i * W;
-        const unsigned top = wave_max(max(pair[i] & 0x7FFFu, (pair[i] >> 16) & 0x7FFFu));
+        const unsigned first = pair[i] & 0x7FFFu, second = (pair[i] >> 16) & 0x7FFFu;
         float to_log2;
-        const float power = query_power(top, scale_log2e, to_log2);
+        unsigned border;
+        const float power = query_power(wave_max(max(first, second)), scale_log2e, to_log2, border);
+        lost |= min(first - 1, second - 1) < border - 1;
         const int at = head * D + (((lane * kPair / 8) ^ (head % (D / 8))) * 8 + lane * kPair % 8);
         s_query[at] = static_cast<_Float16>(__uint_as_float(pair[i] << 16) * power);
         if (kPair == 2) s_query[at + 1] = static_cast<_Float16>(__uint_as_float(pair[i] & 0xFFFF0000u) * power);
         if (lane == 0) s_scale[head] = to_log2;
     }
+    const bool wave_lost = __ballot(lost) != 0ull;
+    if (lane == 0) s_lost[wave] = wave_lost;
     __syncthreads();
     if (wave < waves) {
         halfx8 qf[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const halfx8*>(s_query + (col * (D / 8) + ((quarter * KS + ks) ^ (col % (D / 8)))) * 8);
-        const float to_log2 = s_scale[col];
+        float to_log2 = s_scale[col];
+        const int lost_of = s_lost[lane % W];
         const NarrowPlaces<D> at(lane, wave * kTileBytes);
-        for (int tile = wave; tile < n_tiles; tile += W) {
+        auto live_rows = [&]() {
             unsigned live = 0;
 #pragma unroll
             for (int i = 0; i < 2; ++i) live |= (static_cast<unsigned>(__ballot(s_now[i] >= 0)) & 0xFFFFu) << (16 * i);
+            return live;
+        };
+        for (int tile = wave; tile < n_tiles; tile += W) {
+            const unsigned live = live_rows();
             floatx4 x[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -686,6 +816,27 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
             for (int i = 0; i < 2; ++i) next[i] = u.entry(tile + 2 * W, col + 16 * i);
             if (live == 0) continue;
             narrow_take<D, DS>(acc, m_ref, l_sum, x, live, to_log2, col, quarter, lds, at, part);
+        }
+        // Asked only now, and by every wave alike: asked before the loop, what leads to the loop was waiting for the answer, 0.2 us of 5.2 to 9.5.
+        if (__builtin_expect(needs_bare(lost_of != 0, to_log2), 0)) {
+            to_log2 = __builtin_fabsf(product.to_log2);
+            m_ref = -__builtin_huge_valf();
+            l_sum = 0.0f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = floatx4{0, 0, 0, 0};
+            bf16x8 qb[KS];
+            bare_query<D>(qa + (row_q * H + min(h0 + col, H - 1)) * D, quarter, product, qb);
+            for (int tile = wave; tile < n_tiles; tile += W) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) s_now[i] = u.row(u.entry(tile, col + 16 * i), tile, col + 16 * i);
+                const unsigned live = live_rows();
+                if (live == 0) continue;
+                const int row[2] = {max(s_now[0], 0), max(s_now[1], 0)};
+                const NarrowPlaces<D> here(fresh(lane), wave * kTileBytes);
+                floatx4 x[2];
+                bare_scores<D, DS>(codes_b, scales_b, row, qb, product.exponent, lds, here, quarter, part, x);
+                narrow_take<D, DS>(acc, m_ref, l_sum, x, live, to_log2, col, quarter, lds, here, part);
+            }
         }
         l_sum += __shfl_xor(l_sum, 16);
         l_sum += __shfl_xor(l_sum, 32);
@@ -726,15 +877,6 @@ void quantized_attention_few_kernel(const __bf16* __restrict__ qa, const unsigne
             lse[row_q * H + h] = l_all == 0.0f ? -__builtin_huge_valf() : log_sum(m_all, l_all);
     }
 }
-
-// The product of a query and a row where the query's bf16 values enter as they are, which may be anything bf16 holds: to_log2 * <q, 2^exponent V> is
-// the logit in log2 units.  V is below 2^16 and D 2^7 at most, so exponent -27 keeps every sum below 2^124, and where |scale| is below 1 what fp32
-// then loses at its lower end is nothing to the logit.  With larger scales a sum that fp32 cannot hold is of a logit it cannot hold either, and from 2^32
-// on, where the lower end matters, the rows are 2^27 times as large.  It costs nothing: the exponent is added to a row's scale byte as that is shifted.
-struct BareProduct {
-    float to_log2;
-    int exponent;
-};
 
 // A query's heads as the first product's operand, one wave: head 32 hb + lane % 32, values D/2 * (lane / 32) + 8 ks .. + 8; of H heads the last
 // stands in for those there are not.  Whole lines are read and parted out through 4 KiB of LDS: read head by head into the registers a line
@@ -915,6 +1057,13 @@ struct Call {
     hipStream_t stream;
 };
 
+BareProduct bare_product(float scale_log2e) {
+    const float size = std::fabs(scale_log2e);
+    if (size == 0.0f) return {1.1754944e-38f, -64};
+    const int exponent = size < 1.0f ? -27 : size < 4294967296.0f ? 0 : 27;
+    return {std::ldexp(scale_log2e, -exponent), exponent};
+}
+
 template <int D, int HW, bool NARROW>
 hipError_t launch_attention(const Call& c, float* out, float* lse) {
     static std::atomic<size_t> allowed[64];
@@ -923,8 +1072,8 @@ hipError_t launch_attention(const Call& c, float* out, float* lse) {
     if (e != hipSuccess) return e;
     const int64_t rows = static_cast<int64_t>(c.d.B) * c.d.S;
     hipLaunchKernelGGL((quantized_attention_kernel<D, HW, NARROW>), dim3(static_cast<unsigned>(rows)), dim3(64 * HW), lds, c.stream, c.qa,
-                       c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e, out,
-                       lse);
+                       c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, c.scale_log2e,
+                       bare_product(c.scale_log2e), out, lse);
     return hipGetLastError();
 }
 
@@ -939,7 +1088,7 @@ hipError_t launch_few(const Call& c, float* out, float* lse) {
     const int64_t grid = (n_queries + kXcds - 1) / kXcds * kXcds * head_blocks * DS;
     hipLaunchKernelGGL((quantized_attention_few_kernel<D, DS, WAVES>), dim3(static_cast<unsigned>(grid)), dim3(64 * WAVES), kBytes, c.stream, c.qa,
                        c.codes, c.scales, c.lengths, c.idx, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, n_queries, head_blocks,
-                       c.scale_log2e, out, lse);
+                       c.scale_log2e, bare_product(c.scale_log2e), out, lse);
     return hipGetLastError();
 }
 
@@ -969,12 +1118,6 @@ hipError_t launch_few(const Call& c, float* out, float* lse) {
     const bool wide = c.k + c.n_win > 1536;
     if (blocks <= 128) return wide ? launch_few<D, 2, 16>(c, out, lse) : launch_few<D, 2, 8>(c, out, lse);
     return wide && blocks <= 256 ? launch_few<D, 1, 16>(c, out, lse) : launch_few<D, 1, 8>(c, out, lse);
-}
-
-BareProduct bare_product(float scale_log2e) {
-    const float size = std::fabs(scale_log2e);
-    const int exponent = size < 1.0f ? -27 : size < 4294967296.0f ? 0 : 27;
-    return {std::ldexp(scale_log2e, -exponent), exponent};
 }
 
 template <int D, int HB, int WAVES>

@@ -1,10 +1,62 @@
-"""GPU: the 4-bit cache's attention and accumulated weights at the ends of what their arguments may be."""
+"""GPU: the 4-bit cache's attention and accumulated weights at the ends of what their arguments may be: values of a query far from one
+another, products beyond fp32 that the softmax scale brings back."""
 import pytest
 import torch
 
 from tests.test_gpu_cache import NONE, _check, _problem
 
 pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------- values of a head far from one another
+def _far_apart(seed, B, S, H, D, T, k, low, high, heads):
+    """Queries of size 2^low with one value of 2^high in some heads, where the rows of the cache have zeros."""
+    q, codes, scales, idx = _problem(seed, B, S, H, D, T, k, None, NONE, 1)
+    at = D // 2 + 3
+    q = (q.float() * 2.0 ** low).to(torch.bfloat16)
+    q[:, :, heads, at] = 2.0 ** high
+    codes[:, :, at // 2] &= 0x0F  # value `at` is odd: the high half
+    return q, codes, scales, idx
+
+
+@pytest.mark.parametrize("S,H,D", [(1, 64, 128), (3, 20, 64), (40, 64, 128), (300, 64, 128), (300, 40, 128), (300, 16, 128), (300, 33, 64),
+                                   (300, 64, 64), (700, 9, 64), (300, 20, 128)])
+@pytest.mark.parametrize("high", [31, 32, 36, 40, 126])
+def test_a_value_far_above_the_others(S, H, D, high):
+    """The logits consist of what lies far below a head's largest value: to the same tolerance as any others."""
+    print(f"S={S} H={H} D={D} high={high}", flush=True)
+    q, codes, scales, idx = _far_apart(high, 1, S, H, D, 150, 70, 0, high, slice(0, None, 3))
+    _check(q, codes, scales, None, idx, 1, NONE, 33, 0.1)
+    if high in (32, 126):
+        _check(q, codes, scales, None, idx, 1, NONE, 33, -0.1)
+        _check(q, codes, scales, None, idx, 1, NONE, 33, 0.0)
+
+
+@pytest.mark.parametrize("S,H,D", [(1, 64, 128), (300, 64, 128), (300, 40, 64), (300, 16, 128)])
+@pytest.mark.parametrize("low,high,scale", [(-110, 0, 1e32), (-110, 100, 1e32), (-60, 60, 1e17), (60, 120, 1e-19), (100, 127, 1e-31), (-126, -80, 1e37),
+                                            (-10, 126, 1e2)])
+def test_values_far_apart_and_far_from_one(S, H, D, low, high, scale):
+    print(f"S={S} H={H} D={D} low={low} high={high} scale={scale}", flush=True)
+    q, codes, scales, idx = _far_apart(S, 1, S, H, D, 150, 70, low, high, slice(1, None, 2))
+    _check(q, codes, scales, None, idx, 1, NONE, 33, scale)
+
+
+@pytest.mark.parametrize("S", [1, 30, 300])
+def test_denormal_values_that_the_scale_brings_back(S):
+    """Queries of bf16's denormal numbers, alone and beside values that rows of zeros meet."""
+    q, codes, scales, idx = _problem(3, 1, S, 20, 64, 150, 70, None, NONE, 1, q_size=2.0 ** -128)
+    _check(q, codes, scales, None, idx, 1, NONE, 9, 2.0 ** 125)
+    q[:, :, ::2, 5] = 2.0 ** -20
+    codes[:, :, 2] &= 0x0F
+    _check(q, codes, scales, None, idx, 1, NONE, 9, 2.0 ** 125)
+
+
+@pytest.mark.parametrize("S", [1, 300])
+def test_rows_of_zeros_under_the_largest_queries(S):
+    """All logits are 0, whatever scale and query: every row counts alike."""
+    q, codes, scales, idx = _problem(3, 1, S, 33, 128, 100, 40, None, NONE, 1, q_size=2.0 ** 120)
+    codes[:] = 0x80  # zeros of either sign
+    _check(q, codes, scales, None, idx, 1, NONE, 9, 2.0 ** 100)
 
 
 # ---------------------------------------------------------------------------------- products that fp32 cannot hold
