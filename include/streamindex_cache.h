@@ -71,9 +71,10 @@ si_status si_quantized_attention(const void* qa, const void* codes, const void* 
  *   lse        device [B,S,H] f32    as that call wrote it
  *   weights    device [B,T] f32      rows that are in no U(t) stay as they are
  *   workspace  device, si_accumulate_workspace_bytes(dims) bytes: none with S = 1 (may be NULL then), else 8 B T
- * A query with a head whose lse is NaN adds nothing.
- * A query's heads are summed in fp32, queries in 64-bit fixed point (units of 2^-32), so that the same call gives the
- * same bits. */
+ * A query with a head whose lse is NaN adds nothing; no other adds more than H to a row.
+ * A query's heads are summed in fp32, queries in 64-bit fixed point, in units of the power of two at or above S H over 2^63, so that the same
+ * call gives the same bits: what a query gives a row is off by half a unit beside fp32's rounding, and S = 1 has no units.  An lse is as good as
+ * fp32, so a weight is off by about |lse| 2^-23 relative to itself. */
 size_t si_accumulate_workspace_bytes(const si_dims* dims);
 si_status si_accumulate_weights(const void* qa, const void* codes, const void* scales, const int32_t* lengths,
                                 const int32_t* idx, const si_dims* dims, int32_t m, int32_t k, si_mask_mode mask_mode,

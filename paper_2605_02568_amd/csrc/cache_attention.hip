@@ -965,16 +965,18 @@ __device__ __forceinline__ void weigh_tiles(const __bf16* __restrict__ qa, const
                 for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[hb][4 * a + j], product.to_log2, minus_lse[j]));
             }
         sum += other_half(sum);
-        // a sum that is no number (some head's lse is none) is not added: it would stay in the weights for good, and has no fixed-point form
-        if (half == 0 && s >= 0 && sum < 4294967296.0f) add(s, sum);
+        // A sum that is no number (some head's lse is none) is not added: it would stay in the weights for good, and has no fixed-point form.  A head
+        // gives a row 1 at most, whatever the rounding of a large lse makes of it.
+        if (half == 0 && s >= 0 && sum == sum) add(s, fminf(sum, static_cast<float>(H)));
     }
 }
 
-// A sum in units of 2^-32, to the nearest: whole part and fraction apart, both exact in fp32.
-__device__ __forceinline__ unsigned long long to_fixed(float sum) {
-    const float whole = __builtin_truncf(sum);
-    const unsigned lo = static_cast<unsigned>(__builtin_rintf((sum - whole) * 4294967296.0f));
-    return (static_cast<unsigned long long>(static_cast<unsigned>(whole)) << 32) + lo;
+// A sum in units of 1 / per_unit (a power of two), to the nearest: both halves are exact in fp32 but where the sum is below 2^24 units.
+__device__ __forceinline__ unsigned long long to_fixed(float sum, float per_unit) {
+    const float units = sum * per_unit;
+    const float high = __builtin_floorf(units * (1.0f / 4294967296.0f));
+    const unsigned low = static_cast<unsigned>(__builtin_rintf(__builtin_fmaf(high, -4294967296.0f, units)));
+    return (static_cast<unsigned long long>(static_cast<unsigned>(high)) << 32) | low;
 }
 
 constexpr int kWeightWaves = 4;
@@ -986,7 +988,7 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
                                const unsigned char* __restrict__ scales, const int32_t* __restrict__ lengths,
                                const int32_t* __restrict__ idx, int64_t n_queries, int n_parts, int per, int S, int H, int T, int m, int mask_mode,
                                int k, int n_win, BareProduct product, const float* __restrict__ lse, float* __restrict__ weights,
-                               unsigned long long* __restrict__ sums) {
+                               unsigned long long* __restrict__ sums, float per_unit) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[kWeightWaves][kWeighBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // all workgroups of a query are on one XCD, as in the kernel for few queries
@@ -1001,7 +1003,7 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
     const int64_t first_row = static_cast<int64_t>(b) * T;
     weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, first_row, u, part * per, min(u.count(), (part + 1) * per), product, lds[wave],
                        [&](int s, float sum) {
-                           if (sums) atomicAdd(sums + first_row + s, to_fixed(sum));
+                           if (sums) atomicAdd(sums + first_row + s, to_fixed(sum, per_unit));
                            else weights[first_row + s] += sum;
                        });
 }
@@ -1015,7 +1017,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(3)))
 void gather_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                            const int32_t* __restrict__ lengths, const int32_t* __restrict__ idx, int n_groups, int S, int H, int T, int m,
                            int mask_mode, int k, int n_win, BareProduct product, const float* __restrict__ lse,
-                           unsigned long long* __restrict__ sums) {
+                           unsigned long long* __restrict__ sums, float per_unit) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     unsigned long long* const s_sums = reinterpret_cast<unsigned long long*>(lds + WAVES * kWeighBytes);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1028,7 +1030,7 @@ void gather_weights_kernel(const __bf16* __restrict__ qa, const unsigned char* _
         const int64_t row_q = static_cast<int64_t>(b) * S + t;
         const Tiles u = tiles_of(idx, qa, row_q, t, k, held, n_win, m, mask_mode);
         weigh_tiles<D, HB>(qa, codes, scales, lse, row_q, H, static_cast<int64_t>(b) * T, u, 0, u.count(), product, lds + wave * kWeighBytes,
-                           [&](int s, float sum) { atomicAdd(s_sums + s, to_fixed(sum)); });
+                           [&](int s, float sum) { atomicAdd(s_sums + s, to_fixed(sum, per_unit)); });
     }
     __syncthreads();
     for (int i = threadIdx.x; i < T; i += 64 * WAVES)
@@ -1039,9 +1041,9 @@ __global__ void clear_sums_kernel(unsigned long long* sums, int64_t n) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
         sums[i] = 0;
 }
-__global__ void add_sums_kernel(const unsigned long long* __restrict__ sums, int64_t n, float* __restrict__ weights) {
+__global__ void add_sums_kernel(const unsigned long long* __restrict__ sums, int64_t n, double unit, float* __restrict__ weights) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
-        if (sums[i]) weights[i] = static_cast<float>(weights[i] + static_cast<double>(sums[i]) * (1.0 / 4294967296.0));
+        if (sums[i]) weights[i] = static_cast<float>(weights[i] + static_cast<double>(sums[i]) * unit);
 }
 
 constexpr int64_t kMostQueries = (int64_t{1} << 24) - 8;
@@ -1120,6 +1122,14 @@ hipError_t launch_few(const Call& c, float* out, float* lse) {
     return wide && blocks <= 256 ? launch_few<D, 1, 16>(c, out, lse) : launch_few<D, 1, 8>(c, out, lse);
 }
 
+// Units of 1: as fine as 64 bits allow where all S queries and H heads give a row 1 each, S H = 2^30 at most.  With units of 2^-32 for every call, what
+// a query gave below 2^-33 was nothing, and eviction ranked such rows by their numbers: all but one where one row's logits are 30 above the others'.
+double sums_per_unit(const si_dims& d) {
+    int bits = 0;
+    while ((int64_t{1} << bits) < static_cast<int64_t>(d.S) * d.H_I) ++bits;
+    return std::ldexp(1.0, 63 - bits);
+}
+
 template <int D, int HB, int WAVES>
 hipError_t launch_gather(const Call& c, int most_groups, const float* lse, unsigned long long* sums) {
     static std::atomic<size_t> allowed[64];
@@ -1129,7 +1139,7 @@ hipError_t launch_gather(const Call& c, int most_groups, const float* lse, unsig
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((gather_weights_kernel<D, HB, WAVES>), dim3(static_cast<unsigned>(c.d.B) * n_groups), dim3(64 * WAVES), lds, c.stream, c.qa,
                        c.codes, c.scales, c.lengths, c.idx, n_groups, c.d.S, c.d.H_I, c.d.T, c.m, c.mask_mode, c.k, c.n_win, bare_product(c.scale_log2e),
-                       lse, sums);
+                       lse, sums, static_cast<float>(sums_per_unit(c.d)));
     return hipGetLastError();
 }
 
@@ -1156,7 +1166,7 @@ hipError_t launch_weights(const Call& c, const float* lse, float* weights, unsig
     const int64_t grid = (rows + kXcds - 1) / kXcds * kXcds * ((n_parts + kWeightWaves - 1) / kWeightWaves);
     hipLaunchKernelGGL((accumulate_weights_kernel<D, HB>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWeightWaves), 0, c.stream, c.qa, c.codes,
                        c.scales, c.lengths, c.idx, rows, n_parts, per, c.d.S, c.d.H_I,
-                       c.d.T, c.m, c.mask_mode, c.k, c.n_win, bare_product(c.scale_log2e), lse, weights, sums);
+                       c.d.T, c.m, c.mask_mode, c.k, c.n_win, bare_product(c.scale_log2e), lse, weights, sums, static_cast<float>(sums_per_unit(c.d)));
     return hipGetLastError();
 }
 
@@ -1228,7 +1238,7 @@ si_status si_accumulate_weights(const void* qa, const void* codes, const void* s
                            : (two ? launch_weights<64, 2>(c, lse, weights, sums) : launch_weights<64, 1>(c, lse, weights, sums));
     }
     if (e == hipSuccess && sums) {
-        hipLaunchKernelGGL(add_sums_kernel, dim3(blocks), dim3(256), 0, c.stream, sums, n, weights);
+        hipLaunchKernelGGL(add_sums_kernel, dim3(blocks), dim3(256), 0, c.stream, sums, n, 1.0 / sums_per_unit(*dims), weights);
         e = hipGetLastError();
     }
     return report(e);

@@ -1,9 +1,12 @@
 """GPU: the 4-bit cache's attention and accumulated weights at the ends of what their arguments may be: values of a query far from one
-another, products beyond fp32 that the softmax scale brings back."""
+another, products beyond fp32 that the softmax scale brings back, rows that receive little."""
+import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_cache import NONE, _check, _problem
+import paper_2605_02568_amd as P
+from tests import cache_reference as R
+from tests.test_gpu_cache import DEV, NONE, _check, _gpu, _problem
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +72,65 @@ def test_products_beyond_fp32(S, H, D, q_size, spread, scale):
     q = (q.double().clamp(-1.5, 1.5) * q_size).to(torch.bfloat16)
     assert bool(torch.isfinite(q.float()).all())
     _check(q, codes, scales, None, idx, 1, NONE, 33, scale)
+
+
+# ---------------------------------------------------------------------------------- rows that receive little
+def _weights(q, codes, scales, idx, scale):
+    """weights of a call on nothing, with the library's own lse."""
+    B, S, H, D = q.shape
+    T = codes.shape[1]
+    args = (q.to(DEV), _gpu(codes), _gpu(scales), None, _gpu(idx), 1, NONE, 0, scale)
+    out, lse = torch.empty((B, S, H, D), device=DEV), torch.empty((B, S, H), device=DEV)
+    P.si_quantized_attention(*args, out, lse)
+    weights = torch.zeros((B, T), device=DEV)
+    nbytes = P.si_accumulate_workspace_bytes(B, S, H, D, T)
+    P.si_accumulate_weights(*args, lse, weights, torch.full((max(16, nbytes),), 0xAB, dtype=torch.uint8, device=DEV))
+    return weights
+
+
+@pytest.mark.parametrize("above", [20.0, 25.0, 30.0])
+@pytest.mark.parametrize("B,S,H,T", [(1, 1, 64, 480), (1, 2, 64, 480), (1, 64, 64, 480), (1, 150, 64, 480), (2, 200, 20, 480), (1, 130, 64, 5000),
+                                     (1, 40, 33, 16000)])
+def test_rows_that_receive_little(B, S, H, T, above):
+    """A row `above` over the others in every head takes nearly everything; what the others receive keeps the accuracy that ranking them
+    needs, whatever the number of queries."""
+    print(f"B={B} S={S} H={H} T={T} above={above}", flush=True)
+    D, n = 64, 480
+    g = torch.Generator().manual_seed(S)
+    q = torch.randn((B, S, H, D), generator=g).to(torch.bfloat16)
+    q[..., 0] = 1.0
+    rows = 0.25 * torch.randn((B, T, D), generator=g)
+    rows[..., :32] = 0.0
+    rows[:, 7, :32] = 0.0
+    rows[:, 7, 0] = above
+    codes, scales = R.pack(*R.quantize(rows.to(torch.bfloat16).double().numpy()))
+    idx = np.tile(np.arange(n, dtype=np.int32), (B, S, 1))
+    weights = _weights(q, codes, scales, idx, 1.0)
+    got = weights.double().cpu().numpy()
+    _, _, given, _, _, tol = R.attend(q.double().numpy(), R.values(codes, scales), None, idx, 1, NONE, 0, 1.0)
+    # The reference's tolerance has half a unit of 2^-32 a query.  A unit is S H / 2^63, its power of two rounded up, and S > 1 queries are
+    # each rounded to half of one; the sum once to fp32.
+    unit = 2.0 ** (np.ceil(np.log2(S * H)) - 63) if S > 1 else 0.0
+    tol = tol[:, :n] - S * 2.0 ** -33 + S * unit / 2 + R.U * given[:, :n]
+    off = np.abs(got[:, :n] - given[:, :n])
+    assert np.all(off <= tol), float((off / tol).max())
+    assert np.all(got[:, n:] == 0)
+    assert np.all(off <= 2e-3 * given[:, :n]), float((off / given[:, :n]).max())
+    # the rows that stay are those that the exact weights keep, but for rows that its tolerance cannot tell apart from the border
+    n_keep = n // 2
+    kept = torch.empty((B, n_keep), dtype=torch.int32, device=DEV)
+    P.si_evict_rows(weights[:, :n].contiguous(), None, n_keep, 0, 0, [], kept, None,
+                    torch.empty(P.si_evict_workspace_bytes(B, n), dtype=torch.uint8, device=DEV))
+    for b in range(B):
+        border = np.sort(given[b, :n])[n - n_keep]
+        sure = np.flatnonzero(given[b, :n] - tol[b] > border + np.delete(tol[b], 7).max())
+        assert len(sure) > 0.9 * n_keep
+        assert np.isin(sure, kept[b].cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("S", [1, 7, 200])
+def test_no_row_receives_more_than_all(S):
+    """lse so large that its rounding is a matter of powers of two: a query gives a row at most 1 a head."""
+    q, codes, scales, idx = _problem(8, 1, S, 40, 64, 90, 30, None, NONE, 1, q_size=1e6)
+    weights = _weights(q, codes, scales, idx, 50.0).double().cpu().numpy()
+    assert np.all(np.isfinite(weights)) and np.all(weights >= 0) and np.all(weights <= S * 40)
