@@ -339,9 +339,11 @@ def _stream_on(stream, gpu: int) -> int:
     return int(stream.cuda_stream)
 
 
+@functools.lru_cache(maxsize=1024)
 def _int32(*sizes) -> None:
-    if max(sizes) >= 2 ** 31:
-        raise ValueError(f"sizes {sizes}: the library takes sizes below 2^31")
+    """Whole numbers that become int32, which ctypes would cut to their lowest 32 bits without a word."""
+    if max(sizes) >= 2 ** 31 or min(sizes) < -2 ** 31:
+        raise ValueError(f"{sizes}: the library takes numbers from -2^31 to 2^31 - 1")
 
 
 @functools.lru_cache(maxsize=1024)
@@ -376,8 +378,9 @@ def si_dequantize_rows(codes, scales, start, rows, stream=None):
     _check(load().si_dequantize_rows(c, s, at, dims, r, st), "si_dequantize_rows")
 
 
-def _quantized_call(qa, codes, scales, lengths, idx):
+def _quantized_call(qa, codes, scales, lengths, idx, m, mask_mode, n_win):
     """GPU, pointers, sizes as the library takes them, k."""
+    _int32(m, mask_mode, n_win)
     qs, cs = qa.shape, codes.shape
     if len(qs) != 4 or len(cs) != 3:
         raise ValueError("qa must be [B,S,H,D], codes [B,T,D/2], scales [B,T,D/32]")
@@ -399,7 +402,7 @@ def _quantized_call(qa, codes, scales, lengths, idx):
 def si_quantized_attention(qa, codes, scales, lengths, idx, m, mask_mode, n_win, scale, out, lse=None, stream=None):
     """Attention over TopK(t) U Window(t) on a 4-bit cache: qa [B,S,H,D] bf16, codes [B,T,D/2] and scales [B,T,D/32] uint8,
     lengths int32 [B] or None (= T), idx [B,S,k] int32 or None (no list), out [B,S,H,D] f32, lse [B,S,H] f32 or None."""
-    gpu, q, c, s, held, lists, dims, k = _quantized_call(qa, codes, scales, lengths, idx)
+    gpu, q, c, s, held, lists, dims, k = _quantized_call(qa, codes, scales, lengths, idx, m, mask_mode, n_win)
     if out.shape != qa.shape:
         raise ValueError(f"out must be {tuple(qa.shape)}")
     if lse is not None and lse.shape != qa.shape[:3]:
@@ -416,7 +419,7 @@ def si_accumulate_workspace_bytes(B, S, H, D, T) -> int:
 def si_accumulate_weights(qa, codes, scales, lengths, idx, m, mask_mode, n_win, scale, lse, weights, workspace=None, stream=None):
     """Adds what every cache row receives of the softmax of an si_quantized_attention call (same arguments, lse as it wrote
     it) to weights [B,T] f32; workspace: uint8 GPU tensor of si_accumulate_workspace_bytes, None where that is 0."""
-    gpu, q, c, s, held, lists, dims, k = _quantized_call(qa, codes, scales, lengths, idx)
+    gpu, q, c, s, held, lists, dims, k = _quantized_call(qa, codes, scales, lengths, idx, m, mask_mode, n_win)
     if lse.shape != qa.shape[:3] or weights.shape != codes.shape[:2]:
         raise ValueError(f"lse must be {tuple(qa.shape[:3])}, weights {tuple(codes.shape[:2])}")
     ws, ws_bytes = None, 0 if workspace is None else workspace.numel()
