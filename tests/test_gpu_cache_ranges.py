@@ -1,12 +1,12 @@
 """GPU: the 4-bit cache's attention and accumulated weights at the ends of what their arguments may be: values of a query far from one
-another, products beyond fp32 that the softmax scale brings back, rows that receive little."""
+another, products beyond fp32 that the softmax scale brings back, rows that receive little, every kernel that adds weights up."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_02568_amd as P
 from tests import cache_reference as R
-from tests.test_gpu_cache import DEV, NONE, _check, _gpu, _problem
+from tests.test_gpu_cache import CAUSAL, DEV, NONE, _check, _gpu, _problem
 
 pytestmark = pytest.mark.gpu
 
@@ -134,3 +134,28 @@ def test_no_row_receives_more_than_all(S):
     q, codes, scales, idx = _problem(8, 1, S, 40, 64, 90, 30, None, NONE, 1, q_size=1e6)
     weights = _weights(q, codes, scales, idx, 50.0).double().cpu().numpy()
     assert np.all(np.isfinite(weights)) and np.all(weights >= 0) and np.all(weights <= S * 40)
+
+
+# ---------------------------------------------------------------------------------- every kernel that adds weights up
+@pytest.mark.parametrize("T", [4096, 4097, 15360, 15361])
+@pytest.mark.parametrize("H,D", [(64, 128), (33, 64), (32, 128), (5, 64)])
+def test_weights_of_prompts_in_long_caches(T, H, D):
+    """Around the lengths at which the sums of many queries are kept elsewhere."""
+    print(f"T={T} H={H} D={D}", flush=True)
+    q, codes, scales, idx = _problem(T + H, 1, 130, H, D, T, 40, [T - 1], NONE, 1)
+    _check(q, codes, scales, [T - 1], idx, 1, NONE, 9, 1.0 / np.sqrt(D))
+
+
+@pytest.mark.parametrize("B,S,H,D,T", [(70, 16, 20, 64, 100), (9, 127, 40, 128, 60), (64, 16, 33, 128, 4500), (63, 16, 8, 64, 300)])
+def test_weights_of_short_prompts_in_batches(B, S, H, D, T):
+    """Around the number of queries from which on the sums are kept in LDS."""
+    print(f"B={B} S={S} H={H} D={D} T={T}", flush=True)
+    q, codes, scales, idx = _problem(S + B, B, S, H, D, T, 24, None, CAUSAL, 1)
+    _check(q, codes, scales, None, idx, 1, CAUSAL, 5, 1.0 / np.sqrt(D))
+
+
+def test_weights_of_many_queries_in_a_long_cache():
+    """More queries than waves fit the chip, whose sums go to the workspace at once."""
+    B, S, H, D, T = 1, 2500, 4, 64, 15400
+    q, codes, scales, idx = _problem(4, B, S, H, D, T, 33, None, NONE, 1)
+    _check(q, codes, scales, None, idx, 1, NONE, 7, 0.125)
