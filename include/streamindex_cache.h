@@ -57,7 +57,9 @@ si_status si_dequantize_rows(const void* codes, const void* scales, const int32_
  *   idx      device [B,S,k] int32   0 <= k <= 4096; may be NULL with k = 0
  *   out      device [B,S,H,D] f32,  lse device [B,S,H] f32 or NULL
  * fp32 products, statistics and sums; the weights enter the second product with 22 mantissa bits, or to 2^-32 of their sum where that
- * is more.
+ * is more.  A head's values and scale may be as far apart as they like: what is lost is what fp32 loses of the logits.
+ * Lists that si_indexer_topk makes are of all T rows: where batches hold fewer, rows behind lengths[b] take places in them, which are skipped here.
+ * A caller keeps such rows from being chosen by a call of si_indexer_topk a batch, with that batch's rows as T; otherwise a list holds that many fewer.
  * A head whose query is not finite, or whose logits are not, gets NaN in out and lse, and no other head does.  scale has to be finite,
  * scale * log2(e) too (SI_ERR_INVALID_ARG).
  * No workspace.  The same call gives the same bits; calls of other numbers of queries may differ in a query's last places. */

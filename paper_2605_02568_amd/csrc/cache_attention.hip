@@ -6,8 +6,9 @@
 //   weights[s]  += sum_{t,h} exp( scale * <qa[t,h,:], V[s,:]> - lse[t,h] )
 //
 // V[s, 32 j + i] = code * 2^e(s, j).  Codes times their power are exact in fp16 (exponents -13 .. 13), and so are the queries once a
-// head is scaled by a power of two, which goes into the softmax scale.  So the first product is that of the bf16 operands, and the second one
-// takes the weights in two fp16 parts, 22 mantissa bits, at the cost that two bf16 parts with 16 bits would have.
+// head is scaled by a power of two, which goes into the softmax scale; heads whose values lie too far apart for that are multiplied in bf16.  So the
+// first product is that of the bf16 operands, and the second one takes the weights in two fp16 parts, up to 22 mantissa bits, at the cost that two
+// bf16 parts with 16 bits would have.
 
 #include <hip/hip_runtime.h>
 
@@ -42,8 +43,9 @@ typedef unsigned short shortx2 __attribute__((ext_vector_type(2)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLog2eRest = 1.925962989e-8f;  // log2(e) - kLog2e: left out of an lse of 7, 9e-8 too much for every row alike
 constexpr float kLn2 = 0.6931471805599453f;
-// The weights are 2^7 times exp2(x - reference): at most 2^15 with the slack of 2^8, so that both fp16 parts of
-// a weight are normal numbers down to 2^-18 of the reference's weight.
+// The weights are 2^7 times exp2(x - reference): at most 2^15 with the slack of 2^8.  The first fp16 part is a normal number down to 2^-21 of the
+// reference's weight; the second one, whose step is 2^-24 at least, adds 11 bits to it down to 2^-9, and below that leaves a weight off by up to 2^-25
+// as it is held, 2^-32 of the reference's.
 constexpr float kWeightShift = 7.0f;
 
 // Between what some lanes of a wave write to LDS and others of it read there: the hardware does a wave's LDS accesses in order, and this keeps
@@ -77,8 +79,8 @@ struct BareProduct {
 // A lane's part of a query's head, 8 bf16 values an element, as the products take it: fp16, times a power of two that brings the head's
 // largest magnitude into [2^14, 2^15), with the sign of the softmax scale; values of exponents down to 31 below the largest one's stay exact.  The
 // factor |scale| log2(e) over that power takes a product of these operands to the log2 domain.  A block of heads one of which holds smaller values
-// too, or needs a factor that fp32 does not hold, takes the bare product instead, at twice the conversions: rows of zeros where the query's large
-// values are would leave logits that consist of what fp16 lost.
+// too, or needs a factor that fp32 does not hold, takes the bare product instead, at twice the conversions (all heads of 16384 queries of 640 rows
+// 471 -> 665 us, of 32 queries of 1152 9.6 -> 16.6): rows of zeros where the query's large values are would leave logits that consist of what fp16 lost.
 
 // Magnitudes of a head's values, as bf16's bits: in the low half the largest, in the high half 2^16 less the smallest that is not 0 (or 0).  Of two
 // parts: the larger of each half.
@@ -592,9 +594,9 @@ __device__ __forceinline__ void narrow_query(const __bf16* __restrict__ qa, cons
 
 // One workgroup = one query; wave w owns heads [32 w, 32 w + 32) and goes through the query's list (attention_set.h) by itself: each wave turns the
 // codes it needs into a tile of its own, which costs the conversions twice and no barrier (a tile shared by two waves: 560 us, a wave by itself 520).
-// Bound by power and issue together: 16384 queries of 640 rows, 64 heads of 128, take 445 to 515 us (300 GFLOP, 450 with the second part of the
-// weights; the first kernel after a pause is the fastest); the clock is then 1.82 GHz, the matrix pipe 53 % busy, the vector units 64 %, the units that
-// return gathered codes 79 %.  The form si_sparse_attention has of this, on rows of 256 bytes in place of 68, takes 475 to 500.
+// 16384 queries of 640 rows, 64 heads of 128, take 445 to 515 us (300 GFLOP, 450 with the second part of the weights; the first kernel after a pause
+// is the fastest).  The units that return gathered codes are busiest, 79 %: every row is gathered by both waves of a query.  The vector units are busy
+// 63 %, the matrix pipe 53 %, at 1.82 GHz, which is what the power drawn leaves.  The form si_sparse_attention has of this, on rows of 256 bytes in place of 68, takes 475 to 500.
 // Dynamic LDS: a tile of 32 x D fp16 a wave, the list.
 template <int D, int HW, bool NARROW>
 __global__ __launch_bounds__(64 * HW) __attribute__((amdgpu_waves_per_eu(3)))
@@ -1008,8 +1010,8 @@ void accumulate_weights_kernel(const __bf16* __restrict__ qa, const unsigned cha
                        });
 }
 
-// Many queries of few rows: 8192 of 640 of 2048 rows, 64 heads of 128, take 95 us of 106 in this kernel: vector units 57 %, matrix pipe 36 %, issue of
-// three waves a SIMD the rest (without exponentials 12 us less, without products 27, without reads of rows 15).  A workgroup adds up in LDS what its queries (every n_groups-th wave's worth of a batch) give the batch's rows,
+// Many queries of few rows: 8192 of 640 of 2048 rows, 64 heads of 128, take 95 us of 99 to 103 in this kernel.  The units that return gathered codes are
+// busy 70 %, vector units 59 %, matrix pipe 37 % (without exponentials 12 us less, without products 27, without reads of rows 15).  A workgroup adds up in LDS what its queries (every n_groups-th wave's worth of a batch) give the batch's rows,
 // and then adds that to the workspace, row after row.  Added up there at once, the sums wait for one another: 8192 queries of 640 of 2048 rows took
 // 657 us, 12 adds a nanosecond.
 template <int D, int HB, int WAVES>
@@ -1104,14 +1106,15 @@ hipError_t launch_attention(const Call& c, float* out, float* lse) {
     return H <= 48 ? launch_attention<D, 2, true>(c, out, lse) : launch_attention<D, 2, false>(c, out, lse);
 }
 
-// Blocks of 16 heads of all queries, and the rows a query may attend to, decide.  Measured (us; B queries of 64 heads of 128, 4 B blocks):
+// Blocks of 16 heads of all queries, and the rows a query may attend to by its list and window (the host does not know how many are held), decide.
+// Measured at 64 heads of 128, and taken for other numbers and sizes of heads as it is (us; B queries of 64 heads of 128, 4 B blocks):
 // the kernel for many queries against this one's, rows 1152: B = 32 33 -> 9.5, 128 34 -> 16, 192 34 -> 23, 256 35 -> 29, 384 47 -> 40, 512 47 -> 52;
 // 384 rows: 128 15 -> 9, 192 15.2 -> 13.1, 256 15.8 -> 16.0; 64 rows: 32 5.5 -> 4.6, 160 6.9 -> 8.7.
 bool few_queries(const si_dims& d, int k, int n_win) {
     const int64_t blocks = static_cast<int64_t>(d.B) * d.S * ((d.H_I + kFewHeads - 1) / kFewHeads);
     return blocks <= 512 || (blocks < 1024 && k + n_win >= 384) || (blocks <= 1536 && k + n_win >= 1024);
 }
-// Halves of d where these fit the chip's compute units once (B = 32: 10.4 -> 9.5, B = 48: 10.6 -> 13.4); 16 waves where a workgroup has a unit to
+// Measured at 64 heads of 128, as above.  Halves of d where these fit the chip's compute units once (B = 32: 10.4 -> 9.5, B = 48: 10.6 -> 13.4); 16 waves where a workgroup has a unit to
 // itself and more than five tiles a wave (B = 32, rows 1152 / 1536 / 2048 / 4096: 8 waves 9.5 / 11.7 / 14.3 / 23.8, 16 waves 9.8 / 11.2 / 13.2 / 20.1;
 // B = 64: 11.0 / 13.5 / 17.0 / - and 11.6 / 13.5 / 16.0 / -).
 template <int D>
@@ -1150,6 +1153,8 @@ static_assert(8 * kWeighBytes + kGatherRows * 8 <= 159 * 1024, "the longest cach
 // Measured (us): sums in the workspace at once / 8 waves, 256 workgroups / 4 waves, 768 workgroups, 64 heads of 128: 8192 queries of 640 of 2048 rows
 // 657 / 116 / 106, 4000 of 1128 of 4000 381 / 104 / 95, 2 x 6000 of 428 of 6000 358 / 124 / 137, 10000 of 164 of 10000 114 / 63 / 90, 300 of 100 of 300
 // 22 / 16 / 17; few queries, whose tiles are then not shared out: 64 of 640 of 4000 8.7 / 28 / 22, 64 x 4 of 640 of 8192 16 / 25 / 26.
+// Longer caches take the sums in the workspace at once, at 17 to 22 rows a nanosecond (65536 queries of 640 of 16384 rows 2.4 ms, 262144 of 1152 of 65536
+// 13.8 ms) in place of 38 to 46 (61440 of 640 of 15360 0.82 ms): their adds, scattered over all rows, bound them, for 16 heads as for 64.
 bool gathers(const si_dims& d) {
     return d.T <= kGatherRows && (d.S >= 128 || (d.S >= 16 && static_cast<int64_t>(d.B) * d.S >= 1024));
 }

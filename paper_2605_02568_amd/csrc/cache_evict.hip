@@ -6,7 +6,8 @@
 // stay, and of those that equal it as many of the first as there is room for.  Then each workgroup takes a chunk of rows, lists those that stay
 // (where its list begins is known from the counts of the chunks before it) and copies what belongs to them.  Small calls do all of it in one launch.
 //
-// The copies bound long and many rows: 2 * n_keep * (bytes of a row in all arrays), 208 MB of 32 batches in 31.5 us after 11.5 for the borders;
+// The copies bound long and many rows: 2 * (rows that stay) * (bytes of a row in all arrays), 191 MB of 32 batches of 8205 to 16411 rows in 48.5 us where
+// nothing of it is in the caches (32 on the same arrays again), right behind 12.5 for the borders;
 // 1 x 262144 rows, 104 MB, 19.5 after 24 of five launches that each hold little more than their chain of dependent steps (groups of half as many rows,
 // half or twice the threads: within 3 %).  Few rows take 7.5 us, a launch and that chain.
 
@@ -643,7 +644,7 @@ si_status si_evict_rows(const float* weights, const int32_t* lengths, int32_t B,
         return report(hipGetLastError());
     }
     if (T <= kMostSelectRows) {
-static std::atomic<size_t> allowed[64];
+        static std::atomic<size_t> allowed[64];
         const size_t lds = static_cast<size_t>((T + 63) / 64 * 64) * sizeof(uint32_t);
         e = allow_lds(evict_select_kernel, lds, allowed);
         if (e != hipSuccess) return report(e);
