@@ -6,7 +6,7 @@ import torch
 
 import paper_2605_02568_amd as P
 from tests import cache_reference as R
-from tests.test_gpu_cache import CAUSAL, DEV, NONE, _check, _gpu, _problem
+from tests.test_gpu_cache import CAUSAL, DEV, NONE, _check, _gpu, _problem, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -33,6 +33,38 @@ def test_a_value_far_above_the_others(S, H, D, high):
     if high in (32, 126):
         _check(q, codes, scales, None, idx, 1, NONE, 33, -0.1)
         _check(q, codes, scales, None, idx, 1, NONE, 33, 0.0)
+
+
+@pytest.mark.parametrize("S,H,D,T,k", [(1, 64, 128, 1700, 1600), (1, 20, 64, 1700, 1600), (40, 64, 128, 1700, 1600), (40, 64, 64, 1700, 1600),
+                                       (40, 64, 64, 150, 70), (1, 5, 128, 40, 3)])
+def test_a_value_far_above_the_others_of_few_queries(S, H, D, T, k):
+    """Every number of waves and share of d that few queries come with."""
+    print(f"S={S} H={H} D={D} T={T} k={k}", flush=True)
+    q, codes, scales, idx = _far_apart(T + S, 1, S, H, D, T, k, 0, 50, slice(0, None, 5))
+    _check(q, codes, scales, None, idx, 1, NONE, 3, 0.1)
+
+
+@pytest.mark.parametrize("S,H,D", [(2, 33, 128), (400, 48, 64), (400, 33, 128)])
+def test_values_far_apart_in_batches_that_hold_little(S, H, D):
+    """Batches with all rows, none, some and one; queries without any; rising logits."""
+    q, codes, scales, idx = _far_apart(S, 4, S, H, D, 150, 70, 4, 60, slice(0, None, 3))
+    _check(q, codes, scales, [150, 0, 31, 1], idx, 1, NONE, 0, 0.3)
+    _check(q, codes, scales, [150, 0, 31, 1], idx, 1, CAUSAL, 20, -0.3)
+
+
+@pytest.mark.parametrize("S,H,D", [(2, 33, 128), (300, 64, 128), (300, 16, 64), (300, 48, 128)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_queries_that_are_not_finite_beside_values_far_apart(S, H, D, bad):
+    """The head (not one of those with far values) has NaN, no other head of the block anything else than without it."""
+    q, codes, scales, idx = _far_apart(S, 1, S, H, D, 150, 70, 0, 60, slice(0, None, 3))
+    idx[0, S - 1] = np.arange(70)
+    clean, clean_lse, _ = _run(q, codes, scales, None, idx, 1, NONE, 9, 0.1)
+    q[0, S - 1, H - 2, 5] = bad
+    out, lse, weights = _run(q, codes, scales, None, idx, 1, NONE, 9, 0.1)
+    assert np.isnan(lse[0, S - 1, H - 2]) and np.all(np.isnan(out[0, S - 1, H - 2]))
+    out[0, S - 1, H - 2], lse[0, S - 1, H - 2] = clean[0, S - 1, H - 2], clean_lse[0, S - 1, H - 2]
+    assert np.array_equal(out, clean) and np.array_equal(lse, clean_lse)
+    assert np.all(np.isfinite(weights))
 
 
 @pytest.mark.parametrize("S,H,D", [(1, 64, 128), (300, 64, 128), (300, 40, 64), (300, 16, 128)])
