@@ -23,6 +23,7 @@ SI_ERR_HIP = -4
 SI_MASK_NONE = 0
 SI_MASK_CAUSAL_BLOCK = 1
 SI_MAX_ROW_MOVES = 8
+SI_ALL_ROWS = 2 ** 31 - 1
 SI_PROFILE_CLASSES = 7
 PROFILE_CLASS_NAMES = ("score_tile", "filter_scores", "compact", "finalize", "init", "fused", "fused_narrow")
 
@@ -36,6 +37,7 @@ EXPORTS = (
     "si_version",
     "si_quantize_rows", "si_dequantize_rows", "si_quantized_attention", "si_accumulate_workspace_bytes",
     "si_accumulate_weights", "si_evict_workspace_bytes", "si_evict_rows",
+    "si_store_pages", "si_load_pages", "si_paged_workspace_bytes", "si_paged_attention", "si_prompt_attention",
 )
 
 
@@ -49,6 +51,16 @@ class si_plan(Structure):
 
 class si_row_move(Structure):
     _fields_ = [("src", c_void_p), ("dst", c_void_p), ("row_bytes", c_int32)]
+
+
+class si_paged_cache(Structure):
+    _fields_ = [("K", c_void_p), ("V", c_void_p), ("K_scales", c_void_p), ("V_scales", c_void_p), ("table", c_void_p),
+                ("B", c_int32), ("table_pages", c_int32), ("n_pages", c_int32), ("page_rows", c_int32), ("H_kv", c_int32), ("D", c_int32),
+                ("bits", c_int32)]
+
+
+class si_packed_dims(Structure):
+    _fields_ = [("B", c_int32), ("N_q", c_int32), ("N_k", c_int32), ("H", c_int32), ("H_kv", c_int32), ("D", c_int32)]
 
 
 class StreamIndexError(RuntimeError):
@@ -141,6 +153,18 @@ def load():
     L.si_evict_rows.restype = c_int32
     L.si_evict_rows.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p,
                                 c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.si_store_pages.restype = c_int32
+    L.si_store_pages.argtypes = [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
+    L.si_load_pages.restype = c_int32
+    L.si_load_pages.argtypes = [c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    L.si_paged_workspace_bytes.restype = c_size_t
+    L.si_paged_workspace_bytes.argtypes = [c_int32] * 5
+    L.si_paged_attention.restype = c_int32
+    L.si_paged_attention.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_float, c_void_p,
+                                     c_void_p, c_void_p, c_size_t, c_void_p]
+    L.si_prompt_attention.restype = c_int32
+    L.si_prompt_attention.argtypes = [c_void_p, c_void_p, c_void_p, POINTER(si_packed_dims), c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                      c_int32, c_float, c_void_p, c_void_p, c_void_p]
     _lib = L
     return L
 
@@ -470,6 +494,151 @@ def si_evict_rows(weights, lengths, n_keep, n_sink, n_recent, moves, kept, new_l
         _ptr(weights, torch.float32, gpu, "weights"), _per_batch(lengths, B, gpu, "lengths"), B, T, n_keep, n_sink, n_recent, table,
         len(moves), _ptr(kept, torch.int32, gpu, "kept"), _per_batch(new_lengths, B, gpu, "new_lengths"),
         _ptr(workspace, torch.uint8, gpu, "workspace"), workspace.numel(), _stream_on(stream, gpu)), "si_evict_rows")
+
+
+# ---- dense attention over a paged cache and over packed prompts (include/streamindex_pages.h, include/streamindex_prompt.h)
+# A si_paged_cache, packed at once: fields one by one would cost the host more than the launch.
+_cache_layout = struct.Struct("=5Q7i4x")
+
+
+def _paged_cache(table, K, V, k_scales, v_scales):
+    """GPU of a call, packed si_paged_cache, its sizes (B, H_kv, D)."""
+    ts, ks = table.shape, K.shape
+    if len(ts) != 2 or len(ks) != 4:
+        raise ValueError("table must be [B, pages of a sequence], K and V [n_pages, H_kv, page_rows, D]")
+    dtype = K.dtype
+    if dtype is torch.bfloat16:
+        bits = 16
+        if k_scales is not None or v_scales is not None:
+            raise ValueError("a cache in 16 bits has no scales")
+    elif dtype is torch.uint8:
+        bits = 8
+        if k_scales is None or k_scales.shape != ks[:3]:
+            raise ValueError(f"k_scales must be {tuple(ks[:3])}")
+        if (V is None) != (v_scales is None) or (V is not None and v_scales.shape != ks[:3]):
+            raise ValueError(f"v_scales must be {tuple(ks[:3])}, None where V is")
+    else:
+        raise TypeError(f"K must be torch.bfloat16 or torch.uint8, got {dtype}")
+    if V is not None and V.shape != ks:
+        raise ValueError(f"V must be {tuple(ks)}")
+    gpu = _gpu_of(table, "table")
+    (B, wide), (n_pages, H, rows, D) = ts, ks
+    _int32(B, wide, n_pages, H, rows, D)
+    packed = _cache_layout.pack(
+        _ptr(K, dtype, gpu, "K"), 0 if V is None else _ptr(V, dtype, gpu, "V"),
+        0 if k_scales is None else _ptr(k_scales, torch.uint8, gpu, "k_scales"), 0 if v_scales is None else _ptr(v_scales, torch.uint8, gpu, "v_scales"),
+        _ptr(table, torch.int32, gpu, "table"), B, wide, n_pages, rows, H, D, bits)
+    return gpu, packed, B, H, D
+
+
+def _offsets_of(offsets, B, gpu: int, name: str):
+    """Pointer of an optional int32 [B + 1] tensor."""
+    if offsets is None:
+        return None
+    if offsets.shape != (B + 1,):
+        raise ValueError(f"{name} must be [{B + 1}]")
+    return _ptr(offsets, torch.int32, gpu, name)
+
+
+def _packed_rows(rows, H, D, gpu: int, name: str):
+    """Pointer and number of packed rows [N,H,D] bf16."""
+    if len(rows.shape) != 3 or rows.shape[1] != H or rows.shape[2] != D:
+        raise ValueError(f"{name} must be [N, {H}, {D}], got {tuple(rows.shape)}")
+    return _ptr(rows, torch.bfloat16, gpu, name), rows.shape[0]
+
+
+def si_store_pages(k_rows, v_rows, offsets, start, table, K, V, k_scales=None, v_scales=None, stream=None):
+    """Packed rows [N,H_kv,D] bf16 of keys and values into the pages of a cache: K and V [n_pages,H_kv,page_rows,D], bf16 or (with k_scales and
+    v_scales [n_pages,H_kv,page_rows]) uint8; packed row offsets[b] + i becomes row start[b] + i of sequence b (offsets: int32 [B+1] or None:
+    equal shares; start: int32 [B] or None = 0), which is in page table[b, row / page_rows] (int32 [B,pages]).  V and v_rows None: a row's keys are its values."""
+    gpu, cache, B, H, D = _paged_cache(table, K, V, k_scales, v_scales)
+    k, N = _packed_rows(k_rows, H, D, gpu, "k_rows")
+    v = None
+    if v_rows is not None:
+        v, n = _packed_rows(v_rows, H, D, gpu, "v_rows")
+        if n != N:
+            raise ValueError(f"v_rows must be {tuple(k_rows.shape)}")
+    _int32(N)
+    _check(load().si_store_pages(k, v, N, _offsets_of(offsets, B, gpu, "offsets"), _per_batch(start, B, gpu, "start"), cache,
+                                 _stream_on(stream, gpu)), "si_store_pages")
+
+
+def si_load_pages(table, K, V, k_scales, v_scales, offsets, start, k_rows, v_rows, stream=None):
+    """The way back: rows start[b] + i of sequence b into packed rows offsets[b] + i of k_rows and v_rows [N,H_kv,D] bf16 (either may be None), as
+    the values that are held, zeros where the sequence has no such row."""
+    gpu, cache, B, H, D = _paged_cache(table, K, V, k_scales, v_scales)
+    k = v = None
+    N = 0
+    if k_rows is not None:
+        k, N = _packed_rows(k_rows, H, D, gpu, "k_rows")
+    if v_rows is not None:
+        v, n = _packed_rows(v_rows, H, D, gpu, "v_rows")
+        if k is not None and n != N:
+            raise ValueError(f"v_rows must be {tuple(k_rows.shape)}")
+        N = n
+    _int32(N)
+    _check(load().si_load_pages(cache, N, _offsets_of(offsets, B, gpu, "offsets"), _per_batch(start, B, gpu, "start"), k, v,
+                                _stream_on(stream, gpu)), "si_load_pages")
+
+
+def si_paged_workspace_bytes(B, S, H, H_kv, D) -> int:
+    _int32(B, S, H, H_kv, D)
+    return int(load().si_paged_workspace_bytes(B, S, H, H_kv, D))
+
+
+def si_paged_attention(q, table, K, V, k_scales, v_scales, lengths, first, m, mask_mode, n_win, scale, out, lse, workspace, stream=None):
+    """Attention of q [B,S,H,D] bf16, S positions of each sequence from first[b] on (int32 [B] or None = 0), over the rows that the sequences hold
+    (lengths: int32 [B] or None: as many as the table has room for) in a cache as of si_store_pages, all legal ones (n_win = SI_ALL_ROWS) or the
+    last n_win; out [B,S,H,D] bf16, lse [B,S,H] f32 or None; workspace: uint8 GPU tensor of si_paged_workspace_bytes."""
+    gpu, cache, B, H_kv, D = _paged_cache(table, K, V, k_scales, v_scales)
+    qs = q.shape
+    if len(qs) != 4 or qs[0] != B or qs[3] != D:
+        raise ValueError(f"q must be [{B}, S, H, {D}], got {tuple(qs)}")
+    if out.shape != qs:
+        raise ValueError(f"out must be {tuple(qs)}")
+    if lse is not None and lse.shape != qs[:3]:
+        raise ValueError(f"lse must be {tuple(qs[:3])}")
+    S, H = qs[1], qs[2]
+    _int32(S, H, m, mask_mode, n_win)
+    _check(load().si_paged_attention(
+        _ptr(q, torch.bfloat16, gpu, "q"), cache, S, H, _per_batch(lengths, B, gpu, "lengths"), _per_batch(first, B, gpu, "first"), m, mask_mode,
+        n_win, float(scale), _ptr(out, torch.bfloat16, gpu, "out"), None if lse is None else _ptr(lse, torch.float32, gpu, "lse"),
+        _ptr(workspace, torch.uint8, gpu, "workspace"), workspace.numel(), _stream_on(stream, gpu)), "si_paged_attention")
+
+
+@functools.lru_cache(maxsize=1024)
+def _packed_sizes(B, N_q, N_k, H, H_kv, D):
+    _int32(B, N_q, N_k, H, H_kv, D)
+    return byref(si_packed_dims(B, N_q, N_k, H, H_kv, D))
+
+
+def si_prompt_attention(q, K, V, q_offsets, k_offsets, first, m, mask_mode, n_win, scale, out, lse=None, stream=None):
+    """Attention of packed sequences: queries q [N_q,H,D] over rows K and V [N_k,H_kv,D], all bf16 (V None: a row's keys are its values); sequence b has
+    the queries from q_offsets[b] and the rows from k_offsets[b] on (int32 [B+1]; None: equal shares; both None: first's number, else one sequence), its
+    queries are at positions first[b] + i (int32 [B] or None = 0); n_win = SI_ALL_ROWS: no window; out [N_q,H,D] bf16, lse [N_q,H] f32 or None."""
+    qs, ks = q.shape, K.shape
+    if len(qs) != 3 or len(ks) != 3 or ks[2] != qs[2]:
+        raise ValueError(f"q must be [N_q,H,D], K [N_k,H_kv,D], got {tuple(qs)} and {tuple(ks)}")
+    if V is not None and V.shape != ks:
+        raise ValueError(f"V must be {tuple(ks)}")
+    if out.shape != qs:
+        raise ValueError(f"out must be {tuple(qs)}")
+    if lse is not None and lse.shape != qs[:2]:
+        raise ValueError(f"lse must be {tuple(qs[:2])}")
+    B = 1
+    for t, more in ((q_offsets, 1), (k_offsets, 1), (first, 0)):
+        if t is not None:
+            if len(t.shape) != 1:
+                raise ValueError("q_offsets and k_offsets must be [B+1], first [B]")
+            B = t.shape[0] - more
+            break
+    gpu = _gpu_of(q, "q")
+    _int32(m, mask_mode, n_win)
+    _check(load().si_prompt_attention(
+        _ptr(q, torch.bfloat16, gpu, "q"), _ptr(K, torch.bfloat16, gpu, "K"), None if V is None else _ptr(V, torch.bfloat16, gpu, "V"),
+        _packed_sizes(B, qs[0], ks[0], qs[1], ks[1], qs[2]), _offsets_of(q_offsets, B, gpu, "q_offsets"), _offsets_of(k_offsets, B, gpu, "k_offsets"),
+        _per_batch(first, B, gpu, "first"), m, mask_mode, n_win, float(scale), _ptr(out, torch.bfloat16, gpu, "out"),
+        None if lse is None else _ptr(lse, torch.float32, gpu, "lse"), _stream_on(stream, gpu)), "si_prompt_attention")
 
 
 def si_score_tile(q, K, w, m, mask_mode, s0, t0, c_S, c_T, tile, stream=None):

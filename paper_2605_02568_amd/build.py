@@ -13,7 +13,7 @@ OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libstreamindex.so")
 
 SOURCES = ["score_tile.hip", "fused.hip", "topk.hip", "rows.hip", "short_rows.hip", "driver.hip", "attention.hip",
-           "cache_rows.hip", "cache_attention.hip", "cache_evict.hip"]
+           "cache_rows.hip", "cache_attention.hip", "cache_evict.hip", "pages.hip", "paged_attention.hip", "prompt_attention.hip"]
 # a stand-alone measurement program (register-only MFMA/VALU issue probe), not linked into the library
 PROBE_SOURCE = "issue_probe.hip"
 PROBE = os.path.join(PKG, "issue_probe")

@@ -1,0 +1,349 @@
+// Dense attention of packed prompts (si_prompt_attention).
+//
+//   out[i,g,:] = sum_{s in seen(t)} exp(x_s - lse) V[s,h,:],  x_s = scale <q[i,g,:], K[s,h,:]>,  lse = ln sum exp(x_s),  t = first[b] + i
+//
+// Bound by the matrix pipe: 4 D operations a pair of query and row, whose rows all workgroups of a head find in their XCD's L2.
+// The queries and heads that share a head of keys and values are the columns of one product (column r of a sequence: query r / G, head r % G
+// of the group of G), 256 of them a workgroup, 32 a wave; so short prompts and large groups fill a workgroup, and the masked part of a tile
+// on the diagonal is as small as 256 / G queries.  The workgroup's waves share tiles of 64 rows, which go straight from memory to LDS, one on its
+// way while the one before is used.  Per tile and wave:
+//   S^T[64 rows x 32 columns] = Ktile q^T   v_mfma_f32_32x32x16_bf16: a lane has 32 rows of one column, so a column's statistics are in-lane
+//   p = exp2(x - m_ref)                     reference of a column raised (and the sums rescaled) only when a lane's sum of weights
+//                                           passes 2^10; fp32
+//   O^T[D x 32] += Vtile^T P^T              P^T is an operand straight from the registers of S^T (the rows' order inside the
+//                                           contraction is the same on both sides), Vtile^T comes from LDS by transposing reads
+// p is rounded to bf16 for that product only; the sum of weights is of p itself.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "attention_set.h"
+#include "dense.h"
+#include "streamindex_prompt.h"
+#include "wave_ops.h"
+
+namespace si {
+
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kColumns = 32 * kWaves;   // of a workgroup
+constexpr int kRows = 64;               // of a tile
+constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a tile beyond which the reference is raised
+
+struct Call {
+    const __bf16* q;
+    const __bf16* K;
+    const __bf16* V;
+    Packed queries, rows;
+    const int32_t* first;
+    __bf16* out;
+    float* lse;
+    float scale_log2e;
+    int H, H_kv, G, m, mask_mode, n_win;
+    int slots;  // of 256 columns, of all sequences
+};
+
+__device__ __forceinline__ int uniform_max(int x) { return __builtin_amdgcn_readfirstlane(wave_max(x)); }
+__device__ __forceinline__ int uniform_min(int x) { return -__builtin_amdgcn_readfirstlane(wave_max(-x)); }
+
+// Orders the lanes of a wave's LDS accesses for the compiler; the hardware keeps a wave's LDS instructions in order.
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+// Starts a wave's loads of a tile, from the `bytes` bytes at k and at v, each lane's 16 bytes i from offset[i] on: into LDS at `to` + 1024 i the
+// keys, `apart` behind them the values.  What lies at or past `bytes` is not read and lands as zeros.
+template <int LOADS>
+__device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v, int bytes, const int (&offset)[LOADS], unsigned char* to, int apart) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __attribute__((address_space(3))) void lds_void;
+    const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(k), 0, bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(v), 0, bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(to + apart + i * 1024), 16, offset[i], 0, 0, 0);
+    }
+#else
+    (void)k; (void)v; (void)bytes; (void)offset; (void)to; (void)apart;
+#endif
+}
+
+template <int D>
+constexpr int lds_bytes() { return 4 * kRows * D * 2 + kWaves * 16 * 32 * 4; }  // two tiles of keys and values; weights of 16 rows a wave
+
+// Grid: (slots of columns, the last ones first) x heads of keys and values, heads next to each other so that with 8 of them each has an XCD.  A sequence's
+// slots begin at (its first packed column) / 256 + (its number): slots enough for any lengths, with no sum over the sequences before.
+template <int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+void prompt_attention_kernel(Call c) {
+    constexpr int KS = D / 16;      // steps along d of the first product
+    constexpr int DB = D / 32;      // blocks of 32 rows of O^T
+    constexpr int kRowBytes = D * 2;
+    constexpr int kPieces = D / 8;  // 16-byte pieces of a row
+    constexpr int kTileBytes = kRows * kRowBytes;
+    constexpr int kLoads = kTileBytes / 1024 / kWaves;  // of a wave, of a tile's keys or values
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int col = lane & 31, half = lane >> 5;
+    const int hk = blockIdx.x % c.H_kv;
+    const int u = c.slots - 1 - blockIdx.x / c.H_kv;
+
+    auto slot_of = [&](int b) { return max(c.queries.at(b), static_cast<int64_t>(0)) * c.G / kColumns + b; };
+    const int b = last_not_above(c.queries.B, u, slot_of);
+    int q_first, q_last, k_first, k_last;
+    c.queries.rows(b, q_first, q_last);
+    c.rows.rows(b, k_first, k_last);
+    const int n_columns = (q_last - q_first) * c.G;
+    const int64_t r0 = (u - slot_of(b)) * kColumns;
+    if (r0 < 0 || r0 >= n_columns) return;
+    const int held = k_last - k_first;
+    const int64_t first = c.first ? c.first[b] : 0;
+
+    // what this lane's column sees
+    const int column = min(static_cast<int>(r0) + wave * 32 + col, n_columns - 1);  // columns that there are not repeat the last one
+    const int query = column / c.G;
+    const int legal = c.n_win > 0 ? legal_rows(first + query, held, c.m, c.mask_mode) : 0;
+    const int from = max(0, legal - c.n_win);
+    // what all columns of the wave see, and any; then any of the workgroup
+    const int all_from = uniform_max(from), all_to = uniform_min(legal);
+    const int any_from = uniform_min(from), any_to = uniform_max(legal);
+    const int last_query = (min(static_cast<int>(r0) + kColumns, n_columns) - 1) / c.G;
+    const int end = c.n_win > 0 ? legal_rows(first + last_query, held, c.m, c.mask_mode) : 0;
+    const int begin = max(0, legal_rows(first + static_cast<int>(r0) / c.G, held, c.m, c.mask_mode) - c.n_win) / kRows * kRows;
+    const int64_t q_row = static_cast<int64_t>(q_first + query) * c.H + hk * c.G + column % c.G;
+
+    // ---- a tile's keys and values, by 1 KiB pieces of LDS; rows at or past the last one that anybody sees land as zeros
+    const int stride = c.H_kv * kRowBytes;
+    int lane_offset[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int unit = (wave * kLoads + i) * 64 + lane, r = unit / kPieces;
+        lane_offset[i] = r * stride + ((unit % kPieces) ^ row_swizzle<D>(r)) * 16;
+    }
+    auto request = [&](int s0, int buffer) {
+        const int n = min(kRows, end - s0);
+        const int bytes = (n - 1) * stride + kRowBytes;
+        const int64_t at = (static_cast<int64_t>(k_first + s0) * c.H_kv + hk) * D;
+        request_pieces<kLoads>(c.K + at, c.V + at, bytes, lane_offset, lds + buffer * 2 * kTileBytes + wave * kLoads * 1024, kTileBytes);
+    };
+    if (begin < end) request(begin, 0);
+
+    // queries: lane has column col, d = 16 ks + 8 half .. + 7.  A negative scale goes into the query (exact), a scale of 0 makes zeros of it.
+    float to_log2 = __builtin_fabsf(c.scale_log2e);
+    bf16x8 qf[KS];
+    {
+        const uintx4* const src = reinterpret_cast<const uintx4*>(c.q + q_row * D);
+        const unsigned sign = c.scale_log2e < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, src[2 * ks + half] ^ sign);
+        if (to_log2 == 0.0f) {
+            to_log2 = 1.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) qf[ks][j] = static_cast<__bf16>(static_cast<float>(qf[ks][j]) * 0.0f);
+        }
+    }
+    int ka[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ka[ks] = tile_slot<D>(col, 2 * ks + half) * 16;
+    // transposing reads: source lane s of a group of 16 points at 4 consecutive d of row 4 half + s / 4 (+ 8, + 16 ..), at d = 32 db + 16 (group % 2) + 4 (s % 4)
+    int va[DB][2];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int r = 8 * w + 4 * half + ((lane & 15) >> 2);
+            const int d = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+            va[db][w] = kTileBytes + tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
+        }
+
+    const floatx16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    floatx16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = zero16;
+    float m_ref = -__builtin_huge_valf(), l_sum = 0.0f;
+
+    int buffer = 0;
+    for (int s0 = begin; s0 < end; s0 += kRows, buffer ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of the tile is there
+        __syncthreads();
+        if (s0 + kRows < end) request(s0 + kRows, buffer ^ 1);
+        if (s0 >= any_to || s0 + kRows <= any_from) continue;
+        const unsigned char* const tile = lds + buffer * 2 * kTileBytes;
+        const bool masked = s0 < all_from || s0 + kRows > all_to;
+
+        // register j of block i: row 32 i + 8 (j / 4) + 4 half + j % 4
+        floatx16 x[2] = {zero16, zero16};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + ka[ks] + i * 32 * kRowBytes);
+                x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], x[i], 0, 0, 0);
+            }
+        bool odd_values = false;
+        if (masked) {
+            float low = -__builtin_huge_valf();
+            asm volatile("" : "+v"(low));
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int s = s0 + 32 * i + 8 * (j >> 2) + 4 * half + (j & 3);
+                    if (s < from || s >= legal) x[i][j] = low;
+                }
+            // values that are not finite, of rows that some column sees and another may not
+            bool odd = false;
+#pragma unroll 4
+            for (int j = 0; j < kTileBytes / 1024; ++j) {
+                const uintx4 v = *reinterpret_cast<const uintx4*>(tile + kTileBytes + (j * 64 + lane) * 16);
+                odd |= any_not_finite(v);
+            }
+            odd_values = __ballot(odd) != 0ull;
+        }
+        float p[32], sum;
+        auto exponentials = [&]() {
+            const float shift = m_ref == -__builtin_huge_valf() ? 0.0f : -m_ref;
+            sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 4][j & 15], to_log2, shift));
+                sum += p[j];
+            }
+        };
+        exponentials();
+        const bool raise = !(sum <= kMostWeight) || m_ref == -__builtin_huge_valf();
+        unsigned long long over = __ballot(raise);
+        if (over != 0ull) {
+            over |= over >> 32;  // bit i: column i, in either half
+            float highest = x[0][0];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) highest = fmaxf(highest, x[j >> 4][j & 15]);
+            highest *= to_log2;
+            highest = fmaxf(highest, other_half(highest));
+            const float m_new = (over >> col) & 1 ? fmaxf(highest, m_ref) : m_ref;
+            const float alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+            l_sum *= alpha;
+            m_ref = m_new;
+            exponentials();
+        }
+        l_sum += sum;
+        // contraction index e of step s <-> tile row 16 s + 8 (e / 4) + 4 half + e % 4 on both operands
+        auto weights_of = [&](int s) {
+            bf16x8 pf;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x2 two = __builtin_convertvector(floatx2{p[8 * s + 2 * j], p[8 * s + 2 * j + 1]}, bf16x2);
+                pf[2 * j] = two[0];
+                pf[2 * j + 1] = two[1];
+            }
+            return pf;
+        };
+        auto values_of = [&](int s, int db) {
+            typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+            const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(tile + va[db][0] + s * 16 * kRowBytes));
+            const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(tile + va[db][1] + s * 16 * kRowBytes));
+            return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        };
+        if (!odd_values) {
+#pragma unroll
+            for (int s = 0; s < kRows / 16; ++s) {
+                const bf16x8 pf = weights_of(s);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values_of(s, db), pf, acc[db], 0, 0, 0);
+            }
+        } else {
+            // values that are not finite by themselves, row by row: 0 times a NaN must not enter a column that does not see it
+            float* const weights = reinterpret_cast<float*>(lds + 4 * kTileBytes) + wave * (16 * 32);
+#pragma unroll
+            for (int s = 0; s < kRows / 16; ++s) {
+                const bf16x8 pf = weights_of(s);
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_or_zero(values_of(s, db)), pf, acc[db], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) weights[(8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = p[8 * s + j];
+                wave_order();
+#pragma unroll 1
+                for (int r = 16 * s; r < 16 * s + 16; ++r) {
+                    const float w = weights[(r & 15) * 32 + col];
+                    const bool sees = s0 + r >= from && s0 + r < legal;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int a = 0; a < 4; ++a)
+                            add_not_finite(acc[db], 4 * a, *reinterpret_cast<const bf16x4*>(tile + kTileBytes + tile_slot<D>(r, 4 * db + a) * 16 + half * 8),
+                                           w, sees);
+                }
+                wave_order();
+            }
+        }
+    }
+
+    // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4
+    const float l = l_sum + other_half(l_sum);
+    if (static_cast<int>(r0) + wave * 32 + col >= n_columns) return;
+    const bool none = m_ref == -__builtin_huge_valf() && l == 0.0f;
+    const float inv = none ? 0.0f : 1.0f / l;
+    __bf16* const o = c.out + q_row * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            bf16x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = static_cast<__bf16>(acc[db][4 * a + e] * inv);
+            *reinterpret_cast<bf16x4*>(o + 32 * db + 8 * a + 4 * half) = v;
+        }
+    if (c.lse && half == 0) c.lse[q_row] = none ? -__builtin_huge_valf() : log_of(m_ref, l);
+}
+
+template <int D>
+hipError_t launch(const Call& c, hipStream_t stream) {
+    static std::atomic<size_t> allowed[64];
+    const hipError_t e = allow_lds(prompt_attention_kernel<D>, lds_bytes<D>(), allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((prompt_attention_kernel<D>), dim3(static_cast<unsigned>(c.slots) * c.H_kv), dim3(kThreads), lds_bytes<D>(), stream, c);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+}  // namespace si
+
+using namespace si;
+
+extern "C" {
+
+si_status si_prompt_attention(const void* q, const void* K, const void* V, const si_packed_dims* dims, const int32_t* q_offsets,
+                              const int32_t* k_offsets, const int32_t* first, int32_t m, si_mask_mode mask_mode, int32_t n_win, float scale,
+                              void* out, float* lse, void* stream) {
+    if (!q || !K || !dims || !out) return SI_ERR_INVALID_ARG;
+    const si_packed_dims& d = *dims;
+    if (d.B < 1 || d.N_q < 1 || d.N_k < 1 || d.H < 1 || d.H_kv < 1 || d.D < 1 || d.H % d.H_kv != 0 || m < 1 || n_win < 0) return SI_ERR_INVALID_ARG;
+    if (mask_mode != SI_MASK_NONE && mask_mode != SI_MASK_CAUSAL_BLOCK) return SI_ERR_INVALID_ARG;
+    if ((!q_offsets && d.N_q % d.B != 0) || (!k_offsets && d.N_k % d.B != 0)) return SI_ERR_INVALID_ARG;
+    const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+    if (!std::isfinite(scale) || !std::isfinite(scale_log2e)) return SI_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return SI_ERR_INVALID_ARG;
+    if (!aligned4(q_offsets) || !aligned4(k_offsets) || !aligned4(first) || !aligned4(lse)) return SI_ERR_INVALID_ARG;
+    if ((d.D != 64 && d.D != 128) || d.H > 1024 || d.N_q > (1 << 30) || d.N_k > (1 << 30) || d.B > (1 << 20) ||
+        (static_cast<int64_t>(d.N_q) + d.B) * d.H >= (1 << 30))
+        return SI_ERR_UNSUPPORTED_SHAPE;
+    const int G = d.H / d.H_kv;
+    const int slots = static_cast<int>(static_cast<int64_t>(d.N_q) * G / kColumns + d.B);
+    if (static_cast<int64_t>(slots) * d.H_kv >= (1 << 23)) return SI_ERR_UNSUPPORTED_SHAPE;  // a launch has fewer than 2^32 threads
+    const Call c = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(K), static_cast<const __bf16*>(V ? V : K),
+                    {q_offsets, d.B, d.N_q}, {k_offsets, d.B, d.N_k}, first, static_cast<__bf16*>(out), lse, scale_log2e,
+                    d.H, d.H_kv, G, m, mask_mode, n_win, slots};
+    return report(d.D == 128 ? launch<128>(c, static_cast<hipStream_t>(stream)) : launch<64>(c, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
