@@ -54,11 +54,12 @@ __device__ __forceinline__ int last_not_above(int B, int64_t u, Slot slot) {
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Legal rows of position t among `rows` (Section 4.2), none where t < 0.
-__device__ __forceinline__ int legal_rows(int64_t t, int rows, int m, int mask_mode) {
+// Legal rows of position t = first + i among `rows` (Section 4.2), none where t < 0.  t + 1 is below 2^32, as first < 2^31 and i < 2^30.
+__device__ __forceinline__ int legal_rows(int first, int i, int rows, int m, int mask_mode) {
     if (mask_mode == SI_MASK_NONE) return rows;
-    if (t < 0) return 0;
-    return t + 1 < static_cast<int64_t>(m) * rows ? static_cast<int>((t + 1) / m) : rows;
+    if (static_cast<int64_t>(first) + i < 0) return 0;
+    const uint32_t n = static_cast<uint32_t>(first) + static_cast<uint32_t>(i) + 1u;
+    return static_cast<int>(min(m == 1 ? n : n / static_cast<uint32_t>(m), static_cast<uint32_t>(rows)));
 }
 
 // 2^e of a scale byte.

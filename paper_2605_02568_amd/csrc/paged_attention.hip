@@ -63,8 +63,8 @@ __device__ __forceinline__ int held_rows(const Call& c, int b) {
 }
 __device__ __forceinline__ Rows rows_of(const Call& c, int b) {
     const int held = held_rows(c, b);
-    const int64_t first = c.first ? c.first[b] : 0;
-    return {max(0, legal_rows(first, held, c.m, c.mask_mode) - c.n_win), c.n_win > 0 ? legal_rows(first + c.S - 1, held, c.m, c.mask_mode) : 0};
+    const int first = c.first ? c.first[b] : 0;
+    return {max(0, legal_rows(first, 0, held, c.m, c.mask_mode) - c.n_win), c.n_win > 0 ? legal_rows(first, c.S - 1, held, c.m, c.mask_mode) : 0};
 }
 
 // The chunk of a workgroup, or the chunks of a sequence.
@@ -154,20 +154,20 @@ void paged_attention_kernel(Call c) {
     // what the columns see
     const int R = c.S * c.G;
     const int held = held_rows(c, b);
-    const int64_t first = c.first ? c.first[b] : 0;
+    const int first = c.first ? c.first[b] : 0;
     const Rows rows = rows_of(c, b);
     int legal[NB], from[NB], q_row[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r = min((block * NB + nb) * 16 + col, R - 1);  // columns that there are not repeat the last one
         const int i = r / c.G;
-        legal[nb] = legal_rows(first + i, held, c.m, c.mask_mode);
+        legal[nb] = legal_rows(first, i, held, c.m, c.mask_mode);
         from[nb] = max(0, legal[nb] - c.n_win);
         q_row[nb] = (b * c.S + i) * c.H + hk * c.G + r % c.G;
     }
     // rows that all positions see: from the last one's first to the first one's last
-    const int all_from = max(0, legal_rows(first + c.S - 1, held, c.m, c.mask_mode) - c.n_win);
-    const int all_to = legal_rows(first, held, c.m, c.mask_mode);
+    const int all_from = max(0, legal_rows(first, c.S - 1, held, c.m, c.mask_mode) - c.n_win);
+    const int all_to = legal_rows(first, 0, held, c.m, c.mask_mode);
 
     // queries: lane has column col; step ks of the contraction is d = 32 ks + 8 quarter .. + 7 in 16 bits, and in 8, where a lane loads 16 codes of a row,
     // d = 64 (ks / 2) + 16 quarter + 8 (ks % 2) .. + 7.  A negative scale goes into the query (exact), a scale of 0 makes zeros of it.

@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "attention_set.h"
 #include "dense.h"
@@ -101,19 +102,19 @@ void prompt_attention_kernel(Call c) {
     const int64_t r0 = (u - slot_of(b)) * kColumns;
     if (r0 < 0 || r0 >= n_columns) return;
     const int held = k_last - k_first;
-    const int64_t first = c.first ? c.first[b] : 0;
+    const int first = c.first ? c.first[b] : 0;
 
     // what this lane's column sees
     const int column = min(static_cast<int>(r0) + wave * 32 + col, n_columns - 1);  // columns that there are not repeat the last one
     const int query = column / c.G;
-    const int legal = c.n_win > 0 ? legal_rows(first + query, held, c.m, c.mask_mode) : 0;
+    const int legal = c.n_win > 0 ? legal_rows(first, query, held, c.m, c.mask_mode) : 0;
     const int from = max(0, legal - c.n_win);
     // what all columns of the wave see, and any; then any of the workgroup
     const int all_from = uniform_max(from), all_to = uniform_min(legal);
     const int any_from = uniform_min(from), any_to = uniform_max(legal);
     const int last_query = (min(static_cast<int>(r0) + kColumns, n_columns) - 1) / c.G;
-    const int end = c.n_win > 0 ? legal_rows(first + last_query, held, c.m, c.mask_mode) : 0;
-    const int begin = max(0, legal_rows(first + static_cast<int>(r0) / c.G, held, c.m, c.mask_mode) - c.n_win) / kRows * kRows;
+    const int end = c.n_win > 0 ? legal_rows(first, last_query, held, c.m, c.mask_mode) : 0;
+    const int begin = max(0, legal_rows(first, static_cast<int>(r0) / c.G, held, c.m, c.mask_mode) - c.n_win) / kRows * kRows;
     const int64_t q_row = static_cast<int64_t>(q_first + query) * c.H + hk * c.G + column % c.G;
 
     // ---- a tile's keys and values, by 1 KiB pieces of LDS; rows at or past the last one that anybody sees land as zeros
@@ -166,17 +167,11 @@ void prompt_attention_kernel(Call c) {
     floatx16 acc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db] = zero16;
-    float m_ref = -__builtin_huge_valf(), l_sum = 0.0f;
+    float shift = __builtin_huge_valf(), l_sum = 0.0f;  // minus the reference; no reference yet makes every weight too large or NaN
 
-    int buffer = 0;
-    for (int s0 = begin; s0 < end; s0 += kRows, buffer ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of the tile is there
-        __syncthreads();
-        if (s0 + kRows < end) request(s0 + kRows, buffer ^ 1);
-        if (s0 >= any_to || s0 + kRows <= any_from) continue;
-        const unsigned char* const tile = lds + buffer * 2 * kTileBytes;
-        const bool masked = s0 < all_from || s0 + kRows > all_to;
-
+    // One tile for this wave.  MASKED: some column does not see some row of it.
+    auto take = [&](int s0, const unsigned char* tile, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
         // register j of block i: row 32 i + 8 (j / 4) + 4 half + j % 4
         floatx16 x[2] = {zero16, zero16};
 #pragma unroll
@@ -187,38 +182,32 @@ void prompt_attention_kernel(Call c) {
                 x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], x[i], 0, 0, 0);
             }
         bool odd_values = false;
-        if (masked) {
-            float low = -__builtin_huge_valf();
-            asm volatile("" : "+v"(low));
+        if constexpr (MASKED) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int s = s0 + 32 * i + 8 * (j >> 2) + 4 * half + (j & 3);
-                    if (s < from || s >= legal) x[i][j] = low;
+                    if (s < from || s >= legal) x[i][j] = -__builtin_huge_valf();
                 }
             // values that are not finite, of rows that some column sees and another may not
             bool odd = false;
 #pragma unroll 4
-            for (int j = 0; j < kTileBytes / 1024; ++j) {
-                const uintx4 v = *reinterpret_cast<const uintx4*>(tile + kTileBytes + (j * 64 + lane) * 16);
-                odd |= any_not_finite(v);
-            }
+            for (int j = 0; j < kTileBytes / 1024; ++j)
+                odd |= any_not_finite(*reinterpret_cast<const uintx4*>(tile + kTileBytes + (j * 64 + lane) * 16));
             odd_values = __ballot(odd) != 0ull;
         }
         float p[32], sum;
-        auto exponentials = [&]() {
-            const float shift = m_ref == -__builtin_huge_valf() ? 0.0f : -m_ref;
+        auto exponentials = [&](float by) {
             sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 4][j & 15], to_log2, shift));
+                p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 4][j & 15], to_log2, by));
                 sum += p[j];
             }
         };
-        exponentials();
-        const bool raise = !(sum <= kMostWeight) || m_ref == -__builtin_huge_valf();
-        unsigned long long over = __ballot(raise);
+        exponentials(shift);
+        unsigned long long over = __ballot(!(sum <= kMostWeight));
         if (over != 0ull) {
             over |= over >> 32;  // bit i: column i, in either half
             float highest = x[0][0];
@@ -226,13 +215,13 @@ void prompt_attention_kernel(Call c) {
             for (int j = 1; j < 32; ++j) highest = fmaxf(highest, x[j >> 4][j & 15]);
             highest *= to_log2;
             highest = fmaxf(highest, other_half(highest));
-            const float m_new = (over >> col) & 1 ? fmaxf(highest, m_ref) : m_ref;
-            const float alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+            const float raised = (over >> col) & 1 ? fminf(-highest, shift) : shift;
+            const float alpha = raised == shift ? 1.0f : __builtin_amdgcn_exp2f(raised - shift);
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] *= alpha;
             l_sum *= alpha;
-            m_ref = m_new;
-            exponentials();
+            shift = raised;
+            exponentials(shift == __builtin_huge_valf() ? 0.0f : shift);  // a column that has seen nothing yet
         }
         l_sum += sum;
         // contraction index e of step s <-> tile row 16 s + 8 (e / 4) + 4 half + e % 4 on both operands
@@ -252,22 +241,20 @@ void prompt_attention_kernel(Call c) {
             const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(tile + va[db][1] + s * 16 * kRowBytes));
             return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
         };
-        if (!odd_values) {
 #pragma unroll
-            for (int s = 0; s < kRows / 16; ++s) {
-                const bf16x8 pf = weights_of(s);
+        for (int s = 0; s < kRows / 16; ++s) {
+            const bf16x8 pf = weights_of(s);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values_of(s, db), pf, acc[db], 0, 0, 0);
+            for (int db = 0; db < DB; ++db) {
+                const bf16x8 vf = values_of(s, db);
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(MASKED ? finite_or_zero(vf) : vf, pf, acc[db], 0, 0, 0);
             }
-        } else {
+        }
+        if (MASKED && odd_values) {
             // values that are not finite by themselves, row by row: 0 times a NaN must not enter a column that does not see it
             float* const weights = reinterpret_cast<float*>(lds + 4 * kTileBytes) + wave * (16 * 32);
 #pragma unroll
             for (int s = 0; s < kRows / 16; ++s) {
-                const bf16x8 pf = weights_of(s);
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_or_zero(values_of(s, db)), pf, acc[db], 0, 0, 0);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) weights[(8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = p[8 * s + j];
                 wave_order();
@@ -285,7 +272,35 @@ void prompt_attention_kernel(Call c) {
                 wave_order();
             }
         }
+    };
+
+    // The tile at s0 is there for all waves, and the one before is done with; the next is asked for.
+    int buffer = 0;
+    auto arrive = [&](int s0) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of the tile
+        __syncthreads();
+        if (s0 + kRows < end) request(s0 + kRows, buffer ^ 1);
+        const unsigned char* const tile = lds + buffer * 2 * kTileBytes;
+        buffer ^= 1;
+        return tile;
+    };
+    // Every wave meets every tile's barrier; tiles that all its columns see whole have a loop of their own.
+    const int whole_from = (all_from + kRows - 1) / kRows * kRows, whole_to = all_to / kRows * kRows;
+    int s0 = begin;
+    while (s0 < end) {
+        if (s0 < whole_from || s0 >= whole_to) {
+            const unsigned char* const tile = arrive(s0);
+            if (s0 < any_to && s0 + kRows > any_from) take(s0, tile, std::true_type{});
+            s0 += kRows;
+        } else {
+#pragma unroll 1
+            for (; s0 < whole_to; s0 += kRows) {
+                const unsigned char* const tile = arrive(s0);
+                take(s0, tile, std::false_type{});
+            }
+        }
     }
+    const float m_ref = -shift;
 
     // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4
     const float l = l_sum + other_half(l_sum);
