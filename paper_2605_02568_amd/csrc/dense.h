@@ -77,13 +77,15 @@ __device__ __forceinline__ void codes_to_bf16(uintx4 codes, float power, uintx4 
         }
 }
 
-// bf16 values that are not finite, among 8; and the 8 with zeros in their place.
-__device__ __forceinline__ bool any_not_finite(uintx4 v) {
-    bool odd = false;
+// Not 0 where one of 8 bf16 values is not finite: an exponent of ones carries into the bit of the sign.
+__device__ __forceinline__ unsigned not_finite(bf16x8 x) {
+    const uintx4 v = __builtin_bit_cast(uintx4, x);
+    unsigned found = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) odd |= (v[w] & 0x7F80u) == 0x7F80u || (v[w] & 0x7F800000u) == 0x7F800000u;
-    return odd;
+    for (int w = 0; w < 4; ++w) found |= (v[w] & 0x7F807F80u) + 0x00800080u;
+    return found & 0x80008000u;
 }
+// The 8 with zeros in their place.
 __device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 x) {
     uintx4 v = __builtin_bit_cast(uintx4, x);
 #pragma unroll

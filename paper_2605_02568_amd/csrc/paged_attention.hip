@@ -321,7 +321,7 @@ void paged_attention_kernel(Call c) {
 #pragma unroll
             for (int j = 0; j < kTileKeys * kRowBytes / 1024; ++j) {
                 const uintx4 v = *reinterpret_cast<const uintx4*>(tile_lds + (j * 64 + lane) * 16);
-                odd |= any_not_finite(v);
+                odd |= not_finite(__builtin_bit_cast(bf16x8, v)) != 0;
             }
             odd_values = __ballot(odd) != 0ull;
         }

@@ -32,7 +32,9 @@ constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kColumns = 32 * kWaves;   // of a workgroup
 constexpr int kRows = 64;               // of a tile
-constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a tile beyond which the reference is raised
+constexpr int kSlots = 3;               // tiles in LDS: two in use, one on its way
+constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a block beyond which the reference is raised,
+constexpr float kMostShift = 8.0f;      // or where the maximum is known, its distance from the reference in log2 units
 
 struct Call {
     const __bf16* q;
@@ -54,25 +56,25 @@ __device__ __forceinline__ int uniform_min(int x) { return -__builtin_amdgcn_rea
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 // Starts a wave's loads of a tile, from the `bytes` bytes at k and at v, each lane's 16 bytes i from offset[i] on: into LDS at `to` + 1024 i the
-// keys, `apart` behind them the values.  What lies at or past `bytes` is not read and lands as zeros.
+// keys, `apart` behind them the values (none where v is NULL).  What lies at or past `bytes` is not read and lands as zeros.
 template <int LOADS>
 __device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v, int bytes, const int (&offset)[LOADS], unsigned char* to, int apart) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef __attribute__((address_space(3))) void lds_void;
     const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(k), 0, bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, 0);
+    if (!v) return;
     const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(v), 0, bytes, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(to + apart + i * 1024), 16, offset[i], 0, 0, 0);
-    }
+    for (int i = 0; i < LOADS; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(to + apart + i * 1024), 16, offset[i], 0, 0, 0);
 #else
     (void)k; (void)v; (void)bytes; (void)offset; (void)to; (void)apart;
 #endif
 }
 
 template <int D>
-constexpr int lds_bytes() { return 4 * kRows * D * 2 + kWaves * 16 * 32 * 4; }  // two tiles of keys and values; weights of 16 rows a wave
+constexpr int lds_bytes() { return kSlots * 2 * kRows * D * 2 + kWaves * 32 * 32 * 4; }  // tiles of keys and values; weights of a block a wave
 
 // Grid: (slots of columns, the last ones first) x heads of keys and values, heads next to each other so that with 8 of them each has an XCD.  A sequence's
 // slots begin at (its first packed column) / 256 + (its number): slots enough for any lengths, with no sum over the sequences before.
@@ -129,7 +131,7 @@ void prompt_attention_kernel(Call c) {
         const int n = min(kRows, end - s0);
         const int bytes = (n - 1) * stride + kRowBytes;
         const int64_t at = (static_cast<int64_t>(k_first + s0) * c.H_kv + hk) * D;
-        request_pieces<kLoads>(c.K + at, c.V + at, bytes, lane_offset, lds + buffer * 2 * kTileBytes + wave * kLoads * 1024, kTileBytes);
+        request_pieces<kLoads>(c.K + at, c.V ? c.V + at : nullptr, bytes, lane_offset, lds + buffer * 2 * kTileBytes + wave * kLoads * 1024, kTileBytes);
     };
     if (begin < end) request(begin, 0);
 
@@ -153,6 +155,7 @@ void prompt_attention_kernel(Call c) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) ka[ks] = tile_slot<D>(col, 2 * ks + half) * 16;
     // transposing reads: source lane s of a group of 16 points at 4 consecutive d of row 4 half + s / 4 (+ 8, + 16 ..), at d = 32 db + 16 (group % 2) + 4 (s % 4)
+    const int apart = c.V ? kTileBytes : 0;  // values behind the keys, or the keys' rows
     int va[DB][2];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -160,7 +163,7 @@ void prompt_attention_kernel(Call c) {
         for (int w = 0; w < 2; ++w) {
             const int r = 8 * w + 4 * half + ((lane & 15) >> 2);
             const int d = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-            va[db][w] = kTileBytes + tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
+            va[db][w] = apart + tile_slot<D>(r, d / 8) * 16 + ((d % 8) / 4) * 8;
         }
 
     const floatx16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -169,135 +172,176 @@ void prompt_attention_kernel(Call c) {
     for (int db = 0; db < DB; ++db) acc[db] = zero16;
     float shift = __builtin_huge_valf(), l_sum = 0.0f;  // minus the reference; no reference yet makes every weight too large or NaN
 
-    // One tile for this wave.  MASKED: some column does not see some row of it.
-    auto take = [&](int s0, const unsigned char* tile, auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        // register j of block i: row 32 i + 8 (j / 4) + 4 half + j % 4
-        floatx16 x[2] = {zero16, zero16};
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + ka[ks] + i * 32 * kRowBytes);
-                x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], x[i], 0, 0, 0);
-            }
-        bool odd_values = false;
-        if constexpr (MASKED) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int s = s0 + 32 * i + 8 * (j >> 2) + 4 * half + (j & 3);
-                    if (s < from || s >= legal) x[i][j] = -__builtin_huge_valf();
-                }
-            // values that are not finite, of rows that some column sees and another may not
-            bool odd = false;
-#pragma unroll 4
-            for (int j = 0; j < kTileBytes / 1024; ++j)
-                odd |= any_not_finite(*reinterpret_cast<const uintx4*>(tile + kTileBytes + (j * 64 + lane) * 16));
-            odd_values = __ballot(odd) != 0ull;
-        }
-        float p[32], sum;
-        auto exponentials = [&](float by) {
-            sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 4][j & 15], to_log2, by));
-                sum += p[j];
-            }
-        };
-        exponentials(shift);
-        unsigned long long over = __ballot(!(sum <= kMostWeight));
-        if (over != 0ull) {
-            over |= over >> 32;  // bit i: column i, in either half
-            float highest = x[0][0];
-#pragma unroll
-            for (int j = 1; j < 32; ++j) highest = fmaxf(highest, x[j >> 4][j & 15]);
-            highest *= to_log2;
-            highest = fmaxf(highest, other_half(highest));
-            const float raised = (over >> col) & 1 ? fminf(-highest, shift) : shift;
-            const float alpha = raised == shift ? 1.0f : __builtin_amdgcn_exp2f(raised - shift);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] *= alpha;
-            l_sum *= alpha;
-            shift = raised;
-            exponentials(shift == __builtin_huge_valf() ? 0.0f : shift);  // a column that has seen nothing yet
-        }
-        l_sum += sum;
-        // contraction index e of step s <-> tile row 16 s + 8 (e / 4) + 4 half + e % 4 on both operands
-        auto weights_of = [&](int s) {
-            bf16x8 pf;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x2 two = __builtin_convertvector(floatx2{p[8 * s + 2 * j], p[8 * s + 2 * j + 1]}, bf16x2);
-                pf[2 * j] = two[0];
-                pf[2 * j + 1] = two[1];
-            }
-            return pf;
-        };
-        auto values_of = [&](int s, int db) {
-            typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-            const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(tile + va[db][0] + s * 16 * kRowBytes));
-            const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(tile + va[db][1] + s * 16 * kRowBytes));
-            return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-        };
-#pragma unroll
-        for (int s = 0; s < kRows / 16; ++s) {
-            const bf16x8 pf = weights_of(s);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const bf16x8 vf = values_of(s, db);
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(MASKED ? finite_or_zero(vf) : vf, pf, acc[db], 0, 0, 0);
-            }
-        }
-        if (MASKED && odd_values) {
-            // values that are not finite by themselves, row by row: 0 times a NaN must not enter a column that does not see it
-            float* const weights = reinterpret_cast<float*>(lds + 4 * kTileBytes) + wave * (16 * 32);
-#pragma unroll
-            for (int s = 0; s < kRows / 16; ++s) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) weights[(8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = p[8 * s + j];
-                wave_order();
-#pragma unroll 1
-                for (int r = 16 * s; r < 16 * s + 16; ++r) {
-                    const float w = weights[(r & 15) * 32 + col];
-                    const bool sees = s0 + r >= from && s0 + r < legal;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-#pragma unroll
-                        for (int a = 0; a < 4; ++a)
-                            add_not_finite(acc[db], 4 * a, *reinterpret_cast<const bf16x4*>(tile + kTileBytes + tile_slot<D>(r, 4 * db + a) * 16 + half * 8),
-                                           w, sees);
-                }
-                wave_order();
-            }
-        }
+    auto read_values = [&](const unsigned char* keys, int i) {  // 16 rows of 32 d, by the place of their block's keys; i = s * DB + db
+        typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(keys + va[i % DB][0] + i / DB * 16 * kRowBytes));
+        const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(keys + va[i % DB][1] + i / DB * 16 * kRowBytes));
+        return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
     };
 
-    // The tile at s0 is there for all waves, and the one before is done with; the next is asked for.
-    int buffer = 0;
+    floatx16 x;  // scores of a block of 32 rows: register j has row 8 (j / 4) + 4 half + j % 4
+    auto score = [&](const unsigned char* keys) {
+        x = zero16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(keys + ka[ks]), qf[ks], x, 0, 0, 0);
+    };
+    auto two_weights = [&](bf16x8 (&pf)[2], int j, float p0, float p1) {
+        const bf16x2 two = __builtin_convertvector(floatx2{p0, p1}, bf16x2);
+        pf[j / 8][j % 8] = two[0];
+        pf[j / 8][j % 8 + 1] = two[1];
+    };
+    // The reference of the columns in `over` (bit i: column i) becomes at least `highest`, in log2 units.
+    auto raise = [&](unsigned over, float highest) {
+        highest = fmaxf(highest, other_half(highest));
+        const float raised = (over >> col) & 1 ? fminf(-highest, shift) : shift;
+        const float alpha = raised == shift ? 1.0f : __builtin_amdgcn_exp2f(raised - shift);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+        l_sum *= alpha;
+        shift = raised;
+    };
+
+    // A block of which some column does not see some row.
+    auto take_masked = [&](int s0, const unsigned char* block) {
+        score(block);
+        float highest = -__builtin_huge_valf();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int s = s0 + 8 * (j >> 2) + 4 * half + (j & 3);
+            if (s < from || s >= legal) x[j] = -__builtin_huge_valf();
+            highest = fmaxf(highest, x[j]);
+        }
+        highest *= to_log2;
+        unsigned long long over = __ballot(!(highest + shift <= kMostShift));
+        if (over != 0ull) raise(static_cast<unsigned>(over | (over >> 32)), highest);
+        const float by = shift == __builtin_huge_valf() ? 0.0f : shift;  // a column that has seen nothing yet
+        bf16x8 pf[2];
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to_log2, by));
+            x[j + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], to_log2, by));
+            l_sum += x[j] + x[j + 1];
+            two_weights(pf, j, x[j], x[j + 1]);
+        }
+        bf16x8 vf[2 * DB];
+        unsigned found = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) {
+            vf[i] = read_values(block, i);
+            found |= not_finite(vf[i]);
+        }
+        // values that are not finite go in by themselves, row by row: 0 times a NaN must not enter a column that does not see it
+        const bool odd = __ballot(found != 0) != 0ull;
+        if (odd) {
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) vf[i] = finite_or_zero(vf[i]);
+            float* const weights = reinterpret_cast<float*>(lds + kSlots * 2 * kTileBytes) + wave * (32 * 32);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) weights[(8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = x[j];
+            wave_order();
+#pragma unroll 1
+            for (int r = 0; r < 32; ++r) {
+                const float w = weights[r * 32 + col];
+                const bool sees = s0 + r >= from && s0 + r < legal;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int a = 0; a < 4; ++a)
+                        add_not_finite(acc[db], 4 * a, *reinterpret_cast<const bf16x4*>(block + apart + tile_slot<D>(r, 4 * db + a) * 16 + half * 8), w, sees);
+            }
+            wave_order();
+        }
+        // contraction index e of part i / DB <-> row 16 (i / DB) + 8 (e / 4) + 4 half + e % 4 of the block on both operands
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], pf[i / DB], acc[i % DB], 0, 0, 0);
+    };
+
+    // The tile at s0 is there for all waves, and none uses the slot of the one after it; that is asked for.
+    int slot = 0;
     auto arrive = [&](int s0) {
         __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of the tile
         __syncthreads();
-        if (s0 + kRows < end) request(s0 + kRows, buffer ^ 1);
-        const unsigned char* const tile = lds + buffer * 2 * kTileBytes;
-        buffer ^= 1;
+        const unsigned char* const tile = lds + slot * 2 * kTileBytes;
+        slot = slot == kSlots - 1 ? 0 : slot + 1;
+        if (s0 + kRows < end) request(s0 + kRows, slot);
         return tile;
     };
-    // Every wave meets every tile's barrier; tiles that all its columns see whole have a loop of their own.
+
+    // Tiles that all columns see whole: a pipeline over blocks of 32 rows.  A step has block g's weights from its scores, while the matrix pipe
+    // adds block g - 1's values and makes block g + 1's scores, instruction by instruction: after each product a part of the weights and a read from LDS
+    // for a product half a step later.
+    bf16x8 vf[2 * DB], pf[2];  // values of the block before, and its weights
+    auto step = [&](const unsigned char* block, const unsigned char* after) {
+        constexpr int kProducts = KS + 2 * DB, kEach = 16 / kProducts;
+        static_assert(KS == 2 * DB && kProducts * kEach == 16, "products and weights go together");
+        floatx16 xn = zero16;
+        bf16x8 kf[KS], pn[2];
+        float p[16], sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kProducts; ++n) {
+            if (n < KS) {
+                acc[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n], pf[n / DB], acc[n % DB], 0, 0, 0);
+                kf[n] = *reinterpret_cast<const bf16x8*>(after + ka[n]);
+            } else {
+                xn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n - KS], qf[n - KS], xn, 0, 0, 0);
+                vf[n - KS] = read_values(block, n - KS);
+            }
+#pragma unroll
+            for (int e = n * kEach; e < (n + 1) * kEach; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], to_log2, shift));
+                if (e > 0) sum += p[e - 1];
+                if (e > 1 && e % 2 == 0) two_weights(pn, e - 2, p[e - 2], p[e - 1]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum += p[15];
+        two_weights(pn, 14, p[14], p[15]);
+        unsigned long long over = __ballot(!(sum <= kMostWeight));
+        if (__builtin_expect(over != 0ull, 0)) {
+            score(block);  // again: that costs the few blocks that come here less than keeping the scores costs all others
+            float highest = x[0];
+#pragma unroll
+            for (int j = 1; j < 16; ++j) highest = fmaxf(highest, x[j]);
+            raise(static_cast<unsigned>(over | (over >> 32)), highest * to_log2);
+            sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to_log2, shift)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], to_log2, shift));
+                sum += p0 + p1;
+                two_weights(pn, j, p0, p1);
+            }
+        }
+        l_sum += sum;
+        x = xn;
+        pf[0] = pn[0];
+        pf[1] = pn[1];
+    };
+
+    // Every wave meets every tile's barrier.
     const int whole_from = (all_from + kRows - 1) / kRows * kRows, whole_to = all_to / kRows * kRows;
     int s0 = begin;
     while (s0 < end) {
+        const unsigned char* tile = arrive(s0);
         if (s0 < whole_from || s0 >= whole_to) {
-            const unsigned char* const tile = arrive(s0);
-            if (s0 < any_to && s0 + kRows > any_from) take(s0, tile, std::true_type{});
-            s0 += kRows;
-        } else {
 #pragma unroll 1
-            for (; s0 < whole_to; s0 += kRows) {
-                const unsigned char* const tile = arrive(s0);
-                take(s0, tile, std::false_type{});
+            for (int i = 0; i < kRows; i += 32, s0 += 32)
+                if (s0 < any_to && s0 + 32 > any_from) take_masked(s0, tile + i * kRowBytes);
+        } else {
+            score(tile);
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) vf[i] = __builtin_bit_cast(bf16x8, uintx4{0, 0, 0, 0});
+            pf[0] = pf[1] = vf[0];
+#pragma unroll 1
+            for (;;) {
+                step(tile, tile + 32 * kRowBytes);
+                s0 += kRows;
+                const unsigned char* const next = s0 < whole_to ? arrive(s0) : tile;  // behind the last block the scores are not used
+                step(tile + 32 * kRowBytes, next);
+                if (s0 >= whole_to) break;
+                tile = next;
             }
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], pf[i / DB], acc[i % DB], 0, 0, 0);
         }
     }
     const float m_ref = -shift;
@@ -355,7 +399,7 @@ si_status si_prompt_attention(const void* q, const void* K, const void* V, const
     const int G = d.H / d.H_kv;
     const int slots = static_cast<int>(static_cast<int64_t>(d.N_q) * G / kColumns + d.B);
     if (static_cast<int64_t>(slots) * d.H_kv >= (1 << 23)) return SI_ERR_UNSUPPORTED_SHAPE;  // a launch has fewer than 2^32 threads
-    const Call c = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(K), static_cast<const __bf16*>(V ? V : K),
+    const Call c = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(K), static_cast<const __bf16*>(V),
                     {q_offsets, d.B, d.N_q}, {k_offsets, d.B, d.N_k}, first, static_cast<__bf16*>(out), lse, scale_log2e,
                     d.H, d.H_kv, G, m, mask_mode, n_win, slots};
     return report(d.D == 128 ? launch<128>(c, static_cast<hipStream_t>(stream)) : launch<64>(c, static_cast<hipStream_t>(stream)));
