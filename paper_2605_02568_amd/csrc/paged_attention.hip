@@ -28,9 +28,9 @@ namespace si {
 
 namespace {
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kMinTiles = kWaves;       // of a chunk: one a wave
+constexpr int kMinTiles = 2 * kWaves;   // of a chunk
 constexpr int kWorkgroups = 1024;       // about as many in all
 constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a tile beyond which the reference is raised
 constexpr int kMaxSequences = 1 << 14;
@@ -121,22 +121,100 @@ __device__ __forceinline__ float quarters_sum(float x) {
 // Orders the lanes of a wave's LDS accesses for the compiler; the hardware keeps a wave's LDS instructions in order.
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-template <int D, int NB>
+// LDS of a wave: its tiles on the way, each keys, then values, then in 8 bits the scale bytes of either; and weights of a column block, for rows of
+// values that are not finite.
+template <int D, int BITS>
+struct Tile {
+    static constexpr int kRowBytes = D * BITS / 8;
+    static constexpr int kBytes = kTileKeys * kRowBytes;          // keys, or values
+    static constexpr int kAll = 2 * kBytes + (BITS == 8 ? 256 : 0);
+    static constexpr int kRing = 16384 / (2 * kBytes);            // tiles on the way: 16 KB a wave, 128 KB a compute unit
+    static constexpr int kPieces = kRowBytes / 16;                // of a row
+    static constexpr int kHalfLoads = kBytes / 2048;              // 1 KB loads of 16 rows
+    static constexpr int kLoads = 4 * kHalfLoads + (BITS == 8);   // of a tile
+    static constexpr int kWaveBytes = kRing * kAll + kTileKeys * 16 * 4;
+    // Pieces of a row are swizzled so that lanes served together meet different banks: by the row reads of the first product (a piece of rows 0 .. 3 and 8 .. 11,
+    // or of 8 rows in a row) and by the transposing reads of the second (two pieces of 4 rows; in 8 bits a piece of 8).
+    __device__ static int swizzle(int row) {
+        if constexpr (BITS == 16) return row_swizzle<D>(row);
+        if constexpr (D == 128) return ((row >> 1) & 1) | ((row >> 2) & 2) | (row & 4);
+        return ((row >> 3) & 1) | ((row >> 1) & 2);
+    }
+    __device__ static int place(int row, int piece) { return (row * kPieces + (piece ^ swizzle(row))) * 16; }
+};
+template <int D, int BITS, int NB>
 constexpr int lds_bytes() {
-    constexpr int kTiles = kWaves * kTileKeys * D * 2;          // a tile of values a wave
-    constexpr int kWeights = kWaves * kTileKeys * 16 * 4;       // weights of a column block, for rows of values that are not finite
-    constexpr int kJoin = kWaves * NB * 16 * (D + 2) * 4;       // sums, reference and sum of weights of each wave
-    return kTiles + kWeights > kJoin ? kTiles + kWeights : kJoin;
+    constexpr int kTiles = kWaves * Tile<D, BITS>::kWaveBytes;
+    constexpr int kJoin = kWaves * NB * 16 * (D + 2) * 4;  // sums, reference and sum of weights of each wave
+    return kTiles > kJoin ? kTiles : kJoin;
+}
+
+// Starts the loads of 16 rows of keys, or of values: `bytes` bytes from src on, each lane's 16 bytes i at offset[i], to LDS at `to` + 1024 i.
+// What lies at or past `bytes` is not read and lands as zeros.  The rows are read once: they need not stay in the caches.
+template <int N>
+__device__ __forceinline__ void request_half(const char* src, int bytes, const int (&offset)[N], unsigned char* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __attribute__((address_space(3))) void lds_void;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < N; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, 2);
+#else
+    (void)src; (void)bytes; (void)offset; (void)to;
+#endif
+}
+// One dword a lane, to LDS at `to` + 4 lane.
+__device__ __forceinline__ void request_dword(const unsigned char* src, unsigned char* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __attribute__((address_space(3))) void lds_void;
+    typedef __attribute__((address_space(1))) const void gbl_void;
+    __builtin_amdgcn_global_load_lds((gbl_void*)src, (lds_void*)to, 4, 0, 0);
+#else
+    (void)src; (void)to;
+#endif
+}
+// All but the last N of the wave's loads have arrived.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64, "a counter of 6 bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ unsigned lds_address(const unsigned char* p) {
+    typedef __attribute__((address_space(3))) const unsigned char lds_byte;
+    return static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_byte*)p));
+}
+// Transposing reads of 4 times 16 d of values, and the wait for them.  (As builtins they would wait for all loads on their way to LDS.)
+// 16 bits: of rows 4 quarter .. + 3, and of the rows APART bytes behind; 8 bits: of rows 8 quarter .. + 7.
+template <int APART>
+__device__ __forceinline__ void read_columns(const unsigned (&at)[4], uintx2 (&lo)[4], uintx2 (&hi)[4]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %3, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(lo[2]), "=&v"(lo[3]), "=&v"(hi[0]), "=&v"(hi[1]), "=&v"(hi[2]), "=&v"(hi[3])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(APART)
+        : "memory");
+}
+__device__ __forceinline__ void read_columns(const unsigned (&at)[4], uintx2 (&codes)[4]) {
+    asm volatile(
+        "ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(codes[0]), "=&v"(codes[1]), "=&v"(codes[2]), "=&v"(codes[3])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+        : "memory");
 }
 
 // Grid: (chunks x heads of the cache x column blocks), the blocks of a chunk and head on one XCD.
 template <int D, int BITS, int NB>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_attention_kernel(Call c) {
-    constexpr int KS = D / 32;                  // steps along d of the first product
-    constexpr int DB = D / 16;                  // blocks of 16 rows of O^T
-    constexpr int kRowBytes = D * 2;            // in LDS
-    constexpr int kLoads = BITS == 16 ? 2 * KS : KS;   // 16-byte loads a lane of a tile's keys, or of its values
+    using T = Tile<D, BITS>;
+    constexpr int KS = D / 32;  // steps along d of the first product
+    constexpr int DB = D / 16;  // blocks of 16 rows of O^T
+    constexpr int kRing = T::kRing;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -151,11 +229,56 @@ void paged_attention_kernel(Call c) {
     if (chunk.b < 0) return;
     const int b = chunk.b;
 
-    // what the columns see
     const int R = c.S * c.G;
     const int held = held_rows(c, b);
     const int first = c.first ? c.first[b] : 0;
     const Rows rows = rows_of(c, b);
+    const int first_tile = rows.lo / kTileKeys + (which - chunk.first) * chunk.n_tiles;
+    const int last_tile = min(first_tile + chunk.n_tiles, rows.lo / kTileKeys + rows.tiles());
+    const int n_mine = max(0, (last_tile - first_tile - wave + kWaves - 1) / kWaves);  // this wave's tiles: first_tile + wave, then every fourth
+    unsigned char* const ring = lds + wave * T::kWaveBytes;
+    float* const weights_lds = reinterpret_cast<float*>(ring + kRing * T::kAll);
+
+    // ---- tiles: 16 + 16 rows, each half in one page.  Lane i has the page of half i of the next 32 tiles.
+    int offset[T::kHalfLoads];
+#pragma unroll
+    for (int i = 0; i < T::kHalfLoads; ++i) {
+        const int unit = i * 64 + lane, r = unit / T::kPieces;
+        offset[i] = r * T::kRowBytes + ((unit % T::kPieces) ^ T::swizzle(r)) * 16;
+    }
+    int pages = 0;
+    const auto request = [&](int k) {  // the wave's tile k, into its place of the ring; returns which rows some position sees
+        if (k % 32 == 0) {
+            const int s = (first_tile + wave + (k + lane / 2) * kWaves) * kTileKeys + 16 * (lane & 1);
+            pages = c.table[static_cast<int64_t>(b) * c.table_pages + min(s >> c.page_lg, c.table_pages - 1)];
+            asm volatile("" : "+v"(pages));  // waited for here, not wherever a page is looked up, where tiles would be waited for too
+        }
+        const int s0 = (first_tile + wave + k * kWaves) * kTileKeys;
+        unsigned char* const to = ring + k % kRing * T::kAll;
+        int64_t row[2];
+        unsigned live = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int s = s0 + 16 * u, page = __builtin_amdgcn_readlane(pages, 2 * (k % 32) + u);
+            const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages);
+            const int n = __builtin_amdgcn_readfirstlane(there ? min(max(rows.hi - s, 0), 16) : 0);
+            row[u] = ((static_cast<int64_t>(there ? page : 0) * c.H_kv + hk) << c.page_lg) + (s & ((1 << c.page_lg) - 1));
+            live |= (0xFFFFu >> (16 - n)) << (16 * u);
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+                request_half(static_cast<const char*>(c.data[w]) + row[u] * T::kRowBytes, n * T::kRowBytes, offset, to + w * T::kBytes + u * (T::kBytes / 2));
+        }
+        if constexpr (BITS == 8) {  // lanes 0 .. 7 the keys' scale bytes, 8 .. 15 the values'
+            const unsigned char* const scales = (lane & 8) ? c.scales[1] : c.scales[0];
+            request_dword(scales + ((lane & 4) ? row[1] : row[0]) + 4 * (lane & 3), to + 2 * T::kBytes);
+        }
+        return s0 < rows.lo ? live & (~0u << (rows.lo - s0)) : live;
+    };
+    unsigned live[kRing];
+#pragma unroll
+    for (int k = 0; k < kRing; ++k) live[k] = k < n_mine ? request(k) : 0u;
+
+    // ---- what the columns see, and what all of them do: from the last position's first row to the first one's last
     int legal[NB], from[NB], q_row[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -163,13 +286,12 @@ void paged_attention_kernel(Call c) {
         const int i = r / c.G;
         legal[nb] = legal_rows(first, i, held, c.m, c.mask_mode);
         from[nb] = max(0, legal[nb] - c.n_win);
-        q_row[nb] = (b * c.S + i) * c.H + hk * c.G + r % c.G;
+        q_row[nb] = (b * c.S + i) * c.H + hk * c.G + (r - i * c.G);
     }
-    // rows that all positions see: from the last one's first to the first one's last
     const int all_from = max(0, legal_rows(first, c.S - 1, held, c.m, c.mask_mode) - c.n_win);
     const int all_to = legal_rows(first, 0, held, c.m, c.mask_mode);
 
-    // queries: lane has column col; step ks of the contraction is d = 32 ks + 8 quarter .. + 7 in 16 bits, and in 8, where a lane loads 16 codes of a row,
+    // queries: lane has column col; step ks of the contraction is d = 32 ks + 8 quarter .. + 7 in 16 bits, and in 8, where a lane reads 16 codes of a row,
     // d = 64 (ks / 2) + 16 quarter + 8 (ks % 2) .. + 7.  A negative scale goes into the query (exact), a scale of 0 makes zeros of it.
     float to_log2 = __builtin_fabsf(c.scale_log2e);
     bf16x8 qf[NB][KS];
@@ -193,69 +315,15 @@ void paged_attention_kernel(Call c) {
                 for (int j = 0; j < 8; ++j) qf[nb][ks][j] = static_cast<__bf16>(static_cast<float>(qf[nb][ks][j]) * 0.0f);
     }
 
-    const int first_tile = rows.lo / kTileKeys + (which - chunk.first) * chunk.n_tiles;
-    const int last_tile = min(first_tile + chunk.n_tiles, rows.lo / kTileKeys + rows.tiles());
-
-    unsigned char* const tile_lds = lds + wave * (kTileKeys * kRowBytes);
-    float* const weights_lds = reinterpret_cast<float*>(lds + kWaves * kTileKeys * kRowBytes) + wave * (kTileKeys * 16);
-
-    // A tile's rows are 16 + 16, each half in one page.
-    struct Place {
-        int64_t row[2];  // of the pages' arrays
-        bool there[2];
-    };
-    auto place = [&](int tile) {
-        Place p;
+    // Row of the tile that score j of a lane is of: half j / 4 of the matrix instruction's rows has, in 16 bits, the tile's rows in order, so that a
+    // lane's rows are 4 quarter .. + 3 of either half; in 8 bits rows 8 (r / 4) + 4 (j / 4) + r % 4, so that they are 8 in a row, as the transposing
+    // read of 8 bits wants them.
+    auto row_of = [&](int j) { return BITS == 16 ? 16 * (j >> 2) + 4 * quarter + (j & 3) : 8 * quarter + j; };
+    int key_at[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int s = tile * kTileKeys + 16 * u;
-            const int page = c.table[static_cast<int64_t>(b) * c.table_pages + min(s >> c.page_lg, c.table_pages - 1)];
-            p.there[u] = static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages);
-            p.row[u] = ((static_cast<int64_t>(p.there[u] ? page : 0) * c.H_kv + hk) << c.page_lg) + (s & ((1 << c.page_lg) - 1));
-        }
-        return p;
-    };
-    // keys: lane has row col (+ 16 u), quarter's pieces of it
-    uintx4 kraw[kLoads];
-    int kpower[2];
-    auto load_keys = [&](const Place& p) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uintx4* const src = static_cast<const uintx4*>(c.data[0]) + (p.row[u] + col) * (D * BITS / 128);
-#pragma unroll
-            for (int j = 0; j < kLoads / 2; ++j) kraw[u * (kLoads / 2) + j] = src[4 * j + quarter];
-            if constexpr (BITS == 8) kpower[u] = c.scales[0][p.row[u] + col];
-        }
-    };
-    // values: a wave's load j has the 64 consecutive 16-byte units of the tile from 64 j on
-    uintx4 vraw[kLoads];
-    int vpower[kLoads];
-    constexpr int kUnits = D * BITS / 128;  // of a row
-    auto load_values = [&](const Place& p) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int u = j / (kLoads / 2), unit = (j % (kLoads / 2)) * 64 + lane;
-            vraw[j] = (static_cast<const uintx4*>(c.data[1]) + p.row[u] * kUnits)[unit];
-            if constexpr (BITS == 8) vpower[j] = c.scales[1][p.row[u] + unit / kUnits];
-        }
-    };
-    auto values_to_lds = [&](unsigned live) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int unit = (j % (kLoads / 2)) * 64 + lane, r = j / (kLoads / 2) * 16 + unit / kUnits, piece = unit % kUnits;
-            uintx4 x[2] = {vraw[j], vraw[j]};
-            if constexpr (BITS == 8) codes_to_bf16(vraw[j], scale_power(vpower[j]), x);
-            if (live != 0xFFFFFFFFu && !((live >> r) & 1)) x[0] = x[1] = uintx4{0, 0, 0, 0};  // rows that no position sees may hold anything
-            if constexpr (BITS == 16) {
-                *reinterpret_cast<uintx4*>(tile_lds + tile_slot<D>(r, piece) * 16) = x[0];
-            } else {
-                *reinterpret_cast<uintx4*>(tile_lds + tile_slot<D>(r, 2 * piece) * 16) = x[0];
-                *reinterpret_cast<uintx4*>(tile_lds + tile_slot<D>(r, 2 * piece + 1) * 16) = x[1];
-            }
-        }
-    };
-    // transposing read of 16 d of 4 rows by 16 lanes: lane s of the 16 points at 4 consecutive d of row 4 quarter + s / 4, and gets d = s of the four rows
-    const int vat = tile_slot<D>(4 * quarter + (col >> 2), (col & 3) / 2) * 16 + (col & 1) * 8;
+    for (int u = 0; u < 2; ++u) key_at[u] = T::place(BITS == 16 ? 16 * u + col : 8 * (col >> 2) + 4 * u + (col & 3), quarter);
+    // transposing reads: source lane s of 16 points, in 16 bits, at 4 consecutive d of row 4 quarter + s / 4, in 8 at 8 consecutive d of row 8 quarter + s / 2
+    const int value_at = BITS == 16 ? T::place(4 * quarter + (col >> 2), (col & 3) / 2) + (col & 1) * 8 : T::place(8 * quarter + (col >> 1), 0) + (col & 1) * 8;
 
     floatx4 acc[NB][DB];
     float m_ref[NB], l_sum[NB];
@@ -267,77 +335,56 @@ void paged_attention_kernel(Call c) {
         for (int db = 0; db < DB; ++db) acc[nb][db] = floatx4{0, 0, 0, 0};
     }
 
-    Place here = {};
-    if (first_tile + wave < last_tile) {
-        here = place(first_tile + wave);
-        load_keys(here);
-        load_values(here);
-    }
-    for (int tile = first_tile + wave; tile < last_tile; tile += kWaves) {
-        const int s0 = tile * kTileKeys;
-        const bool more = tile + kWaves < last_tile;
-        const Place then = more ? place(tile + kWaves) : here;
-        // rows that some position sees
-        unsigned live = (here.there[0] ? 0xFFFFu : 0u) | (here.there[1] ? 0xFFFF0000u : 0u);
-        if (s0 < rows.lo) live &= ~0u << (rows.lo - s0);
-        if (s0 + kTileKeys > rows.hi) live &= ~0u >> (s0 + kTileKeys - rows.hi);
-        const bool masked = live != 0xFFFFFFFFu || s0 < all_from || s0 + kTileKeys > all_to;
-        here = then;
+#pragma unroll 1
+    for (int k = 0; k < n_mine; ++k) {
+        if (k + kRing <= n_mine) wait_loads<(kRing - 1) * T::kLoads>();
+        else wait_loads<0>();
+        const int s0 = (first_tile + wave + k * kWaves) * kTileKeys;
+        const unsigned char* const tile = ring + k % kRing * T::kAll;
+        const bool masked = live[0] != 0xFFFFFFFFu || s0 < all_from || s0 + kTileKeys > all_to;
 
         floatx4 x[NB][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            uintx4 kf[KS];
+            bf16x8 kf[KS];
             if constexpr (BITS == 16) {
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) kf[ks] = kraw[u * KS + ks];
+                for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const bf16x8*>(tile + (key_at[u] ^ (64 * ks)));
             } else {
+                const float power = scale_power(tile[2 * T::kBytes + 8 * (col >> 2) + 4 * u + (col & 3)]);
 #pragma unroll
                 for (int j = 0; j < KS / 2; ++j) {
                     uintx4 two[2];
-                    codes_to_bf16(kraw[u * (KS / 2) + j], scale_power(kpower[u]), two);
-                    kf[2 * j] = two[0];
-                    kf[2 * j + 1] = two[1];
+                    codes_to_bf16(*reinterpret_cast<const uintx4*>(tile + (key_at[u] ^ (64 * j))), power, two);
+                    kf[2 * j] = __builtin_bit_cast(bf16x8, two[0]);
+                    kf[2 * j + 1] = __builtin_bit_cast(bf16x8, two[1]);
                 }
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 x[nb][u] = floatx4{0, 0, 0, 0};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    x[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[ks]), qf[nb][ks], x[nb][u], 0, 0, 0);
+                for (int ks = 0; ks < KS; ++ks) x[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], qf[nb][ks], x[nb][u], 0, 0, 0);
             }
         }
-        if (more) load_keys(then);
-        wave_order();  // the tile before has been read
-        values_to_lds(live);
-        if (more) load_values(then);
-        wave_order();
+        uintx2 value_scales = {0, 0};
+        if constexpr (BITS == 8) value_scales = *reinterpret_cast<const uintx2*>(tile + 2 * T::kBytes + kTileKeys + 8 * quarter);
 
-        bool odd_values = false;
-        if (masked) {
-            // values that are not finite, of rows that some position sees and another may not
-            bool odd = false;
-#pragma unroll
-            for (int j = 0; j < kTileKeys * kRowBytes / 1024; ++j) {
-                const uintx4 v = *reinterpret_cast<const uintx4*>(tile_lds + (j * 64 + lane) * 16);
-                odd |= not_finite(__builtin_bit_cast(bf16x8, v)) != 0;
-            }
-            odd_values = __ballot(odd) != 0ull;
-        }
+        bf16x8 pf[NB];
+        unsigned mine[NB];  // rows that this column sees
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            unsigned mine = 0xFFFFFFFFu;  // rows that this column sees
+            mine[nb] = 0xFFFFFFFFu;
             if (masked) {
-                mine = live;
+                mine[nb] = live[0];
                 const int lo = from[nb] - s0, hi = legal[nb] - s0;
-                if (lo > 0) mine &= lo >= kTileKeys ? 0u : ~0u << lo;
-                if (hi < kTileKeys) mine &= hi <= 0 ? 0u : ~0u >> (kTileKeys - hi);
+                if (lo > 0) mine[nb] &= lo >= kTileKeys ? 0u : ~0u << lo;
+                if (hi < kTileKeys) mine[nb] &= hi <= 0 ? 0u : ~0u >> (kTileKeys - hi);
                 float low = -__builtin_huge_valf();
                 asm volatile("" : "+v"(low));
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (!((mine >> (16 * (j >> 2) + 4 * quarter + (j & 3))) & 1)) x[nb][j >> 2][j & 3] = low;
+                    if (!((mine[nb] >> row_of(j)) & 1)) x[nb][j >> 2][j & 3] = low;
             }
             float p[8], sum;
             auto exponentials = [&]() {
@@ -367,44 +414,93 @@ void paged_attention_kernel(Call c) {
                 exponentials();
             }
             l_sum[nb] += sum;
-            bf16x8 pf;
+            if constexpr (BITS == 8) {  // the values' powers of two go into the weights: exact
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x2 two = __builtin_convertvector(floatx2{p[2 * j], p[2 * j + 1]}, bf16x2);
-                pf[2 * j] = two[0];
-                pf[2 * j + 1] = two[1];
-            }
-            // contraction index e <-> tile row 16 (e / 4) + 4 quarter + e % 4 on both operands
-            auto values = [&](int db) {
-                typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-                const unsigned char* const at = tile_lds + (vat ^ (32 * db));
-                const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
-                const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 16 * kRowBytes));
-                return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            };
-            if (!odd_values) {
-#pragma unroll
-                for (int db = 0; db < DB; ++db) acc[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values(db), pf, acc[nb][db], 0, 0, 0);
-            } else {
-                // values that are not finite by themselves, row by row: 0 times a NaN must not enter a column that does not see it
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-                    acc[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(finite_or_zero(values(db)), pf, acc[nb][db], 0, 0, 0);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) weights_lds[(16 * (j >> 2) + 4 * quarter + (j & 3)) * 16 + col] = p[j];
-                wave_order();
-#pragma unroll 1
-                for (int r = 0; r < kTileKeys; ++r) {
-                    const float w = weights_lds[r * 16 + col];
-                    const bool sees = (mine >> r) & 1;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-                        add_not_finite(acc[nb][db], 0, *reinterpret_cast<const bf16x4*>(tile_lds + tile_slot<D>(r, 2 * db + quarter / 2) * 16 + (quarter & 1) * 8),
-                                       w, sees);
+                for (int j = 0; j < 8; ++j) {
+                    p[j] *= scale_power((value_scales[j >> 2] >> (8 * (j & 3))) & 0xFF);
+                    if (masked && !((mine[nb] >> row_of(j)) & 1)) p[j] = 0.0f;  // a row that is not seen may have any scale byte
                 }
-                wave_order();
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const bf16x2 two = __builtin_convertvector(floatx2{p[j], p[j + 1]}, bf16x2);
+                pf[nb][j] = two[0];
+                pf[nb][j + 1] = two[1];
             }
         }
+
+        // contraction index j <-> row_of(j) on both operands
+        const unsigned at = lds_address(tile + T::kBytes);
+#pragma unroll
+        for (int db0 = 0; db0 < DB; db0 += 4) {
+            unsigned from_lds[4];
+            bf16x8 vf[4];
+            unsigned found = 0;
+            if constexpr (BITS == 16) {
+                uintx2 lo[4], hi[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) from_lds[i] = at + (value_at ^ (32 * (db0 + i)));
+                read_columns<16 * T::kRowBytes>(from_lds, lo, hi);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vf[i] = __builtin_bit_cast(bf16x8, uintx4{lo[i][0], lo[i][1], hi[i][0], hi[i][1]});
+                if (masked)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) found |= not_finite(vf[i]);
+            } else {
+                uintx2 codes[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) from_lds[i] = at + (value_at ^ (16 * (db0 + i)));
+                read_columns(from_lds, codes);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uintx4 out[2];
+                    codes_to_bf16(uintx4{codes[i][0], codes[i][1], 0, 0}, 1.0f, out);
+                    vf[i] = __builtin_bit_cast(bf16x8, out[0]);
+                    if (masked)
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) found |= ((codes[i][w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+                }
+            }
+            // values that are not finite go in by themselves, row by row: 0 times a NaN must not enter a column that does not see it
+            if (masked && __ballot(found != 0) != 0ull) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vf[i] = finite_or_zero(vf[i]);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) weights_lds[row_of(j) * 16 + col] = static_cast<float>(pf[nb][j]);
+                    wave_order();
+#pragma unroll 1
+                    for (int r = 0; r < kTileKeys; ++r) {
+                        const float w = weights_lds[r * 16 + col];
+                        const bool sees = (mine[nb] >> r) & 1;
+                        const unsigned char* const values = tile + T::kBytes;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            bf16x4 v;
+                            if constexpr (BITS == 16) {
+                                v = *reinterpret_cast<const bf16x4*>(values + T::place(r, 2 * (db0 + i) + quarter / 2) + (quarter & 1) * 8);
+                            } else {
+                                uintx4 out[2];
+                                codes_to_bf16(uintx4{*reinterpret_cast<const unsigned*>(values + T::place(r, db0 + i) + 4 * quarter), 0, 0, 0}, 1.0f, out);
+                                const bf16x8 eight = __builtin_bit_cast(bf16x8, out[0]);
+                                v = bf16x4{eight[0], eight[1], eight[2], eight[3]};
+                            }
+                            add_not_finite(acc[nb][db0 + i], 0, v, w, sees);
+                        }
+                    }
+                    wave_order();
+                }
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[nb][db0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[nb], acc[nb][db0 + i], 0, 0, 0);
+        }
+        wait_lds();  // the tile has been read: its place is free
+#pragma unroll
+        for (int i = 1; i < kRing; ++i) live[i - 1] = live[i];
+        live[kRing - 1] = k + kRing < n_mine ? request(k + kRing) : 0u;
     }
 
     // ---- the workgroup's waves join: references, then sums
@@ -462,33 +558,71 @@ void paged_attention_kernel(Call c) {
     }
 }
 
-// Chunks of a sequence together: a wave a query's head.
+// Chunks of a sequence together: a workgroup a query's head, its waves every fourth chunk.
 template <int D>
 __global__ __launch_bounds__(256) void join_chunks_kernel(Call c) {
-    const int lane = threadIdx.x & 63;
-    const int row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (b * S + i) * H + head
+    constexpr int kPer = D / 64;  // values a lane
+    __shared__ float s_top[4], s_sum[4], s_out[4][D];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int row = blockIdx.x;  // (b * S + i) * H + head
     const int per = c.S * c.H;
-    if (row >= c.B * per) return;
-    const int b = row / per;
-    const Chunk chunk = find_chunk(c, b, false);
+    const Chunk chunk = find_chunk(c, row / per, false);
     if (chunk.n <= 1) return;  // written by its workgroup
     const int64_t part0 = static_cast<int64_t>(chunk.first) * per + row % per;
-    float top = -__builtin_huge_valf();
-    for (int i = lane; i < chunk.n; i += 64) top = fmaxf(top, c.parts_sums[(part0 + static_cast<int64_t>(i) * per) * 2]);
-    top = wave_max(top);
-    const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
-    float l = 0.0f, o[D / 64] = {};
-    for (int i = 0; i < chunk.n; ++i) {
-        const int64_t part = part0 + static_cast<int64_t>(i) * per;
-        const float m = c.parts_sums[part * 2];
-        const float a = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - shift);
-        l += a * c.parts_sums[part * 2 + 1];
+    float top = -__builtin_huge_valf(), l = 0.0f, o[kPer] = {};
+    constexpr int kAtOnce = 8;
+    for (int i0 = wave; i0 < chunk.n; i0 += 4 * kAtOnce) {
+        float m[kAtOnce], sums[kAtOnce], x[kAtOnce][kPer];
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) o[j] += a * c.parts_out[part * D + lane * (D / 64) + j];
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int64_t part = part0 + static_cast<int64_t>(min(i0 + 4 * j, chunk.n - 1)) * per;
+            const floatx2 two = *reinterpret_cast<const floatx2*>(c.parts_sums + part * 2);
+            m[j] = two[0];
+            sums[j] = two[1];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) x[j][e] = c.parts_out[part * D + lane * kPer + e];
+        }
+        float highest = top;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) highest = fmaxf(highest, m[j]);
+        const float shift = highest == -__builtin_huge_valf() ? 0.0f : highest;
+        const float before = top == highest ? 1.0f : __builtin_amdgcn_exp2f(top - shift);
+        l *= before;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] *= before;
+        top = highest;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (i0 + 4 * j < chunk.n) {
+                const float a = m[j] == top ? 1.0f : __builtin_amdgcn_exp2f(m[j] - shift);
+                l += a * sums[j];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) o[e] += a * x[j][e];
+            }
+    }
+    if (lane == 0) {
+        s_top[wave] = top;
+        s_sum[wave] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) s_out[wave][lane * kPer + e] = o[e];
+    __syncthreads();
+    if (wave != 0) return;
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float a = s_top[w] == top ? 1.0f : __builtin_amdgcn_exp2f(s_top[w] - shift);
+        l += a * s_sum[w];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] += a * s_out[w][lane * kPer + e];
     }
     const float inv = top == -__builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) c.out[static_cast<int64_t>(row) * D + lane * (D / 64) + j] = static_cast<__bf16>(o[j] * inv);
+    for (int e = 0; e < kPer; ++e) c.out[static_cast<int64_t>(row) * D + lane * kPer + e] = static_cast<__bf16>(o[e] * inv);
     if (c.lse && lane == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(top, l);
 }
 
@@ -508,7 +642,7 @@ bool fits(int32_t B, int32_t S, int32_t H) { return H <= 1024 && static_cast<int
 template <int D, int BITS, int NB>
 hipError_t launch(const Call& c, hipStream_t stream) {
     static std::atomic<size_t> allowed[64];
-    constexpr int kBytes = lds_bytes<D, NB>();
+    constexpr int kBytes = lds_bytes<D, BITS, NB>();
     hipError_t e = allow_lds(paged_attention_kernel<D, BITS, NB>, kBytes, allowed);
     if (e != hipSuccess) return e;
     const int64_t most_tiles = ((static_cast<int64_t>(c.table_pages) << c.page_lg) + kTileKeys - 1) / kTileKeys;
@@ -518,7 +652,7 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(kThreads), kBytes, stream, c);
     e = hipGetLastError();
     if (e != hipSuccess || one_each) return e;
-    hipLaunchKernelGGL((join_chunks_kernel<D>), dim3((c.B * c.S * c.H + 3) / 4), dim3(256), 0, stream, c);
+    hipLaunchKernelGGL((join_chunks_kernel<D>), dim3(c.B * c.S * c.H), dim3(256), 0, stream, c);
     return hipGetLastError();
 }
 
