@@ -31,7 +31,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kMinTiles = 2 * kWaves;   // of a chunk
-constexpr int kWorkgroups = 1024;       // about as many in all
+constexpr int kWorkgroups = 512;        // that fit the chip at once: two a compute unit
 constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a tile beyond which the reference is raised
 constexpr int kMaxSequences = 1 << 14;
 
@@ -46,10 +46,11 @@ struct Call {
     float* lse;
     float* parts_out;   // [parts][S * H][D], not divided by their sums
     float* parts_sums;  // [parts][S * H][2]: reference, sum
+    int2* chunks;       // [B]: a sequence's first chunk, and how many it has
     float scale_log2e;
     int B, S, H, H_kv, G, table_pages, n_pages, page_lg, m, mask_mode, n_win;
     int blocks;  // of columns
-    int target;  // chunks of all sequences, beside one more of each
+    int target;  // chunks that fit the chip at once; there are up to twice as many, and one more of each sequence
 };
 
 // Rows that the positions of sequence b see: [lo, hi) all of them together.
@@ -67,41 +68,52 @@ __device__ __forceinline__ Rows rows_of(const Call& c, int b) {
     return {max(0, legal_rows(first, 0, held, c.m, c.mask_mode) - c.n_win), c.n_win > 0 ? legal_rows(first, c.S - 1, held, c.m, c.mask_mode) : 0};
 }
 
-// The chunk of a workgroup, or the chunks of a sequence.
+// The chunk of a workgroup.
 struct Chunk {
-    int b;         // sequence, -1: there is no such chunk
-    int first;     // the sequence's first chunk
-    int n;         // chunks of the sequence
-    int n_tiles;   // tiles of a chunk
+    int b;        // sequence, -1: there is no such chunk
+    int first;    // the sequence's first chunk
+    int n;        // chunks of the sequence
+    int n_tiles;  // tiles of a chunk
 };
-__device__ __forceinline__ int tiles_of_chunks(const Call& c) {
+
+// The chunk with number `which`.  Chunks have as many tiles as it takes for all of them to fit the chip at once; where sequences of different lengths would
+// make that more than a quarter longer than an even share, half as many, twice.  All 64 lanes call it; up to 64 sequences stay in a register.
+__device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
     const int lane = threadIdx.x & 63;
+    const int kept = lane < c.B ? rows_of(c, lane).tiles() : 0;
+    auto tiles_at = [&](int b0) { return b0 == 0 ? kept : b0 + lane < c.B ? rows_of(c, b0 + lane).tiles() : 0; };
     int low = 0, high = 0;  // sums of the tiles' lower 16 bits and of the rest: 2^14 sequences of 2^25 tiles
-    for (int b = lane; b < c.B; b += 64) {
-        const int t = rows_of(c, b).tiles();
+    for (int b0 = 0; b0 < c.B; b0 += 64) {
+        const int t = tiles_at(b0);
         low += t & 0xFFFF;
         high += t >> 16;
     }
     low = lane_value(wave_prefix_sum(low), 63);
     high = lane_value(wave_prefix_sum(high), 63);
     const int64_t total = (static_cast<int64_t>(high) << 16) + low;
-    return static_cast<int>(max(static_cast<int64_t>(kMinTiles), (total + c.target - 1) / c.target));
-}
-__device__ __forceinline__ int chunks_of(const Call& c, int b, int n_tiles) { return max(1, (rows_of(c, b).tiles() + n_tiles - 1) / n_tiles); }
-
-// by_chunk: the sequence that chunk `i` is of; otherwise sequence i's.
-__device__ __forceinline__ Chunk find_chunk(const Call& c, int i, bool by_chunk) {
-    const int lane = threadIdx.x & 63;
-    const int n_tiles = tiles_of_chunks(c);
+    auto length_for = [&](int target) {
+        int n_tiles = static_cast<int>(max(static_cast<int64_t>(kMinTiles), (total + target - 1) / target));
+        for (int i = 0; i < 4; ++i) {
+            int n = 0;
+            for (int b0 = 0; b0 < c.B; b0 += 64) n += b0 + lane < c.B ? max(1, (tiles_at(b0) + n_tiles - 1) / n_tiles) : 0;
+            n = lane_value(wave_prefix_sum(n), 63);
+            if (n <= target) break;
+            n_tiles += max(1, static_cast<int>(static_cast<int64_t>(n_tiles) * (n - target) / target));
+        }
+        return n_tiles;
+    };
+    int n_tiles = length_for(c.target);
+    if (static_cast<int64_t>(n_tiles) * c.target * 4 > 5 * total + 4 * kMinTiles * c.target) n_tiles = length_for(2 * c.target);
     int before = 0;
     for (int b0 = 0; b0 < c.B; b0 += 64) {
-        const int mine = b0 + lane < c.B ? chunks_of(c, b0 + lane, n_tiles) : 0;
+        const int t = tiles_at(b0);
+        const int mine = b0 + lane < c.B ? max(1, (t + n_tiles - 1) / n_tiles) : 0;
         const int upto = wave_prefix_sum(mine);
         const int all = lane_value(upto, 63);
-        if (by_chunk ? i < before + all : i < b0 + 64) {
-            const int l = by_chunk ? static_cast<int>(__popcll(__ballot(before + upto <= i))) : i - b0;
+        if (which < before + all) {
+            const int l = static_cast<int>(__popcll(__ballot(before + upto <= which)));
             const int n = lane_value(mine, l);
-            return {b0 + l, before + lane_value(upto, l) - n, n, n_tiles};
+            return {b0 + l, before + lane_value(upto, l) - n, n, (lane_value(t, l) + n - 1) / n};
         }
         before += all;
     }
@@ -150,14 +162,14 @@ constexpr int lds_bytes() {
 }
 
 // Starts the loads of 16 rows of keys, or of values: `bytes` bytes from src on, each lane's 16 bytes i at offset[i], to LDS at `to` + 1024 i.
-// What lies at or past `bytes` is not read and lands as zeros.  The rows are read once: they need not stay in the caches.
-template <int N>
+// What lies at or past `bytes` is not read and lands as zeros.  ONCE: no other workgroup reads the rows, so they need not stay in the caches.
+template <bool ONCE, int N>
 __device__ __forceinline__ void request_half(const char* src, int bytes, const int (&offset)[N], unsigned char* to) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef __attribute__((address_space(3))) void lds_void;
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < N; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, 2);
+    for (int i = 0; i < N; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, ONCE ? 2 : 0);
 #else
     (void)src; (void)bytes; (void)offset; (void)to;
 #endif
@@ -225,9 +237,10 @@ void paged_attention_kernel(Call c) {
     const int item = (slot / c.blocks) * 8 + blockIdx.x % 8;
     const int hk = item % c.H_kv;
     const int which = item / c.H_kv;
-    const Chunk chunk = find_chunk(c, which, true);
+    const Chunk chunk = find_chunk(c, which);
     if (chunk.b < 0) return;
     const int b = chunk.b;
+    if (which == chunk.first && hk == 0 && block == 0 && threadIdx.x == 0) c.chunks[b] = make_int2(chunk.first, chunk.n);
 
     const int R = c.S * c.G;
     const int held = held_rows(c, b);
@@ -265,8 +278,12 @@ void paged_attention_kernel(Call c) {
             row[u] = ((static_cast<int64_t>(there ? page : 0) * c.H_kv + hk) << c.page_lg) + (s & ((1 << c.page_lg) - 1));
             live |= (0xFFFFu >> (16 - n)) << (16 * u);
 #pragma unroll
-            for (int w = 0; w < 2; ++w)
-                request_half(static_cast<const char*>(c.data[w]) + row[u] * T::kRowBytes, n * T::kRowBytes, offset, to + w * T::kBytes + u * (T::kBytes / 2));
+            for (int w = 0; w < 2; ++w) {
+                const char* const src = static_cast<const char*>(c.data[w]) + row[u] * T::kRowBytes;
+                unsigned char* const half = to + w * T::kBytes + u * (T::kBytes / 2);
+                if (NB == 1 || c.blocks == 1) request_half<true>(src, n * T::kRowBytes, offset, half);
+                else request_half<false>(src, n * T::kRowBytes, offset, half);
+            }
         }
         if constexpr (BITS == 8) {  // lanes 0 .. 7 the keys' scale bytes, 8 .. 15 the values'
             const unsigned char* const scales = (lane & 8) ? c.scales[1] : c.scales[0];
@@ -558,24 +575,26 @@ void paged_attention_kernel(Call c) {
     }
 }
 
-// Chunks of a sequence together: a workgroup a query's head, its waves every fourth chunk.
-template <int D>
+// Chunks of a sequence together.  SPLIT waves take a query's head, each every SPLIT-th chunk.
+template <int D, int SPLIT>
 __global__ __launch_bounds__(256) void join_chunks_kernel(Call c) {
     constexpr int kPer = D / 64;  // values a lane
     __shared__ float s_top[4], s_sum[4], s_out[4][D];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int row = blockIdx.x;  // (b * S + i) * H + head
     const int per = c.S * c.H;
-    const Chunk chunk = find_chunk(c, row / per, false);
-    if (chunk.n <= 1) return;  // written by its workgroup
-    const int64_t part0 = static_cast<int64_t>(chunk.first) * per + row % per;
+    const int row = blockIdx.x * (4 / SPLIT) + wave / SPLIT;  // (b * S + i) * H + head
+    const int part_of = wave % SPLIT;
+    const int2 chunks = row < c.B * per ? c.chunks[row / per] : make_int2(0, 0);
+    const int n = __builtin_amdgcn_readfirstlane(chunks.y);
+    if (SPLIT == 1 ? n <= 1 : __syncthreads_or(n > 1) == 0) return;  // written by its workgroup
+    const int64_t part0 = static_cast<int64_t>(chunks.x) * per + row % per;
     float top = -__builtin_huge_valf(), l = 0.0f, o[kPer] = {};
     constexpr int kAtOnce = 8;
-    for (int i0 = wave; i0 < chunk.n; i0 += 4 * kAtOnce) {
+    for (int i0 = part_of; i0 < n; i0 += SPLIT * kAtOnce) {
         float m[kAtOnce], sums[kAtOnce], x[kAtOnce][kPer];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            const int64_t part = part0 + static_cast<int64_t>(min(i0 + 4 * j, chunk.n - 1)) * per;
+            const int64_t part = part0 + static_cast<int64_t>(min(i0 + SPLIT * j, n - 1)) * per;
             const floatx2 two = *reinterpret_cast<const floatx2*>(c.parts_sums + part * 2);
             m[j] = two[0];
             sums[j] = two[1];
@@ -593,32 +612,36 @@ __global__ __launch_bounds__(256) void join_chunks_kernel(Call c) {
         top = highest;
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            if (i0 + 4 * j < chunk.n) {
+            if (i0 + SPLIT * j < n) {
                 const float a = m[j] == top ? 1.0f : __builtin_amdgcn_exp2f(m[j] - shift);
                 l += a * sums[j];
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) o[e] += a * x[j][e];
             }
     }
-    if (lane == 0) {
-        s_top[wave] = top;
-        s_sum[wave] = l;
-    }
+    if constexpr (SPLIT > 1) {
+        if (lane == 0) {
+            s_top[wave] = top;
+            s_sum[wave] = l;
+        }
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) s_out[wave][lane * kPer + e] = o[e];
-    __syncthreads();
-    if (wave != 0) return;
-    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-    const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
-    l = 0.0f;
+        for (int e = 0; e < kPer; ++e) s_out[wave][lane * kPer + e] = o[e];
+        __syncthreads();
+        if (part_of != 0 || n <= 1) return;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] = 0.0f;
+        for (int w = 1; w < SPLIT; ++w) top = fmaxf(top, s_top[wave + w]);
+        const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
+        const float own = s_top[wave] == top ? 1.0f : __builtin_amdgcn_exp2f(s_top[wave] - shift);
+        l *= own;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float a = s_top[w] == top ? 1.0f : __builtin_amdgcn_exp2f(s_top[w] - shift);
-        l += a * s_sum[w];
+        for (int e = 0; e < kPer; ++e) o[e] *= own;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] += a * s_out[w][lane * kPer + e];
+        for (int w = 1; w < SPLIT; ++w) {
+            const float a = s_top[wave + w] == top ? 1.0f : __builtin_amdgcn_exp2f(s_top[wave + w] - shift);
+            l += a * s_sum[wave + w];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) o[e] += a * s_out[wave + w][lane * kPer + e];
+        }
     }
     const float inv = top == -__builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
@@ -637,6 +660,9 @@ Shape shape_of(int S, int H, int H_kv) {
     return {nb, blocks, std::max(1, (kWorkgroups + H_kv * blocks - 1) / (H_kv * blocks))};
 }
 
+// Chunks that there may be.
+size_t parts_of(const Shape& shape, int B) { return static_cast<size_t>(2) * shape.target + B; }
+
 bool fits(int32_t B, int32_t S, int32_t H) { return H <= 1024 && static_cast<int64_t>(B) * S <= (1 << 22) && static_cast<int64_t>(B) * S * H <= (1 << 22); }
 
 template <int D, int BITS, int NB>
@@ -647,12 +673,14 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     if (e != hipSuccess) return e;
     const int64_t most_tiles = ((static_cast<int64_t>(c.table_pages) << c.page_lg) + kTileKeys - 1) / kTileKeys;
     const bool one_each = most_tiles <= kMinTiles;  // no sequence can have two chunks
-    const int64_t items = static_cast<int64_t>(one_each ? c.B : c.target + c.B) * c.H_kv;
+    const int64_t items = static_cast<int64_t>(one_each ? c.B : 2 * c.target + c.B) * c.H_kv;
     const unsigned grid = static_cast<unsigned>((items + 7) / 8 * 8 * c.blocks);
     hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(kThreads), kBytes, stream, c);
     e = hipGetLastError();
     if (e != hipSuccess || one_each) return e;
-    hipLaunchKernelGGL((join_chunks_kernel<D>), dim3(c.B * c.S * c.H), dim3(256), 0, stream, c);
+    const int rows = c.B * c.S * c.H;
+    if (c.target > 8 * c.B) hipLaunchKernelGGL((join_chunks_kernel<D, 4>), dim3(rows), dim3(256), 0, stream, c);
+    else hipLaunchKernelGGL((join_chunks_kernel<D, 1>), dim3((rows + 3) / 4), dim3(256), 0, stream, c);
     return hipGetLastError();
 }
 
@@ -666,7 +694,7 @@ extern "C" {
 
 size_t si_paged_workspace_bytes(int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t D) {
     if (B < 1 || S < 1 || H < 1 || H_kv < 1 || D < 1 || H % H_kv != 0 || B > kMaxSequences || !fits(B, S, H)) return 0;
-    return static_cast<size_t>(shape_of(S, H, H_kv).target + B) * S * H * (D + 2) * sizeof(float);
+    return parts_of(shape_of(S, H, H_kv), B) * S * H * (D + 2) * sizeof(float) + B * sizeof(int2);
 }
 
 si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t S, int32_t H, const int32_t* lengths, const int32_t* first,
@@ -686,11 +714,12 @@ si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t
     int lg = 0;
     while ((1 << lg) < cache->page_rows) ++lg;
     float* const parts = static_cast<float*>(workspace);
+    const size_t n_parts = parts_of(shape, cache->B);
     const Call c = {static_cast<const __bf16*>(q),
                     {cache->K, cache->V ? cache->V : cache->K},
                     {static_cast<const unsigned char*>(cache->K_scales), static_cast<const unsigned char*>(cache->V ? cache->V_scales : cache->K_scales)},
                     cache->table, lengths, first, static_cast<__bf16*>(out), lse,
-                    parts, parts + static_cast<size_t>(shape.target + cache->B) * S * H * cache->D,
+                    parts, parts + n_parts * S * H * cache->D, reinterpret_cast<int2*>(parts + n_parts * S * H * (cache->D + 2)),
                     scale_log2e, cache->B, S, H, cache->H_kv, H / cache->H_kv, cache->table_pages, cache->n_pages, lg, m, mask_mode, n_win,
                     shape.blocks, shape.target};
     const hipStream_t st = static_cast<hipStream_t>(stream);

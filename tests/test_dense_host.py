@@ -82,7 +82,7 @@ def test_workspace():
     for B, S, H, H_kv, D in ((1, 1, 64, 8, 128), (64, 1, 64, 8, 128), (24, 4, 40, 8, 64), (1 << 14, 1, 1, 1, 64)):
         n = P.si_paged_workspace_bytes(B, S, H, H_kv, D)
         part = S * H * (D + 2) * 4
-        assert n % part == 0 and n // part > B
+        assert (n - 8 * B) % part == 0 and (n - 8 * B) // part > B
         assert n <= 4 * (D + 4) * (131072 + 2 * B * S * H)
     for bad in ((0, 1, 4, 2, 64), (1, 0, 4, 2, 64), (1, 1, 5, 2, 64), (1, 1, 4, 0, 64), (1, 1, 4, 2, 0), ((1 << 14) + 1, 1, 4, 2, 64)):
         assert P.si_paged_workspace_bytes(*bad) == 0
