@@ -28,10 +28,8 @@ namespace si {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
-constexpr int kMinTiles = 2 * kWaves;   // of a chunk
-constexpr int kWorkgroups = 512;        // that fit the chip at once: two a compute unit
+constexpr int kMinTiles = 8;            // of a chunk
+constexpr int kUnits = 256;             // compute units
 constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a tile beyond which the reference is raised
 constexpr int kMaxSequences = 1 << 14;
 
@@ -92,7 +90,8 @@ __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
     high = lane_value(wave_prefix_sum(high), 63);
     const int64_t total = (static_cast<int64_t>(high) << 16) + low;
     auto length_for = [&](int target) {
-        int n_tiles = static_cast<int>(max(static_cast<int64_t>(kMinTiles), (total + target - 1) / target));
+        const int64_t even = (total >> 31) ? (total + target - 1) / target : (static_cast<uint32_t>(total) + target - 1) / target;
+        int n_tiles = static_cast<int>(max(static_cast<int64_t>(kMinTiles), even));
         for (int i = 0; i < 4; ++i) {
             int n = 0;
             for (int b0 = 0; b0 < c.B; b0 += 64) n += b0 + lane < c.B ? max(1, (tiles_at(b0) + n_tiles - 1) / n_tiles) : 0;
@@ -133,8 +132,7 @@ __device__ __forceinline__ float quarters_sum(float x) {
 // Orders the lanes of a wave's LDS accesses for the compiler; the hardware keeps a wave's LDS instructions in order.
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// LDS of a wave: its tiles on the way, each keys, then values, then in 8 bits the scale bytes of either; and weights of a column block, for rows of
-// values that are not finite.
+// A tile on its way in LDS: keys, then values, then in 8 bits the scale bytes of either.
 template <int D, int BITS>
 struct Tile {
     static constexpr int kRowBytes = D * BITS / 8;
@@ -144,7 +142,6 @@ struct Tile {
     static constexpr int kPieces = kRowBytes / 16;                // of a row
     static constexpr int kHalfLoads = kBytes / 2048;              // 1 KB loads of 16 rows
     static constexpr int kLoads = 4 * kHalfLoads + (BITS == 8);   // of a tile
-    static constexpr int kWaveBytes = kRing * kAll + kTileKeys * 16 * 4;
     // Pieces of a row are swizzled so that lanes served together meet different banks: by the row reads of the first product (a piece of rows 0 .. 3 and 8 .. 11,
     // or of 8 rows in a row) and by the transposing reads of the second (two pieces of 4 rows; in 8 bits a piece of 8).
     __device__ static int swizzle(int row) {
@@ -154,12 +151,21 @@ struct Tile {
     }
     __device__ static int place(int row, int piece) { return (row * kPieces + (piece ^ swizzle(row))) * 16; }
 };
+// A workgroup of NB blocks of 16 columns.  With one or two, 4 waves have the queries in registers, and two workgroups share a compute unit.  With four,
+// 64 columns, 8 waves share one copy of the queries in LDS, as a wave's sums take half its registers.
 template <int D, int BITS, int NB>
-constexpr int lds_bytes() {
-    constexpr int kTiles = kWaves * Tile<D, BITS>::kWaveBytes;
-    constexpr int kJoin = kWaves * NB * 16 * (D + 2) * 4;  // sums, reference and sum of weights of each wave
-    return kTiles > kJoin ? kTiles : kJoin;
-}
+struct Group {
+    using T = Tile<D, BITS>;
+    static constexpr bool kSharedQueries = NB == 4;
+    static constexpr int kWaves = NB == 4 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kWaveBytes = T::kRing * T::kAll + 16 * 16 * 4;  // tiles; weights of 16 rows of a block, for values that are not finite
+    static constexpr int kQueries = kWaves * kWaveBytes;                 // where the shared queries begin
+    static constexpr int kAtOnce = NB == 4 ? 1 : NB;                     // blocks that are joined at once
+    static constexpr int kJoin = kWaves * kAtOnce * 16 * (D + 2) * 4;    // sums, reference and sum of weights of each wave
+    static constexpr int kBytes = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);
+    static_assert(kJoin <= kQueries && kBytes <= 160 * 1024, "LDS");
+};
 
 // Starts the loads of 16 rows of keys, or of values: `bytes` bytes from src on, each lane's 16 bytes i at offset[i], to LDS at `to` + 1024 i.
 // What lies at or past `bytes` is not read and lands as zeros.  ONCE: no other workgroup reads the rows, so they need not stay in the caches.
@@ -221,9 +227,12 @@ __device__ __forceinline__ void read_columns(const unsigned (&at)[4], uintx2 (&c
 
 // Grid: (chunks x heads of the cache x column blocks), the blocks of a chunk and head on one XCD.
 template <int D, int BITS, int NB>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__((Group<D, BITS, NB>::kThreads)) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_attention_kernel(Call c) {
     using T = Tile<D, BITS>;
+    using W = Group<D, BITS, NB>;
+    constexpr int kWaves = W::kWaves;
+    constexpr int kThreads = W::kThreads;
     constexpr int KS = D / 32;  // steps along d of the first product
     constexpr int DB = D / 16;  // blocks of 16 rows of O^T
     constexpr int kRing = T::kRing;
@@ -248,8 +257,8 @@ void paged_attention_kernel(Call c) {
     const Rows rows = rows_of(c, b);
     const int first_tile = rows.lo / kTileKeys + (which - chunk.first) * chunk.n_tiles;
     const int last_tile = min(first_tile + chunk.n_tiles, rows.lo / kTileKeys + rows.tiles());
-    const int n_mine = max(0, (last_tile - first_tile - wave + kWaves - 1) / kWaves);  // this wave's tiles: first_tile + wave, then every fourth
-    unsigned char* const ring = lds + wave * T::kWaveBytes;
+    const int n_mine = max(0, (last_tile - first_tile - wave + kWaves - 1) / kWaves);  // this wave's tiles: first_tile + wave, then every kWaves-th
+    unsigned char* const ring = lds + wave * W::kWaveBytes;
     float* const weights_lds = reinterpret_cast<float*>(ring + kRing * T::kAll);
 
     // ---- tiles: 16 + 16 rows, each half in one page.  Lane i has the page of half i of the next 32 tiles.
@@ -310,27 +319,34 @@ void paged_attention_kernel(Call c) {
 
     // queries: lane has column col; step ks of the contraction is d = 32 ks + 8 quarter .. + 7 in 16 bits, and in 8, where a lane reads 16 codes of a row,
     // d = 64 (ks / 2) + 16 quarter + 8 (ks % 2) .. + 7.  A negative scale goes into the query (exact), a scale of 0 makes zeros of it.
-    float to_log2 = __builtin_fabsf(c.scale_log2e);
-    bf16x8 qf[NB][KS];
+    const float to_log2 = c.scale_log2e == 0.0f ? 1.0f : __builtin_fabsf(c.scale_log2e);
+    auto query = [&](int nb, int ks) {
+        const int piece = BITS == 16 ? 4 * ks + quarter : 8 * (ks / 2) + 2 * quarter + ks % 2;
+        uintx4 raw = reinterpret_cast<const uintx4*>(c.q + static_cast<int64_t>(q_row[nb]) * D)[piece];
+        if (c.scale_log2e < 0.0f) raw ^= 0x80008000u;
+        bf16x8 q = __builtin_bit_cast(bf16x8, raw);
+        if (c.scale_log2e == 0.0f)
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const uintx4* const src = reinterpret_cast<const uintx4*>(c.q + static_cast<int64_t>(q_row[nb]) * D);
-        const unsigned sign = c.scale_log2e < 0.0f ? 0x80008000u : 0u;
+            for (int j = 0; j < 8; ++j) q[j] = static_cast<__bf16>(static_cast<float>(q[j]) * 0.0f);
+        return q;
+    };
+    bf16x8 kept[W::kSharedQueries ? 1 : NB][KS];
+    bf16x8* const shared = reinterpret_cast<bf16x8*>(lds + W::kQueries) + lane;  // [nb][ks][lane]
+    if constexpr (W::kSharedQueries) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int piece = BITS == 16 ? 4 * ks + quarter : 8 * (ks / 2) + 2 * quarter + ks % 2;
-            qf[nb][ks] = __builtin_bit_cast(bf16x8, src[piece] ^ sign);
-        }
-    }
-    if (to_log2 == 0.0f) {
-        to_log2 = 1.0f;
+        for (int i = 0; i < NB * KS; ++i)
+            if (i % kWaves == wave) shared[i * 64] = query(i / KS, i % KS);
+        __syncthreads();
+    } else {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) qf[nb][ks][j] = static_cast<__bf16>(static_cast<float>(qf[nb][ks][j]) * 0.0f);
+            for (int ks = 0; ks < KS; ++ks) kept[nb][ks] = query(nb, ks);
     }
+    auto query_of = [&](int nb, int ks) {
+        if constexpr (W::kSharedQueries) return shared[(nb * KS + ks) * 64];
+        else return kept[nb][ks];
+    };
 
     // Row of the tile that score j of a lane is of: half j / 4 of the matrix instruction's rows has, in 16 bits, the tile's rows in order, so that a
     // lane's rows are 4 quarter .. + 3 of either half; in 8 bits rows 8 (r / 4) + 4 (j / 4) + r % 4, so that they are 8 in a row, as the transposing
@@ -361,28 +377,36 @@ void paged_attention_kernel(Call c) {
         const bool masked = live[0] != 0xFFFFFFFFu || s0 < all_from || s0 + kTileKeys > all_to;
 
         floatx4 x[NB][2];
+        float power[2] = {1.0f, 1.0f};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            bf16x8 kf[KS];
-            if constexpr (BITS == 16) {
+            if constexpr (BITS == 8) power[u] = scale_power(tile[2 * T::kBytes + 8 * (col >> 2) + 4 * u + (col & 3)]);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const bf16x8*>(tile + (key_at[u] ^ (64 * ks)));
-            } else {
-                const float power = scale_power(tile[2 * T::kBytes + 8 * (col >> 2) + 4 * u + (col & 3)]);
+            for (int nb = 0; nb < NB; ++nb) x[nb][u] = floatx4{0, 0, 0, 0};
+        }
 #pragma unroll
-                for (int j = 0; j < KS / 2; ++j) {
+        for (int j = 0; j < KS / 2; ++j) {  // two steps at a time, which is what 16 codes are
+            bf16x8 kf[2][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (BITS == 16) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) kf[u][i] = *reinterpret_cast<const bf16x8*>(tile + (key_at[u] ^ (64 * (2 * j + i))));
+                } else {
                     uintx4 two[2];
-                    codes_to_bf16(*reinterpret_cast<const uintx4*>(tile + (key_at[u] ^ (64 * j))), power, two);
-                    kf[2 * j] = __builtin_bit_cast(bf16x8, two[0]);
-                    kf[2 * j + 1] = __builtin_bit_cast(bf16x8, two[1]);
+                    codes_to_bf16(*reinterpret_cast<const uintx4*>(tile + (key_at[u] ^ (64 * j))), power[u], two);
+                    kf[u][0] = __builtin_bit_cast(bf16x8, two[0]);
+                    kf[u][1] = __builtin_bit_cast(bf16x8, two[1]);
                 }
             }
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                x[nb][u] = floatx4{0, 0, 0, 0};
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) x[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], qf[nb][ks], x[nb][u], 0, 0, 0);
-            }
+                for (int nb = 0; nb < NB; ++nb) {
+                    const bf16x8 q = query_of(nb, 2 * j + i);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) x[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][i], q, x[nb][u], 0, 0, 0);
+                }
         }
         uintx2 value_scales = {0, 0};
         if constexpr (BITS == 8) value_scales = *reinterpret_cast<const uintx2*>(tile + 2 * T::kBytes + kTileKeys + 8 * quarter);
@@ -485,28 +509,32 @@ void paged_attention_kernel(Call c) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) weights_lds[row_of(j) * 16 + col] = static_cast<float>(pf[nb][j]);
-                    wave_order();
-#pragma unroll 1
-                    for (int r = 0; r < kTileKeys; ++r) {
-                        const float w = weights_lds[r * 16 + col];
-                        const bool sees = (mine[nb] >> r) & 1;
-                        const unsigned char* const values = tile + T::kBytes;
+                    for (int u = 0; u < 2; ++u) {  // 16 rows at a time: weights j of half u
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            bf16x4 v;
-                            if constexpr (BITS == 16) {
-                                v = *reinterpret_cast<const bf16x4*>(values + T::place(r, 2 * (db0 + i) + quarter / 2) + (quarter & 1) * 8);
-                            } else {
-                                uintx4 out[2];
-                                codes_to_bf16(uintx4{*reinterpret_cast<const unsigned*>(values + T::place(r, db0 + i) + 4 * quarter), 0, 0, 0}, 1.0f, out);
-                                const bf16x8 eight = __builtin_bit_cast(bf16x8, out[0]);
-                                v = bf16x4{eight[0], eight[1], eight[2], eight[3]};
+                        for (int j = 0; j < 4; ++j) weights_lds[(4 * quarter + j) * 16 + col] = static_cast<float>(pf[nb][4 * u + j]);
+                        wave_order();
+#pragma unroll 1
+                        for (int n = 0; n < 16; ++n) {
+                            const int r = BITS == 16 ? 16 * u + n : 8 * (n >> 2) + 4 * u + (n & 3);
+                            const float w = weights_lds[n * 16 + col];
+                            const bool sees = (mine[nb] >> r) & 1;
+                            const unsigned char* const values = tile + T::kBytes;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                bf16x4 v;
+                                if constexpr (BITS == 16) {
+                                    v = *reinterpret_cast<const bf16x4*>(values + T::place(r, 2 * (db0 + i) + quarter / 2) + (quarter & 1) * 8);
+                                } else {
+                                    uintx4 out[2];
+                                    codes_to_bf16(uintx4{*reinterpret_cast<const unsigned*>(values + T::place(r, db0 + i) + 4 * quarter), 0, 0, 0}, 1.0f, out);
+                                    const bf16x8 eight = __builtin_bit_cast(bf16x8, out[0]);
+                                    v = bf16x4{eight[0], eight[1], eight[2], eight[3]};
+                                }
+                                add_not_finite(acc[nb][db0 + i], 0, v, w, sees);
                             }
-                            add_not_finite(acc[nb][db0 + i], 0, v, w, sees);
                         }
+                        wave_order();
                     }
-                    wave_order();
                 }
             }
 #pragma unroll
@@ -521,55 +549,58 @@ void paged_attention_kernel(Call c) {
     }
 
     // ---- the workgroup's waves join: references, then sums
-    __syncthreads();
-    float* const join = reinterpret_cast<float*>(lds);                    // [wave][column][D]
-    float* const join_sums = join + kWaves * NB * 16 * D;                 // [wave][column][2]
+    constexpr int N = W::kAtOnce;                           // blocks of columns
+    float* const join = reinterpret_cast<float*>(lds);      // [wave][column][D]
+    float* const join_sums = join + kWaves * N * 16 * D;    // [wave][column][2]
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int column = nb * 16 + col;
-        const float l = quarters_sum(l_sum[nb]);
-        if (quarter == 0) {
-            join_sums[(wave * NB * 16 + column) * 2] = m_ref[nb];
-            join_sums[(wave * NB * 16 + column) * 2 + 1] = l;
+    for (int nb0 = 0; nb0 < NB; nb0 += N) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int column = i * 16 + col;
+            const float l = quarters_sum(l_sum[nb0 + i]);
+            if (quarter == 0) {
+                join_sums[(wave * N * 16 + column) * 2] = m_ref[nb0 + i];
+                join_sums[(wave * N * 16 + column) * 2 + 1] = l;
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                *reinterpret_cast<floatx4*>(join + (wave * N * 16 + column) * D + (((4 * db + quarter) ^ (col & 7)) * 4)) = acc[nb0 + i][db];
         }
+        __syncthreads();
+        for (int i = threadIdx.x; i < N * 16 * (D / 4); i += kThreads) {
+            const int column = i / (D / 4), piece = i % (D / 4);
+            const int r = (block * NB + nb0) * 16 + column;
+            if (r >= R) continue;
+            float top = -__builtin_huge_valf();
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-            *reinterpret_cast<floatx4*>(join + (wave * NB * 16 + column) * D + (((4 * db + quarter) ^ (col & 7)) * 4)) = acc[nb][db];
-    }
-    __syncthreads();
-    const bool whole = chunk.n == 1;
-    for (int i = threadIdx.x; i < NB * 16 * (D / 4); i += kThreads) {
-        const int column = i / (D / 4), piece = i % (D / 4);
-        const int r = block * NB * 16 + column;
-        if (r >= R) continue;
-        float top = -__builtin_huge_valf();
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_sums[(w * N * 16 + column) * 2]);
+            const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
+            float l = 0.0f;
+            floatx4 o = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_sums[(w * NB * 16 + column) * 2]);
-        const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
-        float l = 0.0f;
-        floatx4 o = {0, 0, 0, 0};
+            for (int w = 0; w < kWaves; ++w) {
+                const float part = join_sums[(w * N * 16 + column) * 2];
+                const float a = part == top ? 1.0f : __builtin_amdgcn_exp2f(part - shift);
+                l += a * join_sums[(w * N * 16 + column) * 2 + 1];
+                o += a * *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
+            }
+            const int position = r / c.G, head = hk * c.G + (r - position * c.G);
+            if (chunk.n == 1) {
+                const int64_t row = (static_cast<int64_t>(b) * c.S + position) * c.H + head;
+                const float inv = top == -__builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
+                bf16x4 v;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float part = join_sums[(w * NB * 16 + column) * 2];
-            const float a = part == top ? 1.0f : __builtin_amdgcn_exp2f(part - shift);
-            l += a * join_sums[(w * NB * 16 + column) * 2 + 1];
-            o += a * *reinterpret_cast<const floatx4*>(join + (w * NB * 16 + column) * D + ((piece ^ (column & 7)) * 4));
-        }
-        const int position = r / c.G, head = hk * c.G + r % c.G;
-        if (whole) {
-            const int64_t row = (static_cast<int64_t>(b) * c.S + position) * c.H + head;
-            const float inv = top == -__builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
-            bf16x4 v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = static_cast<__bf16>(o[j] * inv);
-            *reinterpret_cast<bf16x4*>(c.out + row * D + 4 * piece) = v;
-            if (c.lse && piece == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(top, l);
-        } else {
-            const int64_t row = static_cast<int64_t>(which) * c.S * c.H + position * c.H + head;
-            *reinterpret_cast<floatx4*>(c.parts_out + row * D + 4 * piece) = o;
-            if (piece == 0) {
-                c.parts_sums[row * 2] = top;
-                c.parts_sums[row * 2 + 1] = l;
+                for (int j = 0; j < 4; ++j) v[j] = static_cast<__bf16>(o[j] * inv);
+                *reinterpret_cast<bf16x4*>(c.out + row * D + 4 * piece) = v;
+                if (c.lse && piece == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(top, l);
+            } else {
+                const int64_t row = static_cast<int64_t>(which) * c.S * c.H + position * c.H + head;
+                *reinterpret_cast<floatx4*>(c.parts_out + row * D + 4 * piece) = o;
+                if (piece == 0) {
+                    c.parts_sums[row * 2] = top;
+                    c.parts_sums[row * 2 + 1] = l;
+                }
             }
         }
     }
@@ -655,9 +686,10 @@ struct Shape {
 };
 Shape shape_of(int S, int H, int H_kv) {
     const int R = S * (H / H_kv);
-    const int nb = R <= 16 ? 1 : 2;
+    const int nb = R <= 16 ? 1 : R <= 32 ? 2 : 4;
     const int blocks = (R + 16 * nb - 1) / (16 * nb);
-    return {nb, blocks, std::max(1, (kWorkgroups + H_kv * blocks - 1) / (H_kv * blocks))};
+    const int at_once = nb == 4 ? kUnits : 2 * kUnits;  // workgroups that fit the chip
+    return {nb, blocks, std::max(1, at_once / (H_kv * blocks))};
 }
 
 // Chunks that there may be.
@@ -668,14 +700,14 @@ bool fits(int32_t B, int32_t S, int32_t H) { return H <= 1024 && static_cast<int
 template <int D, int BITS, int NB>
 hipError_t launch(const Call& c, hipStream_t stream) {
     static std::atomic<size_t> allowed[64];
-    constexpr int kBytes = lds_bytes<D, BITS, NB>();
-    hipError_t e = allow_lds(paged_attention_kernel<D, BITS, NB>, kBytes, allowed);
+    using W = Group<D, BITS, NB>;
+    hipError_t e = allow_lds(paged_attention_kernel<D, BITS, NB>, W::kBytes, allowed);
     if (e != hipSuccess) return e;
     const int64_t most_tiles = ((static_cast<int64_t>(c.table_pages) << c.page_lg) + kTileKeys - 1) / kTileKeys;
     const bool one_each = most_tiles <= kMinTiles;  // no sequence can have two chunks
     const int64_t items = static_cast<int64_t>(one_each ? c.B : 2 * c.target + c.B) * c.H_kv;
     const unsigned grid = static_cast<unsigned>((items + 7) / 8 * 8 * c.blocks);
-    hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(kThreads), kBytes, stream, c);
+    hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(W::kThreads), W::kBytes, stream, c);
     e = hipGetLastError();
     if (e != hipSuccess || one_each) return e;
     const int rows = c.B * c.S * c.H;
@@ -723,7 +755,7 @@ si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t
                     scale_log2e, cache->B, S, H, cache->H_kv, H / cache->H_kv, cache->table_pages, cache->n_pages, lg, m, mask_mode, n_win,
                     shape.blocks, shape.target};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-#define SI_LAUNCH(DD, BITS) report(shape.nb == 1 ? launch<DD, BITS, 1>(c, st) : launch<DD, BITS, 2>(c, st))
+#define SI_LAUNCH(DD, BITS) report(shape.nb == 1 ? launch<DD, BITS, 1>(c, st) : shape.nb == 2 ? launch<DD, BITS, 2>(c, st) : launch<DD, BITS, 4>(c, st))
     if (cache->bits == 16) return cache->D == 128 ? SI_LAUNCH(128, 16) : SI_LAUNCH(64, 16);
     return cache->D == 128 ? SI_LAUNCH(128, 8) : SI_LAUNCH(64, 8);
 #undef SI_LAUNCH
