@@ -74,6 +74,9 @@ struct Chunk {
     int n_tiles;  // tiles of a chunk
 };
 
+// Whether sequences may be so many that chunks as long as an even share leave much of the chip idle: a sequence's last chunk costs half of one.
+__host__ __device__ inline bool in_two_rounds(int B, int target) { return 8 * B > target; }
+
 // The chunk with number `which`.  Chunks have as many tiles as it takes for all of them to fit the chip at once; where sequences of different lengths would
 // make that more than a quarter longer than an even share, half as many, twice.  All 64 lanes call it; up to 64 sequences stay in a register.
 __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
@@ -102,7 +105,7 @@ __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
         return n_tiles;
     };
     int n_tiles = length_for(c.target);
-    if (static_cast<int64_t>(n_tiles) * c.target * 4 > 5 * total + 4 * kMinTiles * c.target) n_tiles = length_for(2 * c.target);
+    if (in_two_rounds(c.B, c.target) && static_cast<int64_t>(n_tiles) * c.target * 4 > 5 * total + 4 * kMinTiles * c.target) n_tiles = length_for(2 * c.target);
     int before = 0;
     for (int b0 = 0; b0 < c.B; b0 += 64) {
         const int t = tiles_at(b0);
@@ -163,7 +166,8 @@ struct Group {
     static constexpr int kQueries = kWaves * kWaveBytes;                 // where the shared queries begin
     static constexpr int kAtOnce = NB == 4 ? 1 : NB;                     // blocks that are joined at once
     static constexpr int kJoin = kWaves * kAtOnce * 16 * (D + 2) * 4;    // sums, reference and sum of weights of each wave
-    static constexpr int kBytes = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);
+    static constexpr int kSeen = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);  // where the rows that columns see begin
+    static constexpr int kBytes = kSeen + NB * 16 * 8;
     static_assert(kJoin <= kQueries && kBytes <= 160 * 1024, "LDS");
 };
 
@@ -305,14 +309,14 @@ void paged_attention_kernel(Call c) {
     for (int k = 0; k < kRing; ++k) live[k] = k < n_mine ? request(k) : 0u;
 
     // ---- what the columns see, and what all of them do: from the last position's first row to the first one's last
-    int legal[NB], from[NB], q_row[NB];
-#pragma unroll
+    auto column_of = [&](int nb) { return min((block * NB + nb) * 16 + col, R - 1); };  // columns that there are not repeat the last one
+    auto query_row = [&](int r) { return (b * c.S + r / c.G) * c.H + hk * c.G + r % c.G; };
+    // rows [x, y) that a column sees: every wave writes the same numbers, and reads them where a tile is not seen whole
+    int2* const seen = reinterpret_cast<int2*>(lds + W::kSeen) + col;
+#pragma unroll 1
     for (int nb = 0; nb < NB; ++nb) {
-        const int r = min((block * NB + nb) * 16 + col, R - 1);  // columns that there are not repeat the last one
-        const int i = r / c.G;
-        legal[nb] = legal_rows(first, i, held, c.m, c.mask_mode);
-        from[nb] = max(0, legal[nb] - c.n_win);
-        q_row[nb] = (b * c.S + i) * c.H + hk * c.G + (r - i * c.G);
+        const int legal = legal_rows(first, column_of(nb) / c.G, held, c.m, c.mask_mode);
+        seen[nb * 16] = make_int2(max(0, legal - c.n_win), legal);
     }
     const int all_from = max(0, legal_rows(first, c.S - 1, held, c.m, c.mask_mode) - c.n_win);
     const int all_to = legal_rows(first, 0, held, c.m, c.mask_mode);
@@ -320,9 +324,9 @@ void paged_attention_kernel(Call c) {
     // queries: lane has column col; step ks of the contraction is d = 32 ks + 8 quarter .. + 7 in 16 bits, and in 8, where a lane reads 16 codes of a row,
     // d = 64 (ks / 2) + 16 quarter + 8 (ks % 2) .. + 7.  A negative scale goes into the query (exact), a scale of 0 makes zeros of it.
     const float to_log2 = c.scale_log2e == 0.0f ? 1.0f : __builtin_fabsf(c.scale_log2e);
-    auto query = [&](int nb, int ks) {
+    auto query = [&](int row, int ks) {
         const int piece = BITS == 16 ? 4 * ks + quarter : 8 * (ks / 2) + 2 * quarter + ks % 2;
-        uintx4 raw = reinterpret_cast<const uintx4*>(c.q + static_cast<int64_t>(q_row[nb]) * D)[piece];
+        uintx4 raw = reinterpret_cast<const uintx4*>(c.q + static_cast<int64_t>(row) * D)[piece];
         if (c.scale_log2e < 0.0f) raw ^= 0x80008000u;
         bf16x8 q = __builtin_bit_cast(bf16x8, raw);
         if (c.scale_log2e == 0.0f)
@@ -333,15 +337,16 @@ void paged_attention_kernel(Call c) {
     bf16x8 kept[W::kSharedQueries ? 1 : NB][KS];
     bf16x8* const shared = reinterpret_cast<bf16x8*>(lds + W::kQueries) + lane;  // [nb][ks][lane]
     if constexpr (W::kSharedQueries) {
-#pragma unroll
-        for (int i = 0; i < NB * KS; ++i)
-            if (i % kWaves == wave) shared[i * 64] = query(i / KS, i % KS);
+#pragma unroll 1
+        for (int i = wave; i < NB * KS; i += kWaves) shared[i * 64] = query(query_row(column_of(i / KS)), i % KS);
         __syncthreads();
     } else {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) {
+            const int row = query_row(column_of(nb));
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) kept[nb][ks] = query(nb, ks);
+            for (int ks = 0; ks < KS; ++ks) kept[nb][ks] = query(row, ks);
+        }
     }
     auto query_of = [&](int nb, int ks) {
         if constexpr (W::kSharedQueries) return shared[(nb * KS + ks) * 64];
@@ -359,10 +364,10 @@ void paged_attention_kernel(Call c) {
     const int value_at = BITS == 16 ? T::place(4 * quarter + (col >> 2), (col & 3) / 2) + (col & 1) * 8 : T::place(8 * quarter + (col >> 1), 0) + (col & 1) * 8;
 
     floatx4 acc[NB][DB];
-    float m_ref[NB], l_sum[NB];
+    float shift[NB], l_sum[NB];  // minus the reference; no reference yet makes every weight too large or NaN
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        m_ref[nb] = -__builtin_huge_valf();
+        shift[nb] = __builtin_huge_valf();
         l_sum[nb] = 0.0f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[nb][db] = floatx4{0, 0, 0, 0};
@@ -373,98 +378,125 @@ void paged_attention_kernel(Call c) {
         if (k + kRing <= n_mine) wait_loads<(kRing - 1) * T::kLoads>();
         else wait_loads<0>();
         const int s0 = (first_tile + wave + k * kWaves) * kTileKeys;
-        const unsigned char* const tile = ring + k % kRing * T::kAll;
+        int at_ring = k % kRing * T::kAll;
+        asm volatile("" : "+s"(at_ring));  // addresses in the tile are made where they are needed, not kept in registers through the loop
+        const unsigned char* const tile = ring + at_ring;
         const bool masked = live[0] != 0xFFFFFFFFu || s0 < all_from || s0 + kTileKeys > all_to;
 
         floatx4 x[NB][2];
-        float power[2] = {1.0f, 1.0f};
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if constexpr (BITS == 8) power[u] = scale_power(tile[2 * T::kBytes + 8 * (col >> 2) + 4 * u + (col & 3)]);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) x[nb][u] = floatx4{0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int j = 0; j < KS / 2; ++j) {  // two steps at a time, which is what 16 codes are
-            bf16x8 kf[2][2];
+        auto rows_seen = [&](int nb) {  // of the tile, by this column
+            const int2 r = seen[nb * 16];
+            const int lo = r.x - s0, hi = r.y - s0;
+            unsigned mine = live[0];
+            if (lo > 0) mine &= lo >= kTileKeys ? 0u : ~0u << lo;
+            if (hi < kTileKeys) mine &= hi <= 0 ? 0u : ~0u >> (kTileKeys - hi);
+            return mine;
+        };
+        auto scores = [&]() {
+            float power[2] = {1.0f, 1.0f};
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                if constexpr (BITS == 16) {
+                if constexpr (BITS == 8) power[u] = scale_power(tile[2 * T::kBytes + 8 * (col >> 2) + 4 * u + (col & 3)]);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) kf[u][i] = *reinterpret_cast<const bf16x8*>(tile + (key_at[u] ^ (64 * (2 * j + i))));
-                } else {
-                    uintx4 two[2];
-                    codes_to_bf16(*reinterpret_cast<const uintx4*>(tile + (key_at[u] ^ (64 * j))), power[u], two);
-                    kf[u][0] = __builtin_bit_cast(bf16x8, two[0]);
-                    kf[u][1] = __builtin_bit_cast(bf16x8, two[1]);
-                }
+                for (int nb = 0; nb < NB; ++nb) x[nb][u] = floatx4{0, 0, 0, 0};
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < KS / 2; ++j) {  // two steps at a time, which is what 16 codes are
+                bf16x8 kf[2][2];
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const bf16x8 q = query_of(nb, 2 * j + i);
+                for (int u = 0; u < 2; ++u) {
+                    if constexpr (BITS == 16) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) x[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][i], q, x[nb][u], 0, 0, 0);
+                        for (int i = 0; i < 2; ++i) kf[u][i] = *reinterpret_cast<const bf16x8*>(tile + (key_at[u] ^ (64 * (2 * j + i))));
+                    } else {
+                        uintx4 two[2];
+                        codes_to_bf16(*reinterpret_cast<const uintx4*>(tile + (key_at[u] ^ (64 * j))), power[u], two);
+                        kf[u][0] = __builtin_bit_cast(bf16x8, two[0]);
+                        kf[u][1] = __builtin_bit_cast(bf16x8, two[1]);
+                    }
                 }
-        }
-        uintx2 value_scales = {0, 0};
-        if constexpr (BITS == 8) value_scales = *reinterpret_cast<const uintx2*>(tile + 2 * T::kBytes + kTileKeys + 8 * quarter);
-
-        bf16x8 pf[NB];
-        unsigned mine[NB];  // rows that this column sees
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            mine[nb] = 0xFFFFFFFFu;
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const bf16x8 q = query_of(nb, 2 * j + i);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) x[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][i], q, x[nb][u], 0, 0, 0);
+                    }
+                if (NB == 4) __builtin_amdgcn_sched_barrier(0);  // no operands further ahead: there are no registers for them
+            }
             if (masked) {
-                mine[nb] = live[0];
-                const int lo = from[nb] - s0, hi = legal[nb] - s0;
-                if (lo > 0) mine[nb] &= lo >= kTileKeys ? 0u : ~0u << lo;
-                if (hi < kTileKeys) mine[nb] &= hi <= 0 ? 0u : ~0u >> (kTileKeys - hi);
                 float low = -__builtin_huge_valf();
                 asm volatile("" : "+v"(low));
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (!((mine[nb] >> row_of(j)) & 1)) x[nb][j >> 2][j & 3] = low;
-            }
-            float p[8], sum;
-            auto exponentials = [&]() {
-                const float shift = m_ref[nb] == -__builtin_huge_valf() ? 0.0f : -m_ref[nb];
-                sum = 0.0f;
+                for (int nb = 0; nb < NB; ++nb) {
+                    const unsigned mine = rows_seen(nb) >> row_of(0);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nb][j >> 2][j & 3], to_log2, shift));
-                    sum += p[j];
+                    for (int j = 0; j < 8; ++j)
+                        if (!((mine >> (row_of(j) - row_of(0))) & 1)) x[nb][j >> 2][j & 3] = low;
                 }
-            };
-            exponentials();
-            unsigned long long over = __ballot(!(sum <= kMostWeight) || m_ref[nb] == -__builtin_huge_valf());
-            if (over != 0ull) {
-                over |= over >> 32;
-                over |= over >> 16;  // bit i: column i, in any quarter
+            }
+        };
+        // weights, in place of the scores
+        float sum[NB];
+        auto exponentials = [&](int nb, float by) {
+            sum[nb] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x[nb][j >> 2][j & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nb][j >> 2][j & 3], to_log2, by));
+                sum[nb] += x[nb][j >> 2][j & 3];
+            }
+        };
+        scores();
+        bool over = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            exponentials(nb, shift[nb]);
+            over |= !(sum[nb] <= kMostWeight);
+        }
+        if (__builtin_expect(__ballot(over) != 0ull, 0)) {
+            // the scores again: that costs the few tiles that come here less than keeping them costs all others
+            scores();
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                unsigned long long raise = __ballot(!(sum[nb] <= kMostWeight));
+                raise |= raise >> 32;
+                raise |= raise >> 16;  // bit i: column i, in any quarter
                 float highest = x[nb][0][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) highest = fmaxf(highest, x[nb][j >> 2][j & 3]);
                 highest = quarters_max(highest * to_log2);
-                const float m_new = (over >> col) & 1 ? fmaxf(highest, m_ref[nb]) : m_ref[nb];
-                const float alpha = m_new == m_ref[nb] ? 1.0f : __builtin_amdgcn_exp2f(m_ref[nb] - m_new);
+                const float raised = (raise >> col) & 1 ? fminf(-highest, shift[nb]) : shift[nb];
+                const float alpha = raised == shift[nb] ? 1.0f : __builtin_amdgcn_exp2f(raised - shift[nb]);
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[nb][db] *= alpha;
                 l_sum[nb] *= alpha;
-                m_ref[nb] = m_new;
-                exponentials();
+                shift[nb] = raised;
+                exponentials(nb, raised == __builtin_huge_valf() ? 0.0f : raised);  // a column that has seen nothing yet
             }
-            l_sum[nb] += sum;
-            if constexpr (BITS == 8) {  // the values' powers of two go into the weights: exact
+        }
+        float powers[8];  // of the values: they go into the weights, which is exact
+        if constexpr (BITS == 8) {
+            const unsigned alive = live[0] >> row_of(0);
+            const uintx2 bytes = *reinterpret_cast<const uintx2*>(tile + 2 * T::kBytes + kTileKeys + 8 * quarter);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    p[j] *= scale_power((value_scales[j >> 2] >> (8 * (j & 3))) & 0xFF);
-                    if (masked && !((mine[nb] >> row_of(j)) & 1)) p[j] = 0.0f;  // a row that is not seen may have any scale byte
-                }
+            for (int j = 0; j < 8; ++j) {
+                powers[j] = scale_power((bytes[j >> 2] >> (8 * (j & 3))) & 0xFF);
+                if (masked && !((alive >> j) & 1)) powers[j] = 0.0f;  // a row that nobody sees may have any scale byte
             }
+        }
+        bf16x8 pf[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            l_sum[nb] += sum[nb];
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
-                const bf16x2 two = __builtin_convertvector(floatx2{p[j], p[j + 1]}, bf16x2);
+                float p0 = x[nb][j >> 2][j & 3], p1 = x[nb][j >> 2][(j & 3) + 1];
+                if constexpr (BITS == 8) {
+                    p0 *= powers[j];
+                    p1 *= powers[j + 1];
+                }
+                const bf16x2 two = __builtin_convertvector(floatx2{p0, p1}, bf16x2);
                 pf[nb][j] = two[0];
                 pf[nb][j + 1] = two[1];
             }
@@ -508,6 +540,7 @@ void paged_attention_kernel(Call c) {
                 for (int i = 0; i < 4; ++i) vf[i] = finite_or_zero(vf[i]);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
+                    const unsigned mine = rows_seen(nb);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {  // 16 rows at a time: weights j of half u
 #pragma unroll
@@ -517,7 +550,7 @@ void paged_attention_kernel(Call c) {
                         for (int n = 0; n < 16; ++n) {
                             const int r = BITS == 16 ? 16 * u + n : 8 * (n >> 2) + 4 * u + (n & 3);
                             const float w = weights_lds[n * 16 + col];
-                            const bool sees = (mine[nb] >> r) & 1;
+                            const bool sees = (mine >> r) & 1;
                             const unsigned char* const values = tile + T::kBytes;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
@@ -560,7 +593,7 @@ void paged_attention_kernel(Call c) {
             const int column = i * 16 + col;
             const float l = quarters_sum(l_sum[nb0 + i]);
             if (quarter == 0) {
-                join_sums[(wave * N * 16 + column) * 2] = m_ref[nb0 + i];
+                join_sums[(wave * N * 16 + column) * 2] = -shift[nb0 + i];
                 join_sums[(wave * N * 16 + column) * 2 + 1] = l;
             }
 #pragma unroll
@@ -705,7 +738,9 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     if (e != hipSuccess) return e;
     const int64_t most_tiles = ((static_cast<int64_t>(c.table_pages) << c.page_lg) + kTileKeys - 1) / kTileKeys;
     const bool one_each = most_tiles <= kMinTiles;  // no sequence can have two chunks
-    const int64_t items = static_cast<int64_t>(one_each ? c.B : 2 * c.target + c.B) * c.H_kv;
+    const int64_t chunks = std::min<int64_t>((in_two_rounds(c.B, c.target) ? 2 : 1) * static_cast<int64_t>(c.target) + c.B,
+                                             c.B * ((most_tiles + kMinTiles - 1) / kMinTiles));
+    const int64_t items = chunks * c.H_kv;
     const unsigned grid = static_cast<unsigned>((items + 7) / 8 * 8 * c.blocks);
     hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(W::kThreads), W::kBytes, stream, c);
     e = hipGetLastError();
