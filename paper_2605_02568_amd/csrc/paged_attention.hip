@@ -164,8 +164,8 @@ struct Group {
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kWaveBytes = T::kRing * T::kAll + 16 * 16 * 4;  // tiles; weights of 16 rows of a block, for values that are not finite
     static constexpr int kQueries = kWaves * kWaveBytes;                 // where the shared queries begin
-    static constexpr int kAtOnce = NB == 4 ? 1 : NB;                     // blocks that are joined at once
-    static constexpr int kJoin = kWaves * kAtOnce * 16 * (D + 2) * 4;    // sums, reference and sum of weights of each wave
+    static constexpr int kAtOnce = NB == 4 ? 2 : NB;                     // blocks that are joined at once
+    static constexpr int kJoin = kWaves * (kAtOnce * 16 * D + NB * 16 * 2) * 4;  // sums of each wave; reference and sum of weights
     static constexpr int kSeen = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);  // where the rows that columns see begin
     static constexpr int kBytes = kSeen + NB * 16 * 8;
     static_assert(kJoin <= kQueries && kBytes <= 160 * 1024, "LDS");
@@ -337,9 +337,14 @@ void paged_attention_kernel(Call c) {
     bf16x8 kept[W::kSharedQueries ? 1 : NB][KS];
     bf16x8* const shared = reinterpret_cast<bf16x8*>(lds + W::kQueries) + lane;  // [nb][ks][lane]
     if constexpr (W::kSharedQueries) {
-#pragma unroll 1
-        for (int i = wave; i < NB * KS; i += kWaves) shared[i * 64] = query(query_row(column_of(i / KS)), i % KS);
-        __syncthreads();
+        constexpr int kEach = NB * KS / kWaves;
+        bf16x8 mine[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine[i] = query(query_row(column_of((i * kWaves + wave) / KS)), (i * kWaves + wave) % KS);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) shared[(i * kWaves + wave) * 64] = mine[i];
+        wait_lds();
+        __builtin_amdgcn_s_barrier();
     } else {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -581,59 +586,70 @@ void paged_attention_kernel(Call c) {
         live[kRing - 1] = k + kRing < n_mine ? request(k + kRing) : 0u;
     }
 
-    // ---- the workgroup's waves join: references, then sums
-    constexpr int N = W::kAtOnce;                           // blocks of columns
-    float* const join = reinterpret_cast<float*>(lds);      // [wave][column][D]
-    float* const join_sums = join + kWaves * N * 16 * D;    // [wave][column][2]
+    // ---- the workgroup's waves join: references first, then sums that have them.  The barriers wait for LDS only, not for what goes to memory.
+    auto barrier = [&]() {
+        wait_lds();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    constexpr int N = W::kAtOnce;                                          // blocks of columns
+    float* const join = reinterpret_cast<float*>(lds);                     // [wave][column][D]
+    floatx2* const parts = reinterpret_cast<floatx2*>(join + kWaves * N * 16 * D);  // [column][wave]: minus the reference, sum of weights
+    barrier();  // all tiles have been read
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const float l = quarters_sum(l_sum[nb]);
+        if (quarter == 0) parts[(nb * 16 + col) * kWaves + wave] = floatx2{shift[nb], l};
+    }
+    barrier();
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        float lowest = __builtin_huge_valf();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) lowest = fminf(lowest, parts[(nb * 16 + col) * kWaves + w][0]);
+        const float own = shift[nb] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - shift[nb]);  // shift is the larger one: 0 where it is infinite
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[nb][db] *= own;
+    }
 #pragma unroll
     for (int nb0 = 0; nb0 < NB; nb0 += N) {
-        __syncthreads();
+        if (nb0 > 0) barrier();
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int column = i * 16 + col;
-            const float l = quarters_sum(l_sum[nb0 + i]);
-            if (quarter == 0) {
-                join_sums[(wave * N * 16 + column) * 2] = -shift[nb0 + i];
-                join_sums[(wave * N * 16 + column) * 2 + 1] = l;
-            }
+        for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int db = 0; db < DB; ++db)
-                *reinterpret_cast<floatx4*>(join + (wave * N * 16 + column) * D + (((4 * db + quarter) ^ (col & 7)) * 4)) = acc[nb0 + i][db];
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < N * 16 * (D / 4); i += kThreads) {
+                *reinterpret_cast<floatx4*>(join + (wave * N * 16 + i * 16 + col) * D + (((4 * db + quarter) ^ (col & 7)) * 4)) = acc[nb0 + i][db];
+        barrier();
+#pragma unroll
+        for (int i0 = 0; i0 < N * 16 * (D / 4); i0 += kThreads) {
+            const int i = i0 + static_cast<int>(threadIdx.x);
             const int column = i / (D / 4), piece = i % (D / 4);
             const int r = (block * NB + nb0) * 16 + column;
-            if (r >= R) continue;
-            float top = -__builtin_huge_valf();
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_sums[(w * N * 16 + column) * 2]);
-            const float shift = top == -__builtin_huge_valf() ? 0.0f : top;
-            float l = 0.0f;
+            if (i >= N * 16 * (D / 4) || r >= R) continue;
             floatx4 o = {0, 0, 0, 0};
+            float lowest = __builtin_huge_valf(), l = 0.0f;
+            floatx2 part[kWaves];
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float part = join_sums[(w * N * 16 + column) * 2];
-                const float a = part == top ? 1.0f : __builtin_amdgcn_exp2f(part - shift);
-                l += a * join_sums[(w * N * 16 + column) * 2 + 1];
-                o += a * *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
+                part[w] = parts[(nb0 * 16 + column) * kWaves + w];
+                lowest = fminf(lowest, part[w][0]);
+                o += *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
             }
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) l += part[w][1] * (part[w][0] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - part[w][0]));
             const int position = r / c.G, head = hk * c.G + (r - position * c.G);
             if (chunk.n == 1) {
                 const int64_t row = (static_cast<int64_t>(b) * c.S + position) * c.H + head;
-                const float inv = top == -__builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
+                const float inv = lowest == __builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
                 bf16x4 v;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = static_cast<__bf16>(o[j] * inv);
                 *reinterpret_cast<bf16x4*>(c.out + row * D + 4 * piece) = v;
-                if (c.lse && piece == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(top, l);
+                if (c.lse && piece == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(-lowest, l);
             } else {
                 const int64_t row = static_cast<int64_t>(which) * c.S * c.H + position * c.H + head;
                 *reinterpret_cast<floatx4*>(c.parts_out + row * D + 4 * piece) = o;
-                if (piece == 0) {
-                    c.parts_sums[row * 2] = top;
-                    c.parts_sums[row * 2 + 1] = l;
-                }
+                if (piece == 0) *reinterpret_cast<floatx2*>(c.parts_sums + row * 2) = floatx2{-lowest, l};
             }
         }
     }
