@@ -147,7 +147,7 @@ struct Tile {
     static constexpr int kLoads = 4 * kHalfLoads + (BITS == 8);   // of a tile
     // Pieces of a row are swizzled so that lanes served together meet different banks: by the row reads of the first product (a piece of rows 0 .. 3 and 8 .. 11,
     // or of 8 rows in a row) and by the transposing reads of the second (two pieces of 4 rows; in 8 bits a piece of 8).
-    __device__ static int swizzle(int row) {
+    __device__ static constexpr int swizzle(int row) {
         if constexpr (BITS == 16) return row_swizzle<D>(row);
         if constexpr (D == 128) return ((row >> 1) & 1) | ((row >> 2) & 2) | (row & 4);
         return ((row >> 3) & 1) | ((row >> 1) & 2);
@@ -165,21 +165,22 @@ struct Group {
     static constexpr int kWaveBytes = T::kRing * T::kAll + 16 * 16 * 4;  // tiles; weights of 16 rows of a block, for values that are not finite
     static constexpr int kQueries = kWaves * kWaveBytes;                 // where the shared queries begin
     static constexpr int kAtOnce = NB == 4 ? 2 : NB;                     // blocks that are joined at once
-    static constexpr int kJoin = kWaves * (kAtOnce * 16 * D + NB * 16 * 2) * 4;  // sums of each wave; reference and sum of weights
-    static constexpr int kSeen = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);  // where the rows that columns see begin
-    static constexpr int kBytes = kSeen + NB * 16 * 8;
+    static constexpr int kJoin = kWaves * (kAtOnce * 16 * D + NB * 16 * 2) * 4 + NB * 16 * 8;  // sums of each wave; reference and sum of weights, of each and of all
+    static constexpr int kColumns = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);  // where the columns' table begins
+    static constexpr int kBytes = kColumns + NB * 16 * 16;
     static_assert(kJoin <= kQueries && kBytes <= 160 * 1024, "LDS");
 };
 
-// Starts the loads of 16 rows of keys, or of values: `bytes` bytes from src on, each lane's 16 bytes i at offset[i], to LDS at `to` + 1024 i.
+// Starts the loads of 16 rows of keys, or of values: `bytes` bytes from src on, to LDS at `to`, 1 KB at a time.  A load's rows follow the one's before, so its
+// offset in memory and in LDS is the instruction's, and a lane's place among them, `offset`, changes by the swizzle of the rows' number only.
 // What lies at or past `bytes` is not read and lands as zeros.  ONCE: no other workgroup reads the rows, so they need not stay in the caches.
-template <bool ONCE, int N>
-__device__ __forceinline__ void request_half(const char* src, int bytes, const int (&offset)[N], unsigned char* to) {
+template <typename T, bool ONCE, int I = 0>
+__device__ __forceinline__ void request_half(const char* src, int bytes, int offset, unsigned char* to) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef __attribute__((address_space(3))) void lds_void;
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00020000);
-#pragma unroll
-    for (int i = 0; i < N; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + i * 1024), 16, offset[i], 0, 0, ONCE ? 2 : 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)to, 16, offset ^ (T::swizzle(I * (64 / T::kPieces)) * 16), 0, I * 1024, ONCE ? 2 : 0);
+    if constexpr (I + 1 < T::kHalfLoads) request_half<T, ONCE, I + 1>(src, bytes, offset, to);
 #else
     (void)src; (void)bytes; (void)offset; (void)to;
 #endif
@@ -266,12 +267,7 @@ void paged_attention_kernel(Call c) {
     float* const weights_lds = reinterpret_cast<float*>(ring + kRing * T::kAll);
 
     // ---- tiles: 16 + 16 rows, each half in one page.  Lane i has the page of half i of the next 32 tiles.
-    int offset[T::kHalfLoads];
-#pragma unroll
-    for (int i = 0; i < T::kHalfLoads; ++i) {
-        const int unit = i * 64 + lane, r = unit / T::kPieces;
-        offset[i] = r * T::kRowBytes + ((unit % T::kPieces) ^ T::swizzle(r)) * 16;
-    }
+    const int offset = lane / T::kPieces * T::kRowBytes + ((lane % T::kPieces) ^ T::swizzle(lane / T::kPieces)) * 16;
     int pages = 0;
     const auto request = [&](int k) {  // the wave's tile k, into its place of the ring; returns which rows some position sees
         if (k % 32 == 0) {
@@ -283,6 +279,8 @@ void paged_attention_kernel(Call c) {
         unsigned char* const to = ring + k % kRing * T::kAll;
         int64_t row[2];
         unsigned live = 0;
+        int at = offset;
+        asm volatile("" : "+v"(at));  // the swizzled places are made here, not kept in registers through the loop
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int s = s0 + 16 * u, page = __builtin_amdgcn_readlane(pages, 2 * (k % 32) + u);
@@ -294,8 +292,8 @@ void paged_attention_kernel(Call c) {
             for (int w = 0; w < 2; ++w) {
                 const char* const src = static_cast<const char*>(c.data[w]) + row[u] * T::kRowBytes;
                 unsigned char* const half = to + w * T::kBytes + u * (T::kBytes / 2);
-                if (NB == 1 || c.blocks == 1) request_half<true>(src, n * T::kRowBytes, offset, half);
-                else request_half<false>(src, n * T::kRowBytes, offset, half);
+                if (NB == 1 || c.blocks == 1) request_half<T, true>(src, n * T::kRowBytes, at, half);
+                else request_half<T, false>(src, n * T::kRowBytes, at, half);
             }
         }
         if constexpr (BITS == 8) {  // lanes 0 .. 7 the keys' scale bytes, 8 .. 15 the values'
@@ -309,15 +307,14 @@ void paged_attention_kernel(Call c) {
     for (int k = 0; k < kRing; ++k) live[k] = k < n_mine ? request(k) : 0u;
 
     // ---- what the columns see, and what all of them do: from the last position's first row to the first one's last
-    auto column_of = [&](int nb) { return min((block * NB + nb) * 16 + col, R - 1); };  // columns that there are not repeat the last one
-    auto query_row = [&](int r) { return (b * c.S + r / c.G) * c.H + hk * c.G + r % c.G; };
-    // rows [x, y) that a column sees: every wave writes the same numbers, and reads them where a tile is not seen whole
-    int2* const seen = reinterpret_cast<int2*>(lds + W::kSeen) + col;
-#pragma unroll 1
-    for (int nb = 0; nb < NB; ++nb) {
-        const int legal = legal_rows(first, column_of(nb) / c.G, held, c.m, c.mask_mode);
-        seen[nb * 16] = make_int2(max(0, legal - c.n_win), legal);
+    // a column's query, the rows [y, z) that it sees, and its place among the sequence's results: every wave makes the same table, a lane a column
+    int4* const columns = reinterpret_cast<int4*>(lds + W::kColumns);
+    if (lane < NB * 16) {
+        const int r = min(block * NB * 16 + lane, R - 1), i = r / c.G;  // columns that there are not repeat the last one
+        const int legal = legal_rows(first, i, held, c.m, c.mask_mode);
+        columns[lane] = make_int4(i * c.H + hk * c.G + (r - i * c.G), max(0, legal - c.n_win), legal, 0);
     }
+    wave_order();
     const int all_from = max(0, legal_rows(first, c.S - 1, held, c.m, c.mask_mode) - c.n_win);
     const int all_to = legal_rows(first, 0, held, c.m, c.mask_mode);
 
@@ -326,7 +323,7 @@ void paged_attention_kernel(Call c) {
     const float to_log2 = c.scale_log2e == 0.0f ? 1.0f : __builtin_fabsf(c.scale_log2e);
     auto query = [&](int row, int ks) {
         const int piece = BITS == 16 ? 4 * ks + quarter : 8 * (ks / 2) + 2 * quarter + ks % 2;
-        uintx4 raw = reinterpret_cast<const uintx4*>(c.q + static_cast<int64_t>(row) * D)[piece];
+        uintx4 raw = reinterpret_cast<const uintx4*>(c.q + (static_cast<int64_t>(b) * c.S * c.H + row) * D)[piece];
         if (c.scale_log2e < 0.0f) raw ^= 0x80008000u;
         bf16x8 q = __builtin_bit_cast(bf16x8, raw);
         if (c.scale_log2e == 0.0f)
@@ -340,7 +337,7 @@ void paged_attention_kernel(Call c) {
         constexpr int kEach = NB * KS / kWaves;
         bf16x8 mine[kEach];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) mine[i] = query(query_row(column_of((i * kWaves + wave) / KS)), (i * kWaves + wave) % KS);
+        for (int i = 0; i < kEach; ++i) mine[i] = query(columns[(i * kWaves + wave) / KS * 16 + col].x, (i * kWaves + wave) % KS);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) shared[(i * kWaves + wave) * 64] = mine[i];
         wait_lds();
@@ -348,7 +345,7 @@ void paged_attention_kernel(Call c) {
     } else {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const int row = query_row(column_of(nb));
+            const int row = columns[nb * 16 + col].x;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) kept[nb][ks] = query(row, ks);
         }
@@ -369,10 +366,12 @@ void paged_attention_kernel(Call c) {
     const int value_at = BITS == 16 ? T::place(4 * quarter + (col >> 2), (col & 3) / 2) + (col & 1) * 8 : T::place(8 * quarter + (col >> 1), 0) + (col & 1) * 8;
 
     floatx4 acc[NB][DB];
-    float shift[NB], l_sum[NB];  // minus the reference; no reference yet makes every weight too large or NaN
+    // minus the reference.  It begins as 0, which stays wherever the first tile's weights are neither too large nor too small, as they mostly are; where a
+    // column has seen nothing yet it is infinite, which makes every weight too large or NaN.
+    float shift[NB], l_sum[NB], least = 1.0f / kMostWeight;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        shift[nb] = __builtin_huge_valf();
+        shift[nb] = n_mine > 0 ? 0.0f : __builtin_huge_valf();
         l_sum[nb] = 0.0f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[nb][db] = floatx4{0, 0, 0, 0};
@@ -390,8 +389,8 @@ void paged_attention_kernel(Call c) {
 
         floatx4 x[NB][2];
         auto rows_seen = [&](int nb) {  // of the tile, by this column
-            const int2 r = seen[nb * 16];
-            const int lo = r.x - s0, hi = r.y - s0;
+            const int4 r = columns[nb * 16 + col];
+            const int lo = r.y - s0, hi = r.z - s0;
             unsigned mine = live[0];
             if (lo > 0) mine &= lo >= kTileKeys ? 0u : ~0u << lo;
             if (hi < kTileKeys) mine &= hi <= 0 ? 0u : ~0u >> (kTileKeys - hi);
@@ -457,22 +456,23 @@ void paged_attention_kernel(Call c) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             exponentials(nb, shift[nb]);
-            over |= !(sum[nb] <= kMostWeight);
+            over |= !(sum[nb] <= kMostWeight && sum[nb] >= least);
         }
         if (__builtin_expect(__ballot(over) != 0ull, 0)) {
             // the scores again: that costs the few tiles that come here less than keeping them costs all others
             scores();
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                unsigned long long raise = __ballot(!(sum[nb] <= kMostWeight));
+                unsigned long long raise = __ballot(!(sum[nb] <= kMostWeight && sum[nb] >= least));
                 raise |= raise >> 32;
                 raise |= raise >> 16;  // bit i: column i, in any quarter
                 float highest = x[nb][0][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) highest = fmaxf(highest, x[nb][j >> 2][j & 3]);
                 highest = quarters_max(highest * to_log2);
-                const float raised = (raise >> col) & 1 ? fminf(-highest, shift[nb]) : shift[nb];
-                const float alpha = raised == shift[nb] ? 1.0f : __builtin_amdgcn_exp2f(raised - shift[nb]);
+                // on the first tile the reference may fall, too; there is nothing yet to rescale
+                const float raised = (raise >> col) & 1 ? (k == 0 ? -highest : fminf(-highest, shift[nb])) : shift[nb];
+                const float alpha = k == 0 || raised == shift[nb] ? 1.0f : __builtin_amdgcn_exp2f(raised - shift[nb]);
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[nb][db] *= alpha;
                 l_sum[nb] *= alpha;
@@ -580,6 +580,7 @@ void paged_attention_kernel(Call c) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[nb][db0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[nb], acc[nb][db0 + i], 0, 0, 0);
         }
+        least = 0.0f;
         wait_lds();  // the tile has been read: its place is free
 #pragma unroll
         for (int i = 1; i < kRing; ++i) live[i - 1] = live[i];
@@ -595,6 +596,7 @@ void paged_attention_kernel(Call c) {
     constexpr int N = W::kAtOnce;                                          // blocks of columns
     float* const join = reinterpret_cast<float*>(lds);                     // [wave][column][D]
     floatx2* const parts = reinterpret_cast<floatx2*>(join + kWaves * N * 16 * D);  // [column][wave]: minus the reference, sum of weights
+    floatx2* const all = parts + kWaves * NB * 16;                         // [column]: minus the reference, sum of weights, of all waves
     barrier();  // all tiles have been read
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -605,9 +607,20 @@ void paged_attention_kernel(Call c) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         float lowest = __builtin_huge_valf();
+        floatx2 part[kWaves];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) lowest = fminf(lowest, parts[(nb * 16 + col) * kWaves + w][0]);
-        const float own = shift[nb] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - shift[nb]);  // shift is the larger one: 0 where it is infinite
+        for (int w = 0; w < kWaves; ++w) {
+            part[w] = parts[(nb * 16 + col) * kWaves + w];
+            lowest = fminf(lowest, part[w][0]);
+        }
+        // shift is the larger one: 0 where it is infinite
+        const float own = shift[nb] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - shift[nb]);
+        if (wave == nb % kWaves) {
+            float l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) l += part[w][1] * (part[w][0] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - part[w][0]));
+            if (quarter == 0) all[nb * 16 + col] = floatx2{lowest, l};
+        }
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[nb][db] *= own;
     }
@@ -624,32 +637,25 @@ void paged_attention_kernel(Call c) {
         for (int i0 = 0; i0 < N * 16 * (D / 4); i0 += kThreads) {
             const int i = i0 + static_cast<int>(threadIdx.x);
             const int column = i / (D / 4), piece = i % (D / 4);
-            const int r = (block * NB + nb0) * 16 + column;
-            if (i >= N * 16 * (D / 4) || r >= R) continue;
+            if (i >= N * 16 * (D / 4) || (block * NB + nb0) * 16 + column >= R) continue;
             floatx4 o = {0, 0, 0, 0};
-            float lowest = __builtin_huge_valf(), l = 0.0f;
-            floatx2 part[kWaves];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                part[w] = parts[(nb0 * 16 + column) * kWaves + w];
-                lowest = fminf(lowest, part[w][0]);
-                o += *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
-            }
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) l += part[w][1] * (part[w][0] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - part[w][0]));
-            const int position = r / c.G, head = hk * c.G + (r - position * c.G);
+            for (int w = 0; w < kWaves; ++w) o += *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
+            const floatx2 sums = all[nb0 * 16 + column];
+            const int place = columns[nb0 * 16 + column].x;
             if (chunk.n == 1) {
-                const int64_t row = (static_cast<int64_t>(b) * c.S + position) * c.H + head;
-                const float inv = lowest == __builtin_huge_valf() && l == 0.0f ? 0.0f : 1.0f / l;
+                const int64_t row = static_cast<int64_t>(b) * c.S * c.H + place;
+                const bool none = sums[0] == __builtin_huge_valf() && sums[1] == 0.0f;
+                const float inv = none ? 0.0f : 1.0f / sums[1];
                 bf16x4 v;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = static_cast<__bf16>(o[j] * inv);
                 *reinterpret_cast<bf16x4*>(c.out + row * D + 4 * piece) = v;
-                if (c.lse && piece == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(-lowest, l);
+                if (c.lse && piece == 0) c.lse[row] = none ? -__builtin_huge_valf() : log_of(-sums[0], sums[1]);
             } else {
-                const int64_t row = static_cast<int64_t>(which) * c.S * c.H + position * c.H + head;
+                const int64_t row = static_cast<int64_t>(which) * c.S * c.H + place;
                 *reinterpret_cast<floatx4*>(c.parts_out + row * D + 4 * piece) = o;
-                if (piece == 0) *reinterpret_cast<floatx2*>(c.parts_sums + row * 2) = floatx2{-lowest, l};
+                if (piece == 0) *reinterpret_cast<floatx2*>(c.parts_sums + row * 2) = floatx2{-sums[0], sums[1]};
             }
         }
     }
