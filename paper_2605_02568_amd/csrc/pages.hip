@@ -34,20 +34,55 @@ __device__ __forceinline__ int64_t row_in_pages(const Pages& p, int b, int64_t a
     return ((static_cast<int64_t>(page) * p.H + h) << p.page_lg) + (at & ((1 << p.page_lg) - 1));
 }
 
-// Sequence and position of packed row n; false where it belongs to none.  Lanes of a wave have ascending n.
-__device__ __forceinline__ bool place_of(const Packed& seq, const int32_t* start, int n, int& b, int64_t& at) {
+// Sequences and positions of packed rows n[0], n[1], .. of each lane; b = -1 where a row belongs to none.  first and last are the wave's first and last row.
+template <int PER>
+__device__ __forceinline__ void places_of(const Packed& seq, const int32_t* start, int first, int last, const int (&n)[PER], int (&b)[PER], int64_t (&at)[PER]) {
     if (!seq.offsets) {
         const int per = seq.N / seq.B;
-        b = n / per;
-        at = n - static_cast<int64_t>(b) * per;
-    } else {
-        b = last_not_above(seq.B, __builtin_amdgcn_readfirstlane(n), [&](int i) { return static_cast<int64_t>(seq.offsets[i]); });
-        while (b + 1 < seq.B && seq.offsets[b + 1] <= n) ++b;
-        at = static_cast<int64_t>(n) - seq.offsets[b];
-        if (at < 0 || n >= seq.offsets[b + 1]) return false;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            b[j] = n[j] / per;
+            at[j] = n[j] - static_cast<int64_t>(b[j]) * per + (start ? start[b[j]] : 0);
+        }
+        return;
     }
-    at += start ? start[b] : 0;
-    return true;
+    const int b0 = last_not_above(seq.B, first, [&](int i) { return static_cast<int64_t>(seq.offsets[i]); });
+    const int from = seq.offsets[b0], to = seq.offsets[b0 + 1];
+    if (from <= first && last < to) {  // all of the same sequence, as nearly all waves are
+        const int64_t shift = static_cast<int64_t>(start ? start[b0] : 0) - from;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            b[j] = b0;
+            at[j] = n[j] + shift;
+        }
+        return;
+    }
+    // of several: the offsets behind b0's come 64 at a time, a lane each, and all rows are compared with one after the other
+    const int lane = threadIdx.x & 63;
+    int mine_from[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        b[j] = b0;
+        mine_from[j] = from;
+    }
+    for (int i0 = b0 + 1, n_below = 64; n_below == 64; i0 += 64) {
+        const int offset = i0 + lane < seq.B ? seq.offsets[i0 + lane] : 0x7FFFFFFF;
+        n_below = static_cast<int>(__popcll(__ballot(offset <= last)));
+        for (int i = 0; i < n_below; ++i) {
+            const int o = __builtin_amdgcn_readlane(offset, i);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                mine_from[j] = o <= n[j] ? o : mine_from[j];
+                b[j] = o <= n[j] ? i0 + i : b[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int mine_to = seq.offsets[b[j] + 1], mine_start = start ? start[b[j]] : 0;
+        at[j] = static_cast<int64_t>(n[j]) - mine_from[j] + mine_start;
+        if (n[j] < mine_from[j] || n[j] >= mine_to) b[j] = -1;
+    }
 }
 
 // Biased exponent of a row whose largest magnitude has the bf16 bits `top`: with |x| = 1.f * 2^E, the least e with |x| <= 448 * 2^e = 1.75 * 2^(8 + e) is
@@ -56,74 +91,114 @@ __device__ __forceinline__ int row_exponent(int top) {
     return min(max(((top + 0x1F) >> 7) - 8, 127 + kLowestExponent), 127 + kHighestExponent);
 }
 
-// Thread: 8 values.  Workgroup: kThreads / (D / 8) rows of one head of the keys or of the values (blockIdx.y: tensor and head).
-template <int D, int BITS>
+// A thread takes 8 values of PER rows, a wave PER * 64 / (D / 8) rows in a row of one head of the keys or of the values (blockIdx.y: tensor and head).  Many rows
+// take 4: enough on its way to make up for the trips to the offsets and the table before it (16 prompts of 33,000 rows of 8 heads, 8 bits: in 72 -> 58 us, out
+// 47 -> 33).  Where that would be less than a wave a SIMD, 1: a wave's rows are then of fewer sequences (one row of each of 64: 6.5 -> 3.6 us).
+template <int D, int PER>
+struct Share {
+    static constexpr int kUnits = D / 8;             // threads of a row
+    static constexpr int kStep = 64 / kUnits;        // rows of a wave's load
+    static constexpr int kWaveRows = PER * kStep;
+    static constexpr int kRows = kThreads / 64 * kWaveRows;
+    int piece, h, which, first, last;
+    int n[PER], b[PER];
+    int64_t at[PER];
+    bool there[PER];  // such a row is in the call
+    __device__ __forceinline__ Share(const Packed& seq, int H) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        h = blockIdx.y % H;
+        which = blockIdx.y / H;
+        piece = lane % kUnits;
+        const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + wave * kWaveRows;
+        first = static_cast<int>(min(row, static_cast<int64_t>(seq.N) - 1));
+        last = static_cast<int>(min(row + kWaveRows, static_cast<int64_t>(seq.N)) - 1);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            n[j] = min(first + j * kStep + lane / kUnits, seq.N - 1);
+            there[j] = row + j * kStep + lane / kUnits < seq.N;
+        }
+    }
+};
+
+template <int D, int BITS, int kPer>
 __global__ __launch_bounds__(kThreads) void store_pages_kernel(const uintx4* __restrict__ k_rows, const uintx4* __restrict__ v_rows, Packed seq,
                                                                const int32_t* __restrict__ start, Pages pages) {
     constexpr int kUnits = D / 8;
-    const int h = blockIdx.y % pages.H, which = blockIdx.y / pages.H;
-    const int piece = threadIdx.x % kUnits;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / kUnits) + threadIdx.x / kUnits;
-    const int n = static_cast<int>(min(row, static_cast<int64_t>(seq.N) - 1));
-    const uintx4 x = (which ? v_rows : k_rows)[(static_cast<int64_t>(n) * pages.H + h) * kUnits + piece];
-    int b;
-    int64_t at;
-    const bool there = place_of(seq, start, n, b, at) && row < seq.N;
-    const int64_t to = there ? row_in_pages(pages, b, at, h) : -1;
-    if constexpr (BITS == 16) {
-        if (to >= 0) static_cast<uintx4*>(pages.data[which])[to * kUnits + piece] = x;
-    } else {
-        constexpr int kLargest = ((127 + 8 + kHighestExponent) << 7) | 0x60;  // 448 * 2^63
-        int top = 0;
-        uintx4 y = x;
+    Share<D, kPer> s(seq, pages.H);
+    const uintx4* const rows = (s.which ? v_rows : k_rows) + static_cast<int64_t>(s.h) * kUnits + s.piece;
+    uintx4 x[kPer];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int lo = x[j] & 0x7FFF, hi = (x[j] >> 16) & 0x7FFF;
-            top = max(top, lo > 0x7F80 ? 0 : lo);  // a NaN does not count
-            top = max(top, hi > 0x7F80 ? 0 : hi);
-            y[j] = (x[j] & 0x80008000u) | (lo > 0x7F80 ? lo : min(lo, kLargest)) | ((hi > 0x7F80 ? hi : min(hi, kLargest)) << 16);
+    for (int j = 0; j < kPer; ++j) x[j] = rows[static_cast<int64_t>(s.n[j]) * pages.H * kUnits];
+    places_of(seq, start, s.first, s.last, s.n, s.b, s.at);
+    int64_t to[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) to[j] = s.there[j] && s.b[j] >= 0 ? row_in_pages(pages, s.b[j], s.at[j], s.h) : -1;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if constexpr (BITS == 16) {
+            if (to[i] >= 0) static_cast<uintx4*>(pages.data[s.which])[to[i] * kUnits + s.piece] = x[i];
+        } else {
+            constexpr int kLargest = ((127 + 8 + kHighestExponent) << 7) | 0x60;  // 448 * 2^63
+            int top = 0;
+            uintx4 y = x[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int lo = y[j] & 0x7FFF, hi = (y[j] >> 16) & 0x7FFF;
+                top = max(top, lo > 0x7F80 ? 0 : lo);  // a NaN does not count
+                top = max(top, hi > 0x7F80 ? 0 : hi);
+                y[j] = (y[j] & 0x80008000u) | (lo > 0x7F80 ? lo : min(lo, kLargest)) | ((hi > 0x7F80 ? hi : min(hi, kLargest)) << 16);
+            }
+#pragma unroll
+            for (int j = 1; j < kUnits; j *= 2) top = max(top, __shfl_xor(top, j));
+            if (to[i] < 0) continue;
+            const int e = row_exponent(top);
+            const float power = scale_power(e);
+            const bf16x8 v = __builtin_bit_cast(bf16x8, y);
+            shortx2 lo = {0, 0}, hi = {0, 0};
+            lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, bf16x2{v[0], v[1]}, power, false);
+            lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, bf16x2{v[2], v[3]}, power, true);
+            hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, bf16x2{v[4], v[5]}, power, false);
+            hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, bf16x2{v[6], v[7]}, power, true);
+            static_cast<uintx2*>(pages.data[s.which])[to[i] * kUnits + s.piece] = uintx2{__builtin_bit_cast(unsigned, lo), __builtin_bit_cast(unsigned, hi)};
+            if (s.piece == 0) pages.scales[s.which][to[i]] = static_cast<unsigned char>(e);
         }
-#pragma unroll
-        for (int i = 1; i < kUnits; i *= 2) top = max(top, __shfl_xor(top, i));
-        if (to < 0) return;
-        const int e = row_exponent(top);
-        const float power = scale_power(e);
-        const bf16x8 v = __builtin_bit_cast(bf16x8, y);
-        shortx2 lo = {0, 0}, hi = {0, 0};
-        lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, bf16x2{v[0], v[1]}, power, false);
-        lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, bf16x2{v[2], v[3]}, power, true);
-        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, bf16x2{v[4], v[5]}, power, false);
-        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, bf16x2{v[6], v[7]}, power, true);
-        static_cast<uintx2*>(pages.data[which])[to * kUnits + piece] = uintx2{__builtin_bit_cast(unsigned, lo), __builtin_bit_cast(unsigned, hi)};
-        if (piece == 0) pages.scales[which][to] = static_cast<unsigned char>(e);
     }
 }
 
-template <int D, int BITS>
+template <int D, int BITS, int kPer>
 __global__ __launch_bounds__(kThreads) void load_pages_kernel(uintx4* __restrict__ k_rows, uintx4* __restrict__ v_rows, Packed seq,
                                                               const int32_t* __restrict__ start, Pages pages) {
     constexpr int kUnits = D / 8;
-    const int h = blockIdx.y % pages.H, which = blockIdx.y / pages.H;
-    const int piece = threadIdx.x % kUnits;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / kUnits) + threadIdx.x / kUnits;
-    const int n = static_cast<int>(min(row, static_cast<int64_t>(seq.N) - 1));
-    uintx4* const rows = which ? v_rows : k_rows;
-    int b;
-    int64_t at;
-    if (!place_of(seq, start, n, b, at) || row >= seq.N || !rows) return;
-    const int64_t from = row_in_pages(pages, b, at, h);
-    uintx4 x = {0, 0, 0, 0};
-    if (from >= 0) {
-        if constexpr (BITS == 16) {
-            x = static_cast<const uintx4*>(pages.data[which])[from * kUnits + piece];
-        } else {
-            const uintx2 codes = static_cast<const uintx2*>(pages.data[which])[from * kUnits + piece];
-            uintx4 out[2];
-            codes_to_bf16(uintx4{codes[0], codes[1], 0, 0}, scale_power(pages.scales[which][from]), out);
-            x = out[0];
+    Share<D, kPer> s(seq, pages.H);
+    uintx4* const rows = s.which ? v_rows : k_rows;
+    if (!rows) return;
+    places_of(seq, start, s.first, s.last, s.n, s.b, s.at);
+    uintx4 x[kPer];
+    unsigned power[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int64_t from = s.b[j] >= 0 ? row_in_pages(pages, s.b[j], s.at[j], s.h) : -1;
+        x[j] = uintx4{0, 0, 0, 0};
+        power[j] = 127;
+        if (from >= 0) {
+            if constexpr (BITS == 16) {
+                x[j] = static_cast<const uintx4*>(pages.data[s.which])[from * kUnits + s.piece];
+            } else {
+                const uintx2 codes = static_cast<const uintx2*>(pages.data[s.which])[from * kUnits + s.piece];
+                x[j] = uintx4{codes[0], codes[1], 0, 0};
+                power[j] = pages.scales[s.which][from];
+            }
         }
     }
-    rows[(static_cast<int64_t>(n) * pages.H + h) * kUnits + piece] = x;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if constexpr (BITS == 8) {
+            uintx4 out[2];
+            codes_to_bf16(x[j], scale_power(power[j]), out);
+            x[j] = out[0];
+        }
+        if (s.there[j] && s.b[j] >= 0) rows[(static_cast<int64_t>(s.n[j]) * pages.H + s.h) * kUnits + s.piece] = x[j];
+    }
 }
 
 si_status check_rows(const si_paged_cache* cache, int32_t N, const int32_t* offsets, const int32_t* start, const void* k_rows, const void* v_rows) {
@@ -142,8 +217,13 @@ Pages pages_of(const si_paged_cache& c) {
     return {{c.K, c.V}, {static_cast<unsigned char*>(c.K_scales), static_cast<unsigned char*>(c.V_scales)}, c.table, c.table_pages, c.n_pages, lg, c.H_kv};
 }
 
+// Rows a thread takes, and the grid of it.
+int rows_a_thread(const si_paged_cache& c, int32_t N, bool values) {
+    constexpr int kSimds = 1024;
+    return static_cast<int64_t>(N) * c.H_kv * (values ? 2 : 1) * (c.D / 8) >= int64_t{4} * 64 * kSimds ? 4 : 1;
+}
 dim3 grid_for(const si_paged_cache& c, int32_t N, bool values) {
-    const int rows = kThreads / (c.D / 8);
+    const int rows = kThreads / (c.D / 8) * rows_a_thread(c, N, values);
     return dim3(static_cast<unsigned>((static_cast<int64_t>(N) + rows - 1) / rows), static_cast<unsigned>(c.H_kv * (values ? 2 : 1)));
 }
 
@@ -161,19 +241,30 @@ si_status si_store_pages(const void* k_rows, const void* v_rows, int32_t N, cons
     if (ok == SI_ERR_INVALID_ARG) return ok;
     if (!k_rows || (cache->V && !v_rows)) return SI_ERR_INVALID_ARG;
     if (ok != SI_OK) return ok;
+    const int per = rows_a_thread(*cache, N, cache->V != nullptr);
     const dim3 grid = grid_for(*cache, N, cache->V != nullptr);
     const Packed seq = {offsets, cache->B, N};
 #define SI_LAUNCH(DD, BITS)                                                                                                          \
-    hipLaunchKernelGGL((store_pages_kernel<DD, BITS>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                    \
+    if (per == 4) SI_LAUNCH_PER(DD, BITS, 4);                                                                                        \
+    else SI_LAUNCH_PER(DD, BITS, 1)
+#define SI_LAUNCH_PER(DD, BITS, PER)                                                                                                 \
+    hipLaunchKernelGGL((store_pages_kernel<DD, BITS, PER>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                    \
                        static_cast<const uintx4*>(k_rows), static_cast<const uintx4*>(v_rows), seq, start, pages_of(*cache))
     if (cache->bits == 16) {
-        if (cache->D == 128) SI_LAUNCH(128, 16);
-        else SI_LAUNCH(64, 16);
+        if (cache->D == 128) {
+            SI_LAUNCH(128, 16);
+        } else {
+            SI_LAUNCH(64, 16);
+        }
     } else {
-        if (cache->D == 128) SI_LAUNCH(128, 8);
-        else SI_LAUNCH(64, 8);
+        if (cache->D == 128) {
+            SI_LAUNCH(128, 8);
+        } else {
+            SI_LAUNCH(64, 8);
+        }
     }
 #undef SI_LAUNCH
+#undef SI_LAUNCH_PER
     return report(hipGetLastError());
 }
 
@@ -183,19 +274,30 @@ si_status si_load_pages(const si_paged_cache* cache, int32_t N, const int32_t* o
     if (ok == SI_ERR_INVALID_ARG) return ok;
     if ((!k_rows && !v_rows) || (v_rows && !cache->V)) return SI_ERR_INVALID_ARG;
     if (ok != SI_OK) return ok;
+    const int per = rows_a_thread(*cache, N, v_rows != nullptr);
     const dim3 grid = grid_for(*cache, N, v_rows != nullptr);
     const Packed seq = {offsets, cache->B, N};
 #define SI_LAUNCH(DD, BITS)                                                                                                          \
-    hipLaunchKernelGGL((load_pages_kernel<DD, BITS>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                     \
+    if (per == 4) SI_LAUNCH_PER(DD, BITS, 4);                                                                                        \
+    else SI_LAUNCH_PER(DD, BITS, 1)
+#define SI_LAUNCH_PER(DD, BITS, PER)                                                                                                 \
+    hipLaunchKernelGGL((load_pages_kernel<DD, BITS, PER>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                     \
                        static_cast<uintx4*>(k_rows), static_cast<uintx4*>(v_rows), seq, start, pages_of(*cache))
     if (cache->bits == 16) {
-        if (cache->D == 128) SI_LAUNCH(128, 16);
-        else SI_LAUNCH(64, 16);
+        if (cache->D == 128) {
+            SI_LAUNCH(128, 16);
+        } else {
+            SI_LAUNCH(64, 16);
+        }
     } else {
-        if (cache->D == 128) SI_LAUNCH(128, 8);
-        else SI_LAUNCH(64, 8);
+        if (cache->D == 128) {
+            SI_LAUNCH(128, 8);
+        } else {
+            SI_LAUNCH(64, 8);
+        }
     }
 #undef SI_LAUNCH
+#undef SI_LAUNCH_PER
     return report(hipGetLastError());
 }
 
