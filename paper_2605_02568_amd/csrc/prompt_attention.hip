@@ -28,7 +28,6 @@ namespace si {
 
 namespace {
 
-constexpr int kRows = 64;               // of a tile
 constexpr int kSlots = 3;               // tiles in LDS: two in use, one on its way
 constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a block beyond which the reference is raised,
 constexpr float kMostShift = 8.0f;      // or where the maximum is known, its distance from the reference in log2 units
@@ -59,7 +58,6 @@ __device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v,
     constexpr int kStep = 64 / (D / 8);
     const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(k), 0, bytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(v), 0, bytes, 0x00020000);
-    asm volatile("" : "+v"(offset));  // the places of the further pieces are made here, not kept in registers
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         const int at = (offset ^ (row_swizzle<D>(i * kStep) * 16)) + i * kStep * stride;
@@ -71,12 +69,26 @@ __device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v,
 #endif
 }
 
-template <int D, int kWaves>
+// Both halves' values: of the exchange's two results one carries the lower half-wave's in both halves, the other the higher one's.
+__device__ __forceinline__ floatx2 both_halves(float x) {
+    const unsigned bits = __builtin_bit_cast(unsigned, x);
+    const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    const unsigned low = both[0], high = both[1];  // not cast as they are: a cast of either element takes the first
+    return floatx2{__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+// The lane's number where it is not worth a register through the loop.
+__device__ __forceinline__ int lane_again() {
+    int lane;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    return lane;
+}
+
+template <int D, int kWaves, int kRows>
 constexpr int lds_bytes() { return kSlots * 2 * kRows * D * 2 + kWaves * 32 * 32 * 4; }  // tiles of keys and values; weights of a block a wave
 
 // Grid: (slots of columns, the last ones first) x heads of keys and values, heads next to each other so that with 8 of them each has an XCD.  A sequence's
 // slots begin at (its first packed column) / 256 + (its number): slots enough for any lengths, with no sum over the sequences before.
-template <int D, int kWaves>
+template <int D, int kWaves, int kRows>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void prompt_attention_kernel(Call c) {
     constexpr int kColumns = 32 * kWaves;  // of a workgroup
@@ -128,13 +140,13 @@ void prompt_attention_kernel(Call c) {
 
     // ---- a tile's keys and values, by 1 KiB pieces of LDS; rows at or past the last one that anybody sees land as zeros
     const int stride = c.H_kv * kRowBytes;
-    static_assert((kLoads & (kLoads - 1)) == 0, "a load's number and a wave's first row share no bits");
-    const int first_row = wave * kLoads * (64 / kPieces) + lane / kPieces;
-    const int lane_offset = first_row * stride + ((lane % kPieces) ^ row_swizzle<D>(first_row)) * 16;
+    static_assert(kLoads > 0 && (kLoads & (kLoads - 1)) == 0, "a load's number and a wave's first row share no bits");
     auto request = [&](int s0, int buffer) {
         const int n = min(kRows, end - s0);
         const int bytes = (n - 1) * stride + kRowBytes;
         const int64_t at = (static_cast<int64_t>(k_first + s0) * c.H_kv + hk) * D;
+        const int lane2 = lane_again(), first_row = wave * kLoads * (64 / kPieces) + lane2 / kPieces;
+        const int lane_offset = first_row * stride + ((lane2 % kPieces) ^ row_swizzle<D>(first_row)) * 16;
         request_pieces<D, kLoads>(c.K + at, c.V ? c.V + at : nullptr, bytes, lane_offset, stride, lds + buffer * 2 * kTileBytes + wave * kLoads * 1024, kTileBytes);
     };
     if (begin < end) request(begin, 0);
@@ -176,8 +188,9 @@ void prompt_attention_kernel(Call c) {
     };
     // The reference of the columns in `over` (bit i: column i) becomes at least `highest`, in log2 units.
     auto raise = [&](unsigned over, float highest) {
-        highest = fmaxf(highest, other_half(highest));
-        const float raised = (over >> col) & 1 ? fminf(-highest, shift) : shift;
+        const floatx2 of_halves = both_halves(highest);
+        highest = fmaxf(of_halves[0], of_halves[1]);
+        const float raised = (over >> (lane_again() & 31)) & 1 ? fminf(-highest, shift) : shift;
         const float alpha = raised == shift ? 1.0f : __builtin_amdgcn_exp2f(raised - shift);
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] *= alpha;
@@ -328,10 +341,10 @@ void prompt_attention_kernel(Call c) {
             pf[0] = pf[1] = vf[0];
 #pragma unroll 1
             for (;;) {
-                step(tile, tile + 32 * kRowBytes);
+                if constexpr (kRows == 64) step(tile, tile + 32 * kRowBytes);
                 s0 += kRows;
                 const int next = s0 < whole_to ? arrive(s0) : tile;  // behind the last block the scores are not used
-                step(tile + 32 * kRowBytes, next);
+                step(tile + (kRows - 32) * kRowBytes, next);
                 if (s0 >= whole_to) break;
                 tile = next;
             }
@@ -344,11 +357,19 @@ void prompt_attention_kernel(Call c) {
 
     // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4.  64 d of the wave's columns go through its own LDS, so that the results are
     // written by whole lines: 8 bytes a lane and 32 rows at once they took 1.7 us in place of EPILOGUE.
-    const float l = l_sum + other_half(l_sum);
+    const floatx2 l_halves = both_halves(l_sum);
+    const float l = l_halves[0] + l_halves[1];
     const bool none = m_ref == -__builtin_huge_valf() && l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
-    const int left = n_columns - static_cast<int>(r0) - wave * 32;  // columns that there are
-    if (c.lse && half == 0 && col < left) c.lse[q_row] = none ? -__builtin_huge_valf() : log_of(m_ref, l);
+    int r_first = static_cast<int>(r0) + wave * 32;
+    const int lane2 = lane_again(), col2 = lane2 & 31, half2 = lane2 >> 5;
+    asm volatile("" : "+s"(r_first));  // places are made again here, not kept in registers through the loop
+    const int left = n_columns - r_first;  // columns that there are
+    auto row_of = [&](int r) {  // of the results, for column r
+        const int i_query = r / c.G;
+        return static_cast<int64_t>(q_first + i_query) * c.H + hk * c.G + (r - i_query * c.G);
+    };
+    if (c.lse && half2 == 0 && col2 < left) c.lse[row_of(r_first + col2)] = none ? -__builtin_huge_valf() : log_of(m_ref, l);
     unsigned char* const mine = lds + kSlots * 2 * kTileBytes + wave * (32 * 32 * 4);
 #pragma unroll
     for (int db0 = 0; db0 < DB; db0 += 2) {
@@ -360,38 +381,46 @@ void prompt_attention_kernel(Call c) {
                 bf16x4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = static_cast<__bf16>(acc[db0 + i][4 * a + e] * inv);
-                *reinterpret_cast<bf16x4*>(mine + col * 128 + (((4 * i + a) ^ (col & 7)) * 16) + half * 8) = v;
+                *reinterpret_cast<bf16x4*>(mine + col2 * 128 + (((4 * i + a) ^ (col2 & 7)) * 16) + half2 * 8) = v;
             }
         wave_order();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = 8 * i + lane / 8, piece = lane % 8;
+            const int row = 8 * i + lane2 / 8, piece = lane2 % 8;
             const uintx4 v = *reinterpret_cast<const uintx4*>(mine + row * 128 + ((piece ^ (row & 7)) * 16));
-            const int r = static_cast<int>(r0) + wave * 32 + row, i_query = r / c.G;
-            if (row < left)
-                *reinterpret_cast<uintx4*>(c.out + (static_cast<int64_t>(q_first + i_query) * c.H + hk * c.G + (r - i_query * c.G)) * D + 32 * db0 + 8 * piece) = v;
+            if (row < left) *reinterpret_cast<uintx4*>(c.out + row_of(r_first + row) * D + 32 * db0 + 8 * piece) = v;
         }
     }
 }
 
-template <int D, int kWaves>
+template <int D, int kWaves, int kRows>
 hipError_t launch(Call c, int64_t n_columns, hipStream_t stream) {
     static std::atomic<size_t> allowed[64];
-    constexpr int kBytes = lds_bytes<D, kWaves>();
-    const hipError_t e = allow_lds(prompt_attention_kernel<D, kWaves>, kBytes, allowed);
+    constexpr int kBytes = lds_bytes<D, kWaves, kRows>();
+    const hipError_t e = allow_lds(prompt_attention_kernel<D, kWaves, kRows>, kBytes, allowed);
     if (e != hipSuccess) return e;
     c.slots = static_cast<int>(n_columns / (32 * kWaves) + c.queries.B);
-    hipLaunchKernelGGL((prompt_attention_kernel<D, kWaves>), dim3(static_cast<unsigned>(c.slots) * c.H_kv), dim3(64 * kWaves), kBytes, stream, c);
+    hipLaunchKernelGGL((prompt_attention_kernel<D, kWaves, kRows>), dim3(static_cast<unsigned>(c.slots) * c.H_kv), dim3(64 * kWaves), kBytes, stream, c);
     return hipGetLastError();
 }
 
-// 256 columns a workgroup share a tile; where they would leave half of the chip without a workgroup, 128 (512 queries, 64 heads on 8 of 128: 24.8 -> 20.3 us; with
-// twice as many queries both take 38.5, with 2048 88 against 110).
+// Heads of 64: 128 columns a workgroup and tiles of 32 rows, so that three workgroups share a compute unit and one's start and end go by beside the others' products
+// (23 prompts of up to 1,500, 33 heads on 3: 163 us; 256 columns and 64 rows: 177; 8,192 queries, 64 heads on 8: 617 against 636).
+// Heads of 128: 256 columns and 64 rows, which load a tile for twice as many products (8,192 queries, 64 heads on 8: 1,003 us; the smaller form 1,059).  Where
+// that would be fewer workgroups than compute units, the smaller form, two a unit (1,024 queries: 36.9 -> 34.7 us); and where it would be fewer than half as
+// many, 128 columns and 64 rows, of which one fits a unit, so that they spread (512 queries behind 8,192: 198 us in the smaller form, 173 in this).
 template <int D>
 hipError_t launch(const Call& c, hipStream_t stream) {
     constexpr int kUnits = 256;
     const int64_t n_columns = static_cast<int64_t>(c.queries.N) * c.G;
-    return n_columns / 256 * c.H_kv <= kUnits / 2 ? launch<D, 4>(c, n_columns, stream) : launch<D, 8>(c, n_columns, stream);
+    if constexpr (D == 64) {
+        return launch<D, 4, 32>(c, n_columns, stream);
+    } else {
+        const int64_t workgroups = n_columns / 256 * c.H_kv;
+        if (workgroups <= kUnits / 2) return launch<D, 4, 64>(c, n_columns, stream);
+        if (workgroups <= kUnits) return launch<D, 4, 32>(c, n_columns, stream);
+        return launch<D, 8, 64>(c, n_columns, stream);
+    }
 }
 
 }  // namespace
@@ -415,11 +444,9 @@ si_status si_prompt_attention(const void* q, const void* K, const void* V, const
     if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return SI_ERR_INVALID_ARG;
     if (!aligned4(q_offsets) || !aligned4(k_offsets) || !aligned4(first) || !aligned4(lse)) return SI_ERR_INVALID_ARG;
     if ((d.D != 64 && d.D != 128) || d.H > 1024 || d.N_q > (1 << 30) || d.N_k > (1 << 30) || d.B > (1 << 20) ||
-        (static_cast<int64_t>(d.N_q) + d.B) * d.H >= (1 << 30))
+        static_cast<int64_t>(d.N_q) * d.H + int64_t{128} * d.B * d.H_kv >= (1 << 30))  // a launch has fewer than 2^32 threads
         return SI_ERR_UNSUPPORTED_SHAPE;
     const int G = d.H / d.H_kv;
-    const int64_t slots = static_cast<int64_t>(d.N_q) * G / 256 + d.B;
-    if (slots * d.H_kv >= (1 << 23)) return SI_ERR_UNSUPPORTED_SHAPE;  // a launch has fewer than 2^32 threads
     const Call c = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(K), static_cast<const __bf16*>(V),
                     {q_offsets, d.B, d.N_q}, {k_offsets, d.B, d.N_k}, first, static_cast<__bf16*>(out), lse, scale_log2e,
                     d.H, d.H_kv, G, m, mask_mode, n_win, 0};
