@@ -300,10 +300,11 @@ void prompt_attention_kernel(Call c) {
 #pragma unroll
             for (int j = 1; j < 16; ++j) highest = fmaxf(highest, x[j]);
             raise(static_cast<unsigned>(over | (over >> 32)), highest * to_log2);
+            const float by = shift == __builtin_huge_valf() ? 0.0f : shift;  // all scores so far are minus infinity
             sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to_log2, shift)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], to_log2, shift));
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to_log2, by)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], to_log2, by));
                 sum += p0 + p1;
                 two_weights(pn, j, p0, p1);
             }

@@ -292,3 +292,32 @@ def test_prompt_rows_beyond_4_gb():
     P.si_prompt_attention(q.to(DEV), k, v, _ints([0, 0, 100]), _ints([0, far, far + 200]), _ints([0, 100]), 1, CAUSAL, R.ALL, 0.1, out, lse)
     torch.cuda.synchronize()
     _near(out, lse, R.attend(R.to64(q), R.to64(rows[0]), R.to64(rows[1]), 100 + np.arange(100), 1, 1, R.ALL, 0.1))
+
+
+@pytest.mark.parametrize("n_below", [40, 200, 600])
+@pytest.mark.parametrize("D,H,H_kv", [(64, 8, 1), (128, 16, 2), (128, 64, 1)])
+def test_rows_whose_scores_are_minus_infinity(n_below, D, H, H_kv):
+    """An infinite key takes a row's weight: the rows before the first finite one count for nothing, and for that head only."""
+    T, S = 600, 300
+    g = torch.Generator().manual_seed(n_below)
+    k, v = (torch.randn((T, H_kv, D), generator=g).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((S, H, D), generator=g).to(torch.bfloat16)
+    q[..., 3] = q[..., 3].abs() + 0.5
+    finite = k.clone()
+    k[:n_below, 0, 3] = float("-inf")
+    G = H // H_kv
+    out, lse = _prompt(q, k, v, None, None, None, 1, NONE, R.ALL, 0.1)
+    pages_k, pages_v = torch.zeros((2, 40, H_kv, 16, D), dtype=torch.bfloat16, device=DEV)
+    table = _ints([list(range(40))])
+    P.si_store_pages(k.to(DEV), v.to(DEV), None, None, table, pages_k, pages_v)
+    got, got_lse = _paged(q[:2].reshape(1, 2, H, D).contiguous(), table, pages_k, pages_v, None, None, [T], None, 1, NONE, R.ALL, 0.1)
+    if n_below == T:
+        for o, e in ((out, lse), (got[0], got_lse[0])):
+            assert bool((o[:, :G] == 0).all()) and bool(torch.isneginf(e[:, :G]).all())
+    else:
+        want = R.attend(R.to64(q[:, :G]), R.to64(finite[n_below:, :1]), R.to64(v[n_below:, :1]), range(S), 1, 0, R.ALL, 0.1)
+        _near(out[:, :G], lse[:, :G], want)
+        _near(got[0, :, :G], got_lse[0, :, :G], [x[:2] for x in want])
+    if H_kv > 1:
+        want = R.attend(R.to64(q[:, G:]), R.to64(finite[:, 1:]), R.to64(v[:, 1:]), range(S), 1, 0, R.ALL, 0.1)
+        _near(out[:, G:], lse[:, G:], want)
