@@ -48,11 +48,13 @@ struct Call {
 // Orders the lanes of a wave's LDS accesses for the compiler; the hardware keeps a wave's LDS instructions in order.
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
 // Starts a wave's loads of a tile, from the `bytes` bytes at k and at v: LOADS times 1 KB into LDS at `to` the keys, `apart` behind them the values (none
 // where v is NULL).  A lane's first 16 bytes are at `offset`, the next ones `rows` rows of `stride` bytes further, where the swizzle of the row's number differs.
 // What lies at or past `bytes` is not read and lands as zeros.
 template <int D, int LOADS>
-__device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v, int bytes, int offset, int stride, unsigned char* to, int apart) {
+__device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v, int bytes, int offset, int stride, lds_byte* to, int apart) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef __attribute__((address_space(3))) void lds_void;
     constexpr int kStep = 64 / (D / 8);
@@ -76,6 +78,8 @@ __device__ __forceinline__ floatx2 both_halves(float x) {
     const unsigned low = both[0], high = both[1];  // not cast as they are: a cast of either element takes the first
     return floatx2{__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
 }
+// A value that all lanes have, in a scalar register.
+__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 // The lane's number where it is not worth a register through the loop.
 __device__ __forceinline__ int lane_again() {
     int lane;
@@ -99,6 +103,7 @@ void prompt_attention_kernel(Call c) {
     constexpr int kTileBytes = kRows * kRowBytes;
     constexpr int kLoads = kTileBytes / 1024 / kWaves;  // of a wave, of a tile's keys or values
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    lds_byte* const tiles = (lds_byte*)lds;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -141,31 +146,34 @@ void prompt_attention_kernel(Call c) {
     // ---- a tile's keys and values, by 1 KiB pieces of LDS; rows at or past the last one that anybody sees land as zeros
     const int stride = c.H_kv * kRowBytes;
     static_assert(kLoads > 0 && (kLoads & (kLoads - 1)) == 0, "a load's number and a wave's first row share no bits");
-    auto request = [&](int s0, int buffer) {
+    auto request = [&](int s0, lds_byte* to) {
         const int n = min(kRows, end - s0);
         const int bytes = (n - 1) * stride + kRowBytes;
         const int64_t at = (static_cast<int64_t>(k_first + s0) * c.H_kv + hk) * D;
-        const int lane2 = lane_again(), first_row = wave * kLoads * (64 / kPieces) + lane2 / kPieces;
+        const unsigned lane2 = lane_again(), first_row = wave * kLoads * (64 / kPieces) + lane2 / kPieces;
         const int lane_offset = first_row * stride + ((lane2 % kPieces) ^ row_swizzle<D>(first_row)) * 16;
-        request_pieces<D, kLoads>(c.K + at, c.V ? c.V + at : nullptr, bytes, lane_offset, stride, lds + buffer * 2 * kTileBytes + wave * kLoads * 1024, kTileBytes);
+        request_pieces<D, kLoads>(c.K + at, c.V ? c.V + at : nullptr, bytes, lane_offset, stride, to + wave * kLoads * 1024, kTileBytes);
     };
-    if (begin < end) request(begin, 0);
+    if (begin < end) request(begin, tiles);
 
-    const float to_log2 = c.scale_log2e == 0.0f ? 1.0f : __builtin_fabsf(c.scale_log2e);
+    const float to_log2 = uniform(c.scale_log2e == 0.0f ? 1.0f : __builtin_fabsf(c.scale_log2e));
     const int apart = c.V ? kTileBytes : 0;  // values behind the keys, or the keys' rows
     // Places in a block, of which there is one number each: the others follow by exclusive or, as the swizzle is one and blocks begin at multiples of 256 bytes.
     // First product: row col, piece 2 ks + half.
-    const int key_at = tile_slot<D>(col, half) * 16;
-    auto read_keys = [&](int block, int ks) { return *reinterpret_cast<const bf16x8*>(lds + ((block + key_at) ^ (32 * ks))); };
+    int key_at = tile_slot<D>(col, half) * 16;
+    auto read_keys = [&](const lds_byte* block, int ks) {
+        typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+        return *(lds_bf16x8*)((reinterpret_cast<uintptr_t>(block) + key_at) ^ (32 * ks));  // blocks begin at multiples of 256 bytes
+    };
     // Second product, by transposing reads: source lane s of a group of 16 points at 4 consecutive d of row 4 half + s / 4 (+ 8; + 16 for the second part), at
     // d = 32 db + 16 (group % 2) + 4 (s % 4).
-    const int value_at = apart + tile_slot<D>(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
-    auto read_values = [&](int block, int i) {  // 16 rows of 32 d, by the place of their block's keys; i = s * DB + db
+    int value_at = apart + tile_slot<D>(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
+    auto read_values = [&](const lds_byte* block, int i) {  // 16 rows of 32 d, by the place of their block's keys; i = s * DB + db
         typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
         const int s = i / DB, db = i % DB;
-        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(lds + ((block + value_at) ^ (64 * db)) + s * 16 * kRowBytes));
+        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(block + (value_at ^ (64 * db)) + s * 16 * kRowBytes));
         const bf16x4 v1 =
-            __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(lds + ((block + value_at) ^ (64 * db) ^ (row_swizzle<D>(8) * 16)) + (16 * s + 8) * kRowBytes));
+            __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(block + (value_at ^ (64 * db) ^ (row_swizzle<D>(8) * 16)) + (16 * s + 8) * kRowBytes));
         return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
     };
 
@@ -175,8 +183,8 @@ void prompt_attention_kernel(Call c) {
     for (int db = 0; db < DB; ++db) acc[db] = zero16;
     float shift = __builtin_huge_valf(), l_sum = 0.0f;  // minus the reference; no reference yet makes every weight too large or NaN
 
-    floatx16 x;  // scores of a block of 32 rows: register j has row 8 (j / 4) + 4 half + j % 4
-    auto score = [&](int block) {
+    // scores of a block of 32 rows: register j has row 8 (j / 4) + 4 half + j % 4
+    auto score = [&](const lds_byte* block, floatx16& x) {
         x = zero16;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_keys(block, ks), qf[ks], x, 0, 0, 0);
@@ -199,8 +207,9 @@ void prompt_attention_kernel(Call c) {
     };
 
     // A block of which some column does not see some row.
-    auto take_masked = [&](int s0, int block) {
-        score(block);
+    auto take_masked = [&](int s0, const lds_byte* block) {
+        floatx16 x;
+        score(block, x);
         float highest = -__builtin_huge_valf();
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -236,6 +245,7 @@ void prompt_attention_kernel(Call c) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) weights[(8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = x[j];
             wave_order();
+            typedef __attribute__((address_space(3))) const bf16x4 lds_bf16x4;
 #pragma unroll 1
             for (int r = 0; r < 32; ++r) {
                 const float w = weights[r * 32 + col];
@@ -244,7 +254,7 @@ void prompt_attention_kernel(Call c) {
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int a = 0; a < 4; ++a)
-                        add_not_finite(acc[db], 4 * a, *reinterpret_cast<const bf16x4*>(lds + block + apart + tile_slot<D>(r, 4 * db + a) * 16 + half * 8), w, sees);
+                        add_not_finite(acc[db], 4 * a, *(lds_bf16x4*)(block + apart + tile_slot<D>(r, 4 * db + a) * 16 + half * 8), w, sees);
             }
             wave_order();
         }
@@ -254,31 +264,29 @@ void prompt_attention_kernel(Call c) {
     };
 
     // The tile at s0 is there for all waves, and none uses the slot of the one after it; that is asked for.
-    int slot = 0;
-    auto arrive = [&](int s0) {
+    auto after = [&](lds_byte* slot) { return slot == tiles + (kSlots - 1) * 2 * kTileBytes ? tiles : slot + 2 * kTileBytes; };
+    auto arrive = [&](int s0, lds_byte* slot_after) {
         __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of the tile
         __syncthreads();
-        const int tile = slot * 2 * kTileBytes;
-        slot = slot == kSlots - 1 ? 0 : slot + 1;
-        if (s0 + kRows < end) request(s0 + kRows, slot);
-        return tile;
+        if (s0 + kRows < end) request(s0 + kRows, slot_after);
     };
 
     // Tiles that all columns see whole: a pipeline over blocks of 32 rows.  A step has block g's weights from its scores, while the matrix pipe
     // adds block g - 1's values and makes block g + 1's scores, instruction by instruction: after each product a part of the weights and a read from LDS
     // for a product half a step later.
     bf16x8 vf[2 * DB], pf[2];  // values of the block before, and its weights
-    auto step = [&](int block, int after) {
+    auto step = [&](const lds_byte* block, const lds_byte* next, floatx16& x, floatx16& xn) {
         constexpr int kProducts = KS + 2 * DB, kEach = 16 / kProducts;
         static_assert(KS == 2 * DB && kProducts * kEach == 16, "products and weights go together");
-        floatx16 xn = zero16;
+        asm volatile("" : "+v"(key_at), "+v"(value_at));  // the other places are made here, not kept in registers through the loop
+        xn = zero16;
         bf16x8 kf[KS], pn[2];
         float p[16], sum = 0.0f;
 #pragma unroll
         for (int n = 0; n < kProducts; ++n) {
             if (n < KS) {
                 acc[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n], pf[n / DB], acc[n % DB], 0, 0, 0);
-                kf[n] = read_keys(after, n);
+                kf[n] = read_keys(next, n);
             } else {
                 xn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n - KS], qf[n - KS], xn, 0, 0, 0);
                 vf[n - KS] = read_values(block, n - KS);
@@ -295,7 +303,7 @@ void prompt_attention_kernel(Call c) {
         two_weights(pn, 14, p[14], p[15]);
         unsigned long long over = __ballot(!(sum <= kMostWeight));
         if (__builtin_expect(over != 0ull, 0)) {
-            score(block);  // again: that costs the few blocks that come here less than keeping the scores costs all others
+            score(block, x);  // again: that costs the few blocks that come here less than keeping the scores costs all others
             float highest = x[0];
 #pragma unroll
             for (int j = 1; j < 16; ++j) highest = fmaxf(highest, x[j]);
@@ -310,14 +318,24 @@ void prompt_attention_kernel(Call c) {
             }
         }
         l_sum += sum;
-        x = xn;
         pf[0] = pn[0];
         pf[1] = pn[1];
     };
 
+    // A tile, with its first block's scores in x; then x or y has those of the next tile's first block.  That tile is at `next`, and the one after it is asked
+    // for, to `to`: of different places, as the compiler has to know (__restrict__), or the transposing reads wait for all that is on its way to LDS.
+    auto take_whole = [&](const lds_byte* __restrict__ now, const lds_byte* __restrict__ next, lds_byte* __restrict__ to, int s0, bool last, floatx16& x, floatx16& y) {
+        if constexpr (kRows == 64) step(now, now + 32 * kRowBytes, x, y);
+        if (!last) arrive(s0 + kRows, to);
+        const lds_byte* const then = last ? now : next;  // behind the last block the scores are not used
+        if constexpr (kRows == 64) step(now + 32 * kRowBytes, then, y, x);
+        else step(now, then, x, y);
+    };
+
     // The queries have arrived with the first tile.  A negative scale goes into them (exact), a scale of 0 makes zeros of them.
     int s0 = begin;
-    int tile = s0 < end ? arrive(s0) : 0;
+    lds_byte* tile = tiles;
+    if (s0 < end) arrive(s0, after(tile));
     if (c.scale_log2e <= 0.0f) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -336,23 +354,41 @@ void prompt_attention_kernel(Call c) {
             for (int i = 0; i < kRows; i += 32, s0 += 32)
                 if (s0 < any_to && s0 + 32 > any_from) take_masked(s0, tile + i * kRowBytes);
         } else {
-            score(tile);
+            floatx16 x, y;
+            score(tile, x);
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) vf[i] = __builtin_bit_cast(bf16x8, uintx4{0, 0, 0, 0});
             pf[0] = pf[1] = vf[0];
-#pragma unroll 1
-            for (;;) {
-                if constexpr (kRows == 64) step(tile, tile + 32 * kRowBytes);
+            auto take = [&](floatx16& x, floatx16& y) {
+                const bool last = s0 + kRows >= whole_to;
+                lds_byte* const next = after(tile);
+                take_whole(tile, next, after(next), s0, last, x, y);
                 s0 += kRows;
-                const int next = s0 < whole_to ? arrive(s0) : tile;  // behind the last block the scores are not used
-                step(tile + (kRows - 32) * kRowBytes, next);
-                if (s0 >= whole_to) break;
-                tile = next;
+                if (!last) tile = next;
+                return last;
+            };
+            if constexpr (kRows == 64) {
+#pragma unroll 1
+                while (!take(x, y)) {}
+            } else {
+                bool last = false;
+                if (((whole_to - s0) / kRows) & 1) {
+                    last = take(x, y);
+                    x = y;
+                }
+#pragma unroll 1
+                while (!last) {
+                    take(x, y);
+                    last = take(y, x);
+                }
             }
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], pf[i / DB], acc[i % DB], 0, 0, 0);
         }
-        if (s0 < end) tile = arrive(s0);
+        if (s0 < end) {
+            tile = after(tile);
+            arrive(s0, after(tile));
+        }
     }
     const float m_ref = -shift;
 
