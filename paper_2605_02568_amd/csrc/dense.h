@@ -30,10 +30,12 @@ struct Packed {
     __device__ int64_t at(int b) const {  // 0 <= b <= B
         return offsets ? offsets[b] : static_cast<int64_t>(b) * (N / B);
     }
-    // [first, last) rows of sequence b, inside 0 .. N whatever the offsets hold
+    // the same inside 0 .. N, whatever the offsets hold
+    __device__ int in_range(int b) const { return static_cast<int>(min(max(at(b), static_cast<int64_t>(0)), static_cast<int64_t>(N))); }
+    // [first, last) rows of sequence b
     __device__ void rows(int b, int& first, int& last) const {
-        first = static_cast<int>(min(max(at(b), static_cast<int64_t>(0)), static_cast<int64_t>(N)));
-        last = static_cast<int>(min(max(at(b + 1), static_cast<int64_t>(first)), static_cast<int64_t>(N)));
+        first = in_range(b);
+        last = max(first, in_range(b + 1));
     }
 };
 

@@ -43,6 +43,10 @@ struct Call {
     float scale_log2e;
     int H, H_kv, G, m, mask_mode, n_win;
     int slots;  // of a workgroup's columns, of all sequences
+    uint32_t by_G;  // 2^(31 + by_shift) / G, rounded up
+    int by_shift;   // least with G <= 2^by_shift
+    // x / G for 0 <= x < 2^30: by_G is too large by less than 1, which makes less than x / 2^(31 + by_shift) <= 1 / (2 G) of a quotient whose fraction is 1 / G below the next one
+    __device__ __forceinline__ int over_G(int x) const { return static_cast<int>(__umulhi(2u * static_cast<uint32_t>(x), by_G) >> by_shift); }
 };
 
 // Orders the lanes of a wave's LDS accesses for the compiler; the hardware keeps a wave's LDS instructions in order.
@@ -111,29 +115,40 @@ void prompt_attention_kernel(Call c) {
     const int hk = blockIdx.x % c.H_kv;
     const int u = c.slots - 1 - blockIdx.x / c.H_kv;
 
-    auto slot_of = [&](int b) { return max(c.queries.at(b), static_cast<int64_t>(0)) * c.G / kColumns + b; };
-    const int b = last_not_above(c.queries.B, u, slot_of);
-    int q_first, q_last, k_first, k_last;
-    c.queries.rows(b, q_first, q_last);
-    c.rows.rows(b, k_first, k_last);
+    auto slot_of = [&](int at, int b) { return at * c.G / kColumns + b; };  // of sequence b, whose first packed query is `at`
+    int b, q_first, q_last, k_first, k_last, first;
+    if (c.queries.B < 64) {  // all that there is to know of the sequences, a lane each, in one trip
+        const int i = min(lane, c.queries.B);
+        const int q_at = c.queries.in_range(i), k_at = c.rows.in_range(i), before = c.first ? c.first[min(lane, c.queries.B - 1)] : 0;
+        b = max(0, static_cast<int>(__popcll(__ballot(lane < c.queries.B && slot_of(q_at, lane) <= u))) - 1);
+        q_first = lane_value(q_at, b);
+        q_last = max(q_first, lane_value(q_at, b + 1));
+        k_first = lane_value(k_at, b);
+        k_last = max(k_first, lane_value(k_at, b + 1));
+        first = lane_value(before, b);
+    } else {
+        b = last_not_above(c.queries.B, u, [&](int i) { return static_cast<int64_t>(slot_of(c.queries.in_range(i), i)); });
+        c.queries.rows(b, q_first, q_last);
+        c.rows.rows(b, k_first, k_last);
+        first = c.first ? c.first[b] : 0;
+    }
     const int n_columns = (q_last - q_first) * c.G;
-    const int64_t r0 = (u - slot_of(b)) * kColumns;
+    const int r0 = (u - slot_of(q_first, b)) * kColumns;
     if (r0 < 0 || r0 >= n_columns) return;
     const int held = k_last - k_first;
-    const int first = c.first ? c.first[b] : 0;
 
     // what this lane's column sees
-    const int column = min(static_cast<int>(r0) + wave * 32 + col, n_columns - 1);  // columns that there are not repeat the last one
-    const int query = column / c.G;
+    const int column = min(r0 + wave * 32 + col, n_columns - 1);  // columns that there are not repeat the last one
+    const int query = c.over_G(column);
     const int legal = c.n_win > 0 ? legal_rows(first, query, held, c.m, c.mask_mode) : 0;
     const int from = max(0, legal - c.n_win);
     // What all columns of the wave see, and any: neither end falls from a column to the next.  Then any of the workgroup.
     const int any_from = lane_value(from, 0), all_from = lane_value(from, 31);
     const int all_to = lane_value(legal, 0), any_to = lane_value(legal, 31);
-    const int last_query = (min(static_cast<int>(r0) + kColumns, n_columns) - 1) / c.G;
+    const int last_query = c.over_G(min(r0 + kColumns, n_columns) - 1);
     const int end = c.n_win > 0 ? legal_rows(first, last_query, held, c.m, c.mask_mode) : 0;
-    const int begin = max(0, legal_rows(first, static_cast<int>(r0) / c.G, held, c.m, c.mask_mode) - c.n_win) / kRows * kRows;
-    const int64_t q_row = static_cast<int64_t>(q_first + query) * c.H + hk * c.G + column % c.G;
+    const int begin = max(0, legal_rows(first, c.over_G(r0), held, c.m, c.mask_mode) - c.n_win) / kRows * kRows;
+    const int64_t q_row = static_cast<int64_t>(q_first + query) * c.H + hk * c.G + (column - query * c.G);
 
     // queries: lane has column col, d = 16 ks + 8 half .. + 7
     bf16x8 qf[KS];
@@ -398,12 +413,12 @@ void prompt_attention_kernel(Call c) {
     const float l = l_halves[0] + l_halves[1];
     const bool none = m_ref == -__builtin_huge_valf() && l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
-    int r_first = static_cast<int>(r0) + wave * 32;
+    int r_first = r0 + wave * 32;
     const int lane2 = lane_again(), col2 = lane2 & 31, half2 = lane2 >> 5;
     asm volatile("" : "+s"(r_first));  // places are made again here, not kept in registers through the loop
     const int left = n_columns - r_first;  // columns that there are
     auto row_of = [&](int r) {  // of the results, for column r
-        const int i_query = r / c.G;
+        const int i_query = c.over_G(r);
         return static_cast<int64_t>(q_first + i_query) * c.H + hk * c.G + (r - i_query * c.G);
     };
     if (c.lse && half2 == 0 && col2 < left) c.lse[row_of(r_first + col2)] = none ? -__builtin_huge_valf() : log_of(m_ref, l);
@@ -484,9 +499,11 @@ si_status si_prompt_attention(const void* q, const void* K, const void* V, const
         static_cast<int64_t>(d.N_q) * d.H + int64_t{128} * d.B * d.H_kv >= (1 << 30))  // a launch has fewer than 2^32 threads
         return SI_ERR_UNSUPPORTED_SHAPE;
     const int G = d.H / d.H_kv;
+    int shift = 0;
+    while ((1 << shift) < G) ++shift;
     const Call c = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(K), static_cast<const __bf16*>(V),
                     {q_offsets, d.B, d.N_q}, {k_offsets, d.B, d.N_k}, first, static_cast<__bf16*>(out), lse, scale_log2e,
-                    d.H, d.H_kv, G, m, mask_mode, n_win, 0};
+                    d.H, d.H_kv, G, m, mask_mode, n_win, 0, static_cast<uint32_t>(((int64_t{1} << (31 + shift)) + G - 1) / G), shift};
     return report(d.D == 128 ? launch<128>(c, static_cast<hipStream_t>(stream)) : launch<64>(c, static_cast<hipStream_t>(stream)));
 }
 
