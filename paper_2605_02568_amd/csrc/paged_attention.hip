@@ -77,6 +77,18 @@ struct Chunk {
 // Whether sequences may be so many that chunks as long as an even share leave much of the chip idle: a sequence's last chunk costs half of one.
 __host__ __device__ inline bool in_two_rounds(int B, int target) { return 8 * B > target; }
 
+// x / n rounded up, for 0 <= x <= 2^25 and n >= kMinTiles: the quotient is at most 2^22 and three roundings of 2^-24 to 2^-23 off, less than 1, so its whole
+// part is off by 1 at most, which the remainder tells.
+__device__ __forceinline__ int over(int x, int n) {
+    int q = static_cast<int>(static_cast<float>(x) * __builtin_amdgcn_rcpf(static_cast<float>(n)));
+    int left = x - q * n;
+    if (left <= -n) {
+        --q;
+        left += n;
+    }
+    return q + (left > 0) + (left > n);
+}
+
 // The chunk with number `which`.  Chunks have as many tiles as it takes for all of them to fit the chip at once; where sequences of different lengths would
 // make that more than a quarter longer than an even share, half as many, twice.  All 64 lanes call it; up to 64 sequences stay in a register.
 __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
@@ -97,10 +109,12 @@ __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
         int n_tiles = static_cast<int>(max(static_cast<int64_t>(kMinTiles), even));
         for (int i = 0; i < 4; ++i) {
             int n = 0;
-            for (int b0 = 0; b0 < c.B; b0 += 64) n += b0 + lane < c.B ? max(1, (tiles_at(b0) + n_tiles - 1) / n_tiles) : 0;
+            for (int b0 = 0; b0 < c.B; b0 += 64) n += b0 + lane < c.B ? max(1, over(tiles_at(b0), n_tiles)) : 0;
             n = lane_value(wave_prefix_sum(n), 63);
             if (n <= target) break;
-            n_tiles += max(1, static_cast<int>(static_cast<int64_t>(n_tiles) * (n - target) / target));
+            // a guess: any length from the even share on does
+            const float more = static_cast<float>(n_tiles) * static_cast<float>(n - target) * __builtin_amdgcn_rcpf(static_cast<float>(target));
+            n_tiles += __builtin_amdgcn_readfirstlane(max(1, static_cast<int>(fminf(more, 1 << 25))));
         }
         return n_tiles;
     };
@@ -109,13 +123,13 @@ __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
     int before = 0;
     for (int b0 = 0; b0 < c.B; b0 += 64) {
         const int t = tiles_at(b0);
-        const int mine = b0 + lane < c.B ? max(1, (t + n_tiles - 1) / n_tiles) : 0;
+        const int mine = b0 + lane < c.B ? max(1, over(t, n_tiles)) : 0;
         const int upto = wave_prefix_sum(mine);
         const int all = lane_value(upto, 63);
         if (which < before + all) {
             const int l = static_cast<int>(__popcll(__ballot(before + upto <= which)));
             const int n = lane_value(mine, l);
-            return {b0 + l, before + lane_value(upto, l) - n, n, (lane_value(t, l) + n - 1) / n};
+            return {b0 + l, before + lane_value(upto, l) - n, n, static_cast<int>((static_cast<uint32_t>(lane_value(t, l)) + n - 1) / static_cast<uint32_t>(n))};
         }
         before += all;
     }
@@ -165,7 +179,7 @@ struct Group {
     static constexpr int kWaveBytes = T::kRing * T::kAll + 16 * 16 * 4;  // tiles; weights of 16 rows of a block, for values that are not finite
     static constexpr int kQueries = kWaves * kWaveBytes;                 // where the shared queries begin
     static constexpr int kAtOnce = NB == 4 ? 2 : NB;                     // blocks that are joined at once
-    static constexpr int kJoin = kWaves * (kAtOnce * 16 * D + NB * 16 * 2) * 4 + NB * 16 * 8;  // sums of each wave; reference and sum of weights, of each and of all
+    static constexpr int kJoin = kWaves * (kAtOnce * 16 * D + NB * 16 * 2) * 4;  // sums of each wave; its reference and sum of weights
     static constexpr int kColumns = kQueries + (kSharedQueries ? NB * 16 * D * 2 : 0);  // where the columns' table begins
     static constexpr int kBytes = kColumns + NB * 16 * 16;
     static_assert(kJoin <= kQueries && kBytes <= 160 * 1024, "LDS");
@@ -587,42 +601,20 @@ void paged_attention_kernel(Call c) {
         live[kRing - 1] = k + kRing < n_mine ? request(k + kRing) : 0u;
     }
 
-    // ---- the workgroup's waves join: references first, then sums that have them.  The barriers wait for LDS only, not for what goes to memory.
+    // ---- the workgroup's waves join.  The barriers wait for LDS only, not for what goes to memory.
     auto barrier = [&]() {
         wait_lds();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    constexpr int N = W::kAtOnce;                                          // blocks of columns
-    float* const join = reinterpret_cast<float*>(lds);                     // [wave][column][D]
+    constexpr int N = W::kAtOnce;                                                   // blocks of columns
+    float* const join = reinterpret_cast<float*>(lds);                              // [wave][column][D]
     floatx2* const parts = reinterpret_cast<floatx2*>(join + kWaves * N * 16 * D);  // [column][wave]: minus the reference, sum of weights
-    floatx2* const all = parts + kWaves * NB * 16;                         // [column]: minus the reference, sum of weights, of all waves
     barrier();  // all tiles have been read
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const float l = quarters_sum(l_sum[nb]);
         if (quarter == 0) parts[(nb * 16 + col) * kWaves + wave] = floatx2{shift[nb], l};
-    }
-    barrier();
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        float lowest = __builtin_huge_valf();
-        floatx2 part[kWaves];
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            part[w] = parts[(nb * 16 + col) * kWaves + w];
-            lowest = fminf(lowest, part[w][0]);
-        }
-        // shift is the larger one: 0 where it is infinite
-        const float own = shift[nb] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - shift[nb]);
-        if (wave == nb % kWaves) {
-            float l = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) l += part[w][1] * (part[w][0] == lowest ? 1.0f : __builtin_amdgcn_exp2f(lowest - part[w][0]));
-            if (quarter == 0) all[nb * 16 + col] = floatx2{lowest, l};
-        }
-#pragma unroll
-        for (int db = 0; db < DB; ++db) acc[nb][db] *= own;
     }
 #pragma unroll
     for (int nb0 = 0; nb0 < NB; nb0 += N) {
@@ -638,10 +630,21 @@ void paged_attention_kernel(Call c) {
             const int i = i0 + static_cast<int>(threadIdx.x);
             const int column = i / (D / 4), piece = i % (D / 4);
             if (i >= N * 16 * (D / 4) || (block * NB + nb0) * 16 + column >= R) continue;
+            floatx2 part[kWaves], sums = {__builtin_huge_valf(), 0.0f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                part[w] = parts[(nb0 * 16 + column) * kWaves + w];
+                sums[0] = fminf(sums[0], part[w][0]);
+            }
             floatx4 o = {0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) o += *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
-            const floatx2 sums = all[nb0 * 16 + column];
+            for (int w = 0; w < kWaves; ++w) {
+                const floatx4 x = *reinterpret_cast<const floatx4*>(join + (w * N * 16 + column) * D + ((piece ^ (column & 7)) * 4));
+                const float alpha = part[w][0] == sums[0] ? 1.0f : __builtin_amdgcn_exp2f(sums[0] - part[w][0]);  // 0 where the wave saw nothing
+                sums[1] = __builtin_fmaf(alpha, part[w][1], sums[1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(alpha, x[e], o[e]);
+            }
             const int place = columns[nb0 * 16 + column].x;
             if (chunk.n == 1) {
                 const int64_t row = static_cast<int64_t>(b) * c.S * c.H + place;
