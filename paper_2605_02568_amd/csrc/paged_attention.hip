@@ -2,19 +2,22 @@
 //
 //   out[b,i,g,:] = sum_{s in seen(t)} exp(x_s - lse) V[s,h,:],  x_s = scale <q[b,i,g,:], K[s,h,:]>,  lse = ln sum exp(x_s),  t = first[b] + i
 //
-// All rows of a sequence are read once, so a call is bound by memory.  The positions and heads that share a head of the cache are the
-// columns of one product (column r: position r / G, head r % G of the group of G), 16 or 32 of them a workgroup.
+// All rows of a sequence are read once, so a call is bound by memory: 64 requests of 1,025 to 8,191 rows, 64 heads of 128 on 8, 16 bits: 1.21 GB in 205 us, 5.9 TB/s
+// (loads alone reach 7.1 here).  Where 64 heads share one row of 8 bits, the vector units (36 % of the time) and the matrix pipe (18 %) take as long together as
+// memory does: 8 requests of 65,536 to 131,072 rows: 203 MB in 59 us, of which the chunks' start, end and join take 18.
+// The positions and heads that share a head of the cache are the columns of one product (column r: position r / G, head r % G of the group of G), 16, 32 or 64 of
+// them a workgroup.
 //
 // The rows are dealt out on the device, as the host does not know the lengths: every wave adds up the sequences' tiles of 32 rows, makes
 // chunks of them so that all sequences together have about as many chunks as the chip takes, and finds the sequence that its workgroup's chunk is of.
-// The waves of a workgroup take the chunk's tiles in turn, each by itself, and join once at the end; chunks of the same sequence are
-// joined by a second kernel.  Per tile and wave:
-//   S^T[32 rows x 16 columns] = Ktile q^T   v_mfma_f32_16x16x32_bf16 from registers: a lane has 8 rows of one column
-//   p = exp2(x - m_ref)                     reference of a column raised (and the sums rescaled) only when a lane's sum of weights
-//                                           passes 2^10; fp32
+// The 4 or 8 waves of a workgroup take the chunk's tiles in turn, each by itself with tiles on their way to a ring of its own in LDS, and join once at the end;
+// chunks of the same sequence are joined by a second kernel.  Per tile and wave:
+//   S^T[32 rows x 16 columns] = Ktile q^T   v_mfma_f32_16x16x32_bf16: a lane has 8 rows of one column; 8-bit codes become bf16 on the way from LDS, exactly
+//   p = exp2(x - m_ref)                     reference of a column 0 to begin with, changed (and the sums rescaled) only when a lane's sum of weights passes
+//                                           2^10, or on the first tile is below 2^-10; fp32
 //   O^T[D x 16] += Vtile^T P^T              P^T is an operand straight from the registers of S^T (the rows' order inside the
 //                                           contraction is the same on both sides), Vtile^T comes from the wave's own tile in LDS by transposing reads
-// p is rounded to bf16 for that product only; the sum of weights is of p itself.
+// p, in 8 bits times the value's power of two, is rounded to bf16 for that product only (off by 2^-8 of itself at most); the sum of weights is of p itself.
 
 #include <hip/hip_runtime.h>
 
@@ -28,7 +31,7 @@ namespace si {
 
 namespace {
 
-constexpr int kMinTiles = 8;            // of a chunk
+constexpr int kMinTiles = 8;            // of a chunk (4 or 16: one request of 2,048 rows as fast, no other call faster)
 constexpr int kUnits = 256;             // compute units
 constexpr float kMostWeight = 1024.0f;  // sum of a lane's weights of a tile beyond which the reference is raised
 constexpr int kMaxSequences = 1 << 14;
@@ -90,7 +93,8 @@ __device__ __forceinline__ int over(int x, int n) {
 }
 
 // The chunk with number `which`.  Chunks have as many tiles as it takes for all of them to fit the chip at once; where sequences of different lengths would
-// make that more than a quarter longer than an even share, half as many, twice.  All 64 lanes call it; up to 64 sequences stay in a register.
+// make that more than a quarter longer than an even share, half as many, twice (64 requests of 1,025 to 8,191 rows on 64 chunks: 223 us at once, 207 in two
+// rounds; 24 of 77 to 5,003, where the length is little more than the share: 28 and 36).  All 64 lanes call it; up to 64 sequences stay in a register.
 __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
     const int lane = threadIdx.x & 63;
     const int kept = lane < c.B ? rows_of(c, lane).tiles() : 0;
@@ -738,7 +742,8 @@ __global__ __launch_bounds__(256) void join_chunks_kernel(Call c) {
     if (c.lse && lane == 0) c.lse[row] = inv == 0.0f ? -__builtin_huge_valf() : log_of(top, l);
 }
 
-// Blocks of 16 columns a wave takes, blocks of a call and chunks of all sequences.
+// Blocks of 16 columns a wave takes, workgroups side by side, and chunks of all sequences: as few blocks as have all columns, as every further workgroup reads
+// the rows again (64 columns, 8 requests of 65,536 to 131,072 rows of 8 bits: 65 us at once, 75 in two workgroups of 32).
 struct Shape {
     int nb, blocks, target;
 };
@@ -770,6 +775,8 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(W::kThreads), W::kBytes, stream, c);
     e = hipGetLastError();
     if (e != hipSuccess || one_each) return e;
+    // Four waves a query's head where a sequence has more than 8 chunks, which is what one wave asks for at a time (8 requests of 32 chunks each: 59 us, with one
+    // wave 63; where there are few chunks the other way round: 64 requests of one to four 207 us, with four waves 211; 24 of two or three 28 and 32).
     const int rows = c.B * c.S * c.H;
     if (c.target > 8 * c.B) hipLaunchKernelGGL((join_chunks_kernel<D, 4>), dim3(rows), dim3(256), 0, stream, c);
     else hipLaunchKernelGGL((join_chunks_kernel<D, 1>), dim3((rows + 3) / 4), dim3(256), 0, stream, c);

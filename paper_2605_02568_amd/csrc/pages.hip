@@ -17,6 +17,7 @@ namespace si {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostBlocks = 1 << 15;  // of a grid's second axis
 
 struct Pages {
     void* data[2];            // keys, values
@@ -24,6 +25,14 @@ struct Pages {
     const int32_t* table;
     int32_t table_pages, n_pages, page_lg, H;
 };
+
+// What a call of many rows reads once goes past the caches, as do the packed rows that it makes: out of the way of what it and the next call read again
+// (16 prompts of 33,000 rows of 8 heads, in and out: 89 -> 80 us; 65,536 rows of 16 bits out: 113 -> 106).  What a call of few rows reads and writes may well be there.
+template <bool ONCE, typename T>
+__device__ __forceinline__ T read(const T* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
 
 // Row of the pages' arrays that position `at` of sequence b has for head h, -1 where there is none.
 __device__ __forceinline__ int64_t row_in_pages(const Pages& p, int b, int64_t at, int h) {
@@ -91,7 +100,8 @@ __device__ __forceinline__ int row_exponent(int top) {
     return min(max(((top + 0x1F) >> 7) - 8, 127 + kLowestExponent), 127 + kHighestExponent);
 }
 
-// A thread takes 8 values of PER rows, a wave PER * 64 / (D / 8) rows in a row of one head of the keys or of the values (blockIdx.y: tensor and head).  Many rows
+// A thread takes 8 values of PER rows, a wave PER * 64 / (D / 8) rows in a row of one head of the keys or of the values.  Tensor and head are the grid's first
+// axis, so that a packed row's heads are read and written at about the same time (the other way round 2 % slower).  Many rows
 // take 4: enough on its way to make up for the trips to the offsets and the table before it (16 prompts of 33,000 rows of 8 heads, 8 bits: in 72 -> 58 us, out
 // 47 -> 33).  Where that would be less than a wave a SIMD, 1: a wave's rows are then of fewer sequences (one row of each of 64: 6.5 -> 3.6 us).
 template <int D, int PER>
@@ -106,10 +116,10 @@ struct Share {
     bool there[PER];  // such a row is in the call
     __device__ __forceinline__ Share(const Packed& seq, int H) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        h = blockIdx.y % H;
-        which = blockIdx.y / H;
+        which = blockIdx.x >= static_cast<unsigned>(H);
+        h = static_cast<int>(blockIdx.x) - which * H;
         piece = lane % kUnits;
-        const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + wave * kWaveRows;
+        const int64_t row = (static_cast<int64_t>(blockIdx.z) * kMostBlocks + blockIdx.y) * kRows + wave * kWaveRows;
         first = static_cast<int>(min(row, static_cast<int64_t>(seq.N) - 1));
         last = static_cast<int>(min(row + kWaveRows, static_cast<int64_t>(seq.N)) - 1);
 #pragma unroll
@@ -128,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void store_pages_kernel(const uintx4* __r
     const uintx4* const rows = (s.which ? v_rows : k_rows) + static_cast<int64_t>(s.h) * kUnits + s.piece;
     uintx4 x[kPer];
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = rows[static_cast<int64_t>(s.n[j]) * pages.H * kUnits];
+    for (int j = 0; j < kPer; ++j) x[j] = read<kPer == 4>(rows + static_cast<int64_t>(s.n[j]) * pages.H * kUnits);
     places_of(seq, start, s.first, s.last, s.n, s.b, s.at);
     int64_t to[kPer];
 #pragma unroll
@@ -182,9 +192,9 @@ __global__ __launch_bounds__(kThreads) void load_pages_kernel(uintx4* __restrict
         power[j] = 127;
         if (from >= 0) {
             if constexpr (BITS == 16) {
-                x[j] = static_cast<const uintx4*>(pages.data[s.which])[from * kUnits + s.piece];
+                x[j] = read<kPer == 4>(static_cast<const uintx4*>(pages.data[s.which]) + from * kUnits + s.piece);
             } else {
-                const uintx2 codes = static_cast<const uintx2*>(pages.data[s.which])[from * kUnits + s.piece];
+                const uintx2 codes = read<kPer == 4>(static_cast<const uintx2*>(pages.data[s.which]) + from * kUnits + s.piece);
                 x[j] = uintx4{codes[0], codes[1], 0, 0};
                 power[j] = pages.scales[s.which][from];
             }
@@ -197,7 +207,11 @@ __global__ __launch_bounds__(kThreads) void load_pages_kernel(uintx4* __restrict
             codes_to_bf16(x[j], scale_power(power[j]), out);
             x[j] = out[0];
         }
-        if (s.there[j] && s.b[j] >= 0) rows[(static_cast<int64_t>(s.n[j]) * pages.H + s.h) * kUnits + s.piece] = x[j];
+        if (s.there[j] && s.b[j] >= 0) {
+            uintx4* const to = rows + (static_cast<int64_t>(s.n[j]) * pages.H + s.h) * kUnits + s.piece;
+            if constexpr (kPer == 4) __builtin_nontemporal_store(x[j], to);
+            else *to = x[j];
+        }
     }
 }
 
@@ -224,7 +238,9 @@ int rows_a_thread(const si_paged_cache& c, int32_t N, bool values) {
 }
 dim3 grid_for(const si_paged_cache& c, int32_t N, bool values) {
     const int rows = kThreads / (c.D / 8) * rows_a_thread(c, N, values);
-    return dim3(static_cast<unsigned>((static_cast<int64_t>(N) + rows - 1) / rows), static_cast<unsigned>(c.H_kv * (values ? 2 : 1)));
+    const int64_t blocks = (static_cast<int64_t>(N) + rows - 1) / rows;
+    return dim3(static_cast<unsigned>(c.H_kv * (values ? 2 : 1)), static_cast<unsigned>(std::min<int64_t>(blocks, kMostBlocks)),
+                static_cast<unsigned>((blocks + kMostBlocks - 1) / kMostBlocks));
 }
 
 }  // namespace

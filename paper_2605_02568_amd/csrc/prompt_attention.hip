@@ -2,22 +2,23 @@
 //
 //   out[i,g,:] = sum_{s in seen(t)} exp(x_s - lse) V[s,h,:],  x_s = scale <q[i,g,:], K[s,h,:]>,  lse = ln sum exp(x_s),  t = first[b] + i
 //
-// Bound by the matrix pipe: 4 D operations a pair of query and row, whose rows all workgroups of a head find in their XCD's L2.
+// Bound by the matrix pipe: 4 D operations a pair of query and row, whose rows all workgroups of a head find in their XCD's L2; with heads of 64, where an
+// exponential comes with half as many operations, by the vector units beside it.  8,192 queries, causal, 64 heads of 128 on 8: 0.995 ms, 1,105 TFLOP/s (a product
+// of 8192^3 by the library runs at 1,214, both at the clock that their power leaves); heads of 64: 0.59 ms, 920.
 // The queries and heads that share a head of keys and values are the columns of one product (column r of a sequence: query r / G, head r % G
-// of the group of G), 256 of them a workgroup, 32 a wave; so short prompts and large groups fill a workgroup, and the masked part of a tile
-// on the diagonal is as small as 256 / G queries.  The workgroup's waves share tiles of 64 rows, which go straight from memory to LDS, one on its
-// way while the one before is used.  Per tile and wave:
-//   S^T[64 rows x 32 columns] = Ktile q^T   v_mfma_f32_32x32x16_bf16: a lane has 32 rows of one column, so a column's statistics are in-lane
+// of the group of G), 32 a wave, 128 or 256 a workgroup; so short prompts and large groups fill a workgroup, and the masked part of a tile
+// on the diagonal is as small as 256 / G queries.  The workgroup's waves share tiles of 32 or 64 rows, which go straight from memory to LDS, one on its
+// way while the one before is used (two on their way: 1 % slower).  Per block of 32 rows and wave:
+//   S^T[32 rows x 32 columns] = K q^T       v_mfma_f32_32x32x16_bf16: a lane has 16 rows of one column, so a column's statistics are in-lane
 //   p = exp2(x - m_ref)                     reference of a column raised (and the sums rescaled) only when a lane's sum of weights
 //                                           passes 2^10; fp32
-//   O^T[D x 32] += Vtile^T P^T              P^T is an operand straight from the registers of S^T (the rows' order inside the
-//                                           contraction is the same on both sides), Vtile^T comes from LDS by transposing reads
-// p is rounded to bf16 for that product only; the sum of weights is of p itself.
+//   O^T[D x 32] += V^T P^T                  P^T is an operand straight from the registers of S^T (the rows' order inside the
+//                                           contraction is the same on both sides), V^T comes from LDS by transposing reads
+// p is rounded to bf16 for that product only (off by 2^-8 of itself at most); the sum of weights is of p itself.
 
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <type_traits>
 
 #include "attention_set.h"
 #include "dense.h"
@@ -55,7 +56,7 @@ __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_A
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
 // Starts a wave's loads of a tile, from the `bytes` bytes at k and at v: LOADS times 1 KB into LDS at `to` the keys, `apart` behind them the values (none
-// where v is NULL).  A lane's first 16 bytes are at `offset`, the next ones `rows` rows of `stride` bytes further, where the swizzle of the row's number differs.
+// where v is NULL).  A lane's first 16 bytes are at `offset`, the next ones 64 / (D / 8) rows of `stride` bytes further, where the swizzle of the row's number differs.
 // What lies at or past `bytes` is not read and lands as zeros.
 template <int D, int LOADS>
 __device__ __forceinline__ void request_pieces(const __bf16* k, const __bf16* v, int bytes, int offset, int stride, lds_byte* to, int apart) {
@@ -95,7 +96,7 @@ template <int D, int kWaves, int kRows>
 constexpr int lds_bytes() { return kSlots * 2 * kRows * D * 2 + kWaves * 32 * 32 * 4; }  // tiles of keys and values; weights of a block a wave
 
 // Grid: (slots of columns, the last ones first) x heads of keys and values, heads next to each other so that with 8 of them each has an XCD.  A sequence's
-// slots begin at (its first packed column) / 256 + (its number): slots enough for any lengths, with no sum over the sequences before.
+// slots begin at (its first packed column) / (columns of a workgroup) + (its number): slots enough for any lengths, with no sum over the sequences before.
 template <int D, int kWaves, int kRows>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void prompt_attention_kernel(Call c) {
@@ -408,7 +409,7 @@ void prompt_attention_kernel(Call c) {
     const float m_ref = -shift;
 
     // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4.  64 d of the wave's columns go through its own LDS, so that the results are
-    // written by whole lines: 8 bytes a lane and 32 rows at once they took 1.7 us in place of EPILOGUE.
+    // written by whole lines (four prompts of 33 to 300: 15.5 us; 8 bytes a lane and 32 rows at once: 17.0).
     const floatx2 l_halves = both_halves(l_sum);
     const float l = l_halves[0] + l_halves[1];
     const bool none = m_ref == -__builtin_huge_valf() && l == 0.0f;
@@ -457,10 +458,11 @@ hipError_t launch(Call c, int64_t n_columns, hipStream_t stream) {
 }
 
 // Heads of 64: 128 columns a workgroup and tiles of 32 rows, so that three workgroups share a compute unit and one's start and end go by beside the others' products
-// (23 prompts of up to 1,500, 33 heads on 3: 163 us; 256 columns and 64 rows: 177; 8,192 queries, 64 heads on 8: 617 against 636).
-// Heads of 128: 256 columns and 64 rows, which load a tile for twice as many products (8,192 queries, 64 heads on 8: 1,003 us; the smaller form 1,059).  Where
-// that would be fewer workgroups than compute units, the smaller form, two a unit (1,024 queries: 36.9 -> 34.7 us); and where it would be fewer than half as
-// many, 128 columns and 64 rows, of which one fits a unit, so that they spread (512 queries behind 8,192: 198 us in the smaller form, 173 in this).
+// (23 prompts of up to 1,500, 33 heads on 3: 164 us; 256 columns and 64 rows: 177; 8,192 queries, 64 heads on 8: 597 against 612).
+// Heads of 128: 256 columns and 64 rows, which load a tile for twice as many products (8,192 queries, 64 heads on 8: 993 us; the smaller form 1,037).  Where
+// that would be fewer workgroups than compute units, the smaller form, two a unit (1,024 queries: 33.3 -> 30.2 us; four prompts of 33 to 300: 17.9 -> 15.6); and where
+// it would be fewer than half as many, 128 columns and 64 rows, of which one fits a unit, so that they spread (512 queries behind 8,192: 163 us in the smaller
+// form, 156 in this; 300 behind 4,000: 79 and 74).
 template <int D>
 hipError_t launch(const Call& c, hipStream_t stream) {
     constexpr int kUnits = 256;
