@@ -26,8 +26,6 @@ struct Pages {
     int32_t table_pages, n_pages, page_lg, H;
 };
 
-// What a call of many rows reads once goes past the caches, as do the packed rows that it makes: out of the way of what it and the next call read again
-// (16 prompts of 33,000 rows of 8 heads, in and out: 89 -> 80 us; 65,536 rows of 16 bits out: 113 -> 106).  What a call of few rows reads and writes may well be there.
 template <bool ONCE, typename T>
 __device__ __forceinline__ T read(const T* p) {
     if constexpr (ONCE) return __builtin_nontemporal_load(p);
@@ -130,7 +128,7 @@ struct Share {
     }
 };
 
-template <int D, int BITS, int kPer>
+template <int D, int BITS, int kPer, bool kOnce>
 __global__ __launch_bounds__(kThreads) void store_pages_kernel(const uintx4* __restrict__ k_rows, const uintx4* __restrict__ v_rows, Packed seq,
                                                                const int32_t* __restrict__ start, Pages pages) {
     constexpr int kUnits = D / 8;
@@ -138,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void store_pages_kernel(const uintx4* __r
     const uintx4* const rows = (s.which ? v_rows : k_rows) + static_cast<int64_t>(s.h) * kUnits + s.piece;
     uintx4 x[kPer];
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = read<kPer == 4>(rows + static_cast<int64_t>(s.n[j]) * pages.H * kUnits);
+    for (int j = 0; j < kPer; ++j) x[j] = read<kOnce>(rows + static_cast<int64_t>(s.n[j]) * pages.H * kUnits);
     places_of(seq, start, s.first, s.last, s.n, s.b, s.at);
     int64_t to[kPer];
 #pragma unroll
@@ -175,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void store_pages_kernel(const uintx4* __r
     }
 }
 
-template <int D, int BITS, int kPer>
+template <int D, int BITS, int kPer, bool kOnce>
 __global__ __launch_bounds__(kThreads) void load_pages_kernel(uintx4* __restrict__ k_rows, uintx4* __restrict__ v_rows, Packed seq,
                                                               const int32_t* __restrict__ start, Pages pages) {
     constexpr int kUnits = D / 8;
@@ -192,9 +190,9 @@ __global__ __launch_bounds__(kThreads) void load_pages_kernel(uintx4* __restrict
         power[j] = 127;
         if (from >= 0) {
             if constexpr (BITS == 16) {
-                x[j] = read<kPer == 4>(static_cast<const uintx4*>(pages.data[s.which]) + from * kUnits + s.piece);
+                x[j] = read<kOnce>(static_cast<const uintx4*>(pages.data[s.which]) + from * kUnits + s.piece);
             } else {
-                const uintx2 codes = read<kPer == 4>(static_cast<const uintx2*>(pages.data[s.which]) + from * kUnits + s.piece);
+                const uintx2 codes = read<kOnce>(static_cast<const uintx2*>(pages.data[s.which]) + from * kUnits + s.piece);
                 x[j] = uintx4{codes[0], codes[1], 0, 0};
                 power[j] = pages.scales[s.which][from];
             }
@@ -209,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void load_pages_kernel(uintx4* __restrict
         }
         if (s.there[j] && s.b[j] >= 0) {
             uintx4* const to = rows + (static_cast<int64_t>(s.n[j]) * pages.H + s.h) * kUnits + s.piece;
-            if constexpr (kPer == 4) __builtin_nontemporal_store(x[j], to);
+            if constexpr (kOnce) __builtin_nontemporal_store(x[j], to);
             else *to = x[j];
         }
     }
@@ -236,6 +234,12 @@ int rows_a_thread(const si_paged_cache& c, int32_t N, bool values) {
     constexpr int kSimds = 1024;
     return static_cast<int64_t>(N) * c.H_kv * (values ? 2 : 1) * (c.D / 8) >= int64_t{4} * 64 * kSimds ? 4 : 1;
 }
+// Whether what a call reads once goes past the caches, as do the packed rows that it makes: out of the way of what it and the next call read again (16 prompts of
+// 33,000 rows of 8 heads in 8 bits, 135 MB of packed rows, in and out: 89 -> 80 us; 65,536 rows of 16 bits out: 113 -> 106).  Packed rows of less than 64 MB may well
+// be in the caches, or the next call finds them there (9,219 rows of 5 heads of 64 out of 8 bits, again and again: 7.9 us, past the caches 9.6).
+bool past_the_caches(const si_paged_cache& c, int32_t N, bool values) {
+    return static_cast<int64_t>(N) * c.H_kv * c.D * (values ? 4 : 2) >= int64_t{64} << 20;
+}
 dim3 grid_for(const si_paged_cache& c, int32_t N, bool values) {
     const int rows = kThreads / (c.D / 8) * rows_a_thread(c, N, values);
     const int64_t blocks = (static_cast<int64_t>(N) + rows - 1) / rows;
@@ -258,13 +262,15 @@ si_status si_store_pages(const void* k_rows, const void* v_rows, int32_t N, cons
     if (!k_rows || (cache->V && !v_rows)) return SI_ERR_INVALID_ARG;
     if (ok != SI_OK) return ok;
     const int per = rows_a_thread(*cache, N, cache->V != nullptr);
+    const bool once = past_the_caches(*cache, N, cache->V != nullptr);
     const dim3 grid = grid_for(*cache, N, cache->V != nullptr);
     const Packed seq = {offsets, cache->B, N};
 #define SI_LAUNCH(DD, BITS)                                                                                                          \
-    if (per == 4) SI_LAUNCH_PER(DD, BITS, 4);                                                                                        \
-    else SI_LAUNCH_PER(DD, BITS, 1)
-#define SI_LAUNCH_PER(DD, BITS, PER)                                                                                                 \
-    hipLaunchKernelGGL((store_pages_kernel<DD, BITS, PER>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                    \
+    if (once) SI_LAUNCH_PER(DD, BITS, 4, true);                                                                                      \
+    else if (per == 4) SI_LAUNCH_PER(DD, BITS, 4, false);                                                                            \
+    else SI_LAUNCH_PER(DD, BITS, 1, false)
+#define SI_LAUNCH_PER(DD, BITS, PER, ONCE)                                                                                              \
+    hipLaunchKernelGGL((store_pages_kernel<DD, BITS, PER, ONCE>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                    \
                        static_cast<const uintx4*>(k_rows), static_cast<const uintx4*>(v_rows), seq, start, pages_of(*cache))
     if (cache->bits == 16) {
         if (cache->D == 128) {
@@ -291,13 +297,15 @@ si_status si_load_pages(const si_paged_cache* cache, int32_t N, const int32_t* o
     if ((!k_rows && !v_rows) || (v_rows && !cache->V)) return SI_ERR_INVALID_ARG;
     if (ok != SI_OK) return ok;
     const int per = rows_a_thread(*cache, N, v_rows != nullptr);
+    const bool once = past_the_caches(*cache, N, v_rows != nullptr);
     const dim3 grid = grid_for(*cache, N, v_rows != nullptr);
     const Packed seq = {offsets, cache->B, N};
 #define SI_LAUNCH(DD, BITS)                                                                                                          \
-    if (per == 4) SI_LAUNCH_PER(DD, BITS, 4);                                                                                        \
-    else SI_LAUNCH_PER(DD, BITS, 1)
-#define SI_LAUNCH_PER(DD, BITS, PER)                                                                                                 \
-    hipLaunchKernelGGL((load_pages_kernel<DD, BITS, PER>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                     \
+    if (once) SI_LAUNCH_PER(DD, BITS, 4, true);                                                                                      \
+    else if (per == 4) SI_LAUNCH_PER(DD, BITS, 4, false);                                                                            \
+    else SI_LAUNCH_PER(DD, BITS, 1, false)
+#define SI_LAUNCH_PER(DD, BITS, PER, ONCE)                                                                                              \
+    hipLaunchKernelGGL((load_pages_kernel<DD, BITS, PER, ONCE>), grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream),                     \
                        static_cast<uintx4*>(k_rows), static_cast<uintx4*>(v_rows), seq, start, pages_of(*cache))
     if (cache->bits == 16) {
         if (cache->D == 128) {

@@ -321,3 +321,44 @@ def test_rows_whose_scores_are_minus_infinity(n_below, D, H, H_kv):
     if H_kv > 1:
         want = R.attend(R.to64(q[:, G:]), R.to64(finite[:, 1:]), R.to64(v[:, 1:]), range(S), 1, 0, R.ALL, 0.1)
         _near(out[:, G:], lse[:, G:], want)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D,H", [(128, 16), (64, 33)])
+@pytest.mark.parametrize("both", [True, False])
+def test_rows_of_large_calls(bits, D, H, both):
+    """64 MB of packed rows and more, of sequences with odd lengths, in and out."""
+    lengths = [4099, 1, 0, 3000, 1200] if both else [9001, 1, 0, 7000, 1200]
+    N, page = sum(lengths), 32
+    assert N * H * D * (4 if both else 2) >= 64 << 20
+    g = torch.Generator(device=DEV).manual_seed(9)
+    k, v = (torch.randn((N, H, D), generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    wide = -(-(max(lengths) + 20) // page)
+    n_pages = 5 * wide
+    table = torch.randperm(n_pages, generator=g, device=DEV).to(torch.int32).view(5, wide)
+    shape = (n_pages, H, page, D)
+    K, V = (torch.full(shape, 7, dtype=torch.bfloat16 if bits == 16 else torch.uint8, device=DEV) for _ in range(2))
+    scales = [None, None] if bits == 16 else [torch.full(shape[:3], 99, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    off, start = _ints([0] + [int(x) for x in np.cumsum(lengths)]), _ints([0, 13, 5, 19, 3])
+    if not both:
+        V, v, scales = None, None, [scales[0], None]
+    print(f"large rows bits={bits} D={D} both={both}", flush=True)
+    P.si_store_pages(k, v, off, start, table, K, V, *scales)
+    k_out, v_out = torch.full_like(k, -3), None if v is None else torch.full_like(v, -3)
+    P.si_load_pages(table, K, V, *scales, off, start, k_out, v_out)
+    torch.cuda.synchronize()
+    for x, got in ((k, k_out), (v, v_out)):
+        if x is None:
+            continue
+        if bits == 16:
+            assert torch.equal(got, x)
+        else:
+            for some in (slice(0, 300), slice(4000, 4300), slice(N - 300, N)):
+                np.testing.assert_array_equal(R.to64(got[some]), R.values(*R.quantize(R.to64(x[some]))))
+    # what no row went to is as it was
+    used = torch.zeros((n_pages * page,), dtype=torch.bool, device=DEV)
+    for b, n in enumerate(lengths):
+        s = int(start[b]) + torch.arange(n, device=DEV)
+        used[table[b, s // page].long() * page + s % page] = True
+    left = K.permute(0, 2, 1, 3).reshape(n_pages * page, -1)[~used]
+    assert bool((left == 7).all())
