@@ -5,7 +5,7 @@
  * lengths, first, table and lse 4-byte; other alignments are refused); work is enqueued on `stream` and the call returns without
  * synchronising; nothing is allocated; only kernel launches are enqueued, so a call can be captured into a HIP graph; argument errors are
  * reported before anything is launched.  Two calls that share a workspace, or of which one writes what the other reads or writes, must not
- * overlap in time.
+ * overlap in time; what a call writes must not overlap what it reads in memory.
  *
  * The cache.  n_pages pages of page_rows rows of H_kv heads of D values, keys and values apart: K and V [n_pages, H_kv, page_rows, D].
  * Row s of sequence b is row s % page_rows of page table[b, s / page_rows].  A number outside 0 .. n_pages - 1 (such as -1) says that the
@@ -76,7 +76,8 @@ si_status si_load_pages(const si_paged_cache* cache, int32_t N, const int32_t* o
  *   out        device [B,S,H,D] bf16;  lse device [B,S,H] f32 or NULL
  *   workspace  device, si_paged_workspace_bytes(B, S, H, H_kv, D) bytes
  * fp32 products, statistics and sums.  A weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the
- * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  What rows hold
+ * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
+ * weight of 0; infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
  * that a position does not see (behind the length, before the window, later positions' rows) never reaches its result, NaN and infinities included.
  * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  The same call gives the same bits. */
 size_t si_paged_workspace_bytes(int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t D);

@@ -2,7 +2,8 @@
  * libstreamindex -- dense attention of whole prompts, or of the next part of them, packed one behind the other.  Same library, same
  * conventions as streamindex.h: caller-owned device pointers, contiguous row-major, 16-byte aligned (offsets, first and lse 4-byte; other
  * alignments are refused); work is enqueued on `stream` and the call returns without synchronising; nothing is allocated; only
- * a kernel launch is enqueued, so a call can be captured into a HIP graph; argument errors are reported before anything is launched.
+ * a kernel launch is enqueued, so a call can be captured into a HIP graph; argument errors are reported before anything is launched.  What
+ * a call writes must not overlap what it reads in memory, or what another call reads or writes at the same time.
  *
  * Sequence b has the queries q_offsets[b] .. q_offsets[b+1] - 1 and the rows k_offsets[b] .. k_offsets[b+1] - 1 of keys and values.  With
  *   t           = first[b] + i           position of its query i
@@ -44,7 +45,8 @@ typedef struct {
  *   n_win      >= 0; SI_ALL_ROWS: no window
  *   out        device [N_q,H,D] bf16;  lse device [N_q,H] f32 or NULL.  Queries that belong to no sequence are left as they were.
  * fp32 products, statistics and sums.  A weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the
- * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  What rows hold
+ * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
+ * weight of 0; infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
  * that a query does not see (later positions, before the window, other sequences) never reaches its result, NaN and infinities included.
  * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  No workspace.  The same call gives the same bits.
  * Limits, SI_ERR_UNSUPPORTED_SHAPE beyond them: D = 64 or 128, H <= 1024, N_q, N_k <= 2^30, B <= 2^20, N_q H + 128 B H_kv < 2^30. */
