@@ -9,7 +9,8 @@
 // them a workgroup.
 //
 // The rows are dealt out on the device, as the host does not know the lengths: every wave adds up the sequences' tiles of 32 rows, makes
-// chunks of them so that all sequences together have about as many chunks as the chip takes, and finds the sequence that its workgroup's chunk is of.
+// chunks of them so that all sequences together have about as many chunks as the chip takes, and finds the sequence that its workgroup's chunk is of; where there
+// are many sequences a kernel before does that for all.
 // The 4 or 8 waves of a workgroup take the chunk's tiles in turn, each by itself with tiles on their way to a ring of its own in LDS, and join once at the end;
 // chunks of the same sequence are joined by a second kernel.  Per tile and wave:
 //   S^T[32 rows x 16 columns] = Ktile q^T   v_mfma_f32_16x16x32_bf16: a lane has 8 rows of one column; 8-bit codes become bf16 on the way from LDS, exactly
@@ -51,7 +52,8 @@ struct Call {
     float scale_log2e;
     int B, S, H, H_kv, G, table_pages, n_pages, page_lg, m, mask_mode, n_win;
     int blocks;  // of columns
-    int target;  // chunks that fit the chip at once; there are up to twice as many, and one more of each sequence
+    int target;  // chunks that fit the chip at once
+    bool one_each;  // no sequence can have two chunks
 };
 
 // Rows that the positions of sequence b see: [lo, hi) all of them together.
@@ -77,8 +79,9 @@ struct Chunk {
     int n_tiles;  // tiles of a chunk
 };
 
-// Whether sequences may be so many that chunks as long as an even share leave much of the chip idle: a sequence's last chunk costs half of one.
-__host__ __device__ inline bool in_two_rounds(int B, int target) { return 8 * B > target; }
+// In how many rounds of workgroups the chunks may go through the chip.  A sequence's last chunk costs half of one, so where there are more sequences than an eighth
+// of the chunks that fit at once, these may leave much of the chip idle; where there are twice as many sequences as such chunks, four rounds and more are needed anyway.
+__host__ __device__ inline int most_rounds(int B, int target) { return 8 * static_cast<int64_t>(B) <= target ? 1 : B <= 2 * static_cast<int64_t>(target) ? 2 : 4; }
 
 // x / n rounded up, for 0 <= x <= 2^25 and n >= kMinTiles: the quotient is at most 2^22 and three roundings of 2^-24 to 2^-23 off, less than 1, so its whole
 // part is off by 1 at most, which the remainder tells.
@@ -92,52 +95,103 @@ __device__ __forceinline__ int over(int x, int n) {
     return q + (left > 0) + (left > n);
 }
 
-// The chunk with number `which`.  Chunks have as many tiles as it takes for all of them to fit the chip at once; where sequences of different lengths would
-// make that more than a quarter longer than an even share, half as many, twice (64 requests of 1,025 to 8,191 rows on 64 chunks: 223 us at once, 207 in two
-// rounds; 24 of 77 to 5,003, where the length is little more than the share: 28 and 36).  All 64 lanes call it; up to 64 sequences stay in a register.
-__device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
-    const int lane = threadIdx.x & 63;
-    const int kept = lane < c.B ? rows_of(c, lane).tiles() : 0;
-    auto tiles_at = [&](int b0) { return b0 == 0 ? kept : b0 + lane < c.B ? rows_of(c, b0 + lane).tiles() : 0; };
-    int low = 0, high = 0;  // sums of the tiles' lower 16 bits and of the rest: 2^14 sequences of 2^25 tiles
-    for (int b0 = 0; b0 < c.B; b0 += 64) {
-        const int t = tiles_at(b0);
-        low += t & 0xFFFF;
-        high += t >> 16;
-    }
-    low = lane_value(wave_prefix_sum(low), 63);
-    high = lane_value(wave_prefix_sum(high), 63);
-    const int64_t total = (static_cast<int64_t>(high) << 16) + low;
-    auto length_for = [&](int target) {
+// Tiles of a chunk, where all sequences together have `total` and count(n) is how many chunks they make of n tiles.  Chunks have as many tiles as it takes for all
+// of them to fit the chip at once; where sequences of different lengths would make that more than a quarter longer than an even share, half as many, twice (64
+// requests of 1,025 to 8,191 rows on 64 chunks: 223 us at once, 207 in two rounds; 24 of 77 to 5,003, where the length is little more than the share: 28 and 36).
+// It is an even share at least, and kMinTiles, so there are at most as many chunks as fit in the rounds, and one more of each sequence.
+template <typename Count>
+__device__ __forceinline__ int chunk_length(const Call& c, int64_t total, Count count) {
+    auto even_for = [&](int target) {
         const int64_t even = (total >> 31) ? (total + target - 1) / target : (static_cast<uint32_t>(total) + target - 1) / target;
-        int n_tiles = static_cast<int>(max(static_cast<int64_t>(kMinTiles), even));
+        return static_cast<int>(min(max(static_cast<int64_t>(kMinTiles), even), int64_t{1} << 25));  // no sequence has more
+    };
+    auto length_for = [&](int target) {
+        const int even = even_for(target);
+        int n_tiles = even;
         for (int i = 0; i < 4; ++i) {
-            int n = 0;
-            for (int b0 = 0; b0 < c.B; b0 += 64) n += b0 + lane < c.B ? max(1, over(tiles_at(b0), n_tiles)) : 0;
-            n = lane_value(wave_prefix_sum(n), 63);
+            const int n = count(n_tiles);
             if (n <= target) break;
-            // a guess: any length from the even share on does
-            const float more = static_cast<float>(n_tiles) * static_cast<float>(n - target) * __builtin_amdgcn_rcpf(static_cast<float>(target));
-            n_tiles += __builtin_amdgcn_readfirstlane(max(1, static_cast<int>(fminf(more, 1 << 25))));
+            const float more = static_cast<float>(n_tiles) * static_cast<float>(n - target) * __builtin_amdgcn_rcpf(static_cast<float>(target));  // a guess
+            n_tiles = min(2 * even, n_tiles + __builtin_amdgcn_readfirstlane(max(1, static_cast<int>(fminf(more, 1 << 25)))));
         }
         return n_tiles;
     };
-    int n_tiles = length_for(c.target);
-    if (in_two_rounds(c.B, c.target) && static_cast<int64_t>(n_tiles) * c.target * 4 > 5 * total + 4 * kMinTiles * c.target) n_tiles = length_for(2 * c.target);
-    int before = 0;
-    for (int b0 = 0; b0 < c.B; b0 += 64) {
-        const int t = tiles_at(b0);
-        const int mine = b0 + lane < c.B ? max(1, over(t, n_tiles)) : 0;
-        const int upto = wave_prefix_sum(mine);
-        const int all = lane_value(upto, 63);
-        if (which < before + all) {
-            const int l = static_cast<int>(__popcll(__ballot(before + upto <= which)));
-            const int n = lane_value(mine, l);
-            return {b0 + l, before + lane_value(upto, l) - n, n, static_cast<int>((static_cast<uint32_t>(lane_value(t, l)) + n - 1) / static_cast<uint32_t>(n))};
-        }
-        before += all;
+    const int rounds = most_rounds(c.B, c.target);
+    if (rounds == 4) return even_for(4 * c.target);
+    const int n_tiles = length_for(c.target);
+    return rounds == 1 || static_cast<int64_t>(n_tiles) * c.target * 4 <= 5 * total + 4 * kMinTiles * c.target ? n_tiles : length_for(2 * c.target);
+}
+
+constexpr int kFewSequences = 64;  // every wave deals them out for itself, a lane each; more are dealt out by a workgroup that does nothing else
+
+// The chunk with number `which`.  All 64 lanes call it.
+__device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
+    auto parts_of = [&](int t, int n) { return static_cast<int>((static_cast<uint32_t>(t) + n - 1) / static_cast<uint32_t>(n)); };
+    if (c.one_each) return {which < c.B ? which : -1, which, 1, which < c.B ? rows_of(c, which).tiles() : 0};
+    if (c.B > kFewSequences) {
+        const int b = last_not_above(c.B, which, [&](int i) { return static_cast<int64_t>(c.chunks[i].x); });
+        const int2 chunk = c.chunks[b];
+        return {which < chunk.x + chunk.y ? b : -1, chunk.x, chunk.y, parts_of(rows_of(c, b).tiles(), chunk.y)};
     }
-    return {-1, 0, 0, n_tiles};
+    const int lane = threadIdx.x & 63;
+    const int t = lane < c.B ? rows_of(c, lane).tiles() : 0;
+    const int low = lane_value(wave_prefix_sum(t & 0xFFFF), 63), high = lane_value(wave_prefix_sum(t >> 16), 63);
+    const int n_tiles = chunk_length(c, (static_cast<int64_t>(high) << 16) + low,
+                                     [&](int n) { return lane_value(wave_prefix_sum(lane < c.B ? max(1, over(t, n)) : 0), 63); });
+    const int mine = lane < c.B ? max(1, over(t, n_tiles)) : 0;
+    const int upto = wave_prefix_sum(mine);
+    if (which >= lane_value(upto, 63)) return {-1, 0, 0, 0};
+    const int b = static_cast<int>(__popcll(__ballot(upto <= which)));
+    const int n = lane_value(mine, b);
+    return {b, lane_value(upto, b) - n, n, parts_of(lane_value(t, b), n)};
+}
+
+// The chunks of more sequences than kFewSequences: one workgroup, a thread up to 16 neighbouring ones.  1,024 requests of 256 rows, 64
+// heads of 128 on 8: 190 us, 4,096 of 64 rows 317; where every wave added them up for itself 710 us and 8.9 ms (128 of 2,048 rows: 177 and 175).
+__global__ __launch_bounds__(1024) void deal_chunks_kernel(Call c) {
+    constexpr int kMost = kMaxSequences / 1024;
+    __shared__ int s_sums[16];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    auto scan = [&](int x, int& all) {  // sum up to this thread, and of all
+        const int upto = wave_prefix_sum(x);
+        if (lane == 63) s_sums[wave] = upto;
+        __syncthreads();
+        const int sums = wave_prefix_sum(lane < 16 ? s_sums[lane] : 0);
+        __syncthreads();
+        all = lane_value(sums, 15);
+        return upto + (wave > 0 ? lane_value(sums, max(wave - 1, 0)) : 0);
+    };
+    const int per = (c.B + 1023) / 1024, b0 = static_cast<int>(threadIdx.x) * per;
+    int t[kMost], low = 0, high = 0;  // lower 16 bits and the rest: 2^14 sequences of 2^25 tiles
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        t[i] = i < per && b0 + i < c.B ? rows_of(c, b0 + i).tiles() : -1;
+        low += t[i] < 0 ? 0 : t[i] & 0xFFFF;
+        high += t[i] < 0 ? 0 : t[i] >> 16;
+    }
+    auto parts = [&](int i, int n) { return t[i] < 0 ? 0 : max(1, over(t[i], n)); };
+    auto mine_of = [&](int n) {
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) mine += parts(i, n);
+        return mine;
+    };
+    int all_low, all_high, all;
+    scan(low, all_low);
+    scan(high, all_high);
+    const int n_tiles = chunk_length(c, (static_cast<int64_t>(all_high) << 16) + all_low, [&](int n) {
+        scan(mine_of(n), all);
+        return all;
+    });
+    const int mine = mine_of(n_tiles);
+    int first = scan(mine, all) - mine;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i)
+        if (t[i] >= 0) {
+            const int n = parts(i, n_tiles);
+            c.chunks[b0 + i] = make_int2(first, n);
+            first += n;
+        }
 }
 
 // Value that lanes l, l ^ 16, l ^ 32 and l ^ 48 hold the most, or the sum, of.
@@ -272,7 +326,7 @@ void paged_attention_kernel(Call c) {
     const Chunk chunk = find_chunk(c, which);
     if (chunk.b < 0) return;
     const int b = chunk.b;
-    if (which == chunk.first && hk == 0 && block == 0 && threadIdx.x == 0) c.chunks[b] = make_int2(chunk.first, chunk.n);
+    if (which == chunk.first && hk == 0 && block == 0 && threadIdx.x == 0 && c.B <= kFewSequences) c.chunks[b] = make_int2(chunk.first, chunk.n);
 
     const int R = c.S * c.G;
     const int held = held_rows(c, b);
@@ -756,7 +810,7 @@ Shape shape_of(int S, int H, int H_kv) {
 }
 
 // Chunks that there may be.
-size_t parts_of(const Shape& shape, int B) { return static_cast<size_t>(2) * shape.target + B; }
+int64_t parts_of(int B, int target) { return static_cast<int64_t>(most_rounds(B, target)) * target + B; }
 
 bool fits(int32_t B, int32_t S, int32_t H) { return H <= 1024 && static_cast<int64_t>(B) * S <= (1 << 22) && static_cast<int64_t>(B) * S * H <= (1 << 22); }
 
@@ -767,14 +821,17 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     hipError_t e = allow_lds(paged_attention_kernel<D, BITS, NB>, W::kBytes, allowed);
     if (e != hipSuccess) return e;
     const int64_t most_tiles = ((static_cast<int64_t>(c.table_pages) << c.page_lg) + kTileKeys - 1) / kTileKeys;
-    const bool one_each = most_tiles <= kMinTiles;  // no sequence can have two chunks
-    const int64_t chunks = std::min<int64_t>((in_two_rounds(c.B, c.target) ? 2 : 1) * static_cast<int64_t>(c.target) + c.B,
-                                             c.B * ((most_tiles + kMinTiles - 1) / kMinTiles));
+    const int64_t chunks = std::min<int64_t>(parts_of(c.B, c.target), c.B * ((most_tiles + kMinTiles - 1) / kMinTiles));
+    if (!c.one_each && c.B > kFewSequences) {
+        hipLaunchKernelGGL(deal_chunks_kernel, dim3(1), dim3(1024), 0, stream, c);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     const int64_t items = chunks * c.H_kv;
     const unsigned grid = static_cast<unsigned>((items + 7) / 8 * 8 * c.blocks);
     hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(W::kThreads), W::kBytes, stream, c);
     e = hipGetLastError();
-    if (e != hipSuccess || one_each) return e;
+    if (e != hipSuccess || c.one_each) return e;
     // Four waves a query's head where a sequence has more than 8 chunks, which is what one wave asks for at a time (8 requests of 32 chunks each: 59 us, with one
     // wave 63; where there are few chunks the other way round: 64 requests of one to four 207 us, with four waves 211; 24 of two or three 28 and 32).
     const int rows = c.B * c.S * c.H;
@@ -793,7 +850,7 @@ extern "C" {
 
 size_t si_paged_workspace_bytes(int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t D) {
     if (B < 1 || S < 1 || H < 1 || H_kv < 1 || D < 1 || H % H_kv != 0 || B > kMaxSequences || !fits(B, S, H)) return 0;
-    return parts_of(shape_of(S, H, H_kv), B) * S * H * (D + 2) * sizeof(float) + B * sizeof(int2);
+    return static_cast<size_t>(parts_of(B, shape_of(S, H, H_kv).target)) * S * H * (D + 2) * sizeof(float) + B * sizeof(int2);
 }
 
 si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t S, int32_t H, const int32_t* lengths, const int32_t* first,
@@ -813,14 +870,14 @@ si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t
     int lg = 0;
     while ((1 << lg) < cache->page_rows) ++lg;
     float* const parts = static_cast<float*>(workspace);
-    const size_t n_parts = parts_of(shape, cache->B);
+    const size_t n_parts = static_cast<size_t>(parts_of(cache->B, shape.target));
     const Call c = {static_cast<const __bf16*>(q),
                     {cache->K, cache->V ? cache->V : cache->K},
                     {static_cast<const unsigned char*>(cache->K_scales), static_cast<const unsigned char*>(cache->V ? cache->V_scales : cache->K_scales)},
                     cache->table, lengths, first, static_cast<__bf16*>(out), lse,
                     parts, parts + n_parts * S * H * cache->D, reinterpret_cast<int2*>(parts + n_parts * S * H * (cache->D + 2)),
                     scale_log2e, cache->B, S, H, cache->H_kv, H / cache->H_kv, cache->table_pages, cache->n_pages, lg, m, mask_mode, n_win,
-                    shape.blocks, shape.target};
+                    shape.blocks, shape.target, static_cast<int64_t>(cache->table_pages) * cache->page_rows <= kMinTiles * kTileKeys};
     const hipStream_t st = static_cast<hipStream_t>(stream);
 #define SI_LAUNCH(DD, BITS) report(shape.nb == 1 ? launch<DD, BITS, 1>(c, st) : shape.nb == 2 ? launch<DD, BITS, 2>(c, st) : launch<DD, BITS, 4>(c, st))
     if (cache->bits == 16) return cache->D == 128 ? SI_LAUNCH(128, 16) : SI_LAUNCH(64, 16);

@@ -4,7 +4,7 @@ import pytest
 
 from tests.test_cache_scratch_host import scratch_bytes  # noqa: F401
 
-KERNELS = {"store_pages_kernel": 12, "load_pages_kernel": 12, "paged_attention_kernel": 12, "join_chunks_kernel": 4, "prompt_attention_kernel": 4}
+KERNELS = {"store_pages_kernel": 12, "load_pages_kernel": 12, "paged_attention_kernel": 12, "join_chunks_kernel": 4, "deal_chunks_kernel": 1, "prompt_attention_kernel": 4}
 
 
 @pytest.mark.parametrize("kernel,forms", KERNELS.items())

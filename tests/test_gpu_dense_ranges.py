@@ -362,3 +362,46 @@ def test_rows_of_large_calls(bits, D, H, both):
         used[table[b, s // page].long() * page + s % page] = True
     left = K.permute(0, 2, 1, 3).reshape(n_pages * page, -1)[~used]
     assert bool((left == 7).all())
+
+
+@pytest.mark.parametrize("B,S,H,H_kv,D,bits,longest", [(65, 1, 8, 8, 64, 16, 600), (1100, 1, 4, 1, 64, 8, 400), (1100, 2, 16, 8, 128, 16, 300), (5000, 1, 8, 2, 64, 16, 90),
+                                                       (16384, 1, 2, 1, 64, 16, 40)])
+def test_more_sequences_than_lanes(B, S, H, H_kv, D, bits, longest):
+    """Mostly short ones, some empty, and three that are far longer than an even share; twice into the same workspace."""
+    rng = np.random.default_rng(B + S)
+    lengths = rng.integers(0, longest + 1, B)
+    lengths[rng.integers(0, B, B // 7)] = 0
+    far = [1, B // 2, B - 1]
+    lengths[far] = [40 * longest, 33, 9 * longest + 1]
+    page = 64
+    wide = -(-int(lengths.max()) // page)
+    first_page = np.concatenate([[0], np.cumsum(-(-lengths // page))])
+    table = np.full((B, wide), -1, dtype=np.int32)
+    for b in range(B):
+        n = first_page[b + 1] - first_page[b]
+        table[b, :n] = first_page[b] + np.arange(n)
+    g = torch.Generator(device=DEV).manual_seed(B)
+    shape = (int(first_page[-1]), H_kv, page, D)
+    if bits == 16:
+        K, V = (torch.randn(shape, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        ks = vs = None
+    else:
+        K, V = (torch.randint(0, 127, shape, generator=g, device=DEV, dtype=torch.uint8) for _ in range(2))
+        ks, vs = (torch.randint(118, 121, shape[:3], generator=g, device=DEV, dtype=torch.uint8) for _ in range(2))
+    q = torch.randn((B, S, H, D), generator=g, device=DEV).to(torch.bfloat16)
+    first = [int(n) - S for n in lengths]
+    print(f"sequences B={B} S={S} H={H}/{H_kv} D={D} bits={bits}", flush=True)
+    out, lse = _paged(q, torch.from_numpy(table).to(DEV), K, V, ks, vs, lengths.tolist(), first, 1, CAUSAL, R.ALL, 0.05)
+    again = _paged(q, torch.from_numpy(table).to(DEV), K, V, ks, vs, lengths.tolist(), first, 1, CAUSAL, R.ALL, 0.05)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    for b in far + sorted(rng.integers(0, B, 40).tolist()):
+        n = int(lengths[b])
+        rows = []
+        for pages, scales in ((K, ks), (V, vs)):
+            x = pages[int(first_page[b]):int(first_page[b + 1])].permute(0, 2, 1, 3).reshape(-1, H_kv, D)[:n]
+            if bits == 8:
+                e = scales[int(first_page[b]):int(first_page[b + 1])].permute(0, 2, 1).reshape(-1, H_kv)[:n].cpu().numpy().astype(np.int64) - 127
+                rows.append(R.values(x.cpu().numpy().astype(np.int64), e))
+            else:
+                rows.append(R.to64(x))
+        _near(out[b], lse[b], R.attend(R.to64(q[b]), *rows, range(first[b], first[b] + S), 1, 1, R.ALL, 0.05), b)
