@@ -459,10 +459,12 @@ hipError_t launch(Call c, int64_t n_columns, hipStream_t stream) {
 
 // Heads of 64: 128 columns a workgroup and tiles of 32 rows, so that three workgroups share a compute unit and one's start and end go by beside the others' products
 // (23 prompts of up to 1,500, 33 heads on 3: 164 us; 256 columns and 64 rows: 177; 8,192 queries, 64 heads on 8: 597 against 612).
-// Heads of 128: 256 columns and 64 rows, which load a tile for twice as many products (8,192 queries, 64 heads on 8: 993 us; the smaller form 1,037).  Where
-// that would be fewer workgroups than compute units, the smaller form, two a unit (1,024 queries: 33.3 -> 30.2 us; four prompts of 33 to 300: 17.9 -> 15.6); and where
-// it would be fewer than half as many, 128 columns and 64 rows, of which one fits a unit, so that they spread (512 queries behind 8,192: 163 us in the smaller
-// form, 156 in this; 300 behind 4,000: 79 and 74).
+// Heads of 128: 256 columns and 64 rows, which load a tile for twice as many products (8,192 queries, 64 heads on 8: 993 us; the smaller form 1,037; 4 prompts of 4,000,
+// 32 heads on 32: 575 and 594).  The smaller form, two a unit, where start and end count for more, as a sequence has few rows to see (16 prompts of 1,000: 391 -> 372 us,
+// 300 of 100: 424 -> 322, 16,384 queries with a window of 128: 268 -> 206; 8 of 2,000: 597 and 600) or few columns, which leave more of 256 than of 128 without work (100
+// parts of 100 queries behind 2,000: 866 -> 789; 30 of 500 behind 2,000: 1,075 and 1,117).  And where 256 columns would be fewer workgroups than compute units (1,024
+// queries: 33.3 -> 30.2 us); where they would be fewer than half as many, 128 columns and 64 rows, of which one fits a unit, so that they spread (512 queries behind 8,192:
+// 163 us in the smaller form, 156 in this; 300 behind 4,000: 79 and 74).
 template <int D>
 hipError_t launch(const Call& c, hipStream_t stream) {
     constexpr int kUnits = 256;
@@ -470,9 +472,10 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     if constexpr (D == 64) {
         return launch<D, 4, 32>(c, n_columns, stream);
     } else {
-        const int64_t workgroups = n_columns / 256 * c.H_kv;
+        const int64_t sequences = c.queries.B, workgroups = std::max(n_columns / 256, sequences) * c.H_kv;
+        const int64_t seen = std::min<int64_t>(c.n_win, c.rows.N / sequences);  // rows, by a sequence of mean length
         if (workgroups <= kUnits / 2) return launch<D, 4, 64>(c, n_columns, stream);
-        if (workgroups <= kUnits) return launch<D, 4, 32>(c, n_columns, stream);
+        if (workgroups <= kUnits || seen < 2048 || n_columns < 1024 * sequences) return launch<D, 4, 32>(c, n_columns, stream);
         return launch<D, 8, 64>(c, n_columns, stream);
     }
 }

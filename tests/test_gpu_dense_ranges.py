@@ -209,11 +209,15 @@ def _prompt(q, k, v, qo, ko, first, m, mask, n_win, scale):
 
 
 @pytest.mark.parametrize("H,H_kv,D,lengths,before,m,n_win", [
-    (32, 4, 128, [2100, 0, 317], [0, 0, 200], 1, R.ALL),     # 256 columns a workgroup
+    (32, 4, 128, [2600, 1500, 317], [0, 700, 2000], 1, R.ALL),  # 256 columns a workgroup
+    (32, 4, 128, [2600, 1500], [0, 700], 1, 2100),
+    (64, 1, 128, [8300, 900], [5, 7400], 4, R.ALL),
+    (64, 2, 128, [2500, 31, 1], [0, 2100, 2777], 1, 2049),
+    (33, 3, 128, [3100, 2], [0, 3000], 1, R.ALL),
+    (32, 4, 128, [2100, 0, 317], [0, 0, 200], 1, R.ALL),     # as many columns in all, but of few rows or in a window: 128 columns, tiles of 32 rows
     (32, 4, 128, [2100, 317], [0, 200], 1, 300),
-    (64, 1, 128, [1200, 900], [5, 0], 4, R.ALL),
     (33, 3, 128, [2500, 31, 1], [0, 0, 777], 1, R.ALL),
-    (16, 2, 128, [1100, 700], [0, 60], 1, 129),              # 128 columns, tiles of 32 rows
+    (16, 2, 128, [1100, 700], [0, 60], 1, 129),              # few: 128 columns, tiles of 64 rows
     (16, 2, 128, [300, 130], [900, 0], 1, R.ALL),            # 128 columns, tiles of 64 rows
     (32, 4, 64, [1500, 200], [0, 99], 1, 64),
 ])
@@ -237,20 +241,20 @@ def test_forms_of_the_prompt(H, H_kv, D, lengths, before, m, n_win):
     assert torch.equal(again[0], out) and torch.equal(again[1], lse)
 
 
-@pytest.mark.parametrize("n,H,H_kv", [(2200, 32, 4), (1100, 16, 2), (300, 16, 2)])
-def test_rows_that_are_not_seen_in_every_form(n, H, H_kv):
+@pytest.mark.parametrize("n,H,H_kv,n_win", [(2600, 32, 4, 2050), (2200, 32, 4, 100), (1100, 16, 2, 100), (300, 16, 2, 100)])
+def test_rows_that_are_not_seen_in_every_form(n, H, H_kv, n_win):
     g = torch.Generator().manual_seed(n)
     q = torch.randn((n, H, 128), generator=g).to(torch.bfloat16)
     k, v = (torch.randn((n, H_kv, 128), generator=g).to(torch.bfloat16) for _ in range(2))
-    clean = _prompt(q, k, v, None, None, None, 1, CAUSAL, 100, 0.1)
-    at = [0, 31, 70, n - 140, n - 1]
+    clean = _prompt(q, k, v, None, None, None, 1, CAUSAL, n_win, 0.1)
+    at = [0, 31, n - 140, n - 1] if n_win > 100 else [0, 31, 70, n - 140, n - 1]
     for s in at:
         v[s] = float("nan")
-    out, lse = _prompt(q, k, v, None, None, None, 1, CAUSAL, 100, 0.1)
+    out, lse = _prompt(q, k, v, None, None, None, 1, CAUSAL, n_win, 0.1)
     t = np.arange(n)
-    seen = np.any([(t >= s) & (t < s + 100) for s in at], axis=0)
+    seen = np.any([(t >= s) & (t < s + n_win) for s in at], axis=0)
     fine = torch.from_numpy(~seen).to(DEV)
-    assert torch.equal(out[fine], clean[0][fine]) and torch.equal(lse, clean[1])
+    assert bool(fine.any()) and torch.equal(out[fine], clean[0][fine]) and torch.equal(lse, clean[1])
     assert bool(torch.isnan(out[~fine]).all())
 
 

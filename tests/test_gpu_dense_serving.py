@@ -139,7 +139,7 @@ def test_attention_on_a_side_stream_and_replayed(lengths, S, H, H_kv, D, bits):
     _replays(call, outputs, call.workspace)
 
 
-@pytest.mark.parametrize("n,H,H_kv,D", [(700, 64, 8, 128), (150, 8, 2, 64), (2300, 32, 4, 128)])
+@pytest.mark.parametrize("n,H,H_kv,D", [(700, 64, 8, 128), (150, 8, 2, 64), (2300, 32, 4, 128), (7000, 16, 2, 128)])
 def test_prompts_on_a_side_stream_and_replayed(n, H, H_kv, D):
     g = torch.Generator().manual_seed(n)
     q = torch.randn((n, H, D), generator=g).to(torch.bfloat16).to(DEV)
