@@ -54,7 +54,7 @@ struct Call {
     int blocks;  // of columns
     int target;  // chunks that fit the chip at once
     int most_tiles;  // of what the positions of a sequence see
-    __host__ __device__ bool one_each() const { return most_tiles <= kMinTiles; }  // no sequence can have two chunks
+    bool one_each;   // a sequence is a chunk
 };
 
 // Rows that the positions of sequence b see: [lo, hi) all of them together.
@@ -128,7 +128,7 @@ constexpr int kFewSequences = 64;  // every wave deals them out for itself, a la
 // The chunk with number `which`.  All 64 lanes call it.
 __device__ __forceinline__ Chunk find_chunk(const Call& c, int which) {
     auto parts_of = [&](int t, int n) { return static_cast<int>((static_cast<uint32_t>(t) + n - 1) / static_cast<uint32_t>(n)); };
-    if (c.one_each()) return {which < c.B ? which : -1, which, 1, which < c.B ? rows_of(c, which).tiles() : 0};
+    if (c.one_each) return {which < c.B ? which : -1, which, 1, which < c.B ? rows_of(c, which).tiles() : 0};
     if (c.B > kFewSequences) {
         const int b = last_not_above(c.B, which, [&](int i) { return static_cast<int64_t>(c.chunks[i].x); });
         const int2 chunk = c.chunks[b];
@@ -821,8 +821,8 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     using W = Group<D, BITS, NB>;
     hipError_t e = allow_lds(paged_attention_kernel<D, BITS, NB>, W::kBytes, allowed);
     if (e != hipSuccess) return e;
-    const int64_t chunks = std::min<int64_t>(parts_of(c.B, c.target), static_cast<int64_t>(c.B) * ((c.most_tiles + kMinTiles - 1) / kMinTiles));
-    if (!c.one_each() && c.B > kFewSequences) {
+    const int64_t chunks = c.one_each ? c.B : std::min<int64_t>(parts_of(c.B, c.target), static_cast<int64_t>(c.B) * ((c.most_tiles + kMinTiles - 1) / kMinTiles));
+    if (!c.one_each && c.B > kFewSequences) {
         hipLaunchKernelGGL(deal_chunks_kernel, dim3(1), dim3(1024), 0, stream, c);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -831,7 +831,7 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     const unsigned grid = static_cast<unsigned>((items + 7) / 8 * 8 * c.blocks);
     hipLaunchKernelGGL((paged_attention_kernel<D, BITS, NB>), dim3(grid), dim3(W::kThreads), W::kBytes, stream, c);
     e = hipGetLastError();
-    if (e != hipSuccess || c.one_each()) return e;
+    if (e != hipSuccess || c.one_each) return e;
     // Four waves a query's head where a sequence has more than 8 chunks, which is what one wave asks for at a time (8 requests of 32 chunks each: 59 us, with one
     // wave 63; where there are few chunks the other way round: 64 requests of one to four 207 us, with four waves 211; 24 of two or three 28 and 32).
     const int rows = c.B * c.S * c.H;
@@ -870,6 +870,9 @@ si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t
     // S positions see n_win + S - 1 rows at most, all of them together: rows that begin and end inside a tile
     const int64_t held = static_cast<int64_t>(cache->table_pages) * cache->page_rows, seen = static_cast<int64_t>(n_win) + S - 1;
     const int64_t most_tiles = std::min((held + kTileKeys - 1) / kTileKeys, (seen + 2 * kTileKeys - 2) / kTileKeys);
+    // Sequences of so few tiles stay whole, which takes one launch instead of two (64 heads of 128 on 8, 512 rows: 14.6 -> 10.1 us, 1,024 rows 13.6 -> 11.2, 64 requests of
+    // them 45 -> 43; 2,048 rows 14.7 and 17.5).  With 64 columns a tile takes longer (512 rows 16.1 -> 13.7, 1,024 rows 16.9 and 18.2).
+    const bool one_each = most_tiles <= (shape.nb == 4 ? 16 : 32);
     int lg = 0;
     while ((1 << lg) < cache->page_rows) ++lg;
     float* const parts = static_cast<float*>(workspace);
@@ -880,7 +883,7 @@ si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t
                     cache->table, lengths, first, static_cast<__bf16*>(out), lse,
                     parts, parts + n_parts * S * H * cache->D, reinterpret_cast<int2*>(parts + n_parts * S * H * (cache->D + 2)),
                     scale_log2e, cache->B, S, H, cache->H_kv, H / cache->H_kv, cache->table_pages, cache->n_pages, lg, m, mask_mode, n_win,
-                    shape.blocks, shape.target, static_cast<int>(most_tiles)};
+                    shape.blocks, shape.target, static_cast<int>(most_tiles), one_each};
     const hipStream_t st = static_cast<hipStream_t>(stream);
 #define SI_LAUNCH(DD, BITS) report(shape.nb == 1 ? launch<DD, BITS, 1>(c, st) : shape.nb == 2 ? launch<DD, BITS, 2>(c, st) : launch<DD, BITS, 4>(c, st))
     if (cache->bits == 16) return cache->D == 128 ? SI_LAUNCH(128, 16) : SI_LAUNCH(64, 16);

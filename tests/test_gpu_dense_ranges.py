@@ -38,16 +38,17 @@ def _paged(q, table, K, V, ks, vs, lengths, first, m, mask, n_win, scale):
 @pytest.mark.parametrize("S,H,H_kv", [(1, 16, 1), (1, 17, 1), (1, 32, 1), (1, 33, 1), (1, 64, 1), (1, 65, 1), (3, 43, 1), (2, 48, 3), (16, 8, 8), (130, 1, 1)])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("bits", [16, 8])
-def test_columns_of_a_workgroup(S, H, H_kv, D, bits):
-    """Around 16, 32, 64 and 128 columns that share a head."""
-    lengths = [301, 77]
-    pages = R.Pages(S + H, lengths, H_kv, D, bits, 16)
+@pytest.mark.parametrize("n_win,wide", [(290, None), (R.ALL, None), (R.ALL, 140), (1300, 140)])
+def test_columns_of_a_workgroup(S, H, H_kv, D, bits, n_win, wide):
+    """Around 16, 32, 64 and 128 columns that share a head; sequences that stay whole, and, where the table has room for long ones, that are dealt out."""
+    lengths = [301, 77] if n_win != 1300 else [2001, 1400]
+    pages = R.Pages(S + H, lengths, H_kv, D, bits, 16, wide=wide)
     q = torch.randn((2, S, H, D), generator=torch.Generator().manual_seed(D)).to(torch.bfloat16)
     first = [max(0, n - S) for n in lengths]
-    print(f"columns S={S} H={H}/{H_kv} D={D} bits={bits}", flush=True)
-    out, lse = _paged(q, *pages.to(DEV), lengths, first, 1, CAUSAL, 290, 0.1)
+    print(f"columns S={S} H={H}/{H_kv} D={D} bits={bits} n_win={n_win} wide={wide}", flush=True)
+    out, lse = _paged(q, *pages.to(DEV), lengths, first, 1, CAUSAL, n_win, 0.1)
     for b, n in enumerate(lengths):
-        _near(out[b], lse[b], R.attend(R.to64(q[b]), pages.k64[b], pages.v64[b], first[b] + np.arange(S), 1, 1, 290, 0.1), b)
+        _near(out[b], lse[b], R.attend(R.to64(q[b]), pages.k64[b], pages.v64[b], first[b] + np.arange(S), 1, 1, n_win, 0.1), b)
 
 
 @pytest.mark.parametrize("B,H,H_kv,longest", [(70, 8, 8, 40), (300, 8, 4, 100), (700, 4, 2, 33), (130, 40, 1, 700)])

@@ -27,10 +27,10 @@ def _near(got, lse, want, what):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-@pytest.mark.parametrize("D,H,H_kv", [(128, 16, 2), (64, 33, 1)])
-def test_requests_from_prompt_to_drafted_positions(bits, D, H, H_kv):
+@pytest.mark.parametrize("D,H,H_kv,room", [(128, 16, 2, 320), (64, 33, 1, 320), (128, 16, 2, 2048), (64, 33, 1, 1600)])
+def test_requests_from_prompt_to_drafted_positions(bits, D, H, H_kv, room):
     g = torch.Generator().manual_seed(bits + D)
-    scale, page, wide, n_pages = 1.0 / np.sqrt(D), 16, 20, 70
+    scale, page, wide, n_pages = 1.0 / np.sqrt(D), 16, room // 16, 3 * room // 16 + 10
     parts = [[130, 61, 7], [33, 100, 1]]  # two parts of each prompt
     B = 3
     total = [sum(p) for p in zip(*parts)]

@@ -161,9 +161,10 @@ CASES = [
 @pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("shared", [False, True])
-def test_attention(case, bits, shared):
+@pytest.mark.parametrize("room", [0, 2500])  # of the table: long sequences are dealt out over the chip
+def test_attention(case, bits, shared, room):
     B, S, lengths, H, H_kv, D, page, mask, m, n_win = case
-    pages = R.Pages(11, lengths, H_kv, D, bits, page, shared=shared)  # NaN wherever no sequence has rows
+    pages = R.Pages(11, lengths, H_kv, D, bits, page, shared=shared, wide=max(-(-max(lengths) // page), -(-room // page)))  # NaN wherever no sequence has rows
     g = torch.Generator().manual_seed(5)
     q = torch.randn((B, S, H, D), generator=g).to(torch.bfloat16)
     first = [max(0, n - S) for n in lengths] if mask == CAUSAL else None
