@@ -339,8 +339,9 @@ void prompt_attention_kernel(Call c) {
     };
 
     // A tile, with its first block's scores in x; then x or y has those of the next tile's first block.  That tile is at `next`, and the one after it is asked
-    // for, to `to`: of different places, as the compiler has to know (__restrict__), or the transposing reads wait for all that is on its way to LDS.
-    auto take_whole = [&](const lds_byte* __restrict__ now, const lds_byte* __restrict__ next, lds_byte* __restrict__ to, int s0, bool last, floatx16& x, floatx16& y) {
+    // for, to `to`, which nothing in here reads, as the compiler has to know (__restrict__): else the transposing reads wait for all that is on its way to LDS
+    // (four prompts of 33 to 300: 17.2 -> 16.6 us, 8,192 queries 1,026 -> 997, 23 prompts of up to 1,500 with heads of 64 180 -> 166).
+    auto take_whole = [&](const lds_byte* now, const lds_byte* next, lds_byte* __restrict__ to, int s0, bool last, floatx16& x, floatx16& y) {
         if constexpr (kRows == 64) step(now, now + 32 * kRowBytes, x, y);
         if (!last) arrive(s0 + kRows, to);
         const lds_byte* const then = last ? now : next;  // behind the last block the scores are not used
