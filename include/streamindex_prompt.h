@@ -14,7 +14,8 @@
  *   out[i,g,:]  = sum_{s in seen(t)} exp(x_s - lse) V[s,h,:],   lse[i,g] = ln sum_{s in seen(t)} exp(x_s);
  *   out = 0 and lse = -inf where nothing is seen.
  * m = 1 is causal attention, m > 1 attention over compressed rows, one per m positions (legal(t) of streamindex.h).  A prompt's next
- * part has first = the number of positions before it and the rows of all of them.
+ * part has first = the number of positions before it and the rows of all of them.  (A part of few queries behind many rows is faster by
+ * si_paged_attention, which splits the rows over the chip: 128 queries behind 8,192 rows, 64 heads of 128 on 8: 52 us against 137.)
  */
 #ifndef STREAMINDEX_PROMPT_H
 #define STREAMINDEX_PROMPT_H

@@ -133,7 +133,8 @@ def _replays(call, outputs, ws=None):
         assert _same(eager, again)
 
 
-@pytest.mark.parametrize("lengths,S,H,H_kv,D,bits", [([3000, 5, 700], 1, 8, 8, 128, 16), ([2000] * 5, 1, 64, 1, 128, 8), ([900, 333], 4, 40, 8, 64, 8), ([100], 1, 8, 2, 64, 16)])
+@pytest.mark.parametrize("lengths,S,H,H_kv,D,bits", [([3000, 5, 700], 1, 8, 8, 128, 16), ([2000] * 5, 1, 64, 1, 128, 8), ([900, 333], 4, 40, 8, 64, 8), ([100], 1, 8, 2, 64, 16),
+                                                         ([1100, 0] + list(range(30, 130)), 1, 8, 4, 64, 16)])
 def test_attention_on_a_side_stream_and_replayed(lengths, S, H, H_kv, D, bits):
     call, outputs = _paged_problem(1, lengths, S, H, H_kv, D, bits)
     _replays(call, outputs, call.workspace)
