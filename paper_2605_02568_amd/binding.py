@@ -513,10 +513,11 @@ def _paged_cache(table, K, V, k_scales, v_scales):
             raise ValueError("a cache in 16 bits has no scales")
     elif dtype is torch.uint8:
         bits = 8
-        if k_scales is None or k_scales.shape != ks[:3]:
-            raise ValueError(f"k_scales must be {tuple(ks[:3])}")
-        if (V is None) != (v_scales is None) or (V is not None and v_scales.shape != ks[:3]):
-            raise ValueError(f"v_scales must be {tuple(ks[:3])}, None where V is")
+        of_rows = ks[:3]
+        if k_scales is None or k_scales.shape != of_rows:
+            raise ValueError(f"k_scales must be {tuple(of_rows)}")
+        if (V is None) != (v_scales is None) or (V is not None and v_scales.shape != of_rows):
+            raise ValueError(f"v_scales must be {tuple(of_rows)}, None where V is")
     else:
         raise TypeError(f"K must be torch.bfloat16 or torch.uint8, got {dtype}")
     if V is not None and V.shape != ks:
@@ -542,9 +543,10 @@ def _offsets_of(offsets, B, gpu: int, name: str):
 
 def _packed_rows(rows, H, D, gpu: int, name: str):
     """Pointer and number of packed rows [N,H,D] bf16."""
-    if len(rows.shape) != 3 or rows.shape[1] != H or rows.shape[2] != D:
-        raise ValueError(f"{name} must be [N, {H}, {D}], got {tuple(rows.shape)}")
-    return _ptr(rows, torch.bfloat16, gpu, name), rows.shape[0]
+    shape = rows.shape
+    if len(shape) != 3 or shape[1] != H or shape[2] != D:
+        raise ValueError(f"{name} must be [N, {H}, {D}], got {tuple(shape)}")
+    return _ptr(rows, torch.bfloat16, gpu, name), shape[0]
 
 
 def si_store_pages(k_rows, v_rows, offsets, start, table, K, V, k_scales=None, v_scales=None, stream=None):
