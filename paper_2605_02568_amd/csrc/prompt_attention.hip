@@ -92,8 +92,12 @@ __device__ __forceinline__ int lane_again() {
     return lane;
 }
 
+// Tiles of keys and values; then 32 rows of 64 d of the results a wave, with the weights of 8 rows in the same place.  With heads of 64 the results go to the tiles' place,
+// behind a barrier more, as three workgroups have to fit a compute unit.
+template <int D>
+constexpr int wave_bytes() { return D == 64 ? 8 * 32 * 4 : 32 * 128; }
 template <int D, int kWaves, int kRows>
-constexpr int lds_bytes() { return kSlots * 2 * kRows * D * 2 + kWaves * 32 * 32 * 4; }  // tiles of keys and values; weights of a block a wave
+constexpr int lds_bytes() { return kSlots * 2 * kRows * D * 2 + kWaves * wave_bytes<D>(); }
 
 // Grid: (slots of columns, the last ones first) x heads of keys and values, heads next to each other so that with 8 of them each has an XCD.  A sequence's
 // slots begin at (its first packed column) / (columns of a workgroup) + (its number): slots enough for any lengths, with no sum over the sequences before.
@@ -257,22 +261,25 @@ void prompt_attention_kernel(Call c) {
         if (odd) {
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) vf[i] = finite_or_zero(vf[i]);
-            float* const weights = reinterpret_cast<float*>(lds + kSlots * 2 * kTileBytes) + wave * (32 * 32);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) weights[(8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = x[j];
-            wave_order();
+            float* const weights = reinterpret_cast<float*>(lds + kSlots * 2 * kTileBytes + wave * wave_bytes<D>());
             typedef __attribute__((address_space(3))) const bf16x4 lds_bf16x4;
+#pragma unroll
+            for (int part = 0; part < 4; ++part) {  // 8 rows at a time
+#pragma unroll
+                for (int j = 0; j < 4; ++j) weights[(4 * half + j) * 32 + col] = x[4 * part + j];
+                wave_order();
 #pragma unroll 1
-            for (int r = 0; r < 32; ++r) {
-                const float w = weights[r * 32 + col];
-                const bool sees = s0 + r >= from && s0 + r < legal;
+                for (int r = 8 * part; r < 8 * part + 8; ++r) {
+                    const float w = weights[(r & 7) * 32 + col];
+                    const bool sees = s0 + r >= from && s0 + r < legal;
 #pragma unroll
-                for (int db = 0; db < DB; ++db)
+                    for (int db = 0; db < DB; ++db)
 #pragma unroll
-                    for (int a = 0; a < 4; ++a)
-                        add_not_finite(acc[db], 4 * a, *(lds_bf16x4*)(block + apart + tile_slot<D>(r, 4 * db + a) * 16 + half * 8), w, sees);
+                        for (int a = 0; a < 4; ++a)
+                            add_not_finite(acc[db], 4 * a, *(lds_bf16x4*)(block + apart + tile_slot<D>(r, 4 * db + a) * 16 + half * 8), w, sees);
+                }
+                wave_order();
             }
-            wave_order();
         }
         // contraction index e of part i / DB <-> row 16 (i / DB) + 8 (e / 4) + 4 half + e % 4 of the block on both operands
 #pragma unroll
@@ -409,7 +416,7 @@ void prompt_attention_kernel(Call c) {
     }
     const float m_ref = -shift;
 
-    // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4.  64 d of the wave's columns go through its own LDS, so that the results are
+    // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4.  64 d of the wave's columns go through LDS, so that the results are
     // written by whole lines (four prompts of 33 to 300: 15.5 us; 8 bytes a lane and 32 rows at once: 17.0).
     const floatx2 l_halves = both_halves(l_sum);
     const float l = l_halves[0] + l_halves[1];
@@ -424,7 +431,9 @@ void prompt_attention_kernel(Call c) {
         return static_cast<int64_t>(q_first + i_query) * c.H + hk * c.G + (r - i_query * c.G);
     };
     if (c.lse && half2 == 0 && col2 < left) c.lse[row_of(r_first + col2)] = none ? -__builtin_huge_valf() : log_of(m_ref, l);
-    unsigned char* const mine = lds + kSlots * 2 * kTileBytes + wave * (32 * 32 * 4);
+    static_assert(kWaves * 32 * 128 <= kSlots * 2 * kTileBytes, "the tiles' place");
+    unsigned char* const mine = lds + (D == 64 ? 0 : kSlots * 2 * kTileBytes) + wave * (32 * 128);
+    if constexpr (D == 64) __syncthreads();  // all tiles have been read
 #pragma unroll
     for (int db0 = 0; db0 < DB; db0 += 2) {
         wave_order();
@@ -458,8 +467,8 @@ hipError_t launch(Call c, int64_t n_columns, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Heads of 64: 128 columns a workgroup and tiles of 32 rows, so that three workgroups share a compute unit and one's start and end go by beside the others' products
-// (23 prompts of up to 1,500, 33 heads on 3: 164 us; 256 columns and 64 rows: 177; 8,192 queries, 64 heads on 8: 597 against 612).
+// Heads of 64: 128 columns a workgroup, so that three share a compute unit and one's start and end go by beside the others' products, and tiles of 64 rows (23 prompts
+// of up to 1,500, 33 heads on 3: 159 us, 8,192 queries, 64 heads on 8: 597; tiles of 32 rows 164 and 610; 256 columns 177 and 612).
 // Heads of 128: 256 columns and 64 rows, which load a tile for twice as many products (8,192 queries, 64 heads on 8: 993 us; the smaller form 1,037; 4 prompts of 4,000,
 // 32 heads on 32: 575 and 594).  The smaller form, two a unit, where start and end count for more, as a sequence has few rows to see (16 prompts of 1,000: 391 -> 372 us,
 // 300 of 100: 424 -> 322, 16,384 queries with a window of 128: 268 -> 206; 8 of 2,000: 597 and 600) or few columns, which leave more of 256 than of 128 without work (100
@@ -471,7 +480,7 @@ hipError_t launch(const Call& c, hipStream_t stream) {
     constexpr int kUnits = 256;
     const int64_t n_columns = static_cast<int64_t>(c.queries.N) * c.G;
     if constexpr (D == 64) {
-        return launch<D, 4, 32>(c, n_columns, stream);
+        return launch<D, 4, 64>(c, n_columns, stream);
     } else {
         const int64_t sequences = c.queries.B, workgroups = std::max(n_columns / 256, sequences) * c.H_kv;
         const int64_t seen = std::min<int64_t>(c.n_win, c.rows.N / sequences);  // rows, by a sequence of mean length

@@ -221,6 +221,7 @@ def _prompt(q, k, v, qo, ko, first, m, mask, n_win, scale):
     (16, 2, 128, [1100, 700], [0, 60], 1, 129),              # few: 128 columns, tiles of 64 rows
     (16, 2, 128, [300, 130], [900, 0], 1, R.ALL),            # 128 columns, tiles of 64 rows
     (32, 4, 64, [1500, 200], [0, 99], 1, 64),
+    (33, 3, 64, [1500, 0, 65, 1], [0, 0, 700, 3], 1, R.ALL),
 ])
 def test_forms_of_the_prompt(H, H_kv, D, lengths, before, m, n_win):
     g = torch.Generator().manual_seed(H + D)
@@ -242,11 +243,12 @@ def test_forms_of_the_prompt(H, H_kv, D, lengths, before, m, n_win):
     assert torch.equal(again[0], out) and torch.equal(again[1], lse)
 
 
-@pytest.mark.parametrize("n,H,H_kv,n_win", [(2600, 32, 4, 2050), (2200, 32, 4, 100), (1100, 16, 2, 100), (300, 16, 2, 100)])
-def test_rows_that_are_not_seen_in_every_form(n, H, H_kv, n_win):
+@pytest.mark.parametrize("n,H,H_kv,n_win,D", [(2600, 32, 4, 2050, 128), (2200, 32, 4, 100, 128), (1100, 16, 2, 100, 128), (300, 16, 2, 100, 128), (1100, 16, 2, 100, 64),
+                                             (2600, 33, 3, 2050, 64)])
+def test_rows_that_are_not_seen_in_every_form(n, H, H_kv, n_win, D):
     g = torch.Generator().manual_seed(n)
-    q = torch.randn((n, H, 128), generator=g).to(torch.bfloat16)
-    k, v = (torch.randn((n, H_kv, 128), generator=g).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((n, H, D), generator=g).to(torch.bfloat16)
+    k, v = (torch.randn((n, H_kv, D), generator=g).to(torch.bfloat16) for _ in range(2))
     clean = _prompt(q, k, v, None, None, None, 1, CAUSAL, n_win, 0.1)
     at = [0, 31, n - 140, n - 1] if n_win > 100 else [0, 31, 70, n - 140, n - 1]
     for s in at:
