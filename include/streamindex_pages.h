@@ -79,7 +79,8 @@ si_status si_load_pages(const si_paged_cache* cache, int32_t N, const int32_t* o
  * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
  * weight of 0; infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
  * that a position does not see (behind the length, before the window, later positions' rows) never reaches its result, NaN and infinities included.
- * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  The same call gives the same bits. */
+ * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  The same call gives the same bits, and no bit of a head's
+ * result depends on the queries of other heads or positions. */
 size_t si_paged_workspace_bytes(int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t D);
 si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t S, int32_t H, const int32_t* lengths, const int32_t* first,
                              int32_t m, si_mask_mode mask_mode, int32_t n_win, float scale, void* out, float* lse, void* workspace,

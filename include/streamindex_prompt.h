@@ -49,7 +49,8 @@ typedef struct {
  * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
  * weight of 0; infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
  * that a query does not see (later positions, before the window, other sequences) never reaches its result, NaN and infinities included.
- * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  No workspace.  The same call gives the same bits.
+ * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  No workspace.  The same call gives the same bits, and no bit of a head's
+ * result depends on the queries of other heads or positions.
  * Limits, SI_ERR_UNSUPPORTED_SHAPE beyond them: D = 64 or 128, H <= 1024, N_q, N_k <= 2^30, B <= 2^20, N_q H + 128 B H_kv < 2^30. */
 si_status si_prompt_attention(const void* q, const void* K, const void* V, const si_packed_dims* dims, const int32_t* q_offsets,
                               const int32_t* k_offsets, const int32_t* first, int32_t m, si_mask_mode mask_mode, int32_t n_win, float scale,

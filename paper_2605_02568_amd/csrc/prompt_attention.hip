@@ -336,7 +336,8 @@ void prompt_attention_kernel(Call c) {
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to_log2, by)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], to_log2, by));
-                sum += p0 + p1;
+                sum += p0;  // in the order of the products above: a column whose reference stays keeps its bits, whatever its neighbours need
+                sum += p1;
                 two_weights(pn, j, p0, p1);
             }
         }
