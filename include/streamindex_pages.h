@@ -77,7 +77,7 @@ si_status si_load_pages(const si_paged_cache* cache, int32_t N, const int32_t* o
  *   workspace  device, si_paged_workspace_bytes(B, S, H, H_kv, D) bytes
  * fp32 products, statistics and sums.  A weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the
  * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
- * weight of 0; infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
+ * weight of 0 (a finite query with no other logits gets out = 0 and lse = -inf); infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
  * that a position does not see (behind the length, before the window, later positions' rows) never reaches its result, NaN and infinities included.
  * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  The same call gives the same bits, and no bit of a head's
  * result depends on the queries of other heads or positions. */

@@ -47,7 +47,7 @@ typedef struct {
  *   out        device [N_q,H,D] bf16;  lse device [N_q,H] f32 or NULL.  Queries that belong to no sequence are left as they were.
  * fp32 products, statistics and sums.  A weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the
  * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
- * weight of 0; infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
+ * weight of 0 (a finite query with no other logits gets out = 0 and lse = -inf); infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
  * that a query does not see (later positions, before the window, other sequences) never reaches its result, NaN and infinities included.
  * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  No workspace.  The same call gives the same bits, and no bit of a head's
  * result depends on the queries of other heads or positions.

@@ -550,7 +550,22 @@ void paged_attention_kernel(Call c) {
                 for (int db = 0; db < DB; ++db) acc[nb][db] *= alpha;
                 l_sum[nb] *= alpha;
                 shift[nb] = raised;
-                exponentials(nb, raised == __builtin_huge_valf() ? 0.0f : raised);  // a column that has seen nothing yet
+                float by = raised == __builtin_huge_valf() ? 0.0f : raised;  // a column that has seen nothing yet
+                // or rows whose logits are all minus infinity: NaN if the query is what makes them so
+                const bool sees = raised == __builtin_huge_valf() && rows_seen(nb) != 0;
+                if (__ballot(sees) != 0ull) {
+                    unsigned found = 0;
+#pragma unroll 1
+                    for (int ks = 0; ks < KS; ++ks) {
+                        if constexpr (W::kSharedQueries) found |= not_finite(query_of(nb, ks));
+                        else found |= not_finite(query(columns[nb * 16 + col].x, ks));
+                    }
+                    unsigned long long odd = __ballot(found != 0);
+                    odd |= odd >> 32;
+                    odd |= odd >> 16;
+                    if (sees && (odd >> col) & 1) by = __builtin_nanf("");
+                }
+                exponentials(nb, by);
             }
         }
         float powers[8];  // of the values: they go into the weights, which is exact

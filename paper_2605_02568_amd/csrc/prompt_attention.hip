@@ -420,9 +420,8 @@ void prompt_attention_kernel(Call c) {
     // ---- register j of block db = d row 32 db + 8 (j / 4) + 4 half + j % 4.  64 d of the wave's columns go through LDS, so that the results are
     // written by whole lines (four prompts of 33 to 300: 15.5 us; 8 bytes a lane and 32 rows at once: 17.0).
     const floatx2 l_halves = both_halves(l_sum);
-    const float l = l_halves[0] + l_halves[1];
-    const bool none = m_ref == -__builtin_huge_valf() && l == 0.0f;
-    const float inv = none ? 0.0f : 1.0f / l;
+    float l = l_halves[0] + l_halves[1];
+    bool none = m_ref == -__builtin_huge_valf() && l == 0.0f;
     int r_first = r0 + wave * 32;
     const int lane2 = lane_again(), col2 = lane2 & 31, half2 = lane2 >> 5;
     asm volatile("" : "+s"(r_first));  // places are made again here, not kept in registers through the loop
@@ -431,6 +430,20 @@ void prompt_attention_kernel(Call c) {
         const int i_query = c.over_G(r);
         return static_cast<int64_t>(q_first + i_query) * c.H + hk * c.G + (r - i_query * c.G);
     };
+    if (__builtin_expect(__ballot(none) != 0ull, 0)) {  // where rows are seen, all logits are minus infinity: NaN if it is the query that makes them so
+        const int r = min(r_first + col2, n_columns - 1);
+        const int to = c.n_win > 0 ? legal_rows(first, c.over_G(r), held, c.m, c.mask_mode) : 0;
+        const bf16x8* const q = reinterpret_cast<const bf16x8*>(c.q + row_of(r) * D);
+        unsigned found = 0;
+#pragma unroll 1
+        for (int ks = 0; ks < KS; ++ks) found |= not_finite(q[2 * ks + half2]);
+        const unsigned long long odd = __ballot(found != 0);
+        if (none && to > 0 && (static_cast<unsigned>(odd | odd >> 32) >> col2) & 1) {
+            l = __builtin_nanf("");
+            none = false;
+        }
+    }
+    const float inv = none ? 0.0f : 1.0f / l;
     if (c.lse && half2 == 0 && col2 < left) c.lse[row_of(r_first + col2)] = none ? -__builtin_huge_valf() : log_of(m_ref, l);
     static_assert(kWaves * 32 * 128 <= kSlots * 2 * kTileBytes, "the tiles' place");
     unsigned char* const mine = lds + (D == 64 ? 0 : kSlots * 2 * kTileBytes) + wave * (32 * 128);
