@@ -45,7 +45,7 @@ typedef struct {
  * N <= 2^27 and N * H_kv * D <= 2^36 for rows in and out; B <= 2^14 and B S H <= 2^22 for the attention. */
 
 /* Rows into the cache.  Packed rows offsets[b] .. offsets[b+1] - 1 become rows start[b], start[b] + 1, .. of sequence b; what would fall
- * outside the table is not stored, and packed rows that belong to no sequence are not read.
+ * outside the table is not stored, and what packed rows hold that belong to no sequence does not matter.
  *   k_rows, v_rows  device [N, H_kv, D] bf16    (v_rows is not used where the cache's V is NULL, and may be NULL)
  *   offsets         device [B + 1] int32, not decreasing, in 0 .. N;  NULL: N / B rows a sequence (N a multiple of B)
  *   start           device [B] int32, >= 0;  NULL = 0
@@ -74,10 +74,14 @@ si_status si_load_pages(const si_paged_cache* cache, int32_t N, const int32_t* o
  *   first      device [B] int32        NULL = 0
  *   n_win      >= 0; SI_ALL_ROWS: no window
  *   out        device [B,S,H,D] bf16;  lse device [B,S,H] f32 or NULL
- *   workspace  device, si_paged_workspace_bytes(B, S, H, H_kv, D) bytes
- * fp32 products, statistics and sums.  A weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the
- * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
- * weight of 0 (a finite query with no other logits gets out = 0 and lse = -inf); infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
+ *   workspace  device, si_paged_workspace_bytes(B, S, H, H_kv, D) bytes: room for the parts of sequences that are split, whatever the lengths are.  The size
+ *              knows neither the table's width nor n_win: a call whose table or window leaves every sequence few rows asks for as much, and uses 8 B bytes at most
+ * fp32 products, statistics and sums: a logit is infinite where <q,K>, or that times scale * log2(e), passes fp32's range, and finite values give
+ * finite results where the number of rows seen times the largest value is at most 2^117, as sums are divided by that of their weights at the end.  A
+ * weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the weights before that.  A head whose
+ * query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a weight of
+ * 0 (a finite query with no other logits gets out = 0 and lse = -inf); infinite or NaN values of a row that is seen make infinities or NaN of out where
+ * they stand.  What rows hold
  * that a position does not see (behind the length, before the window, later positions' rows) never reaches its result, NaN and infinities included.
  * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  The same call gives the same bits, and no bit of a head's
  * result depends on the queries of other heads or positions. */

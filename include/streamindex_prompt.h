@@ -45,12 +45,16 @@ typedef struct {
  *   first      device [B] int32;  NULL = 0
  *   n_win      >= 0; SI_ALL_ROWS: no window
  *   out        device [N_q,H,D] bf16;  lse device [N_q,H] f32 or NULL.  Queries that belong to no sequence are left as they were.
- * fp32 products, statistics and sums.  A weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the
- * weights before that.  A head whose query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a
- * weight of 0 (a finite query with no other logits gets out = 0 and lse = -inf); infinite or NaN values of a row that is seen make infinities or NaN of out where they stand.  What rows hold
+ * fp32 products, statistics and sums: a logit is infinite where <q,K>, or that times scale * log2(e), passes fp32's range, and finite values give
+ * finite results where the number of rows seen times the largest value is at most 2^117, as sums are divided by that of their weights at the end.  A
+ * weight exp(x_s - reference) is rounded to bf16 once, as an operand of the second product; lse is made of the weights before that.  A head whose
+ * query is not finite, or one of whose logits is NaN or +infinity, gets NaN in out and lse, and no other head does.  A logit of -infinity is a weight of
+ * 0 (a finite query with no other logits gets out = 0 and lse = -inf); infinite or NaN values of a row that is seen make infinities or NaN of out where
+ * they stand.  What rows hold
  * that a query does not see (later positions, before the window, other sequences) never reaches its result, NaN and infinities included.
  * scale has to be finite, scale * log2(e) too (SI_ERR_INVALID_ARG).  No workspace.  The same call gives the same bits, and no bit of a head's
  * result depends on the queries of other heads or positions.
+ * There is at least one query and one row (SI_ERR_INVALID_ARG): where no sequence has a row yet, one that belongs to none.
  * Limits, SI_ERR_UNSUPPORTED_SHAPE beyond them: D = 64 or 128, H <= 1024, N_q, N_k <= 2^30, B <= 2^20, N_q H + 128 B H_kv < 2^30. */
 si_status si_prompt_attention(const void* q, const void* K, const void* V, const si_packed_dims* dims, const int32_t* q_offsets,
                               const int32_t* k_offsets, const int32_t* first, int32_t m, si_mask_mode mask_mode, int32_t n_win, float scale,
