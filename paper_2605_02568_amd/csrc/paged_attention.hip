@@ -2,7 +2,8 @@
 //
 //   out[b,i,g,:] = sum_{s in seen(t)} exp(x_s - lse) V[s,h,:],  x_s = scale <q[b,i,g,:], K[s,h,:]>,  lse = ln sum exp(x_s),  t = first[b] + i
 //
-// All rows of a sequence are read once, so a call is bound by memory: 64 requests of 1,025 to 8,191 rows, 64 heads of 128 on 8, 16 bits: 1.21 GB in 205 us, 5.9 TB/s
+// The rows of a sequence are read once for up to 64 columns that share a head; each 64 columns more read them again, from the caches where they find them there
+// (128 positions of 64 heads on 8: 16 workgroups a chunk and head).  So a call of few positions is bound by memory: 64 requests of 1,025 to 8,191 rows, 64 heads of 128 on 8, 16 bits: 1.21 GB in 205 us, 5.9 TB/s
 // (loads alone reach 7.1 here).  Where 64 heads share one row of 8 bits, the vector units (36 % of the time) and the matrix pipe (18 %) take as long together as
 // memory does: 8 requests of 65,536 to 131,072 rows: 203 MB in 59 us, of which the chunks' start, end and join take 18.
 // The positions and heads that share a head of the cache are the columns of one product (column r: position r / G, head r % G of the group of G), 16, 32 or 64 of
@@ -246,7 +247,9 @@ struct Group {
 
 // Starts the loads of 16 rows of keys, or of values: `bytes` bytes from src on, to LDS at `to`, 1 KB at a time.  A load's rows follow the one's before, so its
 // offset in memory and in LDS is the instruction's, and a lane's place among them, `offset`, changes by the swizzle of the rows' number only.
-// What lies at or past `bytes` is not read and lands as zeros.  ONCE: no other workgroup reads the rows, so they need not stay in the caches.
+// What lies at or past `bytes` is not read and lands as zeros.  ONCE: no other workgroup of the sequence reads the rows, so they need not stay in the caches: 64 requests
+// of 4,352 rows, 64 heads of 128 on 8, 16 bits: 175 us, without the hint 197; 8 bits 92 and 106.  Of pages that are in several tables the hint is the wrong one, and the
+// host does not know of them: the same requests with 4,096 rows in common 58 and 53 us (8 bits 52 and 52), 16 with 16,384 in common and 512 of their own 76 and 47.
 template <typename T, bool ONCE, int I = 0>
 __device__ __forceinline__ void request_half(const char* src, int bytes, int offset, unsigned char* to) {
 #if defined(__HIP_DEVICE_COMPILE__)
