@@ -384,6 +384,7 @@ void paged_attention_kernel(Call c) {
 
     // ---- what the columns see, and what all of them do: from the last position's first row to the first one's last
     // a column's query, the rows [y, z) that it sees, and its place among the sequence's results: every wave makes the same table, a lane a column
+    // (the compiler has this store to LDS wait for all tiles on their way there, so the queries are asked for once the first tiles have landed)
     int4* const columns = reinterpret_cast<int4*>(lds + W::kColumns);
     if (lane < NB * 16) {
         const int r = min(block * NB * 16 + lane, R - 1), i = r / c.G;  // columns that there are not repeat the last one
@@ -895,6 +896,8 @@ si_status si_paged_attention(const void* q, const si_paged_cache* cache, int32_t
     while ((1 << lg) < cache->page_rows) ++lg;
     float* const parts = static_cast<float*>(workspace);
     const size_t n_parts = static_cast<size_t>(parts_of(cache->B, shape.target));
+    // Where keys are the values, rows are asked for twice, the second time mostly from the caches: 64 requests of 1,025 to 8,191 rows, 64 heads of 128 on 8, take 123 us in 16
+    // bits and 84 in 8, with values of their own 198 and 112; where 64 heads share a head of 8 bits the loads are not what bounds it (50 and 53 us).
     const Call c = {static_cast<const __bf16*>(q),
                     {cache->K, cache->V ? cache->V : cache->K},
                     {static_cast<const unsigned char*>(cache->K_scales), static_cast<const unsigned char*>(cache->V ? cache->V_scales : cache->K_scales)},
